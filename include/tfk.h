@@ -465,6 +465,92 @@ TFK_API tfk_status tfk_sampled_softmax_xent(const void *z, tfk_dtype dt, int64_t
 TFK_API tfk_status tfk_scatter_apply_sgd(float *var, uint16_t *var_bf16, int64_t rows, int32_t d, const int32_t *idx,
                                  int32_t u, const float *grad_t, int64_t ld, float lr, void *stream);
 
+/* ---------------------------------------------------------------- distillation
+ * The loss of a classifier that learns from another one (Hinton et al. 2015), given by its largest
+ * logits, beside the cross-entropy of Section 4.1's classifiers and the large-vocabulary heads of
+ * Section 4.2.  For each row i < n, with x = logits + bias, u = x / T, and for each class j
+ *   p_j  the sum of the teacher's probabilities of the row's entries q with top_idx[i][q] == j;
+ *        an entry outside [0, c) is none (a shorter list is padded with -1).  Entry probabilities:
+ *          top_lse NULL:  softmax over the row's entries of top[i][q] / T  (renormalised)
+ *          else:          exp(top[i][q] / T - top_lse[i]), top_lse the log-sum-exp of top / T over
+ *                         all of the teacher's classes
+ *   K    the classes with an entry;  p_r = 0 (renormalised), else max(0, 1 - sum_K p_j): what the
+ *        teacher gives to all the others, which then count as one class
+ *   q = softmax(u);  q_r = sum of q_j outside K
+ * the operation is
+ *   soft = sum_K p_j (log p_j - log q_j) + p_r (log p_r - log q_r)      (a term with p = 0 is 0)
+ *   hard = logsumexp(x) - x[labels[i]]
+ *   loss[i]       = weight[i] (alpha T^2 soft + (1 - alpha) hard)
+ *   dlogits[i][j] = scale weight[i] (alpha T (q_j - p_j)               + (1 - alpha) (softmax(x)_j - [j == label]))   j in K
+ *                   scale weight[i] (alpha T q_j (1 - p_r / q_r)       + (1 - alpha) (softmax(x)_j - [j == label]))   else
+ * that is, scale times the gradient of loss[i].  Arithmetic is fp32; the gradient is rounded to dt once.
+ *   logits, dlogits : n rows of c values, type dt, logits_ld / dlogits_ld elements apart (0 = c);
+ *                     dlogits may equal logits with the same row distance (in place), any other
+ *                     overlap is an error.
+ *   bias            : fp32 [c], or NULL for none.
+ *   top, top_idx    : n x k, dense; type top_dt and int32, in any order.
+ *   top_lse         : fp32 [n], or NULL (renormalised).
+ *   labels          : int32 [n], or NULL (alpha must be 1 then); not read where alpha is 1.  A label
+ *                     outside [0, c) is not checked on the host: its row gets a NaN loss and gradients.
+ *   weight          : fp32 [n], or NULL for 1.  A row of weight 0 (padding) gets loss 0 and a zero
+ *                     gradient whatever its logits, lists and label hold.
+ *   loss            : fp32 [n], overwritten.
+ * A row without a teacher (renormalised, and no entry or only entries of -inf) has no soft term.
+ * Logits of -inf are classes without probability: a p_j > 0 there (or a p_r > 0 where all classes
+ * outside K are) makes the loss infinite, and the gradient stays as above with q = 0 (0 outside K).
+ * Logits that are NaN or +inf, or -inf throughout, make the row NaN where a term needs them.
+ * Errors: n < 0, c < 1, k not in 1..1024, a row distance below c (SHAPE); scale not finite, temperature
+ * not in [1e-4, 1e4], alpha not in (0, 1], alpha < 1 without labels (ARG); n > 2^31 - 1 or n times
+ * a row distance > 2^40 (OVERFLOW); NULL, misaligned (to the element) or overlapping buffers (NULL, ALIGN, ALIAS).
+ * n == 0 is a no-op. */
+TFK_API tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld,
+                            const float *bias, const void *top, tfk_dtype top_dt, const int32_t *top_idx, int32_t k,
+                            const float *top_lse, const int32_t *labels, const float *weight, float temperature,
+                            float alpha, float scale, float *loss, void *dlogits, int64_t dlogits_ld, void *stream);
+
+/* ---------------------------------------------------------------- embedding table
+ * The embedding layer of Section 4.2: a Gather of the table's rows that the batch names, and its
+ * gradient, which touches only those rows (the sparse updates of Sections 4.2 and 6.2).
+ *
+ * Lookup:  out[i][j] = scale * table[ids[i]][j]  (formed in fp32, rounded to out_dt once), 0 for an id
+ * outside [0, rows) (padding).  table: rows rows of d values, type dt, table_ld elements apart; ids:
+ * int32 [n]; out: n rows of d, type out_dt, out_ld elements apart (row distances: 0 = d).
+ * Errors: n < 0, rows < 0, d < 1, a row distance below d (SHAPE); scale not finite (ARG); n or rows
+ * > 2^31 - 1, or n or rows times a row distance > 2^40 (OVERFLOW); NULL, misaligned (to the element) or overlapping
+ * buffers (NULL, ALIGN, ALIAS).  n == 0 is a no-op. */
+TFK_API tfk_status tfk_embedding_fwd(const void *table, tfk_dtype dt, int64_t rows, int64_t table_ld, int32_t d,
+                             const int32_t *ids, int64_t n, float scale, void *out, tfk_dtype out_dt, int64_t out_ld,
+                             void *stream);
+
+/* Gradient of the lookup (Section 4.1's backpropagation through the Gather of Section 4.2), dense:
+ *   dtable[r][j] = beta * dtable[r][j] + scale * sum over the i with ids[i] == r of dy[i][j]
+ * dy: n rows of d values, type dt, dy_ld elements apart (0 = d); ids: int32 [n], ids outside
+ * [0, rows) are left out; dtable: dense fp32 rows x d.  beta 0 writes every row (0 where no token
+ * is); beta 1 adds to the rows that have tokens and leaves the others as they are.  The tokens are
+ * grouped by row first and each row's sum is formed in fp32 in a fixed order.
+ *   ws : at least tfk_embedding_workspace_bytes(n, d, rows) bytes, 16-byte aligned, apart from every operand.
+ * Errors: n < 0, rows < 0, d < 1, dy_ld below d (SHAPE); scale not finite, beta not 0 or 1 (ARG); n or
+ * rows > 2^31 - 1, or n dy_ld or rows d > 2^40 (OVERFLOW); NULL, misaligned or overlapping buffers (NULL, ALIGN, ALIAS);
+ * WORKSPACE.  n == 0 writes zeros (beta 0) or nothing. */
+TFK_API tfk_status tfk_embedding_bwd(const void *dy, tfk_dtype dt, int64_t n, int64_t dy_ld, int32_t d, const int32_t *ids,
+                             int64_t rows, float scale, float beta, float *dtable, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/* The gradient and its SGD step in one operation, without a dense gradient (the sparse update that
+ * Section 4.2's sharded embedding layer sends to its variable):
+ *   var[r][j] <- fma(-lr, scale * sum over the i with ids[i] == r of dy[i][j], var[r][j])
+ * for the rows r that have tokens; the others are not touched.  var: dense fp32 rows x d; var_bf16
+ * (optional) its bf16 copy, rewritten for the same rows.  Ids may repeat (tfk_scatter_apply_sgd
+ * wants distinct ones).  dy, ids, ws and errors as tfk_embedding_bwd; lr not finite (ARG).  n == 0 is
+ * a no-op. */
+TFK_API tfk_status tfk_embedding_apply_sgd(float *var, uint16_t *var_bf16, int64_t rows, int32_t d, const int32_t *ids,
+                                   int64_t n, const void *dy, tfk_dtype dt, int64_t dy_ld, float scale, float lr,
+                                   void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace of the two operations above (of Section 4.2), for n tokens; 0 for arguments they refuse and where n or
+ * rows is 0. */
+TFK_API size_t tfk_embedding_workspace_bytes(int64_t n, int32_t d, int64_t rows);
+
 /* Momentum, in place (Section 4.1 lists it among the optimizers built from
  * Variable updates: a per-parameter velocity accumulated over the gradients
  * drives the update).  Velocity form of Sutskever et al. (2013), fp32:
@@ -538,7 +624,7 @@ TFK_API tfk_status tfk_program_create(tfk_program **prog);
 TFK_API void tfk_program_destroy(tfk_program *prog);
 /* Starts recording on the calling thread (previous contents are dropped).  Until
  * tfk_program_end, every tfk_* call on this thread that enqueues work (convolutions, bias/ReLU,
- * pooling, updates, losses, sampled-softmax ops, tfk_stream_wait, marks) runs as usual and, when it
+ * pooling, updates, losses, sampled-softmax and embedding ops, tfk_stream_wait, marks) runs as usual and, when it
  * returns TFK_OK, is appended to the program with its arguments by value: the same pointers,
  * shapes, scalars and streams.  Calls that fail are not appended.  Queries
  * (*_workspace_bytes) are never recorded.  Errors: NULL; ARG (this thread already records). */
@@ -562,7 +648,7 @@ TFK_API tfk_status tfk_program_run(tfk_program *prog);
 TFK_API const char *tfk_status_string(tfk_status s);
 /* Detail of the last non-OK status returned on the calling thread ("" if none). */
 TFK_API const char *tfk_last_error(void);
-/* Version of this interface (incremented when any declaration here changes). */
+/* Version of this interface (incremented when a declaration here changes or goes; a new one leaves it). */
 TFK_API int32_t tfk_abi_version(void);
 
 #ifdef __cplusplus

@@ -2,7 +2,8 @@
 
 ``ops`` binds the C ABI of libtfk.so (include/tfk.h) over torch device
 tensors; ``step.Replica`` drives a whole step of a workload from
-``workloads``.  The HIP library must be built first
+``workloads``; ``sampled`` and ``embedding`` hold a language model's softmax
+heads and embedding table.  The HIP library must be built first
 (``python -m paper_1605_08695_amd.build``); nothing here falls back to the CPU.
 """
-__all__ = ["ops", "step", "workloads", "build"]
+__all__ = ["ops", "step", "workloads", "sampled", "embedding", "build"]

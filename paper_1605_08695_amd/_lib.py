@@ -24,7 +24,8 @@ EXPORTS = ["tfk_conv2d_fwd", "tfk_conv2d_fwd_bias_relu", "tfk_maxpool_bwd_relu_b
            "tfk_maxpool_fwd", "tfk_maxpool_bwd", "tfk_maxpool_fwd_taps", "tfk_maxpool_bwd_taps",
            "tfk_maxpool_bwd_relu_bwd_taps", "tfk_apply_sgd", "tfk_apply_sgd_multi",
            "tfk_apply_momentum", "tfk_apply_adam", "tfk_softmax_xent", "tfk_gather_rows_t",
-           "tfk_sampled_softmax_xent", "tfk_scatter_apply_sgd", "tfk_stream_wait", "tfk_mark_create", "tfk_mark_destroy",
+           "tfk_sampled_softmax_xent", "tfk_scatter_apply_sgd", "tfk_distill_xent", "tfk_embedding_fwd",
+           "tfk_embedding_bwd", "tfk_embedding_apply_sgd", "tfk_embedding_workspace_bytes", "tfk_stream_wait", "tfk_mark_create", "tfk_mark_destroy",
            "tfk_mark_record", "tfk_stream_wait_mark", "tfk_program_create",
            "tfk_program_destroy", "tfk_program_begin", "tfk_program_end", "tfk_program_length", "tfk_program_run",
            "tfk_status_string", "tfk_last_error", "tfk_abi_version"]
@@ -89,12 +90,20 @@ def load(path: str = LIB_PATH):
     lib.tfk_gather_rows_t.argtypes = [vp, st, i64, i32, vp, i32, i32, vp, vp]
     lib.tfk_sampled_softmax_xent.argtypes = [vp, st, i64, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp]
     lib.tfk_scatter_apply_sgd.argtypes = [vp, vp, i64, i32, vp, i32, vp, i64, f32, vp]
+    lib.tfk_distill_xent.argtypes = [vp, st, i64, i32, i64, vp, vp, st, vp, i32, vp, vp, vp, f32, f32, f32, vp, vp,
+                                     i64, vp]
+    lib.tfk_embedding_fwd.argtypes = [vp, st, i64, i64, i32, vp, i64, f32, vp, st, i64, vp]
+    lib.tfk_embedding_bwd.argtypes = [vp, st, i64, i64, i32, vp, i64, f32, f32, vp, vp, sz, vp]
+    lib.tfk_embedding_apply_sgd.argtypes = [vp, vp, i64, i32, vp, i64, vp, st, i64, f32, f32, vp, sz, vp]
+    lib.tfk_embedding_workspace_bytes.argtypes = [i64, i32, i64]
+    lib.tfk_embedding_workspace_bytes.restype = sz
     for name in ("tfk_conv2d_fwd", "tfk_conv2d_fwd_bias_relu", "tfk_conv2d_fwd_bias_relu_maxpool", "tfk_conv2d_bwd_input", "tfk_conv2d_bwd_input_relu_bwd",
                  "tfk_conv2d_bwd_filter", "tfk_conv2d_bwd_filter_noalloc", "tfk_bias_relu_fwd",
                  "tfk_bias_relu_bwd", "tfk_maxpool_fwd", "tfk_maxpool_bwd", "tfk_maxpool_bwd_relu_bwd",
                  "tfk_maxpool_fwd_taps", "tfk_maxpool_bwd_taps", "tfk_maxpool_bwd_relu_bwd_taps", "tfk_apply_sgd",
                  "tfk_apply_sgd_multi", "tfk_apply_momentum", "tfk_apply_adam", "tfk_softmax_xent", "tfk_gather_rows_t",
-                 "tfk_sampled_softmax_xent", "tfk_scatter_apply_sgd"):
+                 "tfk_sampled_softmax_xent", "tfk_scatter_apply_sgd", "tfk_distill_xent", "tfk_embedding_fwd",
+                 "tfk_embedding_bwd", "tfk_embedding_apply_sgd"):
         getattr(lib, name).restype = st
     lib.tfk_last_bias_partials.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(i32)]
     lib.tfk_bias_grad_finish.argtypes = [i32, ctypes.POINTER(vp), ctypes.POINTER(i32), ctypes.POINTER(i32),

@@ -1039,6 +1039,155 @@ tfk_status tfk_scatter_apply_sgd(float *var, uint16_t *var_bf16, int64_t rows, i
                       "scatter_apply_sgd");
 }
 
+// ------------------------------------------------------------------ distillation
+// Rows of `cols` elements a fixed distance apart: resolves ld == 0, checks it and the extent.
+static tfk_status check_rows(const char *name, int64_t n, int64_t cols, int64_t &ld) {
+    if (ld == 0) ld = cols;
+    if (ld < cols) return fail(TFK_ERR_SHAPE, "%s: row distance %lld < %lld", name, (long long)ld, (long long)cols);
+    if (n > INT32_MAX) return fail(TFK_ERR_OVERFLOW, "%s: more than 2^31-1 rows", name);
+    if (n > 0 && ld > ((int64_t)1 << 40) / n) return fail(TFK_ERR_OVERFLOW, "%s: too large", name);
+    return TFK_OK;
+}
+
+static int64_t rows_bytes(int64_t n, int64_t cols, int64_t ld, int64_t es) {
+    return n == 0 ? 0 : ((n - 1) * ld + cols) * es;
+}
+
+tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld, const float *bias,
+                            const void *top, tfk_dtype top_dt, const int32_t *top_idx, int32_t k, const float *top_lse,
+                            const int32_t *labels, const float *weight, float temperature, float alpha, float scale,
+                            float *loss, void *dlogits, int64_t dlogits_ld, void *stream) {
+    RECORDED(tfk_distill_xent, logits, dt, n, c, logits_ld, bias, top, top_dt, top_idx, k, top_lse, labels, weight,
+             temperature, alpha, scale, loss, dlogits, dlogits_ld, stream);
+    if (!valid_dt(dt)) return fail(TFK_ERR_DTYPE, "unknown dtype %d", (int)dt);
+    if (!valid_dt(top_dt)) return fail(TFK_ERR_DTYPE, "unknown dtype %d", (int)top_dt);
+    if (n < 0 || c < 1) return fail(TFK_ERR_SHAPE, "need n >= 0 and c >= 1 (n=%lld, c=%d)", (long long)n, c);
+    if (k < 1 || k > 1024) return fail(TFK_ERR_SHAPE, "k must be in 1..1024 (got %d)", k);
+    TRY(check_rows("logits", n, c, logits_ld));
+    TRY(check_rows("dlogits", n, c, dlogits_ld));
+    if (!isfinite(scale)) return fail(TFK_ERR_ARG, "scale must be finite");
+    if (!(temperature >= 1e-4f && temperature <= 1e4f)) return fail(TFK_ERR_ARG, "temperature must be in [1e-4, 1e4]");
+    if (!(alpha > 0.f && alpha <= 1.f)) return fail(TFK_ERR_ARG, "alpha must be in (0, 1]");
+    if (n == 0) return ok();
+    if (alpha < 1.f && labels == nullptr) return fail(TFK_ERR_ARG, "alpha < 1 needs labels");
+    TRY(need_ptr(logits, "logits"));
+    TRY(need_ptr(top, "top"));
+    TRY(need_ptr(top_idx, "top_idx"));
+    TRY(need_ptr(loss, "loss"));
+    TRY(need_ptr(dlogits, "dlogits"));
+    const int64_t es = esize(dt), ts = esize(top_dt);
+    TRY(need_align(logits, es, "logits"));
+    TRY(need_align(dlogits, es, "dlogits"));
+    TRY(need_align(top, ts, "top"));
+    TRY(need_align(top_idx, 4, "top_idx"));
+    TRY(need_align(bias, 4, "bias"));
+    TRY(need_align(top_lse, 4, "top_lse"));
+    TRY(need_align(labels, 4, "labels"));
+    TRY(need_align(weight, 4, "weight"));
+    TRY(need_align(loss, 4, "loss"));
+    const bool in_place = dlogits == logits && dlogits_ld == logits_ld;
+    const void *p[9] = {dlogits, loss, logits, bias, top, top_idx, top_lse, labels, weight};
+    const int64_t b[9] = {rows_bytes(n, c, dlogits_ld, es), n * 4, rows_bytes(n, c, logits_ld, es), (int64_t)c * 4,
+                          n * k * ts, n * k * 4, n * 4, n * 4, n * 4};
+    for (int i = 0; i < 2; ++i)
+        for (int j = i + 1; j < 9; ++j)
+            if (!(in_place && i == 0 && j == 2) && overlap(p[i], b[i], p[j], b[j]))
+                return fail(TFK_ERR_ALIAS, "dlogits or loss overlaps an operand");
+    // (a hard term of weight 0 is left out: the labels are not read)
+    const DistillArgs a{logits, logits_ld, bias, top, top_idx, top_lse, alpha < 1.f ? labels : nullptr, weight, loss,
+                        dlogits, dlogits_ld, c, k, temperature, alpha, scale};
+    return hip_status(launch_distill(dt == TFK_F32 ? 0 : 1, top_dt == TFK_F32 ? 0 : 1, n, a, (hipStream_t)stream),
+                      "distill_xent");
+}
+
+// ------------------------------------------------------------------ embedding table
+tfk_status tfk_embedding_fwd(const void *table, tfk_dtype dt, int64_t rows, int64_t table_ld, int32_t d, const int32_t *ids,
+                             int64_t n, float scale, void *out, tfk_dtype out_dt, int64_t out_ld, void *stream) {
+    RECORDED(tfk_embedding_fwd, table, dt, rows, table_ld, d, ids, n, scale, out, out_dt, out_ld, stream);
+    if (!valid_dt(dt)) return fail(TFK_ERR_DTYPE, "unknown dtype %d", (int)dt);
+    if (!valid_dt(out_dt)) return fail(TFK_ERR_DTYPE, "unknown dtype %d", (int)out_dt);
+    if (n < 0 || rows < 0 || d < 1) return fail(TFK_ERR_SHAPE, "need n >= 0, rows >= 0 and d >= 1");
+    TRY(check_rows("table", rows, d, table_ld));
+    TRY(check_rows("out", n, d, out_ld));
+    if (!isfinite(scale)) return fail(TFK_ERR_ARG, "scale must be finite");
+    if (n == 0) return ok();
+    if (rows > 0) TRY(need_ptr(table, "table"));
+    TRY(need_ptr(ids, "ids"));
+    TRY(need_ptr(out, "out"));
+    const int64_t es = esize(dt), os = esize(out_dt);
+    TRY(need_align(table, es, "table"));
+    TRY(need_align(ids, 4, "ids"));
+    TRY(need_align(out, os, "out"));
+    const int64_t ob = rows_bytes(n, d, out_ld, os);
+    if (overlap(out, ob, table, rows_bytes(rows, d, table_ld, es)) || overlap(out, ob, ids, n * 4))
+        return fail(TFK_ERR_ALIAS, "out overlaps table or ids");
+    return hip_status(launch_embed_fwd(dt == TFK_F32 ? 0 : 1, table, rows, table_ld, d, ids, n, scale,
+                                       out_dt == TFK_F32 ? 0 : 1, out, out_ld, (hipStream_t)stream),
+                      "embedding_fwd");
+}
+
+size_t tfk_embedding_workspace_bytes(int64_t n, int32_t d, int64_t rows) {
+    if (n <= 0 || rows <= 0 || d < 1 || n > INT32_MAX || rows > INT32_MAX || rows > ((int64_t)1 << 40) / d ||
+        n > ((int64_t)1 << 40) / d)
+        return 0;
+    return embed_ws_bytes(n, d, rows);
+}
+
+// Shared validation of the embedding gradient and update: sums of dy's rows by ids, into dst (rows x d
+// fp32; sh its bf16 copy or null).  whole: dst is written without tokens too.
+static tfk_status check_embed_sum(const void *dy, tfk_dtype dt, int64_t n, int64_t &dy_ld, int32_t d, const int32_t *ids,
+                                  int64_t rows, float scale, const float *dst, const char *dname, const uint16_t *sh,
+                                  bool whole, const void *ws, size_t ws_bytes) {
+    if (!valid_dt(dt)) return fail(TFK_ERR_DTYPE, "unknown dtype %d", (int)dt);
+    if (n < 0 || rows < 0 || d < 1) return fail(TFK_ERR_SHAPE, "need n >= 0, rows >= 0 and d >= 1");
+    int64_t dld = d;
+    TRY(check_rows("dy", n, d, dy_ld));
+    TRY(check_rows(dname, rows, d, dld));
+    if (!isfinite(scale)) return fail(TFK_ERR_ARG, "scale must be finite");
+    const int64_t es = esize(dt), db = rows * d * 4, sb = rows * d * 2, yb = rows_bytes(n, d, dy_ld, es);
+    if (rows > 0 && (n > 0 || whole)) TRY(need_ptr(dst, dname));
+    TRY(need_align(dst, 4, dname));
+    TRY(need_align(sh, 2, "var_bf16"));
+    if (n == 0 || rows == 0) return TFK_OK;
+    TRY(need_ptr(dy, "dy"));
+    TRY(need_ptr(ids, "ids"));
+    TRY(need_align(dy, es, "dy"));
+    TRY(need_align(ids, 4, "ids"));
+    const size_t need = embed_ws_bytes(n, d, rows);
+    TRY(check_ws(const_cast<void *>(ws), ws_bytes, need));
+    const void *p[5] = {dst, sh, ws, dy, ids};
+    const int64_t b[5] = {db, sb, (int64_t)need, yb, n * 4};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 5; ++j)
+            if (overlap(p[i], b[i], p[j], b[j])) return fail(TFK_ERR_ALIAS, "%s, its copy or ws overlaps an operand", dname);
+    return TFK_OK;
+}
+
+tfk_status tfk_embedding_bwd(const void *dy, tfk_dtype dt, int64_t n, int64_t dy_ld, int32_t d, const int32_t *ids,
+                             int64_t rows, float scale, float beta, float *dtable, void *ws, size_t ws_bytes,
+                             void *stream) {
+    RECORDED(tfk_embedding_bwd, dy, dt, n, dy_ld, d, ids, rows, scale, beta, dtable, ws, ws_bytes, stream);
+    if (beta != 0.f && beta != 1.f) return fail(TFK_ERR_ARG, "beta must be 0 or 1");
+    TRY(check_embed_sum(dy, dt, n, dy_ld, d, ids, rows, scale, dtable, "dtable", nullptr, beta == 0.f, ws,
+                        ws_bytes));
+    if (rows == 0 || (n == 0 && beta == 1.f)) return ok();
+    return hip_status(launch_embed_bwd(dt == TFK_F32 ? 0 : 1, dy, n, d, dy_ld, ids, rows, scale, beta, dtable, ws,
+                                       (hipStream_t)stream),
+                      "embedding_bwd");
+}
+
+tfk_status tfk_embedding_apply_sgd(float *var, uint16_t *var_bf16, int64_t rows, int32_t d, const int32_t *ids, int64_t n,
+                                   const void *dy, tfk_dtype dt, int64_t dy_ld, float scale, float lr, void *ws,
+                                   size_t ws_bytes, void *stream) {
+    RECORDED(tfk_embedding_apply_sgd, var, var_bf16, rows, d, ids, n, dy, dt, dy_ld, scale, lr, ws, ws_bytes, stream);
+    if (!isfinite(lr)) return fail(TFK_ERR_ARG, "lr must be finite");
+    TRY(check_embed_sum(dy, dt, n, dy_ld, d, ids, rows, scale, var, "var", var_bf16, false, ws, ws_bytes));
+    if (n == 0 || rows == 0) return ok();
+    return hip_status(launch_embed_sgd(dt == TFK_F32 ? 0 : 1, var, var_bf16, rows, d, ids, n, dy, dy_ld, scale, lr, ws,
+                                       (hipStream_t)stream),
+                      "embedding_apply_sgd");
+}
+
 // ------------------------------------------------------------------ Momentum, Adam
 static tfk_status check_slots(float *var, const float *grad, const float *s1, const float *s2, int64_t n,
                               uint16_t *sh, const char *n1, const char *n2) {

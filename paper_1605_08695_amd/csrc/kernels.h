@@ -176,6 +176,33 @@ hipError_t launch_scatter_sgd(float *var, uint16_t *sh, int64_t rows, int d, con
 // dz = scale * (softmax - onehot); dz may be z.
 hipError_t launch_softmax_xent(int dt, const void *z, const float *bias, const int32_t *labels, int64_t n, int c,
                                float scale, float *loss, void *dz, hipStream_t st);
+// Distillation loss and logit gradient of n rows (a's pointers: see tfk_distill_xent; bias, top_lse, labels
+// and weight may be null; dz may be z).
+struct DistillArgs {
+    const void *z;
+    int64_t zld;
+    const float *bias;
+    const void *top;
+    const int32_t *top_idx;
+    const float *top_lse;
+    const int32_t *labels;
+    const float *weight;
+    float *loss;
+    void *dz;
+    int64_t dld;
+    int c, k;
+    float temperature, alpha, scale;
+};
+hipError_t launch_distill(int dt, int top_dt, int64_t n, const DistillArgs &a, hipStream_t st);
+// Embedding table: lookup of n tokens; the dense gradient of the table (beta 0 or 1); the table's SGD
+// update.  tld, old_, dld: elements between rows of the table, the output and dy.
+hipError_t launch_embed_fwd(int tdt, const void *table, int64_t rows, int64_t tld, int d, const int32_t *ids, int64_t n,
+                            float scale, int odt, void *out, int64_t old_, hipStream_t st);
+size_t embed_ws_bytes(int64_t n, int d, int64_t rows);
+hipError_t launch_embed_bwd(int dt, const void *dy, int64_t n, int d, int64_t dld, const int32_t *ids, int64_t rows,
+                            float scale, float beta, float *dtable, void *ws, hipStream_t st);
+hipError_t launch_embed_sgd(int dt, float *var, uint16_t *sh, int64_t rows, int d, const int32_t *ids, int64_t n,
+                            const void *dy, int64_t dld, float scale, float lr, void *ws, hipStream_t st);
 // Momentum (kind 0, 1 = look-ahead form) and Adam (kind 2) in place over n fp32 elements.
 hipError_t launch_opt(int kind, float *var, float *s1, float *s2, const float *grad, int64_t n, const OptParams &p,
                       uint16_t *sh, hipStream_t st);

@@ -21,7 +21,8 @@ from ._lib import Nhwc, TfkError, Window, TFK_BF16, TFK_F32, check, load
 __all__ = ["conv2d_fwd", "conv2d_fwd_bias_relu", "conv2d_bwd_input", "conv2d_bwd_filter", "conv2d_workspace_bytes", "bias_relu_fwd",
            "bias_relu_bwd", "bias_relu_bwd_workspace_bytes", "maxpool_fwd", "maxpool_bwd", "maxpool_bwd_relu_bwd", "apply_sgd",
            "apply_sgd_multi", "apply_momentum", "apply_adam", "softmax_xent",
-           "gather_rows_t", "sampled_softmax_xent", "scatter_apply_sgd", "stream_wait", "Program", "out_len", "nhwc",
+           "gather_rows_t", "sampled_softmax_xent", "scatter_apply_sgd", "distill_xent", "embedding_fwd", "embedding_bwd",
+           "embedding_apply_sgd", "embedding_workspace_bytes", "stream_wait", "Program", "out_len", "nhwc",
            "window", "TfkError", "abi_version", "DeferredBias", "bias_grad_finish"]
 
 
@@ -570,6 +571,177 @@ def scatter_apply_sgd(var, idx, grad_t, lr, shadow=None, stream=None):
         raise TypeError("var and grad_t are float32, idx int32")
     check(load().tfk_scatter_apply_sgd(_ptr(var), _ptr(shadow), rows, d, _ptr(idx), idx.numel(), _ptr(grad_t), ld,
                                        float(lr), _stream(stream)))
+    return var
+
+
+# ----------------------------------------------------------------------------- rows
+def _rows_of(t, name) -> Tuple[int, int, int]:
+    """(n, c, elements between rows) of a tensor whose last dimension has unit stride and whose others
+    together are n rows a fixed distance apart."""
+    if t.dim() == 2:
+        n, c = t.shape
+        s, s1 = t.stride()
+    else:
+        if t.dim() < 2:
+            raise ValueError("%s must have rows and columns, got shape %s" % (name, tuple(t.shape)))
+        c = t.shape[-1]
+        n = t.numel() // c if c else 0
+        if not t.is_contiguous():
+            raise ValueError("%s with more than two dimensions must be contiguous" % name)
+        s, s1 = c, 1
+    if n < 2:
+        s = c
+    if c == 0 or (c > 1 and s1 != 1 and n > 0) or s < c:
+        raise ValueError("%s must be rows of unit stride that do not overlap, got shape %s, strides %s" %
+                         (name, tuple(t.shape), tuple(t.stride())))
+    return n, c, s
+
+
+def _vector(t, dtype, n, name):
+    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous %s tensor of %d values" % (name, str(dtype).split(".")[-1], n))
+
+
+def _on_device(stream, *tensors):
+    """Every operand must be on the current GPU, whose stream (given or current) the call is enqueued on."""
+    at = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("operands must be on the GPU, got one on %s" % t.device)
+        if at is None:
+            at = t.get_device()
+        if t.get_device() != at:
+            raise ValueError("operands are on different GPUs")
+    if at != torch.cuda.current_device() or (stream is not None and stream.device.index != at):
+        raise ValueError("operands are on GPU %d, which is not the current device or the stream's" % at)
+
+
+# ----------------------------------------------------------------------------- distillation
+def distill_xent(logits, top_idx, top, scale, temperature=1.0, top_lse=None, labels=None, alpha=1.0, weight=None,
+                 bias=None, loss=None, dlogits=None, stream=None):
+    """Distillation from a teacher's k largest logits: returns (loss per row, dlogits), where
+    loss = weight * (alpha T^2 KL(teacher || student) + (1 - alpha) cross-entropy with labels) and
+    dlogits = scale * its gradient.
+
+    logits: rows of c classes (+ bias), dlogits the same shape and type (may be logits: in place).
+    top, top_idx (n x k): the teacher's logits and their classes, -1 for none; renormalised over the
+    list, or with top_lse (the log-sum-exp of all the teacher's logits / temperature) the rest of its
+    mass counts as one more class.  Rows of weight 0 give loss 0 and no gradient.  Not differentiated
+    through the teacher."""
+    n, c, ld = _rows_of(logits, "logits")
+    if top.dim() < 2 or top.shape != top_idx.shape or top.numel() != n * top.shape[-1]:
+        raise ValueError("top and top_idx must share one shape of n rows, got %s and %s" % (tuple(top.shape),
+                                                                                          tuple(top_idx.shape)))
+    if top_idx.dtype != torch.int32 or not (top_idx.is_contiguous() and top.is_contiguous()):
+        raise ValueError("top_idx must be int32, top and top_idx contiguous")
+    _vector(top_lse, torch.float32, n, "top_lse")
+    _vector(labels, torch.int32, n, "labels")
+    _vector(weight, torch.float32, n, "weight")
+    _vector(bias, torch.float32, c, "bias")
+    _vector(loss, torch.float32, n, "loss")
+    dt, tdt = _dt(logits), _dt(top)
+    if dlogits is not None and (dlogits.shape != logits.shape or dlogits.dtype != logits.dtype):
+        raise ValueError("dlogits must have the logits' shape and type")
+    dld = ld if dlogits is logits else (c if dlogits is None else _rows_of(dlogits, "dlogits")[2])
+    _on_device(stream, logits, top, top_idx, top_lse, labels, weight, bias, loss, dlogits)
+    if loss is None:
+        loss = _empty(stream, n, dtype=torch.float32, device=logits.device)
+    if dlogits is None:
+        dlogits = _empty_like(stream, logits)
+    check(load().tfk_distill_xent(_ptr(logits), dt, n, c, ld, _ptr(bias), _ptr(top), tdt, _ptr(top_idx), top.shape[-1],
+                                  _ptr(top_lse), _ptr(labels), _ptr(weight), float(temperature), float(alpha),
+                                  float(scale), _ptr(loss), _ptr(dlogits), dld, _stream(stream)))
+    return loss, dlogits
+
+
+# ----------------------------------------------------------------------------- embedding table
+def _ids(ids):
+    if ids.dtype != torch.int32 or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous int32 tensor")
+    return ids.numel()
+
+
+def embedding_fwd(table, ids, scale=1.0, out=None, out_dtype=None, stream=None):
+    """out[i] = scale * table[ids[i]] (zeros for an id outside the table); table (rows x d) and out of
+    either type (out_dtype, default table's).  Returns out, ids' shape with d columns."""
+    n = _ids(ids)
+    if table.dim() != 2:
+        raise ValueError("table must be rows x d, got shape %s" % (tuple(table.shape),))
+    rows, d, tld = _rows_of(table, "table")
+    dt = _dt(table)
+    shape = tuple(ids.shape) + (d,)
+    if out is None:
+        _on_device(stream, table, ids)
+        out = _empty(stream, shape, dtype=out_dtype or table.dtype, device=table.device)
+        old = d
+    else:
+        if tuple(out.shape) != shape or (out_dtype is not None and out.dtype != out_dtype):
+            raise ValueError("out must be %s%s, got %s of %s" % (shape, " of %s" % out_dtype if out_dtype else "",
+                                                                tuple(out.shape), out.dtype))
+        old = d if len(shape) == 1 else _rows_of(out, "out")[2]
+        _on_device(stream, table, ids, out)
+    check(load().tfk_embedding_fwd(_ptr(table), dt, rows, tld, d, _ptr(ids), n, float(scale), _ptr(out), _dt(out), old,
+                                   _stream(stream)))
+    return out
+
+
+def embedding_workspace_bytes(n, d, rows) -> int:
+    """Workspace of embedding_bwd and embedding_apply_sgd for n tokens of a rows x d table."""
+    return load().tfk_embedding_workspace_bytes(operator.index(n), operator.index(d), operator.index(rows))
+
+
+_embed_need = functools.lru_cache(_KEPT)(embedding_workspace_bytes)
+
+
+def _embed_args(dy, ids, stream, ws, rows, d, *more):
+    """Checks dy (ids' shape with d columns) and the operands' device; returns (n, dy's row distance,
+    workspace, its bytes)."""
+    n = _ids(ids)
+    if tuple(dy.shape) != tuple(ids.shape) + (d,):
+        raise ValueError("dy must be %s, got %s" % (tuple(ids.shape) + (d,), tuple(dy.shape)))
+    ld = d if dy.dim() == 1 and dy.is_contiguous() else _rows_of(dy, "dy")[2]
+    if ws is not None and not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    _on_device(stream, dy, ids, ws, *more)
+    need = _embed_need(n, d, rows)
+    if need and (ws is None or ws.numel() * ws.element_size() < need):
+        ws = _ws(need, dy.device, stream)
+    return n, ld, ws, need
+
+
+def embedding_bwd(dy, ids, rows, scale=1.0, dtable=None, beta=0.0, ws=None, stream=None):
+    """The table's dense fp32 gradient: dtable (rows x d) = beta * dtable + scale * the sum of dy over
+    each row's tokens (beta 0 or 1).  Returns dtable."""
+    d = dy.shape[-1] if dy.dim() else 0
+    rows = operator.index(rows)
+    if dtable is None and beta != 0.0:
+        raise ValueError("beta = 1 adds to a dtable that is given")
+    if dtable is not None and (dtable.dtype != torch.float32 or tuple(dtable.shape) != (rows, d) or
+                               not dtable.is_contiguous()):
+        raise ValueError("dtable must be a contiguous float32 tensor of %d x %d" % (rows, d))
+    dt = _dt(dy)
+    n, ld, ws, need = _embed_args(dy, ids, stream, ws, rows, d, dtable)
+    if dtable is None:
+        dtable = _empty(stream, (rows, d), dtype=torch.float32, device=dy.device)
+    check(load().tfk_embedding_bwd(_ptr(dy), dt, n, ld, d, _ptr(ids), rows, float(scale), float(beta), _ptr(dtable),
+                                   _ptr(ws), need, _stream(stream)))
+    return dtable
+
+
+def embedding_apply_sgd(var, ids, dy, lr, scale=1.0, shadow=None, ws=None, stream=None):
+    """In place: var[r] -= lr * scale * the sum of dy over the tokens of row r, for the rows that have
+    tokens (ids may repeat); shadow (bf16) rewritten there.  Returns var."""
+    if var.dim() != 2 or var.dtype != torch.float32 or not var.is_contiguous():
+        raise ValueError("var must be a contiguous float32 tensor of rows x d")
+    if shadow is not None and (shadow.dtype != torch.bfloat16 or shadow.shape != var.shape or not shadow.is_contiguous()):
+        raise ValueError("shadow must be a contiguous bfloat16 tensor of var's shape")
+    rows, d = var.shape
+    dt = _dt(dy)
+    n, ld, ws, need = _embed_args(dy, ids, stream, ws, rows, d, var, shadow)
+    check(load().tfk_embedding_apply_sgd(_ptr(var), _ptr(shadow), rows, d, _ptr(ids), n, _ptr(dy), dt, ld, float(scale),
+                                         float(lr), _ptr(ws), need, _stream(stream)))
     return var
 
 

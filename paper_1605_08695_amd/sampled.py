@@ -96,12 +96,28 @@ class FullSoftmaxHead:
         self.W_lp = self.W.to(torch.bfloat16)
         self.b = torch.from_numpy(np.asarray(b, np.float32)).to(dev)
 
-    def run(self, h: torch.Tensor, labels: torch.Tensor, stream=None):
+    def _logits(self, h: torch.Tensor, stream):
         n, d = h.shape
-        h4 = h.view(n, 1, 1, d)
-        w4 = self.W_lp.view(1, 1, d, self.vocab)
-        z = ops.conv2d_fwd(h4, w4, 1, (0, 0, 0, 0), stream=stream)
-        loss, dz = ops.softmax_xent(z, labels, 1.0 / n, bias=self.b, dlogits=z, stream=stream)
+        return ops.conv2d_fwd(h.view(n, 1, 1, d), self.W_lp.view(1, 1, d, self.vocab), 1, (0, 0, 0, 0), stream=stream)
+
+    def run(self, h: torch.Tensor, labels: torch.Tensor, stream=None):
+        z = self._logits(h, stream)
+        loss, dz = ops.softmax_xent(z, labels, 1.0 / h.shape[0], bias=self.b, dlogits=z, stream=stream)
+        return loss, self._apply(h, dz, stream)
+
+    def run_distill(self, h: torch.Tensor, top_idx: torch.Tensor, top: torch.Tensor, temperature: float = 1.0,
+                    top_lse=None, labels=None, alpha: float = 1.0, weight=None, stream=None):
+        """run(), learning from a teacher's top logits (and labels, where alpha < 1) instead of labels
+        alone: see ops.distill_xent."""
+        z = self._logits(h, stream)
+        loss, dz = ops.distill_xent(z, top_idx, top, 1.0 / h.shape[0], temperature, top_lse=top_lse, labels=labels,
+                                    alpha=alpha, weight=weight, bias=self.b, dlogits=z, stream=stream)
+        return loss, self._apply(h, dz, stream)
+
+    def _apply(self, h: torch.Tensor, dz: torch.Tensor, stream):
+        """The gradients of h, W and b for the logits' gradient, and the update; returns dh."""
+        n, d = h.shape
+        h4, w4 = h.view(n, 1, 1, d), self.W_lp.view(1, 1, d, self.vocab)
         _, db = ops.bias_relu_bwd(None, dz, dpre=dz, stream=stream)
         dw = ops._empty(stream, (1, 1, d, self.vocab), dtype=torch.float32, device=h.device)
         ops.conv2d_bwd_filter(h4, dz, (1, 1), 1, (0, 0, 0, 0), dw=dw, stream=stream)
@@ -109,4 +125,4 @@ class FullSoftmaxHead:
         ops.conv2d_bwd_input(dz, w4, dh, 1, (0, 0, 0, 0), stream=stream)
         ops.apply_sgd(self.W.view(-1), dw.view(-1), self.lr, shadow=self.W_lp.view(-1), stream=stream)
         ops.apply_sgd(self.b, db, self.lr, stream=stream)
-        return loss, dh.view(n, d)
+        return dh.view(n, d)
