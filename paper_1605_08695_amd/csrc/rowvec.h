@@ -1,0 +1,79 @@
+// 16-byte pieces of rows that start at any element: gfx950 reads and writes 16 bytes at any element
+// address (LLVM's unaligned-access-mode, on for HIP), so rows need no alignment of their own.
+#pragma once
+#include "common.h"
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef u32x4_t u32x4_a2_t __attribute__((aligned(2)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef u32x2_t u32x2_a2_t __attribute__((aligned(2)));
+typedef f32x4_t f32x4_a4_t __attribute__((aligned(4)));
+
+// V elements of T at p as fp32 and back; V = 1, 4 or 8.
+template <typename T, int V>
+struct RowVec;
+
+template <typename T>
+struct RowVec<T, 1> {
+    typedef float raw;
+    __device__ static raw load(const T *p) { return Elem<T>::load(p); }
+    __device__ static void unpack(raw r, float *v) { v[0] = r; }
+    __device__ static void store(T *p, const float *v) { Elem<T>::store(p, v[0]); }
+};
+
+template <>
+struct RowVec<float, 4> {
+    typedef f32x4_t raw;
+    __device__ static raw load(const float *p) { return *reinterpret_cast<const f32x4_a4_t *>(p); }
+    __device__ static void unpack(raw r, float *v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = r[e];
+    }
+    __device__ static void store(float *p, const float *v) {
+        *reinterpret_cast<f32x4_a4_t *>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+    }
+};
+
+template <>
+struct RowVec<float, 8> {
+    struct raw {
+        f32x4_t a, b;
+    };
+    __device__ static raw load(const float *p) { return {RowVec<float, 4>::load(p), RowVec<float, 4>::load(p + 4)}; }
+    __device__ static void unpack(const raw &r, float *v) {
+        RowVec<float, 4>::unpack(r.a, v);
+        RowVec<float, 4>::unpack(r.b, v + 4);
+    }
+    __device__ static void store(float *p, const float *v) {
+        RowVec<float, 4>::store(p, v);
+        RowVec<float, 4>::store(p + 4, v + 4);
+    }
+};
+
+template <>
+struct RowVec<bf16_t, 4> {
+    typedef u32x2_t raw;
+    __device__ static raw load(const bf16_t *p) { return *reinterpret_cast<const u32x2_a2_t *>(p); }
+    __device__ static void store(bf16_t *p, const float *v) {
+        *reinterpret_cast<u32x2_a2_t *>(p) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    }
+};
+
+template <>
+struct RowVec<bf16_t, 8> {
+    typedef u32x4_t raw;
+    __device__ static raw load(const bf16_t *p) { return *reinterpret_cast<const u32x4_a2_t *>(p); }
+    __device__ static void unpack(raw r, float *v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = bf16_to_f32(r[e] & 0xffffu);
+            v[2 * e + 1] = __uint_as_float(r[e] & 0xffff0000u);
+        }
+    }
+    __device__ static void store(bf16_t *p, const float *v) {
+        u32x4_t r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+        *reinterpret_cast<u32x4_a2_t *>(p) = r;
+    }
+};
