@@ -547,8 +547,8 @@ TFK_API tfk_status tfk_embedding_apply_sgd(float *var, uint16_t *var_bf16, int64
                                    int64_t n, const void *dy, tfk_dtype dt, int64_t dy_ld, float scale, float lr,
                                    void *ws, size_t ws_bytes, void *stream);
 
-/* Workspace of the two operations above (of Section 4.2), for n tokens; 0 for arguments they refuse and where n or
- * rows is 0. */
+/* Workspace of the two operations above (of Section 4.2), for n tokens; 0 for arguments they refuse, and where
+ * they need none (few tokens, no rows). */
 TFK_API size_t tfk_embedding_workspace_bytes(int64_t n, int32_t d, int64_t rows);
 
 /* Momentum, in place (Section 4.1 lists it among the optimizers built from

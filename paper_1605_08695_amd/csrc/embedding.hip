@@ -171,7 +171,7 @@ __device__ __forceinline__ void zero_rows(float *dst, int d, uint32_t rows, uint
         }
         return;
     }
-    const int total = local_rows * d;                 // (at most 960 * 255)
+    const int total = local_rows * d;                 // (at most 1024 * 255)
     for (int e = threadIdx.x; e < total; e += NT) {
         const int l = e / d;
         const uint32_t row = place_row(bucket, l, gs, bb);
@@ -179,53 +179,124 @@ __device__ __forceinline__ void zero_rows(float *dst, int d, uint32_t rows, uint
     }
 }
 
-// A stable counting sort of the tokens by row in one launch.  Workgroup b reads all n ids (they stay in
-// the caches), counts those of its bucket per row and wave (each wave has a contiguous range of the
-// tokens) and those of the buckets before it, which gives every (row, wave) its first place, and reads
-// the ids again to put each token into its place: first by bucket, then by row, then by token.  Tokens
-// outside [0, rows) are left out; *nvalid is the number of the others.  zero (or null): the table whose
-// rows without tokens are cleared on the way.
-constexpr int kGroupThreads = 1024, kGroupWaves = kGroupThreads / 64;
+// One bucket's part of a stable counting sort of the tokens by row: a workgroup of NW waves reads all n
+// ids (they stay in the caches), counts those of its bucket per row and wave (each wave has a contiguous
+// range of the tokens), which gives every (row, wave) its first place, and puts each token into its place:
+// by row, then by token.  Ids outside [0, rows) are in no bucket.  A lane keeps its first KEEP ids in
+// registers, and a bit for those of the bucket, between the two turns; further ones are read and placed
+// again (n > NW * 64 * KEEP).
+template <int NW, int KEEP>
+struct BucketSort {
+    static_assert(KEEP <= 64, "one bit per kept id");
+    const int32_t *ids;
+    uint32_t rows, mine, lo, hi;           // this wave's tokens: [lo, hi)
+    int gs, bb, lane, wave;
+    uint32_t v[KEEP];
+    uint64_t hits;
 
-__global__ __launch_bounds__(kGroupThreads) void embed_group_kernel(const int32_t *__restrict__ ids, uint32_t n,
-                                                                    uint32_t rows, int gs, int bb, int local_rows,
-                                                                    int32_t *__restrict__ order,
-                                                                    int32_t *__restrict__ key,
-                                                                    int32_t *__restrict__ nvalid,
-                                                                    float *__restrict__ zero, int d) {
-    extern __shared__ uint32_t cnt[];                 // [local row][wave], and the end
-    __shared__ uint32_t red[2][kGroupWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t mine = blockIdx.x;
-    const int entries = local_rows * kGroupWaves;
-    for (int e = tid; e < entries; e += kGroupThreads) cnt[e] = 0;
-    __syncthreads();
-    const uint32_t per = ((n + kGroupWaves - 1) / kGroupWaves + 63) / 64 * 64;
-    const uint32_t lo = min(n, wave * per), hi = min(n, lo + per);
-    uint32_t before = 0;
-    for (uint32_t base = lo; base < hi; base += 256) {
-        uint32_t v[4];
+    __device__ BucketSort(const int32_t *ids_, uint32_t n, uint32_t rows_, int gs_, int bb_, uint32_t mine_)
+        : ids(ids_), rows(rows_), mine(mine_), gs(gs_), bb(bb_), lane(threadIdx.x & 63),
+          wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), hits(0) {
+        const uint32_t per = ((n + NW - 1) / NW + 63) / 64 * 64;
+        lo = min(n, wave * per);
+        hi = min(n, lo + per);
+    }
+
+    // the bucket of an id (~0: none) and its row's place there
+    __device__ __forceinline__ uint32_t place(uint32_t id, uint32_t &local) const {
+        uint32_t b;
+        row_place(id, gs, bb, b, local);
+        return id < rows ? b : ~0u;
+    }
+
+    // Counts into cnt[local row][wave]; returns this lane's ids of the buckets before.
+    __device__ __forceinline__ uint32_t count(uint32_t *cnt) {
+        uint32_t before = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t i = base + e * 64 + lane;
+        for (int e = 0; e < KEEP; ++e) {
+            if (lo + e * 64 >= hi) break;
+            const uint32_t i = lo + e * 64 + lane;
             v[e] = i < hi ? (uint32_t)ids[i] : ~0u;
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t b, l;
-            row_place(v[e], gs, bb, b, l);
-            const bool ok = v[e] < rows;
-            before += ok && b < mine;
-            if (ok && b == mine) atomicAdd(&cnt[l * kGroupWaves + wave], 1u);
+        for (int e = 0; e < KEEP; ++e) {
+            if (lo + e * 64 >= hi) break;
+            uint32_t l;
+            const uint32_t b = place(v[e], l);
+            before += b < mine;
+            if (b == mine) {
+                atomicAdd(&cnt[l * NW + wave], 1u);
+                hits |= 1ull << e;
+            }
+        }
+        for (uint32_t base = lo + KEEP * 64; base < hi; base += 512) {
+            uint32_t x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t i = base + e * 64 + lane;
+                x[e] = i < hi ? (uint32_t)ids[i] : ~0u;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t l;
+                const uint32_t b = place(x[e], l);
+                before += b < mine;
+                if (b == mine) atomicAdd(&cnt[l * NW + wave], 1u);
+            }
+        }
+        return before;
+    }
+
+    // One id a lane: put(place, token, row) for the lanes with ok, in the order of the lanes.
+    template <typename F>
+    __device__ __forceinline__ void step(uint32_t *cnt, uint32_t base, uint32_t id, bool ok, F put) const {
+        uint64_t left = __ballot(ok);
+        while (left) {                                // one turn per distinct row among the lanes
+            const int lead = __ffsll((unsigned long long)left) - 1;
+            const uint32_t row = __builtin_amdgcn_readlane(id, lead);
+            const bool same = ok && id == row;
+            const uint64_t m = __ballot(same);
+            uint32_t p = 0;
+            if (lane == lead) {
+                uint32_t b, l;
+                row_place(row, gs, bb, b, l);
+                p = atomicAdd(&cnt[l * NW + wave], (uint32_t)__popcll(m));
+            }
+            p = __builtin_amdgcn_readlane(p, lead);
+            if (same) put(p + (uint32_t)__popcll(m & ((1ull << lane) - 1ull)), base + lane, row);
+            left &= ~m;
         }
     }
-    for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
-    if (lane == 0) red[0][wave] = before;
-    __syncthreads();
-    before = 0;
-    for (int w = 0; w < kGroupWaves; ++w) before += red[0][w];
-    // exclusive sums over (row, wave), the buckets before added
-    const int each = (entries + kGroupThreads - 1) / kGroupThreads;
+
+    // Places the tokens; cnt: each (row, wave)'s first place, which moves to the next one's.
+    template <typename F>
+    __device__ __forceinline__ void put(uint32_t *cnt, F f) const {
+#pragma unroll
+        for (int e = 0; e < KEEP; ++e) {
+            if (lo + e * 64 >= hi) break;
+            step(cnt, lo + e * 64, v[e], (hits >> e) & 1, f);
+        }
+        for (uint32_t base = lo + KEEP * 64; base < hi; base += 512) {
+            uint32_t x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t i = base + e * 64 + lane;
+                x[e] = i < hi ? (uint32_t)ids[i] : ~0u;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t l;
+                step(cnt, base + e * 64, x[e], place(x[e], l) == mine, f);
+            }
+        }
+    }
+};
+
+// Exclusive sums of cnt[0 .. entries) in place, from `at`; cnt[entries] and the result are the end.
+template <int NW>
+__device__ __forceinline__ uint32_t scan_counts(uint32_t *cnt, int entries, uint32_t at, uint32_t *red) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int each = (entries + NW * 64 - 1) / (NW * 64);
     const int e0 = min(entries, tid * each), e1 = min(entries, e0 + each);
     uint32_t own = 0;
     for (int e = e0; e < e1; ++e) own += cnt[e];
@@ -234,28 +305,81 @@ __global__ __launch_bounds__(kGroupThreads) void embed_group_kernel(const int32_
         const uint32_t up = __shfl_up(incl, o, 64);
         if (lane >= o) incl += up;
     }
-    if (lane == 63) red[1][wave] = incl;
+    if (lane == 63) red[wave] = incl;
     __syncthreads();
-    uint32_t at = before + incl - own;
-    uint32_t all = before;
-    for (int w = 0; w < kGroupWaves; ++w) {
-        if (w < wave) at += red[1][w];
-        all += red[1][w];
+    uint32_t end = at;
+    at += incl - own;
+    for (int w = 0; w < NW; ++w) {
+        if (w < wave) at += red[w];
+        end += red[w];
     }
     for (int e = e0; e < e1; ++e) {
         const uint32_t c = cnt[e];
         cnt[e] = at;
         at += c;
     }
-    if (tid == 0) {
-        cnt[entries] = all;
-        if (mine == gridDim.x - 1) *nvalid = (int32_t)all;
-    }
+    if (tid == 0) cnt[entries] = end;
     __syncthreads();
-    if (zero != nullptr) {
-        zero_rows<kGroupThreads>(zero, d, rows, mine, gs, bb, local_rows, [&](int l) { return cnt[l * kGroupWaves]; });
-        __syncthreads();
+    return end;
+}
+
+// ------------------------------------------------------------------ many tokens: a sort in two launches
+// Stable, by a digit of the id ((id >> shift) & mask): one round sorts tables of up to 2^kDigitBits rows,
+// two rounds (low digit first) all others.
+//   tiles    each workgroup sorts its contiguous range of the tokens by bucket and leaves where each of the
+//            256 buckets begins in it
+//   buckets  each workgroup takes its bucket's tokens out of every tile, in order, and sorts them by row;
+//            the tokens of the buckets before are the sum of the tiles' beginnings of its own
+// Round two and the sums read the number of tokens left (those with ids in the table) from *nvalid.
+constexpr int kDigitBits = 18, kTileWaves = 4, kTileThreads = 64 * kTileWaves, kBuckets = 256, kMostTiles = 512;
+constexpr int kBucketWaves = 8, kBucketThreads = 64 * kBucketWaves;
+
+struct Digit {
+    int shift, gs;
+    uint32_t mask, rows;
+    __device__ __forceinline__ void place(uint32_t id, uint32_t &bucket, uint32_t &local) const {
+        row_place((id >> shift) & mask, gs, 8, bucket, local);
     }
+};
+
+// The lanes with ok whose x has the same low `bits` bits as this lane's.
+template <int MOST>
+__device__ __forceinline__ uint64_t same_lanes(uint32_t x, int bits, bool ok) {
+    uint64_t m = __ballot(ok);
+#pragma unroll
+    for (int b = 0; b < MOST; ++b) {
+        if (b >= bits) break;
+        const bool one = (x >> b) & 1u;
+        const uint64_t w = __ballot(one);
+        m &= one ? w : ~w;
+    }
+    return m;
+}
+
+// The next places of this lane's entry in cnt[entry][wave], in the order of the lanes (same: the lanes
+// with the same entry; lanes without ok get nothing).
+__device__ __forceinline__ uint32_t take_places(uint32_t *entry, uint64_t same, bool ok, int lane) {
+    const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+    uint32_t p = 0;
+    if (ok && rank == 0) p = atomicAdd(entry, (uint32_t)__popcll(same));
+    return __shfl(p, ok ? __ffsll((unsigned long long)same) - 1 : lane, 64) + rank;
+}
+
+__global__ __launch_bounds__(kTileThreads) void embed_tile_kernel(const int32_t *__restrict__ ids,
+                                                                  const int32_t *__restrict__ tokens, uint32_t n,
+                                                                  const int32_t *__restrict__ nvalid, Digit g,
+                                                                  uint32_t tile, int32_t *__restrict__ ttok,
+                                                                  int32_t *__restrict__ tkey,
+                                                                  int32_t *__restrict__ begin) {
+    __shared__ uint32_t cnt[kBuckets * kTileWaves + 1];
+    __shared__ uint32_t red[kTileWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (nvalid != nullptr) n = (uint32_t)*nvalid;
+    for (int e = threadIdx.x; e < kBuckets * kTileWaves; e += kTileThreads) cnt[e] = 0;
+    __syncthreads();
+    const uint32_t t0 = min(n, blockIdx.x * tile), t1 = min(n, t0 + tile);
+    const uint32_t per = (tile / kTileWaves + 63) / 64 * 64;
+    const uint32_t lo = min(t1, t0 + wave * per), hi = min(t1, lo + per);
     for (uint32_t base = lo; base < hi; base += 256) {
         uint32_t v[4];
 #pragma unroll
@@ -266,34 +390,145 @@ __global__ __launch_bounds__(kGroupThreads) void embed_group_kernel(const int32_
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             uint32_t b, l;
-            row_place(v[e], gs, bb, b, l);
-            const bool ok = v[e] < rows && b == mine;
-            uint64_t left = __ballot(ok);
-            while (left) {                            // one turn per distinct row among the lanes
-                const int lead = __ffsll((unsigned long long)left) - 1;
-                const uint32_t row = __builtin_amdgcn_readlane(v[e], lead);
-                const bool same = ok && v[e] == row;
-                const uint64_t m = __ballot(same);
-                uint32_t p = 0;
-                if (lane == lead) p = atomicAdd(&cnt[l * kGroupWaves + wave], (uint32_t)__popcll(m));
-                p = __builtin_amdgcn_readlane(p, lead);
-                if (same) {
-                    p += (uint32_t)__popcll(m & ((1ull << lane) - 1ull));
-                    order[p] = (int32_t)(base + e * 64 + lane);
-                    key[p] = (int32_t)row;
-                }
-                left &= ~m;
+            g.place(v[e], b, l);
+            if (v[e] < g.rows) atomicAdd(&cnt[b * kTileWaves + wave], 1u);
+        }
+    }
+    __syncthreads();
+    scan_counts<kTileWaves>(cnt, kBuckets * kTileWaves, 0, red);
+    int32_t *const mine = begin + (int64_t)blockIdx.x * (kBuckets + 1);
+    for (int e = threadIdx.x; e <= kBuckets; e += kTileThreads) mine[e] = (int32_t)cnt[e * kTileWaves];
+    __syncthreads();
+    for (uint32_t base = lo; base < hi; base += 256) {
+        uint32_t v[4], tok[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t i = base + e * 64 + lane;
+            v[e] = i < hi ? (uint32_t)ids[i] : ~0u;
+            tok[e] = tokens != nullptr && i < hi ? (uint32_t)tokens[i] : i;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t b, l;
+            g.place(v[e], b, l);
+            const bool ok = v[e] < g.rows;
+            const uint32_t p = take_places(&cnt[b * kTileWaves + wave], same_lanes<8>(b, 8, ok), ok, lane);
+            if (ok) {
+                ttok[t0 + p] = (int32_t)tok[e];
+                tkey[t0 + p] = (int32_t)v[e];
+            }
+        }
+    }
+}
+
+// zero (or null): the table whose rows without tokens are cleared on the way (one round only).
+__global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int32_t *__restrict__ ttok,
+                                                                      const int32_t *__restrict__ tkey,
+                                                                      const int32_t *__restrict__ begin, int tiles,
+                                                                      uint32_t tile, Digit g, int local_rows,
+                                                                      int local_bits, int32_t *__restrict__ order,
+                                                                      int32_t *__restrict__ key,
+                                                                      int32_t *__restrict__ nvalid,
+                                                                      float *__restrict__ zero, int d) {
+    extern __shared__ uint32_t cnt[];                 // [local row][wave], and the end
+    __shared__ uint32_t pre[kMostTiles + 1], src[kMostTiles];        // a tile's first entry; where it is
+    __shared__ uint32_t red[2][kBucketWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int entries = local_rows * kBucketWaves;
+    uint32_t s = 0, e = 0;
+    if (tid < tiles) {
+        s = (uint32_t)begin[(int64_t)tid * (kBuckets + 1) + blockIdx.x];
+        e = (uint32_t)begin[(int64_t)tid * (kBuckets + 1) + blockIdx.x + 1];
+    }
+    for (int q = tid; q < entries; q += kBucketThreads) cnt[q] = 0;
+    uint32_t incl = e - s, before = s;
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t up = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += up;
+    }
+    for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
+    if (lane == 63) {
+        red[0][wave] = incl;
+        red[1][wave] = before;
+    }
+    __syncthreads();
+    uint32_t at = incl - (e - s), m = 0;
+    before = 0;
+    for (int w = 0; w < kBucketWaves; ++w) {
+        if (w < wave) at += red[0][w];
+        m += red[0][w];
+        before += red[1][w];
+    }
+    pre[tid] = at;
+    src[tid] = tid * tile + s;
+    if (tid == 0) pre[kMostTiles] = m;
+    __syncthreads();
+    // entry i of the bucket: in the last tile whose first is not behind it
+    const auto where = [&](uint32_t i) {
+        int t = 0;
+#pragma unroll
+        for (int step = kMostTiles / 2; step > 0; step >>= 1)
+            if (pre[t + step] <= i) t += step;
+        return src[t] + (i - pre[t]);
+    };
+    const uint32_t per = ((m + kBucketWaves - 1) / kBucketWaves + 63) / 64 * 64;
+    const uint32_t lo = min(m, wave * per), hi = min(m, lo + per);
+    constexpr int KEEP = 4;
+    uint32_t at_[KEEP], id[KEEP];
+    for (uint32_t base = lo; base < hi; base += KEEP * 64) {
+#pragma unroll
+        for (int q = 0; q < KEEP; ++q) {
+            const uint32_t i = base + q * 64 + lane;
+            at_[q] = where(i < hi ? i : lo);
+            id[q] = (uint32_t)tkey[at_[q]];
+        }
+#pragma unroll
+        for (int q = 0; q < KEEP; ++q) {
+            uint32_t b, l;
+            g.place(id[q], b, l);
+            if (base + q * 64 + lane < hi) atomicAdd(&cnt[l * kBucketWaves + wave], 1u);
+        }
+    }
+    __syncthreads();
+    const uint32_t end = scan_counts<kBucketWaves>(cnt, entries, before, red[0]);
+    if (blockIdx.x == kBuckets - 1 && tid == 0) *nvalid = (int32_t)end;
+    if (zero != nullptr) {
+        zero_rows<kBucketThreads>(zero, d, g.rows, blockIdx.x, g.gs, 8, local_rows,
+                                  [&](int l) { return cnt[l * kBucketWaves]; });
+        __syncthreads();
+    }
+    for (uint32_t base = lo; base < hi; base += KEEP * 64) {
+        if (per > KEEP * 64) {                        // (else they are still at hand)
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q) {
+                const uint32_t i = base + q * 64 + lane;
+                at_[q] = where(i < hi ? i : lo);
+                id[q] = (uint32_t)tkey[at_[q]];
+            }
+        }
+        uint32_t tok[KEEP];
+#pragma unroll
+        for (int q = 0; q < KEEP; ++q) tok[q] = (uint32_t)ttok[at_[q]];
+#pragma unroll
+        for (int q = 0; q < KEEP; ++q) {
+            uint32_t b, l;
+            g.place(id[q], b, l);
+            const bool ok = base + q * 64 + lane < hi;
+            const uint32_t p = take_places(&cnt[l * kBucketWaves + wave], same_lanes<10>(l, local_bits, ok), ok, lane);
+            if (ok) {
+                order[p] = (int32_t)tok[q];
+                key[p] = (int32_t)id[q];
             }
         }
     }
 }
 
 // ------------------------------------------------------------------ sums of the grouped tokens
-// A wave sums `chunk` consecutive grouped tokens over 64 * V columns, eight rows of dy in flight, and
-// finishes each row of the table whose tokens begin and end in the chunk.  Sums of a row that goes on
-// over the chunk's borders are left in part: [chunk][0] the one that began before, [chunk][1] the one that
-// begins here and goes on.
-constexpr int kMaxChunk = 64;
+// A wave sums the grouped tokens of `chunk` places over 64 * V columns, eight rows of dy in flight, and
+// finishes the rows of the table that begin there and end there or in the next chunk.  A row that goes on
+// beyond (it covers the whole of a chunk that it does not begin in) is left in parts: [chunk][1] in the chunk
+// where it begins, [chunk][0] in the others.
+constexpr int kMaxChunk = 32;
 
 template <typename T, int V, int MODE>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy, int64_t dld, int d, int cblocks, int chunk,
@@ -303,47 +538,66 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy
                                                         float *__restrict__ dst, bf16_t *__restrict__ sh,
                                                         float *__restrict__ part) {
     const int lane = threadIdx.x & 63;
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t ch = wave / cblocks;
-    const int cb = (int)(wave - ch * cblocks);
+    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t ch = id / cblocks;
+    const int cb = (int)(id - ch * cblocks);
     const int nv = *nvalid;
-    const int64_t p0 = ch * chunk;
+    const int64_t p0 = ch * chunk, p1 = p0 + chunk, p2 = p1 + chunk;
     if (p0 >= nv) return;
-    const int cnt = (int)min((int64_t)chunk, nv - p0);
-    // lane l: token and row of place p0 + l; the row before and the row behind
-    const int tok = lane < cnt ? order[p0 + lane] : 0;
-    const int row = lane < cnt ? key[p0 + lane] : -1;
-    const int prev = p0 > 0 ? key[p0 - 1] : -1, next = p0 + cnt < nv ? key[p0 + cnt] : -1;
+    // lane l: token and row of place p0 + l, of this chunk and the next (-1: past the end)
+    const bool in = lane < 2 * chunk && p0 + lane < nv;
+    const int tok = in ? order[p0 + lane] : 0;
+    const int row = in ? key[p0 + lane] : -1;
+    // the rows before, a chunk before, and behind the next chunk
+    const int prev = p0 > 0 ? key[p0 - 1] : -1, prev2 = p0 > chunk ? key[p0 - chunk - 1] : -1;
+    const int behind = p2 < nv ? key[p2] : -1;
+    const auto row_at = [&](int i) { return i < 64 ? __builtin_amdgcn_readlane(row, i) : -1; };
+    const int at1 = p1 < nv ? (chunk < 64 ? row_at(chunk) : -1) : -1;          // the row at the next chunk's first place
+    int cur = row_at(0);
+    bool head = cur == prev;                          // it began before
+    int i = 0;
+    if (head && prev2 != cur && at1 != cur) {         // in the chunk before, and it ends here: not ours
+        const uint64_t other = __ballot(lane < chunk && row != cur);
+        if (other == 0) return;
+        i = __ffsll((unsigned long long)other) - 1;
+        cur = row_at(i);
+        head = false;
+        if (cur < 0) return;
+    }
+    // the last place of this wave: of the chunk, or of the row that goes on into the next and ends there
+    const int last = row_at(chunk - 1);
+    const uint64_t ours = __ballot(row >= 0 && (lane < chunk || (lane < 2 * chunk && row == last)));
+    const bool goes_on = last >= 0 && at1 == last;
+    const bool part1 = goes_on && (behind == last || (head && cur == last));   // ... as a part
+    const int end = goes_on && !part1 ? __popcll(ours) : (int)min((int64_t)chunk, nv - p0);
     int skip;
     const int c0 = lane_columns<V>(d, cb, lane, skip);
     const bool act = skip < V;
     float acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    int cur = __builtin_amdgcn_readlane(row, 0);
-    bool head = cur == prev;
-    float *const slot = part + ch * 2 * d;
-    for (int i0 = 0; i0 < cnt; i0 += 8) {
+    float *const slot = part + ch * 2 * d + c0;
+    const auto finish = [&](bool as_part, bool began) {
+        if (!act) return;
+        if (as_part) {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e >= skip) slot[(began ? d : 0) + e] = acc[e];
+        } else {
+            row_finish<MODE, V>(dst, sh, (int64_t)cur * d + c0, acc, skip, scale, lr);
+        }
+    };
+    for (; i < end; i += 8) {
         typename RowVec<T, V>::raw buf[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int t = __builtin_amdgcn_readlane(tok, i0 + u);      // (token 0 past the end: not used)
-            if (act) buf[u] = RowVec<T, V>::load(dy + t * dld + c0);
-        }
+        for (int u = 0; u < 8; ++u)
+            if (i + u < end && act) buf[u] = RowVec<T, V>::load(dy + __builtin_amdgcn_readlane(tok, i + u) * dld + c0);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            if (i0 + u >= cnt) break;
-            const int r = __builtin_amdgcn_readlane(row, i0 + u);
+            if (i + u >= end) break;
+            const int r = __builtin_amdgcn_readlane(row, i + u);
             if (r != cur) {
-                if (act) {
-                    if (head) {
-#pragma unroll
-                        for (int e = 0; e < V; ++e)
-                            if (e >= skip) slot[c0 + e] = acc[e];
-                    } else {
-                        row_finish<MODE, V>(dst, sh, (int64_t)cur * d + c0, acc, skip, scale, lr);
-                    }
-                }
+                finish(head, false);
                 cur = r;
                 head = false;
 #pragma unroll
@@ -355,112 +609,264 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy
             for (int e = 0; e < V; ++e) acc[e] += f[e];
         }
     }
-    if (!act) return;
-    if (!head && next != cur) {
-        row_finish<MODE, V>(dst, sh, (int64_t)cur * d + c0, acc, skip, scale, lr);
-    } else {
-        float *o = slot + (head ? 0 : d) + c0;
+    finish(head || part1, !head);
+}
+
+// The rows in parts.  A workgroup looks through kJoinWaves chunks, a wave each, for one that a row in parts
+// begins in; its parts over 64 * V columns are then added up by all waves, a contiguous share each, joined
+// in their order.
+constexpr int kJoinWaves = 8;
+
+template <int V, int MODE>
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(int d, int cblocks, int chunk, int64_t groups,
+                                                                     const int32_t *__restrict__ key,
+                                                                     const int32_t *__restrict__ nvalid, float scale,
+                                                                     float lr, float *__restrict__ dst,
+                                                                     bf16_t *__restrict__ sh,
+                                                                     const float *__restrict__ part) {
+    __shared__ float sums[kJoinWaves - 1][64][V + 1];
+    __shared__ int begins[kJoinWaves];                // the row in parts that begins in the wave's chunk, or -1
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int nv = *nvalid;
+    for (int64_t b = blockIdx.x; b < groups; b += gridDim.x) {
+        const int64_t ch0 = b / cblocks * kJoinWaves;
+        const int cb = (int)(b % cblocks);
+        if ((ch0 + 2) * chunk >= nv) return;          // (no chunk from here on has two behind it)
+        const int64_t p0 = (ch0 + wave) * chunk, p1 = p0 + chunk, p2 = p1 + chunk;
+        int row = -1;
+        if (p2 < nv) {
+            const int last = key[p1 - 1];
+            if (key[p1] == last && key[p2] == last && !(p0 > 0 && key[p0 - 1] == last)) row = last;
+        }
+        __syncthreads();
+        if (lane == 0) begins[wave] = row;
+        __syncthreads();
+        for (int w = 0; w < kJoinWaves; ++w) {
+            const int cur = begins[w];
+            if (cur < 0) continue;                    // (uniform over the workgroup)
+            const int64_t ch = ch0 + w;
+            // the number of chunks behind this one that the row is the first of
+            int64_t more = 2;
+            for (;;) {
+                const int64_t q = (ch + 1 + more + lane) * chunk;
+                const uint64_t stop = __ballot(q >= nv || key[q] != cur);
+                if (stop) {
+                    more += __ffsll((unsigned long long)stop) - 1;
+                    break;
+                }
+                more += 64;
+            }
+            int skip;
+            const int c0 = lane_columns<V>(d, cb, lane, skip);
+            float acc[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (e >= skip) o[e] = acc[e];
+            for (int e = 0; e < V; ++e) acc[e] = 0.f;
+            // part 0: this chunk's [1]; part i: chunk ch + i's [0]
+            const int64_t each = (more + 1 + kJoinWaves - 1) / kJoinWaves, i0 = wave * each, i1 = min(more + 1, i0 + each);
+            if (skip < V)
+                for (int64_t i = i0; i < i1; i += 8) {
+                    typename RowVec<float, V>::raw buf[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const int64_t j = min(i + u, i1 - 1);
+                        buf[u] = RowVec<float, V>::load(part + ((ch + j) * 2 + (j == 0)) * d + c0);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        if (i + u >= i1) break;
+                        float f[V];
+                        RowVec<float, V>::unpack(buf[u], f);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) acc[e] += f[e];
+                    }
+                }
+            if (wave > 0)
+#pragma unroll
+                for (int e = 0; e < V; ++e) sums[wave - 1][lane][e] = acc[e];
+            __syncthreads();
+            if (wave == 0 && skip < V) {
+                for (int x = 0; x < kJoinWaves - 1; ++x)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] += sums[x][lane][e];
+                row_finish<MODE, V>(dst, sh, (int64_t)cur * d + c0, acc, skip, scale, lr);
+            }
+            __syncthreads();
+        }
     }
 }
 
-// The rows that go over chunk borders: workgroup (chunk, 64 * V columns), for the row that begins in the
-// chunk and goes on, adds up its part of every chunk, each of 4 waves a contiguous quarter, then the four.
-template <int V, int MODE>
-__global__ __launch_bounds__(256) void embed_join_kernel(int d, int cblocks, int chunk, const int32_t *__restrict__ key,
-                                                         const int32_t *__restrict__ nvalid, float scale, float lr,
-                                                         float *__restrict__ dst, bf16_t *__restrict__ sh,
-                                                         const float *__restrict__ part) {
-    __shared__ float sums[3][64][V + 1];
+// ------------------------------------------------------------------ few tokens: one launch
+// A workgroup sorts its bucket's tokens into LDS and sums its rows itself.  A row of more than kAlone
+// tokens is summed by all waves, each a contiguous part of its tokens, joined in their order; the others
+// go to the waves in turn, per block of columns.
+constexpr int kSmallWaves = 4, kSmallThreads = 64 * kSmallWaves, kAlone = 16;
+
+template <typename T, int V, int MODE, int KEEP>
+__global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__restrict__ dy, int64_t dld, int d,
+                                                                    int cblocks, const int32_t *__restrict__ ids,
+                                                                    uint32_t n, uint32_t rows, int gs, int bb,
+                                                                    int local_rows, float scale, float lr,
+                                                                    float *__restrict__ dst, bf16_t *__restrict__ sh) {
+    extern __shared__ uint32_t cnt[];                 // [local row][wave], the end, then the tokens (16 bits each)
+    __shared__ uint32_t red[kSmallWaves];
+    __shared__ float sums[kSmallWaves - 1][64][V + 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int nv = *nvalid;
-    for (int64_t b = blockIdx.x;; b += gridDim.x) {
-        const int64_t ch = b / cblocks;
-        const int cb = (int)(b - ch * cblocks);
-        const int64_t p0 = ch * chunk, p1 = p0 + chunk;
-        if (p1 >= nv) return;
-        const int cur = key[p1 - 1];
-        if (key[p1] != cur || (p0 > 0 && key[p0 - 1] == cur)) continue;    // ends here, or began before
-        // the number of chunks that the row is the first of
-        int64_t more = 1;
-        for (;;) {
-            const int64_t q = (ch + 1 + more + lane) * chunk;
-            const uint64_t stop = __ballot(q >= nv || key[q] != cur);
-            if (stop) {
-                more += __ffsll((unsigned long long)stop) - 1;
-                break;
-            }
-            more += 64;
-        }
-        int skip;
-        const int c0 = lane_columns<V>(d, cb, lane, skip);
-        float acc[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = 0.f;
-        // entry 0: this chunk's [1]; entry i: chunk ch + i's [0]
-        const int64_t each = (more + 1 + 3) / 4, i0 = wave * each, i1 = min(more + 1, i0 + each);
-        if (skip < V)
-            for (int64_t i = i0; i < i1; ++i) {
-                const float *p = part + ((ch + i) * 2 + (i == 0)) * d + c0;
-                float f[V];
-                RowVec<float, V>::unpack(RowVec<float, V>::load(p), f);
-#pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += f[e];
-            }
-        if (wave > 0)
-#pragma unroll
-            for (int e = 0; e < V; ++e) sums[wave - 1][lane][e] = acc[e];
-        __syncthreads();
-        if (wave == 0 && skip < V) {
-            for (int w = 0; w < 3; ++w)
-#pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += sums[w][lane][e];
-            row_finish<MODE, V>(dst, sh, (int64_t)cur * d + c0, acc, skip, scale, lr);
-        }
+    const int entries = local_rows * kSmallWaves;
+    uint16_t *const list = (uint16_t *)(cnt + entries + 1);
+    for (int e = threadIdx.x; e < entries; e += kSmallThreads) cnt[e] = 0;
+    __syncthreads();
+    BucketSort<kSmallWaves, KEEP> sort(ids, n, rows, gs, bb, blockIdx.x);
+    (void)sort.count(cnt);
+    __syncthreads();
+    scan_counts<kSmallWaves>(cnt, entries, 0, red);
+    if (MODE == kStore) {
+        zero_rows<kSmallThreads>(dst, d, rows, blockIdx.x, gs, bb, local_rows, [&](int l) { return cnt[l * kSmallWaves]; });
         __syncthreads();
     }
+    sort.put(cnt, [&](uint32_t p, uint32_t token, uint32_t) { list[p] = (uint16_t)token; });
+    __syncthreads();
+    // (every (row, wave)'s place has moved to the next one's first)
+    const auto first = [&](int l) { return l == 0 ? 0u : cnt[l * kSmallWaves - 1]; };
+    int turn = 0;
+    for (int l0 = 0; l0 < local_rows; l0 += 64) {
+        const int l = l0 + lane;
+        uint64_t some = __ballot(l < local_rows && first(l) != first(min(l + 1, local_rows)));
+        while (some) {
+            const int j = l0 + __ffsll((unsigned long long)some) - 1;
+            some &= some - 1;
+            const int b = (int)first(j), e = (int)first(j + 1);
+            const uint32_t row = place_row(blockIdx.x, j, gs, bb);
+            const bool all = e - b > kAlone;          // (uniform over the workgroup, like the loops)
+            for (int cb = 0; cb < cblocks; ++cb) {
+                if (!all && turn++ % kSmallWaves != wave) continue;
+                int skip;
+                const int c0 = lane_columns<V>(d, cb, lane, skip);
+                const int each = all ? (e - b + kSmallWaves - 1) / kSmallWaves : e - b;
+                const int t0 = all ? min(e, b + wave * each) : b, t1 = min(e, t0 + each);
+                float acc[V];
+#pragma unroll
+                for (int q = 0; q < V; ++q) acc[q] = 0.f;
+                if (skip < V)
+                    for (int t = t0; t < t1; t += 8) {
+                        typename RowVec<T, V>::raw buf[8];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u)
+                            if (t + u < t1) buf[u] = RowVec<T, V>::load(dy + list[t + u] * dld + c0);
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            if (t + u >= t1) break;
+                            float f[V];
+                            RowVec<T, V>::unpack(buf[u], f);
+#pragma unroll
+                            for (int q = 0; q < V; ++q) acc[q] += f[q];
+                        }
+                    }
+                if (all) {
+                    if (wave > 0)
+#pragma unroll
+                        for (int q = 0; q < V; ++q) sums[wave - 1][lane][q] = acc[q];
+                    __syncthreads();
+                    if (wave == 0)
+                        for (int w = 0; w < kSmallWaves - 1; ++w)
+#pragma unroll
+                            for (int q = 0; q < V; ++q) acc[q] += sums[w][lane][q];
+                }
+                if (skip < V && (!all || wave == 0))
+                    row_finish<MODE, V>(dst, sh, (int64_t)row * d + c0, acc, skip, scale, lr);
+                if (all) __syncthreads();
+            }
+        }
+    }
 }
+
+constexpr int kSmallTokens = 8192;
 
 static size_t list_bytes(int64_t n) { return ((size_t)n * 4 + 15) / 16 * 16; }
 
-// tokens per wave: 64, and fewer down to 16 where there are less than 4096 waves
+// tokens per wave: 32, or 16 where that makes less than 4096 waves
 static int sum_chunk(int64_t n, int cblocks) {
-    int chunk = kMaxChunk;
-    while (chunk > 16 && (n + chunk - 1) / chunk * cblocks < 4096) chunk /= 2;
-    return chunk;
+    return (n + kMaxChunk - 1) / kMaxChunk * cblocks < 4096 ? kMaxChunk / 2 : kMaxChunk;
 }
 
+struct Tiles {
+    int64_t size, count;
+};
+
+static Tiles tiles_of(int64_t n) {
+    Tiles t;
+    t.count = std::min<int64_t>(kMostTiles, (n + 255) / 256);
+    t.size = ((n + t.count - 1) / t.count + 63) / 64 * 64;
+    t.count = (n + t.size - 1) / t.size;
+    return t;
+}
+
+// Few tokens, and few enough buckets: each of them reads all ids.
+static bool sum_small(int64_t n, int64_t rows) { return n <= kSmallTokens && rows <= ((int64_t)960 << 12); }
+
 size_t embed_ws_bytes(int64_t n, int d, int64_t rows) {
-    if (n == 0 || rows == 0) return 0;
+    if (n == 0 || rows == 0 || sum_small(n, rows)) return 0;
     int64_t chunks = 0;                               // of the type that has more
     for (const int v : {d >= 8 ? 8 : 1, d >= 4 ? 4 : 1}) {
         const int chunk = sum_chunk(n, (d + 64 * v - 1) / (64 * v));
         chunks = std::max(chunks, (n + chunk - 1) / chunk);
     }
-    return 16 + 2 * list_bytes(n) + (size_t)chunks * 2 * d * 4;
+    return 16 + 4 * list_bytes(n) + list_bytes(tiles_of(n).count * (kBuckets + 1)) + (size_t)chunks * 2 * d * 4;
 }
 
 template <typename T, int V>
 static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const int32_t *ids, int64_t rows, float scale,
                             int mode, float lr, float *dst, bf16_t *sh, void *ws, hipStream_t st) {
-    const RowSplit s = row_split(rows, d, 8, 960);
-    int32_t *nvalid = (int32_t *)ws, *order = nvalid + 4, *key = order + list_bytes(n) / 4;
-    float *part = (float *)(key + list_bytes(n) / 4);
-    hipLaunchKernelGGL(embed_group_kernel, dim3(1u << s.bb), dim3(kGroupThreads),
-                       (size_t)s.local * kGroupWaves * 4 + 4, st, ids, (uint32_t)n, (uint32_t)rows, s.gs, s.bb, s.local,
-                       order, key, nvalid, mode == kStore ? dst : nullptr, d);
-    const int cblocks = (d + 64 * V - 1) / (64 * V), chunk = sum_chunk(n, cblocks);
-    const int64_t chunks = (n + chunk - 1) / chunk;
-    const dim3 gs((unsigned)((chunks * cblocks + 3) / 4)), gj((unsigned)std::min<int64_t>(chunks * cblocks, 1 << 22));
+    const int cblocks = (d + 64 * V - 1) / (64 * V);
+    if (sum_small(n, rows)) {
+        const RowSplit s = row_split(rows, d, 10, 960);
+        const size_t lds = ((size_t)s.local * kSmallWaves + 1) * 4 + n * 2;
+#define TFK_GO(MODE, KEEP)                                                                                             \
+    hipLaunchKernelGGL((embed_small_kernel<T, V, MODE, KEEP>), dim3(1u << s.bb), dim3(kSmallThreads), lds, st, dy,     \
+                       dld, d, cblocks, ids, (uint32_t)n, (uint32_t)rows, s.gs, s.bb, s.local, scale, lr, dst, sh)
+        if (n <= 16 * kSmallThreads) {
+            if (mode == kStore) TFK_GO(kStore, 16);
+            else if (mode == kAdd) TFK_GO(kAdd, 16);
+            else TFK_GO(kSgd, 16);
+        } else {
+            if (mode == kStore) TFK_GO(kStore, 32);
+            else if (mode == kAdd) TFK_GO(kAdd, 32);
+            else TFK_GO(kSgd, 32);
+        }
+#undef TFK_GO
+        return hipGetLastError();
+    }
+    const size_t list = list_bytes(n) / 4;
+    const Tiles t = tiles_of(n);
+    int32_t *nvalid = (int32_t *)ws, *order = nvalid + 4, *key = order + list, *ttok = key + list, *tkey = ttok + list,
+            *begin = tkey + list;
+    float *part = (float *)(begin + list_bytes(t.count * (kBuckets + 1)) / 4);
+    const int rounds = rows > ((int64_t)1 << kDigitBits) ? 2 : 1;
+    if (mode == kStore && rounds == 2) {
+        const hipError_t e = launch_fill_zero(dst, rows * d, st);
+        if (e != hipSuccess) return e;
+    }
+    for (int r = 0; r < rounds; ++r) {
+        const int64_t values = rounds == 1 ? rows : (r == 0 ? (int64_t)1 << kDigitBits : ((rows - 1) >> kDigitBits) + 1);
+        const RowSplit s = row_split(values, rounds == 1 ? d : 128, 8, 1024);
+        const Digit g{r == 0 ? 0 : kDigitBits, s.gs, rounds == 2 && r == 0 ? (1u << kDigitBits) - 1 : ~0u, (uint32_t)rows};
+        int bits = 0;
+        while ((1 << bits) < s.local) ++bits;
+        hipLaunchKernelGGL(embed_tile_kernel, dim3((unsigned)t.count), dim3(kTileThreads), 0, st, r == 0 ? ids : key,
+                           r == 0 ? nullptr : order, (uint32_t)n, r == 0 ? nullptr : nvalid, g, (uint32_t)t.size, ttok, tkey,
+                           begin);
+        hipLaunchKernelGGL(embed_bucket_kernel, dim3(kBuckets), dim3(kBucketThreads),
+                           ((size_t)s.local * kBucketWaves + 1) * 4, st, ttok, tkey, begin, (int)t.count, (uint32_t)t.size, g,
+                           s.local, bits, order, key, nvalid, mode == kStore && rounds == 1 ? dst : nullptr, d);
+    }
+    const int chunk = sum_chunk(n, cblocks);
+    const int64_t chunks = (n + chunk - 1) / chunk, groups = (chunks + kJoinWaves - 1) / kJoinWaves * cblocks;
+    const dim3 gs((unsigned)((chunks * cblocks + 3) / 4)), gj((unsigned)std::min<int64_t>(groups, 1 << 20));
 #define TFK_GO(MODE)                                                                                                   \
     do {                                                                                                               \
         hipLaunchKernelGGL((embed_sum_kernel<T, V, MODE>), gs, dim3(256), 0, st, dy, dld, d, cblocks, chunk, order,    \
                            key, nvalid, scale, lr, dst, sh, part);                                                     \
-        if (chunks > 1)                                                                                                \
-            hipLaunchKernelGGL((embed_join_kernel<V, MODE>), gj, dim3(256), 0, st, d, cblocks, chunk, key, nvalid,     \
-                               scale, lr, dst, sh, part);                                                              \
+        hipLaunchKernelGGL((embed_join_kernel<V, MODE>), gj, dim3(64 * kJoinWaves), 0, st, d, cblocks, chunk, groups,  \
+                           key, nvalid, scale, lr, dst, sh, part);                                                     \
     } while (0)
     if (mode == kStore) TFK_GO(kStore);
     else if (mode == kAdd) TFK_GO(kAdd);

@@ -227,7 +227,7 @@ def test_empty_and_special_values():
 
 
 def test_other_stream_and_workspace():
-    n, d, rows = 3000, 96, 1000
+    n, d, rows = 30000, 96, 1000
     rng = np.random.default_rng(8)
     ids = _tokens(rng, n, rows, "zipf")
     dy = torch.randn(n, d, device=DEV)

@@ -50,7 +50,7 @@ _SUM = [
 
 
 def _sum_args(kw):
-    a = dict(dy=P + 0x100000, dt=F32, n=10, ld=0, d=8, ids=P + 0x200000, rows=100, scale=1.0, beta=0.0, dst=P, sh=0,
+    a = dict(dy=P + 0x100000, dt=F32, n=10000, ld=0, d=8, ids=P + 0x200000, rows=100, scale=1.0, beta=0.0, dst=P, sh=0,
              lr=0.1, ws=P + 0x300000, wb=1 << 20)
     a.update(kw)
     return a
@@ -77,8 +77,8 @@ def test_embedding_apply_sgd(lib, kw, status):
 def test_embedding_workspace_bytes(lib):
     q = lib.tfk_embedding_workspace_bytes
     assert q(0, 8, 100) == q(-1, 8, 100) == q(10, 0, 100) == q(10, 8, 0) == q(1 << 31, 8, 100) == q(10, 8, 1 << 31) == 0
-    assert q(1, 1, 1) > 0 and q(1000, 8, 100) >= q(10, 8, 100)
-    assert q(1 << 30, 8, 100) >= 8 << 30 or q(1 << 30, 8, 100) >= 4 << 30
+    assert q(10, 8, 100) == 0                                  # few tokens are sorted on chip
+    assert q(10000, 8, 100) >= 80000 and q(1 << 30, 8, 100) >= 8 << 30
 
 
 @pytest.mark.parametrize("kw,status", [
