@@ -156,26 +156,25 @@ __device__ __forceinline__ int lane_columns(int d, int cb, int lane, int &skip) 
     return skip < V ? (int)(c - skip) : 0;
 }
 
-// Zeros in the rows of a bucket that have no token: first(l) is the number of tokens before local row l.
-template <int NT, typename F>
-__device__ __forceinline__ void zero_rows(float *dst, int d, uint32_t rows, uint32_t bucket, int gs, int bb, int local_rows,
-                                          F first) {
-    if (d >= 256) {                                   // a wave per row, 16 bytes a lane
-        const int lane = threadIdx.x & 63;
-        for (int l = threadIdx.x >> 6; l < local_rows; l += NT / 64) {
-            const uint32_t row = place_row(bucket, l, gs, bb);
-            if (row >= rows || first(l) != first(l + 1)) continue;
-            float *p = dst + (int64_t)row * d;
-            const float z[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int c = lane * 4; c < d; c += 256) RowVec<float, 4>::store(p + min(c, d - 4), z);
+// Zeros in columns [c0, c1) of the n rows row(l) that are in the table and have no token (none(l)), a wave
+// per row, 16 bytes a lane; rows of less than 128 columns an element a thread.
+template <int NT, typename R, typename N>
+__device__ __forceinline__ void zero_rows(float *dst, int d, int c0, int c1, uint32_t rows, int n, R row, N none) {
+    if (d < 128) {
+        const int total = n * d;                      // (at most 1024 * 127)
+        for (int e = threadIdx.x; e < total; e += NT) {
+            const int l = e / d, c = e - l * d;
+            if (row(l) < rows && none(l) && c >= c0 && c < c1) dst[(int64_t)row(l) * d + c] = 0.f;
         }
         return;
     }
-    const int total = local_rows * d;                 // (at most 1024 * 255)
-    for (int e = threadIdx.x; e < total; e += NT) {
-        const int l = e / d;
-        const uint32_t row = place_row(bucket, l, gs, bb);
-        if (row < rows && first(l) == first(l + 1)) dst[(int64_t)row * d + (e - l * d)] = 0.f;
+    const int lane = threadIdx.x & 63;
+    const float z[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int l = threadIdx.x >> 6; l < n; l += NT / 64) {
+        const uint32_t r = row(l);
+        if (r >= rows || !none(l)) continue;
+        float *p = dst + (int64_t)r * d;
+        for (int c = c0 + lane * 4; c < c1; c += 256) RowVec<float, 4>::store(p + min(c, c1 - 4), z);
     }
 }
 
@@ -421,7 +420,7 @@ __global__ __launch_bounds__(kTileThreads) void embed_tile_kernel(const int32_t 
     }
 }
 
-// zero (or null): the table whose rows without tokens are cleared on the way (one round only).
+// used (or null; one round only): a byte per row of the table, 1 for rows with tokens.
 __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int32_t *__restrict__ ttok,
                                                                       const int32_t *__restrict__ tkey,
                                                                       const int32_t *__restrict__ begin, int tiles,
@@ -429,7 +428,7 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
                                                                       int local_bits, int32_t *__restrict__ order,
                                                                       int32_t *__restrict__ key,
                                                                       int32_t *__restrict__ nvalid,
-                                                                      float *__restrict__ zero, int d) {
+                                                                      uint8_t *__restrict__ used) {
     extern __shared__ uint32_t cnt[];                 // [local row][wave], and the end
     __shared__ uint32_t pre[kMostTiles + 1], src[kMostTiles];        // a tile's first entry; where it is
     __shared__ uint32_t red[2][kBucketWaves];
@@ -473,7 +472,7 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
     };
     const uint32_t per = ((m + kBucketWaves - 1) / kBucketWaves + 63) / 64 * 64;
     const uint32_t lo = min(m, wave * per), hi = min(m, lo + per);
-    constexpr int KEEP = 4;
+    constexpr int KEEP = 8;
     uint32_t at_[KEEP], id[KEEP];
     for (uint32_t base = lo; base < hi; base += KEEP * 64) {
 #pragma unroll
@@ -492,9 +491,11 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
     __syncthreads();
     const uint32_t end = scan_counts<kBucketWaves>(cnt, entries, before, red[0]);
     if (blockIdx.x == kBuckets - 1 && tid == 0) *nvalid = (int32_t)end;
-    if (zero != nullptr) {
-        zero_rows<kBucketThreads>(zero, d, g.rows, blockIdx.x, g.gs, 8, local_rows,
-                                  [&](int l) { return cnt[l * kBucketWaves]; });
+    if (used != nullptr) {
+        for (int l = tid; l < local_rows; l += kBucketThreads) {
+            const uint32_t row = place_row(blockIdx.x, l, g.gs, 8);
+            if (row < g.rows) used[row] = cnt[l * kBucketWaves] != cnt[(l + 1) * kBucketWaves];
+        }
         __syncthreads();
     }
     for (uint32_t base = lo; base < hi; base += KEEP * 64) {
@@ -531,8 +532,8 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
 constexpr int kMaxChunk = 32;
 
 template <typename T, int V, int MODE>
-__global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy, int64_t dld, int d, int cblocks, int chunk,
-                                                        const int32_t *__restrict__ order,
+__global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy, int64_t n, int64_t dld, int d, int cblocks,
+                                                        int chunk, const int32_t *__restrict__ order,
                                                         const int32_t *__restrict__ key,
                                                         const int32_t *__restrict__ nvalid, float scale, float lr,
                                                         float *__restrict__ dst, bf16_t *__restrict__ sh,
@@ -541,16 +542,18 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy
     const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t ch = id / cblocks;
     const int cb = (int)(id - ch * cblocks);
-    const int nv = *nvalid;
     const int64_t p0 = ch * chunk, p1 = p0 + chunk, p2 = p1 + chunk;
-    if (p0 >= nv) return;
-    // lane l: token and row of place p0 + l, of this chunk and the next (-1: past the end)
-    const bool in = lane < 2 * chunk && p0 + lane < nv;
-    const int tok = in ? order[p0 + lane] : 0;
-    const int row = in ? key[p0 + lane] : -1;
-    // the rows before, a chunk before, and behind the next chunk
+    if (p0 >= n) return;
+    // lane l: token and row of place p0 + l, of this chunk and the next (-1: past the end); the rows before,
+    // a chunk before, and behind the next chunk.  (One round of loads: places past *nvalid hold anything.)
+    const int nv = *nvalid;
+    const bool there = lane < 2 * chunk && p0 + lane < n;
+    const int t_ = there ? order[p0 + lane] : 0, r_ = there ? key[p0 + lane] : -1;
     const int prev = p0 > 0 ? key[p0 - 1] : -1, prev2 = p0 > chunk ? key[p0 - chunk - 1] : -1;
-    const int behind = p2 < nv ? key[p2] : -1;
+    int behind = p2 < n ? key[p2] : -1;
+    if (p0 >= nv) return;
+    const int tok = p0 + lane < nv ? t_ : 0, row = p0 + lane < nv ? r_ : -1;
+    if (p2 >= nv) behind = -1;
     const auto row_at = [&](int i) { return i < 64 ? __builtin_amdgcn_readlane(row, i) : -1; };
     const int at1 = p1 < nv ? (chunk < 64 ? row_at(chunk) : -1) : -1;          // the row at the next chunk's first place
     int cur = row_at(0);
@@ -613,30 +616,75 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy
 }
 
 // The rows in parts.  A workgroup looks through kJoinWaves chunks, a wave each, for one that a row in parts
-// begins in; its parts over 64 * V columns are then added up by all waves, a contiguous share each, joined
-// in their order.
-constexpr int kJoinWaves = 8;
+// begins in, and adds the parts up over 64 * V columns: up to kJoinAlone of them by that wave, more by all
+// waves, a contiguous share each, joined in their order.  Workgroups from `joins` on clear a share of the
+// rows without tokens (used; null: none to clear) -- last in the operation, so that the sums' reads do not
+// wait behind the writes.
+constexpr int kJoinWaves = 8, kJoinThreads = 64 * kJoinWaves, kJoinAlone = 16, kClearRows = 256;
+
+template <int V>
+__device__ __forceinline__ void add_parts(const float *part, int64_t d, int64_t ch, int64_t i0, int64_t i1, float *acc) {
+    for (int64_t i = i0; i < i1; i += 8) {            // part 0: chunk ch's [1]; part i: chunk ch + i's [0]
+        typename RowVec<float, V>::raw buf[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int64_t j = min(i + u, i1 - 1);
+            buf[u] = RowVec<float, V>::load(part + ((ch + j) * 2 + (j == 0)) * d);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (i + u >= i1) break;
+            float f[V];
+            RowVec<float, V>::unpack(buf[u], f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] += f[e];
+        }
+    }
+}
 
 template <int V, int MODE>
-__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(int d, int cblocks, int chunk, int64_t groups,
-                                                                     const int32_t *__restrict__ key,
-                                                                     const int32_t *__restrict__ nvalid, float scale,
-                                                                     float lr, float *__restrict__ dst,
-                                                                     bf16_t *__restrict__ sh,
-                                                                     const float *__restrict__ part) {
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int64_t n, int d, int cblocks, int chunk, int64_t groups,
+                                                                  uint32_t joins, const int32_t *__restrict__ key,
+                                                                  const int32_t *__restrict__ nvalid, float scale, float lr,
+                                                                  float *__restrict__ dst, bf16_t *__restrict__ sh,
+                                                                  const float *__restrict__ part,
+                                                                  const uint8_t *__restrict__ used, uint32_t rows) {
     __shared__ float sums[kJoinWaves - 1][64][V + 1];
-    __shared__ int begins[kJoinWaves];                // the row in parts that begins in the wave's chunk, or -1
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ int begins[kJoinWaves];                // the row in many parts that begins in the wave's chunk, or -1
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (blockIdx.x >= joins) {
+        const uint32_t r0 = (blockIdx.x - joins) * kClearRows;
+        zero_rows<kJoinThreads>(dst, d, 0, d, rows, kClearRows, [&](int l) { return r0 + l; },
+                                [&](int l) { return used[r0 + l] == 0; });
+        return;
+    }
     const int nv = *nvalid;
-    for (int64_t b = blockIdx.x; b < groups; b += gridDim.x) {
+    for (int64_t b = blockIdx.x; b < groups; b += joins) {
         const int64_t ch0 = b / cblocks * kJoinWaves;
         const int cb = (int)(b % cblocks);
-        if ((ch0 + 2) * chunk >= nv) return;          // (no chunk from here on has two behind it)
-        const int64_t p0 = (ch0 + wave) * chunk, p1 = p0 + chunk, p2 = p1 + chunk;
+        const int64_t ch = ch0 + wave, p0 = ch * chunk, p1 = p0 + chunk, p2 = p1 + chunk;
+        int skip;
+        const int c0 = lane_columns<V>(d, cb, lane, skip);
+        float acc[V];
         int row = -1;
-        if (p2 < nv) {
-            const int last = key[p1 - 1];
-            if (key[p1] == last && key[p2] == last && !(p0 > 0 && key[p0 - 1] == last)) row = last;
+        if (p2 < n) {                                 // (one round of loads, with *nvalid's)
+            const int last = key[p1 - 1], next = key[p1], behind = key[p2], before = p0 > 0 ? key[p0 - 1] : -1;
+            const int64_t q = p2 + (1 + lane) * chunk;
+            const int far = q < n ? key[q] : -1;
+            if (p2 < nv && next == last && behind == last && before != last) {
+                const uint64_t stop = __ballot(q >= nv || far != last);
+                const int more = stop ? __ffsll((unsigned long long)stop) + 1 : kJoinAlone;
+                if (more < kJoinAlone) {              // chunks that it is the first row of, and this one
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] = 0.f;
+                    if (skip < V) {
+                        add_parts<V>(part + c0, d, ch, 0, more + 1, acc);
+                        row_finish<MODE, V>(dst, sh, (int64_t)last * d + c0, acc, skip, scale, lr);
+                    }
+                } else {
+                    row = last;
+                }
+            }
         }
         __syncthreads();
         if (lane == 0) begins[wave] = row;
@@ -644,11 +692,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(int d, int 
         for (int w = 0; w < kJoinWaves; ++w) {
             const int cur = begins[w];
             if (cur < 0) continue;                    // (uniform over the workgroup)
-            const int64_t ch = ch0 + w;
-            // the number of chunks behind this one that the row is the first of
-            int64_t more = 2;
+            int64_t more = kJoinAlone;
             for (;;) {
-                const int64_t q = (ch + 1 + more + lane) * chunk;
+                const int64_t q = (ch0 + w + 1 + more + lane) * chunk;
                 const uint64_t stop = __ballot(q >= nv || key[q] != cur);
                 if (stop) {
                     more += __ffsll((unsigned long long)stop) - 1;
@@ -656,30 +702,10 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(int d, int 
                 }
                 more += 64;
             }
-            int skip;
-            const int c0 = lane_columns<V>(d, cb, lane, skip);
-            float acc[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) acc[e] = 0.f;
-            // part 0: this chunk's [1]; part i: chunk ch + i's [0]
             const int64_t each = (more + 1 + kJoinWaves - 1) / kJoinWaves, i0 = wave * each, i1 = min(more + 1, i0 + each);
-            if (skip < V)
-                for (int64_t i = i0; i < i1; i += 8) {
-                    typename RowVec<float, V>::raw buf[8];
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const int64_t j = min(i + u, i1 - 1);
-                        buf[u] = RowVec<float, V>::load(part + ((ch + j) * 2 + (j == 0)) * d + c0);
-                    }
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        if (i + u >= i1) break;
-                        float f[V];
-                        RowVec<float, V>::unpack(buf[u], f);
-#pragma unroll
-                        for (int e = 0; e < V; ++e) acc[e] += f[e];
-                    }
-                }
+            if (skip < V) add_parts<V>(part + c0, d, ch0 + w, i0, i1, acc);
             if (wave > 0)
 #pragma unroll
                 for (int e = 0; e < V; ++e) sums[wave - 1][lane][e] = acc[e];
@@ -696,31 +722,36 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(int d, int 
 }
 
 // ------------------------------------------------------------------ few tokens: one launch
-// A workgroup sorts its bucket's tokens into LDS and sums its rows itself.  A row of more than kAlone
-// tokens is summed by all waves, each a contiguous part of its tokens, joined in their order; the others
-// go to the waves in turn, per block of columns.
-constexpr int kSmallWaves = 4, kSmallThreads = 64 * kSmallWaves, kAlone = 16;
+// Workgroup (bucket, 64 * V columns) sorts the bucket's tokens into LDS and sums its rows itself.  A row of
+// more than kAlone tokens is summed by all waves, each a contiguous part of its tokens, joined in their
+// order; the others go to the waves in turn.
+constexpr int kSmallWaves = 8, kSmallThreads = 64 * kSmallWaves, kAlone = 8;
 
 template <typename T, int V, int MODE, int KEEP>
 __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__restrict__ dy, int64_t dld, int d,
-                                                                    int cblocks, const int32_t *__restrict__ ids,
-                                                                    uint32_t n, uint32_t rows, int gs, int bb,
-                                                                    int local_rows, float scale, float lr,
-                                                                    float *__restrict__ dst, bf16_t *__restrict__ sh) {
+                                                                    const int32_t *__restrict__ ids, uint32_t n,
+                                                                    uint32_t rows, int gs, int bb, int local_rows,
+                                                                    float scale, float lr, float *__restrict__ dst,
+                                                                    bf16_t *__restrict__ sh) {
     extern __shared__ uint32_t cnt[];                 // [local row][wave], the end, then the tokens (16 bits each)
     __shared__ uint32_t red[kSmallWaves];
     __shared__ float sums[kSmallWaves - 1][64][V + 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int entries = local_rows * kSmallWaves;
     uint16_t *const list = (uint16_t *)(cnt + entries + 1);
     for (int e = threadIdx.x; e < entries; e += kSmallThreads) cnt[e] = 0;
     __syncthreads();
     BucketSort<kSmallWaves, KEEP> sort(ids, n, rows, gs, bb, blockIdx.x);
-    (void)sort.count(cnt);
+    sort.count(cnt);
     __syncthreads();
     scan_counts<kSmallWaves>(cnt, entries, 0, red);
+    int skip;
+    const int c0 = lane_columns<V>(d, blockIdx.y, lane, skip);
     if (MODE == kStore) {
-        zero_rows<kSmallThreads>(dst, d, rows, blockIdx.x, gs, bb, local_rows, [&](int l) { return cnt[l * kSmallWaves]; });
+        zero_rows<kSmallThreads>(
+            dst, d, blockIdx.y * 64 * V, min(d, (int)(blockIdx.y + 1) * 64 * V), rows, local_rows,
+            [&](int l) { return place_row(blockIdx.x, l, gs, bb); },
+            [&](int l) { return cnt[l * kSmallWaves] == cnt[(l + 1) * kSmallWaves]; });
         __syncthreads();
     }
     sort.put(cnt, [&](uint32_t p, uint32_t token, uint32_t) { list[p] = (uint16_t)token; });
@@ -735,53 +766,52 @@ __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__r
             const int j = l0 + __ffsll((unsigned long long)some) - 1;
             some &= some - 1;
             const int b = (int)first(j), e = (int)first(j + 1);
-            const uint32_t row = place_row(blockIdx.x, j, gs, bb);
             const bool all = e - b > kAlone;          // (uniform over the workgroup, like the loops)
-            for (int cb = 0; cb < cblocks; ++cb) {
-                if (!all && turn++ % kSmallWaves != wave) continue;
-                int skip;
-                const int c0 = lane_columns<V>(d, cb, lane, skip);
-                const int each = all ? (e - b + kSmallWaves - 1) / kSmallWaves : e - b;
-                const int t0 = all ? min(e, b + wave * each) : b, t1 = min(e, t0 + each);
-                float acc[V];
+            if (!all && turn++ % kSmallWaves != wave) continue;
+            const int each = all ? (e - b + kSmallWaves - 1) / kSmallWaves : e - b;
+            const int t0 = all ? min(e, b + wave * each) : b, t1 = min(e, t0 + each);
+            float acc[V];
 #pragma unroll
-                for (int q = 0; q < V; ++q) acc[q] = 0.f;
-                if (skip < V)
-                    for (int t = t0; t < t1; t += 8) {
-                        typename RowVec<T, V>::raw buf[8];
+            for (int q = 0; q < V; ++q) acc[q] = 0.f;
+            if (skip < V)
+                for (int t = t0; t < t1; t += 8) {
+                    typename RowVec<T, V>::raw buf[8];
 #pragma unroll
-                        for (int u = 0; u < 8; ++u)
-                            if (t + u < t1) buf[u] = RowVec<T, V>::load(dy + list[t + u] * dld + c0);
+                    for (int u = 0; u < 8; ++u)
+                        if (t + u < t1) buf[u] = RowVec<T, V>::load(dy + list[t + u] * dld + c0);
 #pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            if (t + u >= t1) break;
-                            float f[V];
-                            RowVec<T, V>::unpack(buf[u], f);
+                    for (int u = 0; u < 8; ++u) {
+                        if (t + u >= t1) break;
+                        float f[V];
+                        RowVec<T, V>::unpack(buf[u], f);
 #pragma unroll
-                            for (int q = 0; q < V; ++q) acc[q] += f[q];
-                        }
+                        for (int q = 0; q < V; ++q) acc[q] += f[q];
                     }
-                if (all) {
-                    if (wave > 0)
-#pragma unroll
-                        for (int q = 0; q < V; ++q) sums[wave - 1][lane][q] = acc[q];
-                    __syncthreads();
-                    if (wave == 0)
-                        for (int w = 0; w < kSmallWaves - 1; ++w)
-#pragma unroll
-                            for (int q = 0; q < V; ++q) acc[q] += sums[w][lane][q];
                 }
-                if (skip < V && (!all || wave == 0))
-                    row_finish<MODE, V>(dst, sh, (int64_t)row * d + c0, acc, skip, scale, lr);
-                if (all) __syncthreads();
+            if (all) {
+                if (wave > 0)
+#pragma unroll
+                    for (int q = 0; q < V; ++q) sums[wave - 1][lane][q] = acc[q];
+                __syncthreads();
+                if (wave == 0)
+                    for (int w = 0; w < kSmallWaves - 1; ++w)
+#pragma unroll
+                        for (int q = 0; q < V; ++q) acc[q] += sums[w][lane][q];
             }
+            if (skip < V && (!all || wave == 0))
+                row_finish<MODE, V>(dst, sh, (int64_t)place_row(blockIdx.x, j, gs, bb) * d + c0, acc, skip, scale, lr);
+            if (all) __syncthreads();
         }
     }
 }
 
-constexpr int kSmallTokens = 8192;
+constexpr int kSmallTokens = 8192, kSmallKeep = 8;    // (further ids of a lane are read twice)
+constexpr int kSmallBits = 9, kSmallLocal = 960;
 
 static size_t list_bytes(int64_t n) { return ((size_t)n * 4 + 15) / 16 * 16; }
+
+// a byte per row (gradients of one round that store)
+static size_t used_bytes(int64_t rows) { return rows > ((int64_t)1 << kDigitBits) ? 0 : ((size_t)rows + 15) / 16 * 16; }
 
 // tokens per wave: 32, or 16 where that makes less than 4096 waves
 static int sum_chunk(int64_t n, int cblocks) {
@@ -801,7 +831,7 @@ static Tiles tiles_of(int64_t n) {
 }
 
 // Few tokens, and few enough buckets: each of them reads all ids.
-static bool sum_small(int64_t n, int64_t rows) { return n <= kSmallTokens && rows <= ((int64_t)960 << 12); }
+static bool sum_small(int64_t n, int64_t rows) { return n <= kSmallTokens && rows <= ((int64_t)kSmallLocal << 12); }
 
 size_t embed_ws_bytes(int64_t n, int d, int64_t rows) {
     if (n == 0 || rows == 0 || sum_small(n, rows)) return 0;
@@ -810,7 +840,8 @@ size_t embed_ws_bytes(int64_t n, int d, int64_t rows) {
         const int chunk = sum_chunk(n, (d + 64 * v - 1) / (64 * v));
         chunks = std::max(chunks, (n + chunk - 1) / chunk);
     }
-    return 16 + 4 * list_bytes(n) + list_bytes(tiles_of(n).count * (kBuckets + 1)) + (size_t)chunks * 2 * d * 4;
+    return 16 + 4 * list_bytes(n) + list_bytes(tiles_of(n).count * (kBuckets + 1)) + used_bytes(rows) +
+           (size_t)chunks * 2 * d * 4;
 }
 
 template <typename T, int V>
@@ -818,20 +849,15 @@ static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const in
                             int mode, float lr, float *dst, bf16_t *sh, void *ws, hipStream_t st) {
     const int cblocks = (d + 64 * V - 1) / (64 * V);
     if (sum_small(n, rows)) {
-        const RowSplit s = row_split(rows, d, 10, 960);
+        const RowSplit s = row_split(rows, d, kSmallBits, kSmallLocal);
         const size_t lds = ((size_t)s.local * kSmallWaves + 1) * 4 + n * 2;
 #define TFK_GO(MODE, KEEP)                                                                                             \
-    hipLaunchKernelGGL((embed_small_kernel<T, V, MODE, KEEP>), dim3(1u << s.bb), dim3(kSmallThreads), lds, st, dy,     \
-                       dld, d, cblocks, ids, (uint32_t)n, (uint32_t)rows, s.gs, s.bb, s.local, scale, lr, dst, sh)
-        if (n <= 16 * kSmallThreads) {
-            if (mode == kStore) TFK_GO(kStore, 16);
-            else if (mode == kAdd) TFK_GO(kAdd, 16);
-            else TFK_GO(kSgd, 16);
-        } else {
-            if (mode == kStore) TFK_GO(kStore, 32);
-            else if (mode == kAdd) TFK_GO(kAdd, 32);
-            else TFK_GO(kSgd, 32);
-        }
+    hipLaunchKernelGGL((embed_small_kernel<T, V, MODE, KEEP>),                                                        \
+                       dim3(1u << s.bb, cblocks), dim3(kSmallThreads), lds, st, dy, dld, d, ids, (uint32_t)n, (uint32_t)rows, s.gs,      \
+                       s.bb, s.local, scale, lr, dst, sh)
+        if (mode == kStore) TFK_GO(kStore, kSmallKeep);
+        else if (mode == kAdd) TFK_GO(kAdd, kSmallKeep);
+        else TFK_GO(kSgd, kSmallKeep);
 #undef TFK_GO
         return hipGetLastError();
     }
@@ -839,8 +865,10 @@ static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const in
     const Tiles t = tiles_of(n);
     int32_t *nvalid = (int32_t *)ws, *order = nvalid + 4, *key = order + list, *ttok = key + list, *tkey = ttok + list,
             *begin = tkey + list;
-    float *part = (float *)(begin + list_bytes(t.count * (kBuckets + 1)) / 4);
+    uint8_t *used = (uint8_t *)(begin + list_bytes(t.count * (kBuckets + 1)) / 4);
+    float *part = (float *)(used + used_bytes(rows));
     const int rounds = rows > ((int64_t)1 << kDigitBits) ? 2 : 1;
+    if (mode != kStore || rounds == 2) used = nullptr;
     if (mode == kStore && rounds == 2) {
         const hipError_t e = launch_fill_zero(dst, rows * d, st);
         if (e != hipSuccess) return e;
@@ -856,17 +884,19 @@ static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const in
                            begin);
         hipLaunchKernelGGL(embed_bucket_kernel, dim3(kBuckets), dim3(kBucketThreads),
                            ((size_t)s.local * kBucketWaves + 1) * 4, st, ttok, tkey, begin, (int)t.count, (uint32_t)t.size, g,
-                           s.local, bits, order, key, nvalid, mode == kStore && rounds == 1 ? dst : nullptr, d);
+                           s.local, bits, order, key, nvalid, used);
     }
     const int chunk = sum_chunk(n, cblocks);
     const int64_t chunks = (n + chunk - 1) / chunk, groups = (chunks + kJoinWaves - 1) / kJoinWaves * cblocks;
-    const dim3 gs((unsigned)((chunks * cblocks + 3) / 4)), gj((unsigned)std::min<int64_t>(groups, 1 << 20));
+    const unsigned joins = (unsigned)std::min<int64_t>(groups, 1 << 20);
+    const dim3 gs((unsigned)((chunks * cblocks + 3) / 4));
+    const dim3 gj(joins + (used != nullptr ? (unsigned)((rows + kClearRows - 1) / kClearRows) : 0u));
 #define TFK_GO(MODE)                                                                                                   \
     do {                                                                                                               \
-        hipLaunchKernelGGL((embed_sum_kernel<T, V, MODE>), gs, dim3(256), 0, st, dy, dld, d, cblocks, chunk, order,    \
+        hipLaunchKernelGGL((embed_sum_kernel<T, V, MODE>), gs, dim3(256), 0, st, dy, n, dld, d, cblocks, chunk, order, \
                            key, nvalid, scale, lr, dst, sh, part);                                                     \
-        hipLaunchKernelGGL((embed_join_kernel<V, MODE>), gj, dim3(64 * kJoinWaves), 0, st, d, cblocks, chunk, groups,  \
-                           key, nvalid, scale, lr, dst, sh, part);                                                     \
+        hipLaunchKernelGGL((embed_join_kernel<V, MODE>), gj, dim3(kJoinThreads), 0, st, n, d, cblocks, chunk, groups,  \
+                           joins, key, nvalid, scale, lr, dst, sh, part, used, (uint32_t)rows);                        \
     } while (0)
     if (mode == kStore) TFK_GO(kStore);
     else if (mode == kAdd) TFK_GO(kAdd);
