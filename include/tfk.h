@@ -500,8 +500,8 @@ TFK_API tfk_status tfk_scatter_apply_sgd(float *var, uint16_t *var_bf16, int64_t
  * outside K are) makes the loss infinite, and the gradient stays as above with q = 0 (0 outside K).
  * Logits that are NaN or +inf, or -inf throughout, make the row NaN where a term needs them.
  * Errors: n < 0, c < 1, k not in 1..1024, a row distance below c (SHAPE); scale not finite, temperature
- * not in [1e-4, 1e4], alpha not in (0, 1], alpha < 1 without labels (ARG); n > 2^31 - 1 or n times
- * a row distance > 2^40 (OVERFLOW); NULL, misaligned (to the element) or overlapping buffers (NULL, ALIGN, ALIAS).
+ * not in [1e-4, 1e4], alpha not in (0, 1], alpha < 1 without labels (ARG); n > 2^31 - 1, c > 2^30 or n
+ * times a row distance > 2^40 (OVERFLOW); NULL, misaligned (to the element) or overlapping buffers (NULL, ALIGN, ALIAS).
  * n == 0 is a no-op. */
 TFK_API tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld,
                             const float *bias, const void *top, tfk_dtype top_dt, const int32_t *top_idx, int32_t k,

@@ -1063,6 +1063,7 @@ tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n, int32_t
     if (!valid_dt(top_dt)) return fail(TFK_ERR_DTYPE, "unknown dtype %d", (int)top_dt);
     if (n < 0 || c < 1) return fail(TFK_ERR_SHAPE, "need n >= 0 and c >= 1 (n=%lld, c=%d)", (long long)n, c);
     if (k < 1 || k > 1024) return fail(TFK_ERR_SHAPE, "k must be in 1..1024 (got %d)", k);
+    if (c > (1 << 30)) return fail(TFK_ERR_OVERFLOW, "more than 2^30 classes");
     TRY(check_rows("logits", n, c, logits_ld));
     TRY(check_rows("dlogits", n, c, dlogits_ld));
     if (!isfinite(scale)) return fail(TFK_ERR_ARG, "scale must be finite");
@@ -1095,9 +1096,8 @@ tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n, int32_t
                 return fail(TFK_ERR_ALIAS, "dlogits or loss overlaps an operand");
     // (a hard term of weight 0 is left out: the labels are not read)
     const DistillArgs a{logits, logits_ld, bias, top, top_idx, top_lse, alpha < 1.f ? labels : nullptr, weight, loss,
-                        dlogits, dlogits_ld, c, k, temperature, alpha, scale};
-    return hip_status(launch_distill(dt == TFK_F32 ? 0 : 1, top_dt == TFK_F32 ? 0 : 1, n, a, (hipStream_t)stream),
-                      "distill_xent");
+                        dlogits, dlogits_ld, c, k, temperature, alpha, scale, top_dt == TFK_F32 ? 0 : 1};
+    return hip_status(launch_distill(dt == TFK_F32 ? 0 : 1, n, a, (hipStream_t)stream), "distill_xent");
 }
 
 // ------------------------------------------------------------------ embedding table

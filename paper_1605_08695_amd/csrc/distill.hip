@@ -1,8 +1,8 @@
 // Distillation from a teacher's top logits: per row, the loss and its gradient in one launch.
 //
-// With x = logits + bias, u = x / T, K the distinct classes in the row's list, P_j the sum of the
-// teacher's probabilities of class j's entries, P_r what the teacher gives to all other classes (0
-// where its list is renormalised), q = softmax(u), q_r = sum of q over the classes outside K:
+// With x = logits + bias, K the distinct classes in the row's list, P_j the sum of the teacher's
+// probabilities of class j's entries, P_r what the teacher gives to all other classes (0 where its list
+// is renormalised), q = softmax(x / T), q_r = sum of q over the classes outside K:
 //   soft = sum_K P_j (log P_j - log q_j) + P_r (log P_r - log q_r)        (terms with P = 0 are 0)
 //   hard = logsumexp(x) - x_label
 //   loss = w (alpha T^2 soft + (1 - alpha) hard)
@@ -10,208 +10,686 @@
 //   dx_j = scale w (alpha T q_j (q_r - P_r) / q_r    + (1 - alpha) (softmax(x)_j - [j = label]))   else
 // The classes outside K have their own maximum m_r and sum S_r = sum exp((x - m_r) / T), so that
 // q_j / q_r = exp((x_j - m_r) / T) / S_r and log q_r lose nothing where the listed classes hold nearly
-// all of the student's probability.  A bit per class, in LDS, tells the listed ones apart.
+// all of the student's probability.  In the bulk of a row a listed class is -inf (a bit per class, in LDS,
+// tells them apart), its exponential 0; the first wave looks after the listed ones and the label, whose
+// gradients it stores after the bulk's.
+//
+// Exponentials are powers of two, exp(y / T) = 2^(y ct): 2^(x ct - R) by one fma and one exp instruction,
+// with R = m_r ct rounded once and used as it is wherever the sum is.  Rows whose maximum is beyond 1e30
+// (masks of the type's lowest value throughout, infinities, NaN) are shifted first, by exact differences.
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
+#include "rowvec.h"
 
 namespace tfk {
 
-constexpr int kDistillThreads = 256;
-constexpr int kDistillSeg = 65536;                    // classes whose bits are in LDS at a time
+// Where the T = 1 exponentials of the hard term come from: those at T themselves (no hard term, or T = 1),
+// their square (T = 2), their fourth power (T = 4), or exponentials of their own.
+enum { kSame = 0, kSquare = 1, kFourth = 2, kOwn = 3 };
 
-// Block-wide maxima / sums of NV values at once, in a fixed order; every thread gets the results.
-template <int NV, bool MAX>
-__device__ __forceinline__ void block_reduce(float (&v)[NV], float *red) {
-    constexpr int nw = kDistillThreads / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f, kHuge = 1e30f;
+
+__device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ float wave_maxf(float v) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        for (int o = 32; o > 0; o >>= 1) {
-            const float w = __shfl_xor(v[i], o, 64);
-            v[i] = MAX ? fmaxf(v[i], w) : v[i] + w;
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+__device__ __forceinline__ float wave_sumf(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// LDS written by other lanes of this wave is there, and nothing moves across.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// What the first wave finds out about a row and all waves need.
+struct RowShared {
+    float mtop;            // the largest x on the list (-inf: none)
+    float psum;            // sum of the listed P
+    float top[2];          // sums of the listed exponentials at T and at 1, relative to m
+    int soft;              // whether there is a soft term
+    float max[16];         // per wave: maximum outside the list
+    float sum[16][2];      // per wave: sums outside the list at T and at 1
+};
+
+// The row's list in LDS.
+struct RowList {
+    int32_t *cls;          // [k] the entry's class; -1: none, or another entry stands for it
+    float *P;              // [k] its class's probability
+    float *x;              // [k] the student's x there
+    uint32_t *bits;        // a bit per class of a segment
+};
+
+__device__ __forceinline__ void clear_bits(uint32_t *bits, int seg) {
+    u32x4_t *const b4 = reinterpret_cast<u32x4_t *>(bits);
+#pragma unroll 1
+    for (int q = threadIdx.x & 63; q < (seg + 127) / 128; q += 64) b4[q] = u32x4_t{0, 0, 0, 0};
+}
+
+// The first wave: reads the list, forms P, adds up the entries of one class under the first of them, marks
+// the bits of classes [0, seg), and gathers x.
+template <typename T>
+__device__ __forceinline__ void read_list(const DistillArgs &a, int64_t row, const T *z, int seg, const RowList &l,
+                                          RowShared &sh) {
+    const int lane = threadIdx.x & 63, k = a.k, c = a.c;
+    const int32_t *idx = a.top_idx + row * k;
+    float tm = -INFINITY;
+#pragma unroll 1
+    for (int j = lane; j < k; j += 64) {
+        const int32_t i = idx[j];
+        const bool ok = i >= 0 && i < c;
+        float t = a.top_dt == 0 ? ((const float *)a.top)[row * k + j] : bf16_to_f32(((const bf16_t *)a.top)[row * k + j]);
+        if (!ok) t = -INFINITY;
+        l.cls[j] = ok ? i : -1;
+        l.P[j] = t;
+        tm = fmaxf(tm, t != t ? INFINITY : t);
+    }
+    clear_bits(l.bits, seg);
+    wave_sync();
+    tm = wave_maxf(tm);
+    const float invt = 1.f / a.temperature;
+    float ref = 0.f, lse = 0.f;                       // log p = (t - ref) / T - lse
+    if (a.top_lse) {
+        lse = a.top_lse[row];
+    } else {
+        ref = tm;
+#pragma unroll 1
+        for (int j = lane; j < k; j += 64)
+            if (l.cls[j] >= 0) lse += expf((l.P[j] - ref) * invt);
+        lse = logf(wave_sumf(lse));
+    }
+    float psum = 0.f, mtop = -INFINITY;
+    bool twice = false;
+#pragma unroll 1
+    for (int j = lane; j < k; j += 64) {
+        const int32_t i = l.cls[j];
+        float p = 0.f, x = 0.f;
+        if (i >= 0) {
+            p = expf((l.P[j] - ref) * invt - lse);
+            x = Elem<T>::load(z + i) + (a.bias ? a.bias[i] : 0.f);
+            mtop = fmaxf(mtop, x);
+            if (i < seg) twice |= (atomicOr(&l.bits[i >> 5], 1u << (i & 31)) >> (i & 31)) & 1u;
         }
-    __syncthreads();                                  // red may still be read
-    if (lane == 0)
-        for (int i = 0; i < NV; ++i) red[i * nw + wave] = v[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        v[i] = red[i * nw];
-        for (int w = 1; w < nw; ++w) v[i] = MAX ? fmaxf(v[i], red[i * nw + w]) : v[i] + red[i * nw + w];
+        l.P[j] = p;
+        l.x[j] = x;
+        psum += p;
+    }
+    wave_sync();
+    if (__any(twice) || seg < c) {                    // (classes past the segment have no bits to tell by)
+#pragma unroll 1
+        for (int j0 = 0; j0 < k; j0 += 64) {
+            const int j = j0 + lane;
+            const int32_t i = j < k ? l.cls[j] : -1;
+            float p = 0.f;
+            bool first = true;
+            if (i >= 0)
+#pragma unroll 1
+                for (int q = 0; q < k; ++q)
+                    if (l.cls[q] == i) {
+                        if (q < j) {
+                            first = false;
+                            break;
+                        }
+                        p += l.P[q];
+                    }
+            wave_sync();
+            if (i >= 0) l.P[j] = first ? p : -1.f;    // (p adds entries from j on: none of them overwritten yet)
+            wave_sync();
+        }
+#pragma unroll 1
+        for (int j = lane; j < k; j += 64)
+            if (l.P[j] < 0.f) l.cls[j] = -1;
+    }
+    psum = wave_sumf(psum);
+    mtop = wave_maxf(mtop);
+    if (lane == 0) {
+        sh.psum = psum;
+        sh.mtop = mtop;
+        sh.soft = a.top_lse != nullptr || tm > -INFINITY;
     }
 }
 
-template <typename T, typename TT>
-__global__ __launch_bounds__(kDistillThreads) void distill_kernel(DistillArgs a) {
-    extern __shared__ uint32_t smem[];
-    __shared__ float red[4 * kDistillThreads / 64];
-    constexpr int NT = kDistillThreads;
-    const int tid = threadIdx.x, c = a.c, k = a.k;
-    const int seg_words = (min(c, kDistillSeg) + 31) / 32;
-    int32_t *cls = (int32_t *)smem;                   // [k] the entry's class; -1: none, or another entry stands for it
-    float *lp = (float *)(cls + k);                   // [k] the entry's log-probability
-    float *P = lp + k;                                // [k] its class's probability
-    float *xs = P + k;                                // [k] the student's x there
-    uint32_t *bits = (uint32_t *)(xs + k);            // [seg_words]
-    const int64_t row = blockIdx.x;
+// A row's sums and what follows from them, the same in every thread.
+struct RowTotals {
+    float m, mr;           // maxima: of all, outside the list (0: none)
+    bool huge;             // whether x outside the list is taken relative to mr before anything else
+    float ct;              // log2(e) / T
+    float R, R1;           // exponents' references outside the list, at T and at 1 (0 where huge)
+    float relt, rel1;      // 2^(those - m's)
+    float ln_rel;          // log relt
+    float st, s1, logst, qr;
+    float co, ch;          // gradients outside the list: co e + ch e1
+    float gs, at, gb;      // scale w, alpha T, scale w (1 - alpha)
+
+    // x outside the list, as its exponentials want it
+    __device__ __forceinline__ float e(float x) const { return huge ? ex2((x - mr) * ct) : ex2(fmaf(x, ct, -R)); }
+    __device__ __forceinline__ float e1(float x) const { return huge ? ex2((x - mr) * kLog2e) : ex2(fmaf(x, kLog2e, -R1)); }
+
+    __device__ __forceinline__ void maxima(float outside, float mtop, float temperature, int kind) {
+        m = fmaxf(outside, mtop);
+        ct = kLog2e / temperature;
+        mr = outside > -INFINITY ? outside : 0.f;
+        huge = !(fabsf(mr) < kHuge && !(m >= kHuge));
+        R = huge ? 0.f : mr * ct;
+        R1 = huge ? 0.f : (kind == kOwn ? mr * kLog2e : R * temperature);   // (exact: T is 1, 2 or 4 otherwise)
+        const bool none = !(outside > -INFINITY);
+        relt = none ? 0.f : ex2(huge ? (mr - m) * ct : fmaf(-m, ct, R));
+        rel1 = none ? 0.f : ex2(huge ? (mr - m) * kLog2e : fmaf(-m, kLog2e, R1));
+        ln_rel = none ? 0.f : huge ? (mr - m) / temperature : fmaf(-m, ct, R) * kLn2;
+    }
+
+    __device__ __forceinline__ void sums(const DistillArgs &a, float w, float rest, float rest1, const RowShared &sh,
+                                         bool hard, float pr) {
+        st = sh.top[0] + rest * relt;
+        s1 = sh.top[1] + rest1 * rel1;
+        logst = logf(st);
+        qr = rest * relt / st;
+        gs = a.scale * w;
+        at = a.alpha * a.temperature;
+        gb = gs * (1.f - a.alpha);
+        co = !sh.soft ? 0.f : (rest != 0.f ? gs * at * (qr - pr) / rest : gs * at * qr);
+        ch = hard ? gb * rel1 / s1 : 0.f;
+    }
+};
+
+// What the teacher gives to the classes outside the list.
+__device__ __forceinline__ float rest_of(const DistillArgs &a, const RowShared &sh) {
+    const float pr = 1.f - sh.psum;
+    return !a.top_lse || pr < 0.f ? 0.f : pr;         // (NaN stays NaN)
+}
+
+// The first wave: sums of the listed exponentials, relative to m.
+__device__ __forceinline__ void sum_list(const DistillArgs &a, const RowTotals &t, const RowList &l, bool hard, RowShared &sh) {
+    const int lane = threadIdx.x & 63;
+    float s = 0.f, s1 = 0.f;
+#pragma unroll 1
+    for (int j = lane; j < a.k; j += 64)
+        if (l.cls[j] >= 0) {
+            s += ex2((l.x[j] - t.m) * t.ct);
+            if (hard) s1 += ex2((l.x[j] - t.m) * kLog2e);
+        }
+    s = wave_sumf(s);
+    s1 = wave_sumf(s1);
+    if (lane == 0) {
+        sh.top[0] = s;
+        sh.top[1] = s1;
+    }
+}
+
+// The first wave: the loss.
+__device__ __forceinline__ void row_loss(const DistillArgs &a, int64_t row, const RowTotals &t, const RowList &l,
+                                         const RowShared &sh, float rest, float pr, float w, bool hard, float xlab) {
+    const int lane = threadIdx.x & 63;
+    const float invt = 1.f / a.temperature;
+    float kl = 0.f;
+    if (sh.soft) {
+#pragma unroll 1
+        for (int j = lane; j < a.k; j += 64)
+            if (l.cls[j] >= 0) {
+                const float p = l.P[j];
+                if (p != 0.f) kl += p * (logf(p) - ((l.x[j] - t.m) * invt - t.logst));
+            }
+        kl = wave_sumf(kl);
+        if (pr != 0.f) kl += pr * (logf(pr) - (logf(rest) + t.ln_rel - t.logst));
+    }
+    if (lane == 0) {
+        float loss = sh.soft ? a.alpha * a.temperature * a.temperature * kl : 0.f;
+        if (hard) loss += (1.f - a.alpha) * (t.m - xlab + logf(t.s1));
+        a.loss[row] = w * loss;
+    }
+}
+
+// The first wave, after the bulk's stores: the gradients of the listed classes and of the label.
+template <typename T>
+__device__ __forceinline__ void store_list(const DistillArgs &a, const RowTotals &t, const RowList &l, const RowShared &sh,
+                                           bool hard, int lab, float xlab, T *dz) {
+    const int lane = threadIdx.x & 63;
+    bool found = !hard;
+#pragma unroll 1
+    for (int j = lane; j < a.k; j += 64) {
+        const int32_t i = l.cls[j];
+        if (i < 0) continue;
+        float g = sh.soft ? t.gs * t.at * (ex2((l.x[j] - t.m) * t.ct) / t.st - l.P[j]) : 0.f;
+        if (hard) g += t.gb * (ex2((l.x[j] - t.m) * kLog2e) / t.s1 - (i == lab ? 1.f : 0.f));
+        found |= hard && i == lab;
+        Elem<T>::store(dz + i, g);
+    }
+    if (!__any(found) && lane == 0) Elem<T>::store(dz + lab, t.co * t.e(xlab) + t.ch * t.e1(xlab) - t.gb);
+}
+
+template <int POW>
+__device__ __forceinline__ float power(float e) {
+    if (POW == kSquare) return e * e;
+    if (POW == kFourth) return (e * e) * (e * e);
+    return e;
+}
+
+// ------------------------------------------------------------------ rows in registers
+// A workgroup of NT threads has a row of up to NT * NCH * V classes in registers, in fp32: one read of the
+// logits and one write of the gradient.  Piece i of thread t is V classes from (i NT + t) V; the c % V
+// classes behind the last whole piece are one each in the first lanes of the last wave (xt).
+template <typename T>
+__device__ __forceinline__ T *at32(T *p, uint32_t i) {     // (a uniform base and a 32-bit offset)
+    typedef typename std::conditional<std::is_const<T>::value, const char, char>::type C;
+    return reinterpret_cast<T *>(reinterpret_cast<C *>(p) + i * (uint32_t)sizeof(T));
+}
+
+// Waves per SIMD that the registers have to leave room for.
+constexpr int row_waves(int nch) { return nch <= 2 ? 8 : nch <= 4 ? 6 : 4; }
+
+// The same number, as one that nothing computed from it before is known for: what a later phase computes
+// from it (addresses, exponentials) is then computed there, not kept in registers from an earlier one.
+template <typename X>
+__device__ __forceinline__ X fresh(X x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+template <typename T, int NT, int NCH, int POW>
+__global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t n, int bit_words) {
+    constexpr int V = 16 / sizeof(T), NW = NT / 64;
+    extern __shared__ __align__(16) uint32_t smem[];
+    __shared__ RowShared sh;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = a.c, k = a.k, whole = c / V;
+    const int jt = wave == NW - 1 && lane < c - whole * V ? whole * V + lane : -1;      // this lane's class past the pieces
+    RowList l;
+    l.bits = smem;
+    l.cls = (int32_t *)(smem + bit_words);
+    l.P = (float *)(l.cls + k);
+    l.x = l.P + k;
+    const bool hard = a.labels != nullptr;
+    const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (row >= n) return;
+    int tid = fresh(threadIdx.x);
     const T *z = (const T *)a.z + row * a.zld;
     T *dz = (T *)a.dz + row * a.dld;
     const float w = a.weight ? a.weight[row] : 1.f;
-    const bool hard = a.labels != nullptr;
     const int lab = hard ? a.labels[row] : -1;
     const bool bad = hard && (lab < 0 || lab >= c);
-    if (w == 0.f || bad) {                            // (uniform) a row that counts for nothing, or has no loss
-        const float v = w == 0.f ? 0.f : __builtin_nanf("");
-        for (int j = tid; j < c; j += NT) Elem<T>::store(dz + j, v);
-        if (tid == 0) a.loss[row] = v;
+    bool done = w == 0.f || bad;                  // (uniform) a row that counts for nothing, or has no loss
+    float fill = w == 0.f ? 0.f : __builtin_nanf("");
+    typename RowVec<T, V>::raw raw[NCH];
+    float xt = -INFINITY, xlab = 0.f;
+    if (!done) {
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+            if (i * NT + tid < whole) raw[i] = RowVec<T, V>::load(at32(z, (i * NT + tid) * V));
+        if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
+        if (wave == 0) {
+            if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
+            read_list<T>(a, row, z, c, l, sh);
+        }
+        __syncthreads();
+        if (!sh.soft && !hard) {
+            done = true;
+            fill = 0.f;
+        }
+    }
+    if (done) {
+        float f[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = fill;
+        for (int p = tid; p < whole; p += NT) RowVec<T, V>::store(at32(dz, p * V), f);
+        if (jt >= 0) Elem<T>::store(dz + jt, fill);
+        if (tid == 0) a.loss[row] = fill;
         return;
     }
-    const float invt = 1.f / a.temperature, beta = 1.f - a.alpha;
-    const float c1 = 1.44269504088896341f, ct = c1 / a.temperature;   // exp(y / T) = 2^(y ct)
-    const auto load_x = [&](int j) { return Elem<T>::load(z + j) + (a.bias ? a.bias[j] : 0.f); };
-    const float xlab = hard ? load_x(lab) : 0.f;
 
-    // ---- the teacher
-    const int32_t *idx = a.top_idx + row * k;
-    const TT *top = (const TT *)a.top + row * k;
-    float tm[1] = {-INFINITY};
-    for (int j = tid; j < k; j += NT) {
-        const int32_t i = idx[j];
-        const bool ok = i >= 0 && i < c;
-        const float t = ok ? Elem<TT>::load(top + j) : -INFINITY;
-        cls[j] = ok ? i : -1;
-        lp[j] = t;
-        tm[0] = fmaxf(tm[0], t != t ? INFINITY : t);
-    }
-    block_reduce<1, true>(tm, red);
-    const bool soft = a.top_lse != nullptr || tm[0] > -INFINITY;
-    float ref = 0.f, lse[1] = {0.f};                  // log p = (t - ref) / T - lse
-    if (a.top_lse) {
-        lse[0] = a.top_lse[row];
-    } else {
-        ref = tm[0];
-        for (int j = tid; j < k; j += NT)
-            if (cls[j] >= 0) lse[0] += expf((lp[j] - ref) * invt);
-        block_reduce<1, false>(lse, red);
-        lse[0] = logf(lse[0]);
-    }
-    for (int j = tid; j < k; j += NT)
-        if (cls[j] >= 0) {
-            lp[j] = (lp[j] - ref) * invt - lse[0];
-            xs[j] = load_x(cls[j]);
-        }
-    __syncthreads();
-    for (int j = tid; j < k; j += NT) {               // entries of one class are added up by the first
-        const int32_t i = cls[j];
-        float p = 0.f;
-        for (int q = 0; q < k && i >= 0; ++q)
-            if (cls[q] == i) {
-                if (q < j) {
-                    p = -1.f;
-                    break;
-                }
-                p += expf(lp[q]);
+    // x, -inf where listed or past the end; its maximum
+    tid = fresh(tid);
+    float x[NCH][V];
+    if (jt >= 0 && ((l.bits[jt >> 5] >> (jt & 31)) & 1u)) xt = -INFINITY;
+    float mx = xt;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] = -INFINITY;
+        if (i * NT + tid < whole) {
+            const uint32_t j = (i * NT + tid) * V;
+            RowVec<T, V>::unpack(raw[i], x[i]);
+            if (a.bias) {
+                float b[V];
+                RowVec<float, V>::unpack(RowVec<float, V>::load(at32(a.bias, j)), b);
+#pragma unroll
+                for (int e = 0; e < V; ++e) x[i][e] += b[e];
             }
-        P[j] = p;
-    }
-    __syncthreads();
-    for (int j = tid; j < k; j += NT)
-        if (P[j] < 0.f) cls[j] = -1;
-
-    // ---- the student: maxima, then sums, outside the list (relative to mr) and on it (relative to m)
-    const auto mark = [&](int s0) {                   // the bits of the listed among classes s0 ...
-        __syncthreads();
-        for (int q = tid; q < seg_words; q += NT) bits[q] = 0;
-        __syncthreads();
-        for (int j = tid; j < k; j += NT) {
-            const int32_t i = cls[j];
-            if (i >= s0 && i - s0 < kDistillSeg) atomicOr(&bits[(i - s0) >> 5], 1u << ((i - s0) & 31));
+            const uint32_t on = (l.bits[j >> 5] >> (j & 31)) & ((1u << V) - 1u);
+            if (on != 0) {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if ((on >> e) & 1u) x[i][e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) mx = fmaxf(mx, x[i][e]);
         }
-        __syncthreads();
+        if (i % 2 == 1) __builtin_amdgcn_sched_barrier(0);       // (two pieces' bias at a time in registers)
+    }
+    mx = wave_maxf(mx);
+    if (lane == 0) sh.max[wave] = mx;
+    __syncthreads();
+    mx = sh.max[0];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) mx = fmaxf(mx, sh.max[q]);
+    RowTotals t;
+    t.maxima(mx, sh.mtop, a.temperature, POW);
+    if (t.huge) {
+        xt -= t.mr;
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[i][e] -= t.mr;
+    }
+    // sums; x becomes its exponential, unless both of them are needed again
+    float s = 0.f, s1 = 0.f;
+    const auto add = [&](float &v) {
+        const float y = ex2(fmaf(v, t.ct, -t.R));
+        s += y;
+        if (POW == kOwn) s1 += ex2(fmaf(v, kLog2e, -t.R1));
+        else v = y;
     };
-    const auto listed = [&](int j) { return ((bits[j >> 5] >> (j & 31)) & 1u) != 0; };
-    float mx[2] = {-INFINITY, -INFINITY};
-    for (int s0 = 0; s0 < c; s0 += kDistillSeg) {
-        mark(s0);
-        for (int j = tid; j < min(c - s0, kDistillSeg); j += NT)
-            if (!listed(j)) mx[0] = fmaxf(mx[0], load_x(s0 + j));
+    add(xt);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) add(x[i][e]);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    for (int j = tid; j < k; j += NT)
-        if (cls[j] >= 0) mx[1] = fmaxf(mx[1], xs[j]);
-    block_reduce<2, true>(mx, red);
-    const float m = fmaxf(mx[0], mx[1]), mr = mx[0] > -INFINITY ? mx[0] : 0.f;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};              // outside at T, at 1; listed at T, at 1
-    for (int s0 = 0; s0 < c; s0 += kDistillSeg) {
-        if (c > kDistillSeg) mark(s0);
-        for (int j = tid; j < min(c - s0, kDistillSeg); j += NT)
-            if (!listed(j)) {
-                const float x = load_x(s0 + j) - mr;
-                sum[0] += exp2f(x * ct);
-                if (hard) sum[1] += exp2f(x * c1);
-            }
+    s = wave_sumf(s);
+    if (POW != kSame) s1 = wave_sumf(s1);
+    if (lane == 0) {
+        sh.sum[wave][0] = s;
+        sh.sum[wave][1] = s1;
     }
-    for (int j = tid; j < k; j += NT)
-        if (cls[j] >= 0) {
-            sum[2] += exp2f((xs[j] - m) * ct);
-            if (hard) sum[3] += exp2f((xs[j] - m) * c1);
-        }
-    block_reduce<4, false>(sum, red);
-    const float relt = mx[0] > -INFINITY ? exp2f((mr - m) * ct) : 0.f, rel1 = mx[0] > -INFINITY ? exp2f((mr - m) * c1) : 0.f;
-    const float st = sum[2] + sum[0] * relt, s1 = sum[3] + sum[1] * rel1;
-    const float logst = logf(st), qr = sum[0] * relt / st;
-
-    // ---- the loss
-    float pl[2] = {0.f, 0.f};                         // the listed P; their terms
-    for (int j = tid; j < k; j += NT)
-        if (cls[j] >= 0) {
-            const float p = P[j];
-            pl[0] += p;
-            if (p != 0.f) pl[1] += p * (logf(p) - ((xs[j] - m) * invt - logst));
-        }
-    block_reduce<2, false>(pl, red);
-    float pr = a.top_lse ? 1.f - pl[0] : 0.f;
-    if (pr < 0.f) pr = 0.f;
-    if (tid == 0) {
-        float loss = 0.f;
-        if (soft) {
-            if (pr != 0.f) pl[1] += pr * (logf(pr) - (logf(sum[0]) + (mr - m) * invt - logst));
-            loss = a.alpha * a.temperature * a.temperature * pl[1];
-        }
-        if (hard) loss += beta * (m - xlab + logf(s1));
-        a.loss[row] = w * loss;
-    }
-
-    // ---- the gradient, as if no class were listed, then the listed ones
-    const float gs = a.scale * w, at = a.alpha * a.temperature, gb = gs * beta;
-    const float co = !soft ? 0.f : (sum[0] != 0.f ? gs * at * (qr - pr) / sum[0] : gs * at * qr);
-    const float ch = hard ? gb * rel1 / s1 : 0.f;
-    for (int j = tid; j < c; j += NT) {
-        const float x = load_x(j) - mr;
-        float g = soft ? co * exp2f(x * ct) : 0.f;
-        if (hard) g += ch * exp2f(x * c1);
-        if (j == lab) g -= gb;
-        Elem<T>::store(dz + j, g);
-    }
+    if (wave == 0) sum_list(a, t, l, hard, sh);
     __syncthreads();
-    for (int j = tid; j < k; j += NT) {
-        const int32_t i = cls[j];
-        if (i < 0) continue;
-        float g = soft ? gs * at * (exp2f((xs[j] - m) * ct) / st - P[j]) : 0.f;
-        if (hard) g += gb * (exp2f((xs[j] - m) * c1) / s1 - (i == lab ? 1.f : 0.f));
-        Elem<T>::store(dz + i, g);
+    s = sh.sum[0][0];
+    s1 = sh.sum[0][1];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) {
+        s += sh.sum[q][0];
+        s1 += sh.sum[q][1];
+    }
+    if (POW == kSame) s1 = s;                     // (T = 1, or not used)
+    const float pr = rest_of(a, sh);
+    t.sums(a, w, s, s1, sh, hard, pr);
+    const float cs = t.co + t.ch;                 // (kSame: one exponential for both)
+    tid = fresh(tid);
+    const float R = fresh(t.R), R1 = fresh(t.R1);
+    const auto slope = [&](float v) {
+        return POW == kOwn ? t.co * ex2(fmaf(v, t.ct, -R)) + t.ch * ex2(fmaf(v, kLog2e, -R1)) : cs * v;
+    };
+#pragma unroll
+    for (int i = 0; i < NCH; ++i)
+        if (i * NT + tid < whole) {
+            float g[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[e] = slope(x[i][e]);
+            RowVec<T, V>::store(at32(dz, (i * NT + tid) * V), g);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    if (jt >= 0) Elem<T>::store(dz + jt, slope(xt));
+    if (wave == 0) row_loss(a, row, t, l, sh, s, pr, w, hard, xlab);
+    __syncthreads();
+    if (wave == 0) store_list<T>(a, t, l, sh, hard, lab, xlab, dz);
+}
+
+// ------------------------------------------------------------------ long rows
+// Rows that do not fit the registers are read twice: once for the maximum and the sums together (each thread
+// keeps its own running maximum and sums relative to it), once for the gradient; the second read of a row
+// follows the first closely enough to come from the caches.  The bits are those of kSeg classes at a time.
+constexpr int kSeg = 262144, kLongThreads = 1024;
+
+// V values of x from class j: -inf past the end.
+template <typename T, int V>
+__device__ __forceinline__ void load_x(const T *z, const float *bias, int j, int c, float *x) {
+    if (j + V <= c) {
+        RowVec<T, V>::unpack(RowVec<T, V>::load(z + j), x);
+        if (bias) {
+            float b[V];
+            RowVec<float, V>::unpack(RowVec<float, V>::load(bias + j), b);
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] += b[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] = j + e < c ? Elem<T>::load(z + j + e) + (bias ? bias[j + e] : 0.f) : -INFINITY;
     }
 }
 
-hipError_t launch_distill(int dt, int top_dt, int64_t n, const DistillArgs &a, hipStream_t st) {
-    const size_t lds = (size_t)a.k * 16 + (size_t)(std::min(a.c, kDistillSeg) + 31) / 32 * 4;
-#define TFK_GO(T, TT) \
-    hipLaunchKernelGGL((distill_kernel<T, TT>), dim3((unsigned)n), dim3(kDistillThreads), lds, st, a)
-    if (dt == 0 && top_dt == 0) TFK_GO(float, float);
-    else if (dt == 0) TFK_GO(float, bf16_t);
-    else if (top_dt == 0) TFK_GO(bf16_t, float);
-    else TFK_GO(bf16_t, bf16_t);
+template <typename T, int POW>
+__global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs a, int64_t n, int bit_words) {
+    constexpr int V = 16 / sizeof(T), NT = kLongThreads, NW = NT / 64, UN = 4;
+    extern __shared__ __align__(16) uint32_t smem[];
+    __shared__ RowShared sh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = a.c, k = a.k;
+    RowList l;
+    l.bits = smem;
+    l.cls = (int32_t *)(smem + bit_words);
+    l.P = (float *)(l.cls + k);
+    l.x = l.P + k;
+    const bool hard = a.labels != nullptr;
+    const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (row >= n) return;
+    const T *z = (const T *)a.z + row * a.zld;
+    T *dz = (T *)a.dz + row * a.dld;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    const int lab = hard ? a.labels[row] : -1;
+    const bool bad = hard && (lab < 0 || lab >= c);
+    bool done = w == 0.f || bad;                  // (uniform) a row that counts for nothing, or has no loss
+    float fill = w == 0.f ? 0.f : __builtin_nanf("");
+    float xlab = 0.f;
+    if (!done) {
+        if (wave == 0) {
+            if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
+            read_list<T>(a, row, z, min(c, kSeg), l, sh);
+        }
+        __syncthreads();
+        if (!sh.soft && !hard) {
+            done = true;
+            fill = 0.f;
+        }
+    }
+    if (done) {
+        for (int j = tid * V; j < c; j += NT * V) {
+            float f[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = fill;
+            if (j + V <= c) RowVec<T, V>::store(dz + j, f);
+            else
+                for (int e = 0; j + e < c; ++e) Elem<T>::store(dz + j + e, fill);
+        }
+        if (tid == 0) a.loss[row] = fill;
+        return;
+    }
+    // f(x) for every piece of V classes, listed ones -inf
+    const auto outside = [&](bool marked, auto f) {
+        for (int s0 = 0; s0 < c; s0 += kSeg) {
+            if (s0 > 0 || !marked) {              // (read_list has marked the first segment)
+                __syncthreads();
+                if (wave == 0) {
+                    clear_bits(l.bits, min(c, kSeg));
+                    wave_sync();
+                    for (int j = lane; j < k; j += 64) {
+                        const int32_t i = l.cls[j];
+                        if (i >= s0 && i - s0 < kSeg) atomicOr(&l.bits[(i - s0) >> 5], 1u << ((i - s0) & 31));
+                    }
+                }
+                __syncthreads();
+            }
+            const int s1 = min(c, s0 + kSeg);
+            for (int j0 = s0 + tid * V; j0 < s1; j0 += NT * V * UN) {
+                float x[UN][V];
+#pragma unroll
+                for (int u = 0; u < UN; ++u) {
+                    const int j = j0 + u * NT * V;
+                    load_x<T, V>(z, a.bias, j < s1 ? j : c, c, x[u]);
+                    const uint32_t on = j < s1 ? (l.bits[(j - s0) >> 5] >> ((j - s0) & 31)) & ((1u << V) - 1u) : 0u;
+                    if (on != 0) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e)
+                            if ((on >> e) & 1u) x[u][e] = -INFINITY;
+                    }
+                }
+                f(x);
+            }
+        }
+    };
+    const float ct = kLog2e / a.temperature;
+    float M = -INFINITY, r = -kHuge * ct, r1 = -kHuge * kLog2e, s = 0.f, s1 = 0.f;
+    outside(true, [&](float(&x)[UN][V]) {
+        float cm = M;
+#pragma unroll
+        for (int u = 0; u < UN; ++u)
+#pragma unroll
+            for (int e = 0; e < V; ++e) cm = fmaxf(cm, x[u][e]);
+        M = cm;
+        const float at = fminf(fmaxf(cm, -kHuge), kHuge), rn = at * ct;
+        s *= ex2(r - rn);
+        if (POW == kOwn) {
+            const float rn1 = at * kLog2e;
+            s1 *= ex2(r1 - rn1);
+            r1 = rn1;
+        } else if (POW != kSame) {
+            s1 *= power<POW>(ex2(r - rn));
+        }
+        r = rn;
+#pragma unroll
+        for (int u = 0; u < UN; ++u)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float y = ex2(fmaf(x[u][e], ct, -rn));
+                s += y;
+                if (POW == kOwn) s1 += ex2(fmaf(x[u][e], kLog2e, -r1));
+                else if (POW != kSame) s1 += power<POW>(y);
+            }
+    });
+    float mx = wave_maxf(M);
+    if (lane == 0) sh.max[wave] = mx;
+    __syncthreads();
+    mx = sh.max[0];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) mx = fmaxf(mx, sh.max[q]);
+    RowTotals t;
+    t.maxima(mx, sh.mtop, a.temperature, POW);
+    if (t.huge) {                                 // relative to the maximum by exact differences, read again
+        s = s1 = 0.f;
+        outside(c <= kSeg, [&](float(&x)[UN][V]) {
+#pragma unroll
+            for (int u = 0; u < UN; ++u)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float y = ex2((x[u][e] - t.mr) * ct);
+                    s += y;
+                    if (POW == kOwn) s1 += ex2((x[u][e] - t.mr) * kLog2e);
+                    else if (POW != kSame) s1 += power<POW>(y);
+                }
+        });
+    } else {
+        s *= ex2(r - t.R);
+        if (POW == kOwn) s1 *= ex2(r1 - t.R1);
+        else if (POW != kSame) s1 *= power<POW>(ex2(r - t.R));
+    }
+    s = wave_sumf(s);
+    if (POW != kSame) s1 = wave_sumf(s1);
+    if (lane == 0) {
+        sh.sum[wave][0] = s;
+        sh.sum[wave][1] = s1;
+    }
+    if (wave == 0) sum_list(a, t, l, hard, sh);
+    __syncthreads();
+    s = sh.sum[0][0];
+    s1 = sh.sum[0][1];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) {
+        s += sh.sum[q][0];
+        s1 += sh.sum[q][1];
+    }
+    if (POW == kSame) s1 = s;
+    const float pr = rest_of(a, sh);
+    t.sums(a, w, s, s1, sh, hard, pr);
+    const float cs = t.co + t.ch;
+    for (int j0 = tid * V; j0 < c; j0 += NT * V * UN) {
+        float x[UN][V];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) load_x<T, V>(z, a.bias, min(j0 + u * NT * V, c), c, x[u]);
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            const int j = j0 + u * NT * V;
+            if (j >= c) break;
+            float g[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (t.huge) x[u][e] -= t.mr;
+                const float y = ex2(fmaf(x[u][e], ct, -t.R));
+                if (POW == kOwn) g[e] = t.co * y + t.ch * ex2(fmaf(x[u][e], kLog2e, -t.R1));
+                else if (POW == kSame) g[e] = cs * y;
+                else g[e] = t.co * y + t.ch * power<POW>(y);
+            }
+            if (j + V <= c) RowVec<T, V>::store(dz + j, g);
+            else
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (j + e < c) Elem<T>::store(dz + j + e, g[e]);
+        }
+    }
+    if (wave == 0) row_loss(a, row, t, l, sh, s, pr, w, hard, xlab);
+    __syncthreads();
+    if (wave == 0) store_list<T>(a, t, l, sh, hard, lab, xlab, dz);
+}
+
+// ------------------------------------------------------------------ launch
+// A workgroup per row; the threads of one grid dimension have to stay below 2^32.
+static dim3 row_grid(int64_t n) {
+    const int64_t x = std::min<int64_t>(n, 1 << 20);
+    return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+
+template <typename T, int NT, int NCH>
+static void launch_rows(const DistillArgs &a, int64_t n, bool two, size_t lds, int words, hipStream_t st) {
+    const dim3 g = row_grid(n);
+    if (two) hipLaunchKernelGGL((distill_row_kernel<T, NT, NCH, kOwn>), g, dim3(NT), lds, st, a, n, words);
+    else hipLaunchKernelGGL((distill_row_kernel<T, NT, NCH, kSame>), g, dim3(NT), lds, st, a, n, words);
+}
+
+template <typename T>
+static hipError_t launch_typed(const DistillArgs &a, int64_t n, hipStream_t st) {
+    const int pieces = (a.c + (int)(16 / sizeof(T)) - 1) / (int)(16 / sizeof(T));
+    const int words = (std::min(a.c, kSeg) + 127) / 128 * 4;
+    const size_t lds = (size_t)words * 4 + (size_t)a.k * 12;
+    const bool two = a.labels != nullptr && a.temperature != 1.f;
+    if (pieces <= 64 * 2) launch_rows<T, 64, 2>(a, n, two, lds, words, st);
+    else if (pieces <= 64 * 4) launch_rows<T, 64, 4>(a, n, two, lds, words, st);
+    else if (pieces <= 256 * 2) launch_rows<T, 256, 2>(a, n, two, lds, words, st);
+    else if (pieces <= 256 * 4) launch_rows<T, 256, 4>(a, n, two, lds, words, st);
+    else if (pieces <= 512 * 4) launch_rows<T, 512, 4>(a, n, two, lds, words, st);
+    else if (pieces <= 512 * 7) launch_rows<T, 512, 7>(a, n, two, lds, words, st);
+    else if (pieces <= 512 * 10) launch_rows<T, 512, 10>(a, n, two, lds, words, st);
+    else if (pieces <= 1024 * 8) launch_rows<T, 1024, 8>(a, n, two, lds, words, st);
+    else {
+        const dim3 g = row_grid(n);
+        const int kind = !two ? kSame : a.temperature == 2.f ? kSquare : a.temperature == 4.f ? kFourth : kOwn;
+#define TFK_GO(POW) hipLaunchKernelGGL((distill_long_kernel<T, POW>), g, dim3(kLongThreads), lds, st, a, n, words)
+        if (kind == kSame) TFK_GO(kSame);
+        else if (kind == kSquare) TFK_GO(kSquare);
+        else if (kind == kFourth) TFK_GO(kFourth);
+        else TFK_GO(kOwn);
 #undef TFK_GO
+    }
     return hipGetLastError();
+}
+
+hipError_t launch_distill(int dt, int64_t n, const DistillArgs &a, hipStream_t st) {
+    return dt == 0 ? launch_typed<float>(a, n, st) : launch_typed<bf16_t>(a, n, st);
 }
 
 }  // namespace tfk

@@ -291,14 +291,19 @@ struct BucketSort {
     }
 };
 
-// Exclusive sums of cnt[0 .. entries) in place, from `at`; cnt[entries] and the result are the end.
+// Exclusive sums of cnt[0 .. entries) in place, from `at`; cnt[entries] and the result are the end.  entries
+// is a multiple of 4 and cnt 16-byte aligned: a thread has a contiguous range, four at a time.
 template <int NW>
 __device__ __forceinline__ uint32_t scan_counts(uint32_t *cnt, int entries, uint32_t at, uint32_t *red) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int each = (entries + NW * 64 - 1) / (NW * 64);
-    const int e0 = min(entries, tid * each), e1 = min(entries, e0 + each);
+    u32x4_t *const c4 = reinterpret_cast<u32x4_t *>(cnt);
+    const int quads = entries / 4, each = (quads + NW * 64 - 1) / (NW * 64);
+    const int e0 = min(quads, tid * each), e1 = min(quads, e0 + each);
     uint32_t own = 0;
-    for (int e = e0; e < e1; ++e) own += cnt[e];
+    for (int e = e0; e < e1; ++e) {
+        const u32x4_t c = c4[e];
+        own += (c.x + c.y) + (c.z + c.w);
+    }
     uint32_t incl = own;
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t up = __shfl_up(incl, o, 64);
@@ -313,9 +318,9 @@ __device__ __forceinline__ uint32_t scan_counts(uint32_t *cnt, int entries, uint
         end += red[w];
     }
     for (int e = e0; e < e1; ++e) {
-        const uint32_t c = cnt[e];
-        cnt[e] = at;
-        at += c;
+        const u32x4_t c = c4[e];
+        c4[e] = u32x4_t{at, at + c.x, at + c.x + c.y, at + c.x + c.y + c.z};
+        at += (c.x + c.y) + (c.z + c.w);
     }
     if (tid == 0) cnt[entries] = end;
     __syncthreads();
@@ -370,7 +375,7 @@ __global__ __launch_bounds__(kTileThreads) void embed_tile_kernel(const int32_t 
                                                                   uint32_t tile, int32_t *__restrict__ ttok,
                                                                   int32_t *__restrict__ tkey,
                                                                   int32_t *__restrict__ begin) {
-    __shared__ uint32_t cnt[kBuckets * kTileWaves + 1];
+    __shared__ alignas(16) uint32_t cnt[kBuckets * kTileWaves + 1];
     __shared__ uint32_t red[kTileWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (nvalid != nullptr) n = (uint32_t)*nvalid;
@@ -429,7 +434,7 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
                                                                       int32_t *__restrict__ key,
                                                                       int32_t *__restrict__ nvalid,
                                                                       uint8_t *__restrict__ used) {
-    extern __shared__ uint32_t cnt[];                 // [local row][wave], and the end
+    extern __shared__ __align__(16) uint32_t cnt[];                 // [local row][wave], and the end
     __shared__ uint32_t pre[kMostTiles + 1], src[kMostTiles];        // a tile's first entry; where it is
     __shared__ uint32_t red[2][kBucketWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -472,17 +477,22 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
     };
     const uint32_t per = ((m + kBucketWaves - 1) / kBucketWaves + 63) / 64 * 64;
     const uint32_t lo = min(m, wave * per), hi = min(m, lo + per);
-    constexpr int KEEP = 8;
-    uint32_t at_[KEEP], id[KEEP];
-    for (uint32_t base = lo; base < hi; base += KEEP * 64) {
+    constexpr int KEEP = 16;                          // entries that a lane has at hand, and fetches at a time
+    uint32_t tok[KEEP], id[KEEP];
+    const auto fetch = [&](uint32_t base) {
 #pragma unroll
         for (int q = 0; q < KEEP; ++q) {
-            const uint32_t i = base + q * 64 + lane;
-            at_[q] = where(i < hi ? i : lo);
-            id[q] = (uint32_t)tkey[at_[q]];
+            if (base + q * 64 >= hi) break;
+            const uint32_t i = base + q * 64 + lane, at_ = where(i < hi ? i : lo);
+            id[q] = (uint32_t)tkey[at_];
+            tok[q] = (uint32_t)ttok[at_];
         }
+    };
+    for (uint32_t base = lo; base < hi; base += KEEP * 64) {
+        fetch(base);
 #pragma unroll
         for (int q = 0; q < KEEP; ++q) {
+            if (base + q * 64 >= hi) break;
             uint32_t b, l;
             g.place(id[q], b, l);
             if (base + q * 64 + lane < hi) atomicAdd(&cnt[l * kBucketWaves + wave], 1u);
@@ -499,19 +509,10 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
         __syncthreads();
     }
     for (uint32_t base = lo; base < hi; base += KEEP * 64) {
-        if (per > KEEP * 64) {                        // (else they are still at hand)
-#pragma unroll
-            for (int q = 0; q < KEEP; ++q) {
-                const uint32_t i = base + q * 64 + lane;
-                at_[q] = where(i < hi ? i : lo);
-                id[q] = (uint32_t)tkey[at_[q]];
-            }
-        }
-        uint32_t tok[KEEP];
-#pragma unroll
-        for (int q = 0; q < KEEP; ++q) tok[q] = (uint32_t)ttok[at_[q]];
+        if (per > KEEP * 64) fetch(base);             // (else they are still at hand)
 #pragma unroll
         for (int q = 0; q < KEEP; ++q) {
+            if (base + q * 64 >= hi) break;
             uint32_t b, l;
             g.place(id[q], b, l);
             const bool ok = base + q * 64 + lane < hi;
@@ -651,6 +652,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int64_t n, int
                                                                   const uint8_t *__restrict__ used, uint32_t rows) {
     __shared__ float sums[kJoinWaves - 1][64][V + 1];
     __shared__ int begins[kJoinWaves];                // the row in many parts that begins in the wave's chunk, or -1
+    __shared__ int stops[kJoinWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (blockIdx.x >= joins) {
         const uint32_t r0 = (blockIdx.x - joins) * kClearRows;
@@ -692,15 +694,18 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int64_t n, int
         for (int w = 0; w < kJoinWaves; ++w) {
             const int cur = begins[w];
             if (cur < 0) continue;                    // (uniform over the workgroup)
+            // the chunks it is the first row of: each wave looks at 64 more
             int64_t more = kJoinAlone;
-            for (;;) {
-                const int64_t q = (ch0 + w + 1 + more + lane) * chunk;
+            for (bool found = false; !found;) {
+                const int64_t q = (ch0 + w + 1 + more + wave * 64 + lane) * chunk;
                 const uint64_t stop = __ballot(q >= nv || key[q] != cur);
-                if (stop) {
-                    more += __ffsll((unsigned long long)stop) - 1;
-                    break;
+                if (lane == 0) stops[wave] = stop ? __ffsll((unsigned long long)stop) - 1 : 64;
+                __syncthreads();
+                for (int x = 0; x < kJoinWaves && !found; ++x) {
+                    more += stops[x];
+                    found = stops[x] < 64;
                 }
-                more += 64;
+                __syncthreads();
             }
 #pragma unroll
             for (int e = 0; e < V; ++e) acc[e] = 0.f;
@@ -733,7 +738,7 @@ __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__r
                                                                     uint32_t rows, int gs, int bb, int local_rows,
                                                                     float scale, float lr, float *__restrict__ dst,
                                                                     bf16_t *__restrict__ sh) {
-    extern __shared__ uint32_t cnt[];                 // [local row][wave], the end, then the tokens (16 bits each)
+    extern __shared__ __align__(16) uint32_t cnt[];                 // [local row][wave], the end, then the tokens (16 bits each)
     __shared__ uint32_t red[kSmallWaves];
     __shared__ float sums[kSmallWaves - 1][64][V + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

@@ -192,8 +192,9 @@ struct DistillArgs {
     int64_t dld;
     int c, k;
     float temperature, alpha, scale;
+    int top_dt;
 };
-hipError_t launch_distill(int dt, int top_dt, int64_t n, const DistillArgs &a, hipStream_t st);
+hipError_t launch_distill(int dt, int64_t n, const DistillArgs &a, hipStream_t st);
 // Embedding table: lookup of n tokens; the dense gradient of the table (beta 0 or 1); the table's SGD
 // update.  tld, old_, dld: elements between rows of the table, the output and dy.
 hipError_t launch_embed_fwd(int tdt, const void *table, int64_t rows, int64_t tld, int d, const int32_t *ids, int64_t n,

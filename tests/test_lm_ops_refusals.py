@@ -86,7 +86,7 @@ def test_embedding_workspace_bytes(lib):
     (dict(k=1025), SHAPE), (dict(ld=99), SHAPE), (dict(dld=99), SHAPE), (dict(scale=INF), ARG), (dict(T=0.0), ARG),
     (dict(T=-1.0), ARG), (dict(T=NAN), ARG), (dict(T=1e5), ARG), (dict(alpha=0.0), ARG), (dict(alpha=1.5), ARG),
     (dict(alpha=NAN), ARG), (dict(alpha=0.5, labels=0), ARG), (dict(n=1 << 31), OVERFLOW), (dict(n=1 << 30, ld=1 << 11), OVERFLOW),
-    (dict(z=0), NULL), (dict(top=0), NULL), (dict(idx=0), NULL), (dict(loss=0), NULL), (dict(dz=0), NULL),
+    (dict(c=(1 << 30) + 1, n=1), OVERFLOW), (dict(z=0), NULL), (dict(top=0), NULL), (dict(idx=0), NULL), (dict(loss=0), NULL), (dict(dz=0), NULL),
     (dict(z=P + 2), ALIGN), (dict(dz=P + 0x100002), ALIGN), (dict(top=P + 0x200002), ALIGN), (dict(idx=P + 0x210002), ALIGN),
     (dict(bias=P + 0x220001), ALIGN), (dict(lse=P + 0x230002), ALIGN), (dict(labels=P + 0x240002), ALIGN),
     (dict(weight=P + 0x250002), ALIGN), (dict(loss=P + 0x260002), ALIGN), (dict(dz=P + 4), ALIAS),
