@@ -44,6 +44,14 @@ __device__ __forceinline__ float wave_sumf(float v) {
     return v;
 }
 
+// The same number, as one that nothing computed from it before is known for: what a later phase computes
+// from it (addresses, exponentials) is then computed there, not kept in registers from an earlier one.
+template <typename X>
+__device__ __forceinline__ X fresh(X x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // LDS written by other lanes of this wave is there, and nothing moves across.
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -285,14 +293,6 @@ __device__ __forceinline__ T *at32(T *p, uint32_t i) {     // (a uniform base an
 // Waves per SIMD that the registers have to leave room for.
 constexpr int row_waves(int nch) { return nch <= 2 ? 8 : nch <= 4 ? 6 : 4; }
 
-// The same number, as one that nothing computed from it before is known for: what a later phase computes
-// from it (addresses, exponentials) is then computed there, not kept in registers from an earlier one.
-template <typename X>
-__device__ __forceinline__ X fresh(X x) {
-    asm volatile("" : "+v"(x));
-    return x;
-}
-
 template <typename T, int NT, int NCH, int POW>
 __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t n, int bit_words) {
     constexpr int V = 16 / sizeof(T), NW = NT / 64;
@@ -317,12 +317,20 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
     const bool bad = hard && (lab < 0 || lab >= c);
     bool done = w == 0.f || bad;                  // (uniform) a row that counts for nothing, or has no loss
     float fill = w == 0.f ? 0.f : __builtin_nanf("");
+    const bool read_last = a.z != a.dz;           // (in place, the lines are written again at once)
     typename RowVec<T, V>::raw raw[NCH];
     float xt = -INFINITY, xlab = 0.f;
     if (!done) {
+        if (read_last) {
 #pragma unroll
-        for (int i = 0; i < NCH; ++i)
-            if (i * NT + tid < whole) raw[i] = RowVec<T, V>::load(at32(z, (i * NT + tid) * V));
+            for (int i = 0; i < NCH; ++i)
+                if (i * NT + tid < whole) raw[i] = RowVec<T, V>::load_last(at32(z, (i * NT + tid) * V));
+        } else {
+            const int tid_ = fresh(tid);              // (equal addresses would make one plain load of the two)
+#pragma unroll
+            for (int i = 0; i < NCH; ++i)
+                if (i * NT + tid_ < whole) raw[i] = RowVec<T, V>::load(at32(z, (i * NT + tid_) * V));
+        }
         if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
         if (wave == 0) {
             if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
@@ -442,36 +450,275 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
     if (wave == 0) store_list<T>(a, t, l, sh, hard, lab, xlab, dz);
 }
 
+// ------------------------------------------------------------------ wider rows in registers
+// The running maximum and sums of a thread, relative to the maximum: exponents r at T, r1 at 1.
+template <int POW>
+struct Running {
+    float M, ct, r, r1, s, s1;
+    __device__ explicit Running(float ct_) : M(-INFINITY), ct(ct_), r(-kHuge * ct_), r1(-kHuge * kLog2e), s(0.f), s1(0.f) {}
+
+    template <int N>
+    __device__ __forceinline__ void add(const float (&x)[N]) {
+        float cm = M;
+#pragma unroll
+        for (int e = 0; e < N; ++e) cm = fmaxf(cm, x[e]);
+        M = cm;
+        const float at = fminf(fmaxf(cm, -kHuge), kHuge), rn = at * ct, f = ex2(r - rn);
+        s *= f;
+        if (POW == kOwn) {
+            const float rn1 = at * kLog2e;
+            s1 *= ex2(r1 - rn1);
+            r1 = rn1;
+        } else if (POW != kSame) {
+            s1 *= power<POW>(f);
+        }
+        r = rn;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float y = ex2(fmaf(x[e], ct, -rn));
+            s += y;
+            if (POW == kOwn) s1 += ex2(fmaf(x[e], kLog2e, -r1));
+            else if (POW != kSame) s1 += power<POW>(y);
+        }
+    }
+
+    // x as an exact difference from the row's maximum, where that is beyond kHuge (t.huge)
+    __device__ __forceinline__ void add_shifted(float d) {
+        const float y = ex2(d * ct);
+        s += y;
+        if (POW == kOwn) s1 += ex2(d * kLog2e);
+        else if (POW != kSame) s1 += power<POW>(y);
+    }
+
+    // relative to the row's maximum
+    __device__ __forceinline__ void settle(const RowTotals &t) {
+        const float f = ex2(r - t.R);
+        s *= f;
+        if (POW == kOwn) s1 *= ex2(r1 - t.R1);
+        else if (POW != kSame) s1 *= power<POW>(f);
+    }
+};
+
+// The gradient outside the list at x (less t.mr where t.huge).
+template <int POW>
+__device__ __forceinline__ float slope_at(const RowTotals &t, float x) {
+    const float y = ex2(fmaf(x, t.ct, -t.R));
+    if (POW == kOwn) return t.co * y + t.ch * ex2(fmaf(x, kLog2e, -t.R1));
+    if (POW == kSame) return (t.co + t.ch) * y;
+    if (POW == kSquare) return y * fmaf(t.ch, y, t.co);
+    return y * fmaf(t.ch * y, y * y, t.co);
+}
+
+// Pieces of the logits as they were read, with the listed classes made -inf.
+__device__ __forceinline__ void make_inf(u32x4_t &raw, uint32_t on) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if ((on >> (2 * e)) & 1u) raw[e] = (raw[e] & 0xffff0000u) | 0xff80u;
+        if ((on >> (2 * e + 1)) & 1u) raw[e] = (raw[e] & 0xffffu) | 0xff800000u;
+    }
+}
+__device__ __forceinline__ void make_inf(f32x4_t &raw, uint32_t on) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if ((on >> e) & 1u) raw[e] = -INFINITY;
+}
+
+// As distill_row_kernel, with the logits in registers as they were read (half the registers in bf16): the
+// bias is added twice, and the maximum and the sums are formed in one pass, piece by piece.
+template <typename T, int NT, int NCH, int POW>
+__global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64_t n, int bit_words) {
+    constexpr int V = 16 / sizeof(T), NW = NT / 64;
+    extern __shared__ __align__(16) uint32_t smem[];
+    __shared__ RowShared sh;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = a.c, k = a.k, whole = c / V;
+    const int jt = wave == NW - 1 && lane < c - whole * V ? whole * V + lane : -1;      // this lane's class past the pieces
+    RowList l;
+    l.bits = smem;
+    l.cls = (int32_t *)(smem + bit_words);
+    l.P = (float *)(l.cls + k);
+    l.x = l.P + k;
+    const bool hard = a.labels != nullptr;
+    const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (row >= n) return;
+    int tid = threadIdx.x;
+    const T *z = (const T *)a.z + row * a.zld;
+    T *dz = (T *)a.dz + row * a.dld;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    const int lab = hard ? a.labels[row] : -1;
+    const bool bad = hard && (lab < 0 || lab >= c);
+    bool done = w == 0.f || bad;                  // (uniform) a row that counts for nothing, or has no loss
+    float fill = w == 0.f ? 0.f : __builtin_nanf("");
+    typename RowVec<T, V>::raw raw[NCH];
+    float xt = -INFINITY, xlab = 0.f;
+    if (!done) {
+        if (a.z != a.dz) {                        // (in place, the lines are written again at once)
+#pragma unroll
+            for (int i = 0; i < NCH; ++i)
+                if (i * NT + tid < whole) raw[i] = RowVec<T, V>::load_last(at32(z, (i * NT + tid) * V));
+        } else {
+            const int tid_ = fresh(tid);          // (equal addresses would make one plain load of the two)
+#pragma unroll
+            for (int i = 0; i < NCH; ++i)
+                if (i * NT + tid_ < whole) raw[i] = RowVec<T, V>::load(at32(z, (i * NT + tid_) * V));
+        }
+        if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
+        if (wave == 0) {
+            if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
+            read_list<T>(a, row, z, c, l, sh);
+        }
+        __syncthreads();
+        if (!sh.soft && !hard) {
+            done = true;
+            fill = 0.f;
+        }
+    }
+    if (done) {
+        float f[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = fill;
+        for (int p = tid; p < whole; p += NT) RowVec<T, V>::store(at32(dz, p * V), f);
+        if (jt >= 0) Elem<T>::store(dz + jt, fill);
+        if (tid == 0) a.loss[row] = fill;
+        return;
+    }
+    tid = fresh(tid);
+    const auto x_of = [&](int i, float(&x)[V]) {
+        RowVec<T, V>::unpack(raw[i], x);
+        if (a.bias) {
+            float b[V];
+            RowVec<float, V>::unpack(RowVec<float, V>::load(at32(a.bias, (i * NT + tid) * V)), b);
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] += b[e];
+        }
+    };
+    if (jt >= 0 && ((l.bits[jt >> 5] >> (jt & 31)) & 1u)) xt = -INFINITY;
+    Running<POW> run(kLog2e / a.temperature);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+        if (i * NT + tid < whole) {
+            const uint32_t j = (i * NT + tid) * V, on = (l.bits[j >> 5] >> (j & 31)) & ((1u << V) - 1u);
+            if (on != 0) make_inf(raw[i], on);
+            float x[V];
+            x_of(i, x);
+            run.add(x);
+        }
+        if (i % 2 == 1) __builtin_amdgcn_sched_barrier(0);       // (two pieces' bias at a time in registers)
+    }
+    {
+        const float x[1] = {xt};
+        run.add(x);
+    }
+    float mx = wave_maxf(run.M);
+    if (lane == 0) sh.max[wave] = mx;
+    __syncthreads();
+    mx = sh.max[0];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) mx = fmaxf(mx, sh.max[q]);
+    RowTotals t;
+    t.maxima(mx, sh.mtop, a.temperature, POW);
+    const bool huge = __builtin_amdgcn_readfirstlane(t.huge);
+    if (huge) {
+        run.s = run.s1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+            if (i * NT + tid < whole) {
+                float x[V];
+                x_of(i, x);
+#pragma unroll
+                for (int e = 0; e < V; ++e) run.add_shifted(x[e] - t.mr);
+            }
+        xt -= t.mr;
+        run.add_shifted(xt);
+    } else {
+        run.settle(t);
+    }
+    float s = wave_sumf(run.s), s1 = POW != kSame ? wave_sumf(run.s1) : 0.f;
+    if (lane == 0) {
+        sh.sum[wave][0] = s;
+        sh.sum[wave][1] = s1;
+    }
+    if (wave == 0) sum_list(a, t, l, hard, sh);
+    __syncthreads();
+    s = sh.sum[0][0];
+    s1 = sh.sum[0][1];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) {
+        s += sh.sum[q][0];
+        s1 += sh.sum[q][1];
+    }
+    if (POW == kSame) s1 = s;                     // (T = 1, or not used)
+    const float pr = rest_of(a, sh);
+    t.sums(a, w, s, s1, sh, hard, pr);
+    tid = fresh(tid);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+        if (i * NT + tid < whole) {
+            float g[V];
+            x_of(i, g);
+            if (huge)
+#pragma unroll
+                for (int e = 0; e < V; ++e) g[e] -= t.mr;
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[e] = slope_at<POW>(t, g[e]);
+            if (a.away) RowVec<T, V>::store_away(at32(dz, (i * NT + tid) * V), g);
+            else RowVec<T, V>::store(at32(dz, fresh((i * NT + tid) * V)), g);
+        }
+        if (i % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    if (jt >= 0) Elem<T>::store(dz + jt, slope_at<POW>(t, xt));
+    if (wave == 0) row_loss(a, row, t, l, sh, s, pr, w, hard, xlab);
+    __syncthreads();
+    if (wave == 0) store_list<T>(a, t, l, sh, hard, lab, xlab, dz);
+}
+
 // ------------------------------------------------------------------ long rows
 // Rows that do not fit the registers are read twice: once for the maximum and the sums together (each thread
 // keeps its own running maximum and sums relative to it), once for the gradient; the second read of a row
 // follows the first closely enough to come from the caches.  The bits are those of kSeg classes at a time.
-constexpr int kSeg = 262144, kLongThreads = 1024;
+constexpr int kSeg = 262144, kLongThreads = 1024, kLongPieces = 4;
 
-// V values of x from class j: -inf past the end.
-template <typename T, int V>
-__device__ __forceinline__ void load_x(const T *z, const float *bias, int j, int c, float *x) {
-    if (j + V <= c) {
-        RowVec<T, V>::unpack(RowVec<T, V>::load(z + j), x);
-        if (bias) {
-            float b[V];
-            RowVec<float, V>::unpack(RowVec<float, V>::load(bias + j), b);
+// f(j, x) for the pieces of V classes from j0 on, j0 + NT V, ... below j1 (whole pieces), UN at a time; their
+// loads come before all else.
+template <typename T, int V, int UN, int NT, typename F>
+__device__ __forceinline__ void for_pieces(const T *z, const float *bias, int j0, int j1, bool last, F f) {
+    for (int j = j0 + (int)threadIdx.x * V; j < j1; j += UN * NT * V) {
+        typename RowVec<T, V>::raw raw[UN];
+        typename RowVec<float, V>::raw b[UN];
+        if (last) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) x[e] += b[e];
+            for (int u = 0; u < UN; ++u) raw[u] = RowVec<T, V>::load_last(z + min(j + u * NT * V, j1 - V));
+        } else {
+            const int j_ = fresh(j);                  // (equal addresses would make one plain load of the two)
+#pragma unroll
+            for (int u = 0; u < UN; ++u) raw[u] = RowVec<T, V>::load(z + min(j_ + u * NT * V, j1 - V));
         }
-    } else {
+        if (bias)
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[e] = j + e < c ? Elem<T>::load(z + j + e) + (bias ? bias[j + e] : 0.f) : -INFINITY;
+            for (int u = 0; u < UN; ++u) b[u] = RowVec<float, V>::load(bias + min(j + u * NT * V, j1 - V));
+        float x[UN][V];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            RowVec<T, V>::unpack(raw[u], x[u]);
+            if (bias) {
+                float w[V];
+                RowVec<float, V>::unpack(b[u], w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) x[u][e] += w[e];
+            }
+        }
+        f(j, x);
     }
 }
 
 template <typename T, int POW>
 __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs a, int64_t n, int bit_words) {
-    constexpr int V = 16 / sizeof(T), NT = kLongThreads, NW = NT / 64, UN = 4;
+    constexpr int V = 16 / sizeof(T), NT = kLongThreads, NW = NT / 64, UN = kLongPieces;
     extern __shared__ __align__(16) uint32_t smem[];
     __shared__ RowShared sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c = a.c, k = a.k;
+    const int c = a.c, k = a.k, whole = c / V * V;
+    const int jt = wave == NW - 1 && lane < c - whole ? whole + lane : -1;              // this lane's class past the pieces
     RowList l;
     l.bits = smem;
     l.cls = (int32_t *)(smem + bit_words);
@@ -487,8 +734,9 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
     const bool bad = hard && (lab < 0 || lab >= c);
     bool done = w == 0.f || bad;                  // (uniform) a row that counts for nothing, or has no loss
     float fill = w == 0.f ? 0.f : __builtin_nanf("");
-    float xlab = 0.f;
+    float xt = -INFINITY, xlab = 0.f;
     if (!done) {
+        if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
         if (wave == 0) {
             if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
             read_list<T>(a, row, z, min(c, kSeg), l, sh);
@@ -500,18 +748,15 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
         }
     }
     if (done) {
-        for (int j = tid * V; j < c; j += NT * V) {
-            float f[V];
+        float f[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) f[e] = fill;
-            if (j + V <= c) RowVec<T, V>::store(dz + j, f);
-            else
-                for (int e = 0; j + e < c; ++e) Elem<T>::store(dz + j + e, fill);
-        }
+        for (int e = 0; e < V; ++e) f[e] = fill;
+        for (int j = tid * V; j < whole; j += NT * V) RowVec<T, V>::store(dz + j, f);
+        if (jt >= 0) Elem<T>::store(dz + jt, fill);
         if (tid == 0) a.loss[row] = fill;
         return;
     }
-    // f(x) for every piece of V classes, listed ones -inf
+    // f(x) for the pieces' classes, listed ones and those past the end -inf
     const auto outside = [&](bool marked, auto f) {
         for (int s0 = 0; s0 < c; s0 += kSeg) {
             if (s0 > 0 || !marked) {              // (read_list has marked the first segment)
@@ -519,6 +764,7 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
                 if (wave == 0) {
                     clear_bits(l.bits, min(c, kSeg));
                     wave_sync();
+#pragma unroll 1
                     for (int j = lane; j < k; j += 64) {
                         const int32_t i = l.cls[j];
                         if (i >= s0 && i - s0 < kSeg) atomicOr(&l.bits[(i - s0) >> 5], 1u << ((i - s0) & 31));
@@ -526,14 +772,12 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
                 }
                 __syncthreads();
             }
-            const int s1 = min(c, s0 + kSeg);
-            for (int j0 = s0 + tid * V; j0 < s1; j0 += NT * V * UN) {
-                float x[UN][V];
+            const int s1 = min(whole, s0 + kSeg);
+            for_pieces<T, V, UN, NT>(z, a.bias, s0, s1, false, [&](int j, float(&x)[UN][V]) {
 #pragma unroll
                 for (int u = 0; u < UN; ++u) {
-                    const int j = j0 + u * NT * V;
-                    load_x<T, V>(z, a.bias, j < s1 ? j : c, c, x[u]);
-                    const uint32_t on = j < s1 ? (l.bits[(j - s0) >> 5] >> ((j - s0) & 31)) & ((1u << V) - 1u) : 0u;
+                    const int q = j + u * NT * V - s0;
+                    const uint32_t on = q < s1 - s0 ? (l.bits[q >> 5] >> (q & 31)) & ((1u << V) - 1u) : (1u << V) - 1u;
                     if (on != 0) {
 #pragma unroll
                         for (int e = 0; e < V; ++e)
@@ -541,39 +785,17 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
                     }
                 }
                 f(x);
-            }
+            });
+            if (s0 + kSeg >= c && jt >= 0 && ((l.bits[(jt - s0) >> 5] >> ((jt - s0) & 31)) & 1u)) xt = -INFINITY;
         }
     };
-    const float ct = kLog2e / a.temperature;
-    float M = -INFINITY, r = -kHuge * ct, r1 = -kHuge * kLog2e, s = 0.f, s1 = 0.f;
-    outside(true, [&](float(&x)[UN][V]) {
-        float cm = M;
-#pragma unroll
-        for (int u = 0; u < UN; ++u)
-#pragma unroll
-            for (int e = 0; e < V; ++e) cm = fmaxf(cm, x[u][e]);
-        M = cm;
-        const float at = fminf(fmaxf(cm, -kHuge), kHuge), rn = at * ct;
-        s *= ex2(r - rn);
-        if (POW == kOwn) {
-            const float rn1 = at * kLog2e;
-            s1 *= ex2(r1 - rn1);
-            r1 = rn1;
-        } else if (POW != kSame) {
-            s1 *= power<POW>(ex2(r - rn));
-        }
-        r = rn;
-#pragma unroll
-        for (int u = 0; u < UN; ++u)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float y = ex2(fmaf(x[u][e], ct, -rn));
-                s += y;
-                if (POW == kOwn) s1 += ex2(fmaf(x[u][e], kLog2e, -r1));
-                else if (POW != kSame) s1 += power<POW>(y);
-            }
-    });
-    float mx = wave_maxf(M);
+    Running<POW> run(kLog2e / a.temperature);
+    outside(true, [&](float(&x)[UN][V]) { run.add(*reinterpret_cast<float(*)[UN * V]>(&x)); });
+    {
+        const float x[1] = {xt};
+        run.add(x);
+    }
+    float mx = wave_maxf(run.M);
     if (lane == 0) sh.max[wave] = mx;
     __syncthreads();
     mx = sh.max[0];
@@ -581,26 +803,21 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
     for (int q = 1; q < NW; ++q) mx = fmaxf(mx, sh.max[q]);
     RowTotals t;
     t.maxima(mx, sh.mtop, a.temperature, POW);
-    if (t.huge) {                                 // relative to the maximum by exact differences, read again
-        s = s1 = 0.f;
+    const bool huge = __builtin_amdgcn_readfirstlane(t.huge);
+    if (huge) {                                   // (read again)
+        run.s = run.s1 = 0.f;
         outside(c <= kSeg, [&](float(&x)[UN][V]) {
 #pragma unroll
             for (int u = 0; u < UN; ++u)
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float y = ex2((x[u][e] - t.mr) * ct);
-                    s += y;
-                    if (POW == kOwn) s1 += ex2((x[u][e] - t.mr) * kLog2e);
-                    else if (POW != kSame) s1 += power<POW>(y);
-                }
+                for (int e = 0; e < V; ++e) run.add_shifted(x[u][e] - t.mr);
         });
+        xt -= t.mr;
+        run.add_shifted(xt);
     } else {
-        s *= ex2(r - t.R);
-        if (POW == kOwn) s1 *= ex2(r1 - t.R1);
-        else if (POW != kSame) s1 *= power<POW>(ex2(r - t.R));
+        run.settle(t);
     }
-    s = wave_sumf(s);
-    if (POW != kSame) s1 = wave_sumf(s1);
+    float s = wave_sumf(run.s), s1 = POW != kSame ? wave_sumf(run.s1) : 0.f;
     if (lane == 0) {
         sh.sum[wave][0] = s;
         sh.sum[wave][1] = s1;
@@ -614,34 +831,26 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
         s += sh.sum[q][0];
         s1 += sh.sum[q][1];
     }
-    if (POW == kSame) s1 = s;
+    if (POW == kSame) s1 = s;                     // (T = 1, or not used)
     const float pr = rest_of(a, sh);
     t.sums(a, w, s, s1, sh, hard, pr);
-    const float cs = t.co + t.ch;
-    for (int j0 = tid * V; j0 < c; j0 += NT * V * UN) {
-        float x[UN][V];
+    for_pieces<T, V, UN, NT>(z, a.bias, 0, whole, a.z != a.dz, [&](int j, float(&x)[UN][V]) {
+        if (huge)
 #pragma unroll
-        for (int u = 0; u < UN; ++u) load_x<T, V>(z, a.bias, min(j0 + u * NT * V, c), c, x[u]);
+            for (int u = 0; u < UN; ++u)
+#pragma unroll
+                for (int e = 0; e < V; ++e) x[u][e] -= t.mr;
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int j = j0 + u * NT * V;
-            if (j >= c) break;
             float g[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                if (t.huge) x[u][e] -= t.mr;
-                const float y = ex2(fmaf(x[u][e], ct, -t.R));
-                if (POW == kOwn) g[e] = t.co * y + t.ch * ex2(fmaf(x[u][e], kLog2e, -t.R1));
-                else if (POW == kSame) g[e] = cs * y;
-                else g[e] = t.co * y + t.ch * power<POW>(y);
-            }
-            if (j + V <= c) RowVec<T, V>::store(dz + j, g);
-            else
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    if (j + e < c) Elem<T>::store(dz + j + e, g[e]);
+            for (int e = 0; e < V; ++e) g[e] = slope_at<POW>(t, x[u][e]);
+            if (j + u * NT * V >= whole) break;
+            if (a.away) RowVec<T, V>::store_away(dz + j + u * NT * V, g);
+            else RowVec<T, V>::store(dz + fresh(j + u * NT * V), g);
         }
-    }
+    });
+    if (jt >= 0) Elem<T>::store(dz + jt, slope_at<POW>(t, xt));
     if (wave == 0) row_loss(a, row, t, l, sh, s, pr, w, hard, xlab);
     __syncthreads();
     if (wave == 0) store_list<T>(a, t, l, sh, hard, lab, xlab, dz);
@@ -674,11 +883,18 @@ static hipError_t launch_typed(const DistillArgs &a, int64_t n, hipStream_t st) 
     else if (pieces <= 512 * 4) launch_rows<T, 512, 4>(a, n, two, lds, words, st);
     else if (pieces <= 512 * 7) launch_rows<T, 512, 7>(a, n, two, lds, words, st);
     else if (pieces <= 512 * 10) launch_rows<T, 512, 10>(a, n, two, lds, words, st);
-    else if (pieces <= 1024 * 8) launch_rows<T, 1024, 8>(a, n, two, lds, words, st);
     else {
         const dim3 g = row_grid(n);
         const int kind = !two ? kSame : a.temperature == 2.f ? kSquare : a.temperature == 4.f ? kFourth : kOwn;
-#define TFK_GO(POW) hipLaunchKernelGGL((distill_long_kernel<T, POW>), g, dim3(kLongThreads), lds, st, a, n, words)
+#define TFK_GO(POW)                                                                                                   \
+    do {                                                                                                              \
+        if (pieces <= 512 * 16)                                                                                       \
+            hipLaunchKernelGGL((distill_raw_kernel<T, 512, 16, POW>), g, dim3(512), lds, st, a, n, words);            \
+        else if (pieces <= 1024 * 16)                                                                                 \
+            hipLaunchKernelGGL((distill_raw_kernel<T, 1024, 16, POW>), g, dim3(1024), lds, st, a, n, words);          \
+        else                                                                                                          \
+            hipLaunchKernelGGL((distill_long_kernel<T, POW>), g, dim3(kLongThreads), lds, st, a, n, words);           \
+    } while (0)
         if (kind == kSame) TFK_GO(kSame);
         else if (kind == kSquare) TFK_GO(kSquare);
         else if (kind == kFourth) TFK_GO(kFourth);
@@ -688,7 +904,10 @@ static hipError_t launch_typed(const DistillArgs &a, int64_t n, hipStream_t st) 
     return hipGetLastError();
 }
 
-hipError_t launch_distill(int dt, int64_t n, const DistillArgs &a, hipStream_t st) {
+hipError_t launch_distill(int dt, int64_t n, const DistillArgs &args, hipStream_t st) {
+    DistillArgs a = args;
+    // a gradient that no cache could hold for the next operation goes past them
+    a.away = a.z != a.dz && n * a.c * (dt == 0 ? 4 : 2) > ((int64_t)512 << 20);
     return dt == 0 ? launch_typed<float>(a, n, st) : launch_typed<bf16_t>(a, n, st);
 }
 

@@ -32,6 +32,11 @@ struct RowVec<float, 4> {
     __device__ static void store(float *p, const float *v) {
         *reinterpret_cast<f32x4_a4_t *>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
     }
+    __device__ static raw load_last(const float *p) { return __builtin_nontemporal_load(reinterpret_cast<const f32x4_a4_t *>(p)); }
+    __device__ static void store_away(float *p, const float *v) {
+        const f32x4_a4_t r = f32x4_t{v[0], v[1], v[2], v[3]};
+        __builtin_nontemporal_store(r, reinterpret_cast<f32x4_a4_t *>(p));
+    }
 };
 
 template <>
@@ -75,5 +80,12 @@ struct RowVec<bf16_t, 8> {
 #pragma unroll
         for (int e = 0; e < 4; ++e) r[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
         *reinterpret_cast<u32x4_a2_t *>(p) = r;
+    }
+    __device__ static raw load_last(const bf16_t *p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_a2_t *>(p)); }
+    __device__ static void store_away(bf16_t *p, const float *v) {
+        u32x4_a2_t r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+        __builtin_nontemporal_store(r, reinterpret_cast<u32x4_a2_t *>(p));
     }
 };
