@@ -23,6 +23,10 @@
 #include "kernels.h"
 #include "rowvec.h"
 
+// R is a rounded product: an fma that formed it anew inside a difference would see another one.  Where an fma
+// is wanted, it is written.
+#pragma clang fp contract(off)
+
 namespace tfk {
 
 // Where the T = 1 exponentials of the hard term come from: those at T themselves (no hard term, or T = 1),
@@ -82,20 +86,32 @@ __device__ __forceinline__ void clear_bits(uint32_t *bits, int seg) {
     for (int q = threadIdx.x & 63; q < (seg + 127) / 128; q += 64) b4[q] = u32x4_t{0, 0, 0, 0};
 }
 
+// A lane's first entry of the list, asked for before anything else is known about the row.
+struct ListHead {
+    int32_t idx;
+    float t;
+};
+__device__ __forceinline__ float top_at(const DistillArgs &a, int64_t i) {
+    return a.top_dt == 0 ? ((const float *)a.top)[i] : bf16_to_f32(((const bf16_t *)a.top)[i]);
+}
+__device__ __forceinline__ ListHead list_head(const DistillArgs &a, int64_t row) {
+    const int64_t i = row * a.k + min((int)(threadIdx.x & 63), a.k - 1);
+    return {a.top_idx[i], top_at(a, i)};
+}
+
 // The first wave: reads the list, forms P, adds up the entries of one class under the first of them, marks
 // the bits of classes [0, seg), and gathers x.
 template <typename T>
-__device__ __forceinline__ void read_list(const DistillArgs &a, int64_t row, const T *z, int seg, const RowList &l,
-                                          RowShared &sh) {
+__device__ __forceinline__ void read_list(const DistillArgs &a, int64_t row, const ListHead &head, const T *z, int seg,
+                                          const RowList &l, RowShared &sh) {
     const int lane = threadIdx.x & 63, k = a.k, c = a.c;
     const int32_t *idx = a.top_idx + row * k;
     float tm = -INFINITY;
 #pragma unroll 1
     for (int j = lane; j < k; j += 64) {
-        const int32_t i = idx[j];
+        const int32_t i = j < 64 ? head.idx : idx[j];
         const bool ok = i >= 0 && i < c;
-        float t = a.top_dt == 0 ? ((const float *)a.top)[row * k + j] : bf16_to_f32(((const bf16_t *)a.top)[row * k + j]);
-        if (!ok) t = -INFINITY;
+        const float t = !ok ? -INFINITY : j < 64 ? head.t : top_at(a, row * k + j);
         l.cls[j] = ok ? i : -1;
         l.P[j] = t;
         tm = fmaxf(tm, t != t ? INFINITY : t);
@@ -280,6 +296,14 @@ __device__ __forceinline__ float power(float e) {
     return e;
 }
 
+// s + power(e)
+template <int POW>
+__device__ __forceinline__ float add_power(float e, float s) {
+    if (POW == kSquare) return fmaf(e, e, s);
+    if (POW == kFourth) return fmaf(e * e, e * e, s);
+    return s + e;
+}
+
 // ------------------------------------------------------------------ rows in registers
 // A workgroup of NT threads has a row of up to NT * NCH * V classes in registers, in fp32: one read of the
 // logits and one write of the gradient.  Piece i of thread t is V classes from (i NT + t) V; the c % V
@@ -312,6 +336,8 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
     int tid = fresh(threadIdx.x);
     const T *z = (const T *)a.z + row * a.zld;
     T *dz = (T *)a.dz + row * a.dld;
+    ListHead head{};
+    if (wave == 0) head = list_head(a, row);
     const float w = a.weight ? a.weight[row] : 1.f;
     const int lab = hard ? a.labels[row] : -1;
     const bool bad = hard && (lab < 0 || lab >= c);
@@ -320,7 +346,7 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
     const bool read_last = a.z != a.dz;           // (in place, the lines are written again at once)
     typename RowVec<T, V>::raw raw[NCH];
     float xt = -INFINITY, xlab = 0.f;
-    if (!done) {
+    const auto read = [&]() {
         if (read_last) {
 #pragma unroll
             for (int i = 0; i < NCH; ++i)
@@ -331,10 +357,14 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
             for (int i = 0; i < NCH; ++i)
                 if (i * NT + tid_ < whole) raw[i] = RowVec<T, V>::load(at32(z, (i * NT + tid_) * V));
         }
+    };
+    if (NT == 64) read();                         // (short rows: not after the weight and the label)
+    if (!done) {
+        if (NT != 64) read();
         if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
         if (wave == 0) {
             if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
-            read_list<T>(a, row, z, c, l, sh);
+            read_list<T>(a, row, head, z, c, l, sh);
         }
         __syncthreads();
         if (!sh.soft && !hard) {
@@ -433,7 +463,7 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
     tid = fresh(tid);
     const float R = fresh(t.R), R1 = fresh(t.R1);
     const auto slope = [&](float v) {
-        return POW == kOwn ? t.co * ex2(fmaf(v, t.ct, -R)) + t.ch * ex2(fmaf(v, kLog2e, -R1)) : cs * v;
+        return POW == kOwn ? fmaf(t.ch, ex2(fmaf(v, kLog2e, -R1)), t.co * ex2(fmaf(v, t.ct, -R))) : cs * v;
     };
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
@@ -478,7 +508,7 @@ struct Running {
             const float y = ex2(fmaf(x[e], ct, -rn));
             s += y;
             if (POW == kOwn) s1 += ex2(fmaf(x[e], kLog2e, -r1));
-            else if (POW != kSame) s1 += power<POW>(y);
+            else if (POW != kSame) s1 = add_power<POW>(y, s1);
         }
     }
 
@@ -487,7 +517,7 @@ struct Running {
         const float y = ex2(d * ct);
         s += y;
         if (POW == kOwn) s1 += ex2(d * kLog2e);
-        else if (POW != kSame) s1 += power<POW>(y);
+        else if (POW != kSame) s1 = add_power<POW>(y, s1);
     }
 
     // relative to the row's maximum
@@ -503,7 +533,7 @@ struct Running {
 template <int POW>
 __device__ __forceinline__ float slope_at(const RowTotals &t, float x) {
     const float y = ex2(fmaf(x, t.ct, -t.R));
-    if (POW == kOwn) return t.co * y + t.ch * ex2(fmaf(x, kLog2e, -t.R1));
+    if (POW == kOwn) return fmaf(t.ch, ex2(fmaf(x, kLog2e, -t.R1)), t.co * y);
     if (POW == kSame) return (t.co + t.ch) * y;
     if (POW == kSquare) return y * fmaf(t.ch, y, t.co);
     return y * fmaf(t.ch * y, y * y, t.co);
@@ -544,6 +574,8 @@ __global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64
     int tid = threadIdx.x;
     const T *z = (const T *)a.z + row * a.zld;
     T *dz = (T *)a.dz + row * a.dld;
+    ListHead head{};
+    if (wave == 0) head = list_head(a, row);
     const float w = a.weight ? a.weight[row] : 1.f;
     const int lab = hard ? a.labels[row] : -1;
     const bool bad = hard && (lab < 0 || lab >= c);
@@ -565,7 +597,7 @@ __global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64
         if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
         if (wave == 0) {
             if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
-            read_list<T>(a, row, z, c, l, sh);
+            read_list<T>(a, row, head, z, c, l, sh);
         }
         __syncthreads();
         if (!sh.soft && !hard) {
@@ -729,6 +761,8 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
     if (row >= n) return;
     const T *z = (const T *)a.z + row * a.zld;
     T *dz = (T *)a.dz + row * a.dld;
+    ListHead head{};
+    if (wave == 0) head = list_head(a, row);
     const float w = a.weight ? a.weight[row] : 1.f;
     const int lab = hard ? a.labels[row] : -1;
     const bool bad = hard && (lab < 0 || lab >= c);
@@ -739,7 +773,7 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
         if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
         if (wave == 0) {
             if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
-            read_list<T>(a, row, z, min(c, kSeg), l, sh);
+            read_list<T>(a, row, head, z, min(c, kSeg), l, sh);
         }
         __syncthreads();
         if (!sh.soft && !hard) {
@@ -883,14 +917,13 @@ static hipError_t launch_typed(const DistillArgs &a, int64_t n, hipStream_t st) 
     else if (pieces <= 512 * 4) launch_rows<T, 512, 4>(a, n, two, lds, words, st);
     else if (pieces <= 512 * 7) launch_rows<T, 512, 7>(a, n, two, lds, words, st);
     else if (pieces <= 512 * 10) launch_rows<T, 512, 10>(a, n, two, lds, words, st);
+    else if (pieces <= 1024 * 8) launch_rows<T, 1024, 8>(a, n, two, lds, words, st);
     else {
         const dim3 g = row_grid(n);
         const int kind = !two ? kSame : a.temperature == 2.f ? kSquare : a.temperature == 4.f ? kFourth : kOwn;
 #define TFK_GO(POW)                                                                                                   \
     do {                                                                                                              \
-        if (pieces <= 512 * 16)                                                                                       \
-            hipLaunchKernelGGL((distill_raw_kernel<T, 512, 16, POW>), g, dim3(512), lds, st, a, n, words);            \
-        else if (pieces <= 1024 * 16)                                                                                 \
+        if (pieces <= 1024 * 16)                                                                                      \
             hipLaunchKernelGGL((distill_raw_kernel<T, 1024, 16, POW>), g, dim3(1024), lds, st, a, n, words);          \
         else                                                                                                          \
             hipLaunchKernelGGL((distill_long_kernel<T, POW>), g, dim3(kLongThreads), lds, st, a, n, words);           \
