@@ -602,20 +602,18 @@ def _vector(t, dtype, n, name):
         raise ValueError("%s must be a contiguous %s tensor of %d values" % (name, str(dtype).split(".")[-1], n))
 
 
-def _on_device(stream, *tensors):
-    """Every operand must be on the current GPU, whose stream (given or current) the call is enqueued on."""
-    at = None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("operands must be on the GPU, got one on %s" % t.device)
-        if at is None:
-            at = t.get_device()
-        if t.get_device() != at:
-            raise ValueError("operands are on different GPUs")
+def _on_device(stream, first, *others) -> int:
+    """The stream to enqueue on (given or current).  Every operand must be on the current GPU, and the
+    stream of that GPU."""
+    at = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != at:
+            raise ValueError("operands must be on one GPU, got %s and %s" % (first.device, t.device))
+    if at < 0:
+        raise ValueError("operands must be on the GPU, got one on %s" % first.device)
     if at != torch.cuda.current_device() or (stream is not None and stream.device.index != at):
         raise ValueError("operands are on GPU %d, which is not the current device or the stream's" % at)
+    return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
 
 
 # ----------------------------------------------------------------------------- distillation
@@ -645,14 +643,14 @@ def distill_xent(logits, top_idx, top, scale, temperature=1.0, top_lse=None, lab
     if dlogits is not None and (dlogits.shape != logits.shape or dlogits.dtype != logits.dtype):
         raise ValueError("dlogits must have the logits' shape and type")
     dld = ld if dlogits is logits else (c if dlogits is None else _rows_of(dlogits, "dlogits")[2])
-    _on_device(stream, logits, top, top_idx, top_lse, labels, weight, bias, loss, dlogits)
+    st = _on_device(stream, logits, top, top_idx, top_lse, labels, weight, bias, loss, dlogits)
     if loss is None:
         loss = _empty(stream, n, dtype=torch.float32, device=logits.device)
     if dlogits is None:
         dlogits = _empty_like(stream, logits)
     check(load().tfk_distill_xent(_ptr(logits), dt, n, c, ld, _ptr(bias), _ptr(top), tdt, _ptr(top_idx), top.shape[-1],
                                   _ptr(top_lse), _ptr(labels), _ptr(weight), float(temperature), float(alpha),
-                                  float(scale), _ptr(loss), _ptr(dlogits), dld, _stream(stream)))
+                                  float(scale), _ptr(loss), _ptr(dlogits), dld, st))
     return loss, dlogits
 
 
@@ -673,7 +671,7 @@ def embedding_fwd(table, ids, scale=1.0, out=None, out_dtype=None, stream=None):
     dt = _dt(table)
     shape = tuple(ids.shape) + (d,)
     if out is None:
-        _on_device(stream, table, ids)
+        st = _on_device(stream, table, ids)
         out = _empty(stream, shape, dtype=out_dtype or table.dtype, device=table.device)
         old = d
     else:
@@ -681,9 +679,9 @@ def embedding_fwd(table, ids, scale=1.0, out=None, out_dtype=None, stream=None):
             raise ValueError("out must be %s%s, got %s of %s" % (shape, " of %s" % out_dtype if out_dtype else "",
                                                                 tuple(out.shape), out.dtype))
         old = d if len(shape) == 1 else _rows_of(out, "out")[2]
-        _on_device(stream, table, ids, out)
+        st = _on_device(stream, table, ids, out)
     check(load().tfk_embedding_fwd(_ptr(table), dt, rows, tld, d, _ptr(ids), n, float(scale), _ptr(out), _dt(out), old,
-                                   _stream(stream)))
+                                   st))
     return out
 
 
@@ -697,18 +695,18 @@ _embed_need = functools.lru_cache(_KEPT)(embedding_workspace_bytes)
 
 def _embed_args(dy, ids, stream, ws, rows, d, *more):
     """Checks dy (ids' shape with d columns) and the operands' device; returns (n, dy's row distance,
-    workspace, its bytes)."""
+    workspace, its bytes, stream)."""
     n = _ids(ids)
     if tuple(dy.shape) != tuple(ids.shape) + (d,):
         raise ValueError("dy must be %s, got %s" % (tuple(ids.shape) + (d,), tuple(dy.shape)))
     ld = d if dy.dim() == 1 and dy.is_contiguous() else _rows_of(dy, "dy")[2]
     if ws is not None and not ws.is_contiguous():
         raise ValueError("ws must be contiguous")
-    _on_device(stream, dy, ids, ws, *more)
+    st = _on_device(stream, dy, ids, ws, *more)
     need = _embed_need(n, d, rows)
     if need and (ws is None or ws.numel() * ws.element_size() < need):
         ws = _ws(need, dy.device, stream)
-    return n, ld, ws, need
+    return n, ld, ws, need, st
 
 
 def embedding_bwd(dy, ids, rows, scale=1.0, dtable=None, beta=0.0, ws=None, stream=None):
@@ -722,11 +720,11 @@ def embedding_bwd(dy, ids, rows, scale=1.0, dtable=None, beta=0.0, ws=None, stre
                                not dtable.is_contiguous()):
         raise ValueError("dtable must be a contiguous float32 tensor of %d x %d" % (rows, d))
     dt = _dt(dy)
-    n, ld, ws, need = _embed_args(dy, ids, stream, ws, rows, d, dtable)
+    n, ld, ws, need, st = _embed_args(dy, ids, stream, ws, rows, d, dtable)
     if dtable is None:
         dtable = _empty(stream, (rows, d), dtype=torch.float32, device=dy.device)
     check(load().tfk_embedding_bwd(_ptr(dy), dt, n, ld, d, _ptr(ids), rows, float(scale), float(beta), _ptr(dtable),
-                                   _ptr(ws), need, _stream(stream)))
+                                   _ptr(ws), need, st))
     return dtable
 
 
@@ -739,9 +737,9 @@ def embedding_apply_sgd(var, ids, dy, lr, scale=1.0, shadow=None, ws=None, strea
         raise ValueError("shadow must be a contiguous bfloat16 tensor of var's shape")
     rows, d = var.shape
     dt = _dt(dy)
-    n, ld, ws, need = _embed_args(dy, ids, stream, ws, rows, d, var, shadow)
+    n, ld, ws, need, st = _embed_args(dy, ids, stream, ws, rows, d, var, shadow)
     check(load().tfk_embedding_apply_sgd(_ptr(var), _ptr(shadow), rows, d, _ptr(ids), n, _ptr(dy), dt, ld, float(scale),
-                                         float(lr), _ptr(ws), need, _stream(stream)))
+                                         float(lr), _ptr(ws), need, st))
     return var
 
 
