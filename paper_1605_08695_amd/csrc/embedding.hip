@@ -118,20 +118,26 @@ __device__ __forceinline__ uint32_t place_row(uint32_t bucket, uint32_t local, i
 // What becomes of a row's sum g (scaled): stored, added to what is there, or applied as an SGD step.
 enum { kStore = 0, kAdd = 1, kSgd = 2 };
 
+// What is there (kAdd, kSgd): V columns from o, asked for before the sum is known.
+template <int MODE, int V>
+__device__ __forceinline__ typename RowVec<float, V>::raw row_old(const float *dst, int64_t o) {
+    if constexpr (MODE == kStore) return {};
+    else return RowVec<float, V>::load(dst + o);
+}
+
 // V columns from o of the row's result; the first `skip` of them belong to another lane.
 template <int MODE, int V>
-__device__ __forceinline__ void row_finish(float *dst, bf16_t *sh, int64_t o, const float *s, int skip, float scale,
-                                           float lr) {
+__device__ __forceinline__ void row_finish(float *dst, bf16_t *sh, int64_t o, const float *s,
+                                           const typename RowVec<float, V>::raw &old_, int skip, float scale, float lr) {
+    float g[V], old[V];
+    if constexpr (MODE != kStore) RowVec<float, V>::unpack(old_, old);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        g[e] = scale * s[e];
+        if constexpr (MODE == kAdd) g[e] = old[e] + g[e];
+        if constexpr (MODE == kSgd) g[e] = fmaf(-lr, g[e], old[e]);
+    }
     if (skip == 0) {
-        float g[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) g[e] = scale * s[e];
-        if (MODE != kStore) {
-            float old[V];
-            RowVec<float, V>::unpack(RowVec<float, V>::load(dst + o), old);
-#pragma unroll
-            for (int e = 0; e < V; ++e) g[e] = MODE == kAdd ? old[e] + g[e] : fmaf(-lr, g[e], old[e]);
-        }
         RowVec<float, V>::store(dst + o, g);
         if (MODE == kSgd && sh != nullptr) RowVec<bf16_t, V>::store(sh + o, g);
         return;
@@ -139,10 +145,8 @@ __device__ __forceinline__ void row_finish(float *dst, bf16_t *sh, int64_t o, co
 #pragma unroll
     for (int e = 0; e < V; ++e)
         if (e >= skip) {
-            float g = scale * s[e];
-            if (MODE != kStore) g = MODE == kAdd ? dst[o + e] + g : fmaf(-lr, g, dst[o + e]);
-            dst[o + e] = g;
-            if (MODE == kSgd && sh != nullptr) sh[o + e] = (bf16_t)f32_to_bf16(g);
+            dst[o + e] = g[e];
+            if (MODE == kSgd && sh != nullptr) sh[o + e] = (bf16_t)f32_to_bf16(g[e]);
         }
 }
 
@@ -477,25 +481,32 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
     };
     const uint32_t per = ((m + kBucketWaves - 1) / kBucketWaves + 63) / 64 * 64;
     const uint32_t lo = min(m, wave * per), hi = min(m, lo + per);
-    constexpr int KEEP = 16;                          // entries that a lane has at hand, and fetches at a time
+    // entries that a lane has at hand, and fetches at a time; worked on four by four, side by side
+    constexpr int KEEP = 16;
     uint32_t tok[KEEP], id[KEEP];
     const auto fetch = [&](uint32_t base) {
 #pragma unroll
-        for (int q = 0; q < KEEP; ++q) {
-            if (base + q * 64 >= hi) break;
-            const uint32_t i = base + q * 64 + lane, at_ = where(i < hi ? i : lo);
-            id[q] = (uint32_t)tkey[at_];
-            tok[q] = (uint32_t)ttok[at_];
+        for (int q0 = 0; q0 < KEEP; q0 += 4) {
+            if (base + q0 * 64 >= hi) break;
+#pragma unroll
+            for (int q = q0; q < q0 + 4; ++q) {
+                const uint32_t i = base + q * 64 + lane, at_ = where(i < hi ? i : lo);
+                id[q] = (uint32_t)tkey[at_];
+                tok[q] = (uint32_t)ttok[at_];
+            }
         }
     };
     for (uint32_t base = lo; base < hi; base += KEEP * 64) {
         fetch(base);
 #pragma unroll
-        for (int q = 0; q < KEEP; ++q) {
-            if (base + q * 64 >= hi) break;
-            uint32_t b, l;
-            g.place(id[q], b, l);
-            if (base + q * 64 + lane < hi) atomicAdd(&cnt[l * kBucketWaves + wave], 1u);
+        for (int q0 = 0; q0 < KEEP; q0 += 4) {
+            if (base + q0 * 64 >= hi) break;
+#pragma unroll
+            for (int q = q0; q < q0 + 4; ++q) {
+                uint32_t b, l;
+                g.place(id[q], b, l);
+                if (base + q * 64 + lane < hi) atomicAdd(&cnt[l * kBucketWaves + wave], 1u);
+            }
         }
     }
     __syncthreads();
@@ -511,16 +522,26 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
     for (uint32_t base = lo; base < hi; base += KEEP * 64) {
         if (per > KEEP * 64) fetch(base);             // (else they are still at hand)
 #pragma unroll
-        for (int q = 0; q < KEEP; ++q) {
-            if (base + q * 64 >= hi) break;
-            uint32_t b, l;
-            g.place(id[q], b, l);
-            const bool ok = base + q * 64 + lane < hi;
-            const uint32_t p = take_places(&cnt[l * kBucketWaves + wave], same_lanes<10>(l, local_bits, ok), ok, lane);
-            if (ok) {
-                order[p] = (int32_t)tok[q];
-                key[p] = (int32_t)id[q];
+        for (int q0 = 0; q0 < KEEP; q0 += 4) {
+            if (base + q0 * 64 >= hi) break;
+            uint32_t p[4], l[4];
+            uint64_t same[4];
+            bool ok[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint32_t b;
+                g.place(id[q0 + q], b, l[q]);
+                ok[q] = base + (q0 + q) * 64 + lane < hi;
+                same[q] = same_lanes<10>(l[q], local_bits, ok[q]);
             }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) p[q] = take_places(&cnt[l[q] * kBucketWaves + wave], same[q], ok[q], lane);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (ok[q]) {
+                    order[p[q]] = (int32_t)tok[q0 + q];
+                    key[p[q]] = (int32_t)id[q0 + q];
+                }
         }
     }
 }
@@ -581,39 +602,42 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
     float *const slot = part + ch * 2 * d + c0;
-    const auto finish = [&](bool as_part, bool began) {
-        if (!act) return;
-        if (as_part) {
+    const auto as_part = [&](bool began) {
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (e >= skip) slot[(began ? d : 0) + e] = acc[e];
-        } else {
-            row_finish<MODE, V>(dst, sh, (int64_t)cur * d + c0, acc, skip, scale, lr);
-        }
+        for (int e = 0; e < V; ++e)
+            if (act && e >= skip) slot[(began ? d : 0) + e] = acc[e];
     };
-    for (; i < end; i += 8) {
-        typename RowVec<T, V>::raw buf[8];
+    // kAhead tokens at a time; with each that ends its row, what is there in the row
+    constexpr int kAhead = MODE == kStore ? 8 : 4;
+    for (; i < end; i += kAhead) {
+        typename RowVec<T, V>::raw buf[kAhead];
+        typename RowVec<float, V>::raw old[kAhead];
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (i + u < end && act) buf[u] = RowVec<T, V>::load(dy + __builtin_amdgcn_readlane(tok, i + u) * dld + c0);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if (i + u >= end) break;
-            const int r = __builtin_amdgcn_readlane(row, i + u);
-            if (r != cur) {
-                finish(head, false);
-                cur = r;
-                head = false;
-#pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] = 0.f;
+        for (int u = 0; u < kAhead; ++u)
+            if (i + u < end && act) {
+                buf[u] = RowVec<T, V>::load(dy + __builtin_amdgcn_readlane(tok, i + u) * dld + c0);
+                const int r = __builtin_amdgcn_readlane(row, i + u);
+                if (MODE != kStore && (i + u + 1 >= end || __builtin_amdgcn_readlane(row, i + u + 1) != r))
+                    old[u] = row_old<MODE, V>(dst, (int64_t)r * d + c0);
             }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (i + u >= end) break;
             float f[V];
             RowVec<T, V>::unpack(buf[u], f);
 #pragma unroll
             for (int e = 0; e < V; ++e) acc[e] += f[e];
+            const bool over = i + u + 1 >= end;
+            const int r = over ? -1 : __builtin_amdgcn_readlane(row, i + u + 1);
+            if (r == cur) continue;
+            if (head || (over && part1)) as_part(!head);
+            else if (act) row_finish<MODE, V>(dst, sh, (int64_t)cur * d + c0, acc, old[u], skip, scale, lr);
+            cur = r;
+            head = false;
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = 0.f;
         }
     }
-    finish(head || part1, !head);
 }
 
 // The rows in parts.  A workgroup looks through kJoinWaves chunks, a wave each, for one that a row in parts
@@ -680,8 +704,9 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int64_t n, int
 #pragma unroll
                     for (int e = 0; e < V; ++e) acc[e] = 0.f;
                     if (skip < V) {
+                        const auto old = row_old<MODE, V>(dst, (int64_t)last * d + c0);
                         add_parts<V>(part + c0, d, ch, 0, more + 1, acc);
-                        row_finish<MODE, V>(dst, sh, (int64_t)last * d + c0, acc, skip, scale, lr);
+                        row_finish<MODE, V>(dst, sh, (int64_t)last * d + c0, acc, old, skip, scale, lr);
                     }
                 } else {
                     row = last;
@@ -710,7 +735,11 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int64_t n, int
 #pragma unroll
             for (int e = 0; e < V; ++e) acc[e] = 0.f;
             const int64_t each = (more + 1 + kJoinWaves - 1) / kJoinWaves, i0 = wave * each, i1 = min(more + 1, i0 + each);
-            if (skip < V) add_parts<V>(part + c0, d, ch0 + w, i0, i1, acc);
+            typename RowVec<float, V>::raw old{};
+            if (skip < V) {
+                if (wave == 0) old = row_old<MODE, V>(dst, (int64_t)cur * d + c0);
+                add_parts<V>(part + c0, d, ch0 + w, i0, i1, acc);
+            }
             if (wave > 0)
 #pragma unroll
                 for (int e = 0; e < V; ++e) sums[wave - 1][lane][e] = acc[e];
@@ -719,7 +748,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int64_t n, int
                 for (int x = 0; x < kJoinWaves - 1; ++x)
 #pragma unroll
                     for (int e = 0; e < V; ++e) acc[e] += sums[x][lane][e];
-                row_finish<MODE, V>(dst, sh, (int64_t)cur * d + c0, acc, skip, scale, lr);
+                row_finish<MODE, V>(dst, sh, (int64_t)cur * d + c0, acc, old, skip, scale, lr);
             }
             __syncthreads();
         }
@@ -730,7 +759,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int64_t n, int
 // Workgroup (bucket, 64 * V columns) sorts the bucket's tokens into LDS and sums its rows itself.  A row of
 // more than kAlone tokens is summed by all waves, each a contiguous part of its tokens, joined in their
 // order; the others go to the waves in turn.
-constexpr int kSmallWaves = 8, kSmallThreads = 64 * kSmallWaves, kAlone = 8;
+constexpr int kSmallWaves = 8, kSmallThreads = 64 * kSmallWaves, kAlone = 8, kSmallAhead = 8;
 
 template <typename T, int V, int MODE, int KEEP>
 __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__restrict__ dy, int64_t dld, int d,
@@ -775,23 +804,26 @@ __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__r
             if (!all && turn++ % kSmallWaves != wave) continue;
             const int each = all ? (e - b + kSmallWaves - 1) / kSmallWaves : e - b;
             const int t0 = all ? min(e, b + wave * each) : b, t1 = min(e, t0 + each);
+            const int64_t o = (int64_t)place_row(blockIdx.x, j, gs, bb) * d + c0;
+            typename RowVec<float, V>::raw old{};
+            if (skip < V && (!all || wave == 0)) old = row_old<MODE, V>(dst, o);
             float acc[V];
 #pragma unroll
             for (int q = 0; q < V; ++q) acc[q] = 0.f;
             if (skip < V)
-                for (int t = t0; t < t1; t += 8) {
-                    typename RowVec<T, V>::raw buf[8];
+                for (int t = t0; t < t1; t += kSmallAhead) {
+                    typename RowVec<T, V>::raw buf[kSmallAhead];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u)
+                    for (int u = 0; u < kSmallAhead; ++u)
                         if (t + u < t1) buf[u] = RowVec<T, V>::load(dy + list[t + u] * dld + c0);
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        if (t + u >= t1) break;
-                        float f[V];
-                        RowVec<T, V>::unpack(buf[u], f);
+                    for (int u = 0; u < kSmallAhead; ++u)
+                        if (t + u < t1) {
+                            float f[V];
+                            RowVec<T, V>::unpack(buf[u], f);
 #pragma unroll
-                        for (int q = 0; q < V; ++q) acc[q] += f[q];
-                    }
+                            for (int q = 0; q < V; ++q) acc[q] += f[q];
+                        }
                 }
             if (all) {
                 if (wave > 0)
@@ -804,13 +836,13 @@ __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__r
                         for (int q = 0; q < V; ++q) acc[q] += sums[w][lane][q];
             }
             if (skip < V && (!all || wave == 0))
-                row_finish<MODE, V>(dst, sh, (int64_t)place_row(blockIdx.x, j, gs, bb) * d + c0, acc, skip, scale, lr);
+                row_finish<MODE, V>(dst, sh, o, acc, old, skip, scale, lr);
             if (all) __syncthreads();
         }
     }
 }
 
-constexpr int kSmallTokens = 8192, kSmallKeep = 8;    // (further ids of a lane are read twice)
+constexpr int kSmallTokens = 8192, kSmallKeep = 16;    // (further ids of a lane are read twice)
 constexpr int kSmallBits = 9, kSmallLocal = 960;
 
 static size_t list_bytes(int64_t n) { return ((size_t)n * 4 + 15) / 16 * 16; }
