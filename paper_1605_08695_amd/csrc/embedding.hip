@@ -84,19 +84,18 @@ hipError_t launch_embed_fwd(int tdt, const void *table, int64_t rows, int64_t tl
 }
 
 // ------------------------------------------------------------------ tokens grouped by row
-// The rows are dealt to 2^bb buckets: groups of 2^gs consecutive rows (so that a bucket's rows are at
-// least 512 bytes in one piece, however narrow) go round the buckets, each round shifted from the one
-// before.  Neighbouring rows -- the most frequent words, in tables ordered by frequency -- are then in
-// different buckets, and so are rows a power of two apart.
+// The rows are dealt to 2^bb buckets: groups of 2^gs consecutive rows go round the buckets, each round
+// shifted from the one before.  With gs = 0, neighbouring rows -- the most frequent words, in tables ordered
+// by frequency -- are in different buckets, and so are rows a power of two apart; larger groups are for
+// buckets that clear their own rows, at least 512 bytes in one piece however narrow they are.
 struct RowSplit {
     int gs, bb;            // log2 of the rows per group, of the buckets
     int local;             // rows per bucket (upper bound)
 };
 
-static RowSplit row_split(int64_t rows, int d, int bb, int most) {
+static RowSplit row_split(int64_t rows, int gs, int bb, int most) {
     RowSplit s;
-    s.gs = 0;
-    while (((int64_t)d << s.gs) < 128) ++s.gs;
+    s.gs = gs;
     s.bb = bb;
     while (((((rows - 1) >> s.gs) >> s.bb) + 1) << s.gs > most) ++s.bb;
     s.local = (int)(((((rows - 1) >> s.gs) >> s.bb) + 1) << s.gs);
@@ -332,8 +331,9 @@ __device__ __forceinline__ uint32_t scan_counts(uint32_t *cnt, int entries, uint
 }
 
 // ------------------------------------------------------------------ many tokens: a sort in two launches
-// Stable, by a digit of the id ((id >> shift) & mask): one round sorts tables of up to 2^kDigitBits rows,
-// two rounds (low digit first) all others.
+// Stable, by a digit of the id: tables of up to 2^kDigitBits rows take one round with the id itself, all others
+// two, with the low and the high half of a bijection of the 32-bit ids that spreads them (high halves of the
+// ids would be the same few for most tokens; only equal ids have to come together).
 //   tiles    each workgroup sorts its contiguous range of the tokens by bucket and leaves where each of the
 //            256 buckets begins in it
 //   buckets  each workgroup takes its bucket's tokens out of every tile, in order, and sorts them by row;
@@ -343,10 +343,16 @@ constexpr int kDigitBits = 18, kTileWaves = 4, kTileThreads = 64 * kTileWaves, k
 constexpr int kBucketWaves = 8, kBucketThreads = 64 * kBucketWaves;
 
 struct Digit {
-    int shift, gs;
-    uint32_t mask, rows;
+    int half;              // -1: the id; 0, 1: the halves of the spread id
+    uint32_t rows;
     __device__ __forceinline__ void place(uint32_t id, uint32_t &bucket, uint32_t &local) const {
-        row_place((id >> shift) & mask, gs, 8, bucket, local);
+        if (half >= 0) {
+            id *= 2654435769u;                        // (odd: a bijection mod 2^32, as the xor with its own high half is)
+            id ^= id >> 16;
+            id *= 2654435769u;
+            id = half == 0 ? id & 0xffffu : id >> 16;
+        }
+        row_place(id, 0, 8, bucket, local);
     }
 };
 
@@ -514,7 +520,7 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
     if (blockIdx.x == kBuckets - 1 && tid == 0) *nvalid = (int32_t)end;
     if (used != nullptr) {
         for (int l = tid; l < local_rows; l += kBucketThreads) {
-            const uint32_t row = place_row(blockIdx.x, l, g.gs, 8);
+            const uint32_t row = place_row(blockIdx.x, l, 0, 8);
             if (row < g.rows) used[row] = cnt[l * kBucketWaves] != cnt[(l + 1) * kBucketWaves];
         }
         __syncthreads();
@@ -868,7 +874,7 @@ static Tiles tiles_of(int64_t n) {
 }
 
 // Few tokens, and few enough buckets: each of them reads all ids.
-static bool sum_small(int64_t n, int64_t rows) { return n <= kSmallTokens && rows <= ((int64_t)kSmallLocal << 12); }
+static bool sum_small(int64_t n, int64_t rows) { return n <= kSmallTokens && rows <= ((int64_t)kSmallLocal << 10); }
 
 size_t embed_ws_bytes(int64_t n, int d, int64_t rows) {
     if (n == 0 || rows == 0 || sum_small(n, rows)) return 0;
@@ -886,7 +892,10 @@ static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const in
                             int mode, float lr, float *dst, bf16_t *sh, void *ws, hipStream_t st) {
     const int cblocks = (d + 64 * V - 1) / (64 * V);
     if (sum_small(n, rows)) {
-        const RowSplit s = row_split(rows, d, kSmallBits, kSmallLocal);
+        int gs = 0, bb = mode == kStore ? kSmallBits : 3;
+        while (mode == kStore && ((int64_t)d << gs) < 128) ++gs;
+        while (bb < kSmallBits && (8 << bb) < n) ++bb;                // (eight tokens a bucket)
+        const RowSplit s = row_split(rows, gs, bb, kSmallLocal);
         const size_t lds = ((size_t)s.local * kSmallWaves + 1) * 4 + n * 2;
 #define TFK_GO(MODE, KEEP)                                                                                             \
     hipLaunchKernelGGL((embed_small_kernel<T, V, MODE, KEEP>),                                                        \
@@ -911,9 +920,8 @@ static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const in
         if (e != hipSuccess) return e;
     }
     for (int r = 0; r < rounds; ++r) {
-        const int64_t values = rounds == 1 ? rows : (r == 0 ? (int64_t)1 << kDigitBits : ((rows - 1) >> kDigitBits) + 1);
-        const RowSplit s = row_split(values, rounds == 1 ? d : 128, 8, 1024);
-        const Digit g{r == 0 ? 0 : kDigitBits, s.gs, rounds == 2 && r == 0 ? (1u << kDigitBits) - 1 : ~0u, (uint32_t)rows};
+        const RowSplit s = row_split(rounds == 1 ? rows : 1 << 16, 0, 8, 1024);
+        const Digit g{rounds == 1 ? -1 : r, (uint32_t)rows};
         int bits = 0;
         while ((1 << bits) < s.local) ++bits;
         hipLaunchKernelGGL(embed_tile_kernel, dim3((unsigned)t.count), dim3(kTileThreads), 0, st, r == 0 ? ids : key,
