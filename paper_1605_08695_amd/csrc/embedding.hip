@@ -340,7 +340,6 @@ __device__ __forceinline__ uint32_t scan_counts(uint32_t *cnt, int entries, uint
 //            the tokens of the buckets before are the sum of the tiles' beginnings of its own
 // Round two and the sums read the number of tokens left (those with ids in the table) from *nvalid.
 constexpr int kDigitBits = 18, kTileWaves = 4, kTileThreads = 64 * kTileWaves, kBuckets = 256, kMostTiles = 512;
-constexpr int kBucketWaves = 8, kBucketThreads = 64 * kBucketWaves;
 
 struct Digit {
     int half;              // -1: the id; 0, 1: the halves of the spread id
@@ -379,6 +378,18 @@ __device__ __forceinline__ uint32_t take_places(uint32_t *entry, uint64_t same, 
     return __shfl(p, ok ? __ffsll((unsigned long long)same) - 1 : lane, 64) + rank;
 }
 
+// Counts this lane's entry (ok): the lanes that have the first one's at once (a frequent word is in most
+// lanes, and an atomic takes the lanes of one address one by one), the others each by itself.
+__device__ __forceinline__ void count_place(uint32_t *cnt, uint32_t entry, bool ok, int lane) {
+    const uint64_t all = __ballot(ok);
+    if (all == 0) return;
+    const int lead = __ffsll((unsigned long long)all) - 1;
+    const uint32_t e0 = __builtin_amdgcn_readlane(entry, lead);
+    const bool with = ok && entry == e0;
+    const uint64_t m = __ballot(with);
+    if (ok && (!with || lane == lead)) atomicAdd(&cnt[entry], with ? (uint32_t)__popcll(m) : 1u);
+}
+
 __global__ __launch_bounds__(kTileThreads) void embed_tile_kernel(const int32_t *__restrict__ ids,
                                                                   const int32_t *__restrict__ tokens, uint32_t n,
                                                                   const int32_t *__restrict__ nvalid, Digit g,
@@ -405,7 +416,7 @@ __global__ __launch_bounds__(kTileThreads) void embed_tile_kernel(const int32_t 
         for (int e = 0; e < 4; ++e) {
             uint32_t b, l;
             g.place(v[e], b, l);
-            if (v[e] < g.rows) atomicAdd(&cnt[b * kTileWaves + wave], 1u);
+            count_place(cnt, b * kTileWaves + wave, v[e] < g.rows, lane);
         }
     }
     __syncthreads();
@@ -436,7 +447,8 @@ __global__ __launch_bounds__(kTileThreads) void embed_tile_kernel(const int32_t 
 }
 
 // used (or null; one round only): a byte per row of the table, 1 for rows with tokens.
-__global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int32_t *__restrict__ ttok,
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void embed_bucket_kernel(const int32_t *__restrict__ ttok,
                                                                       const int32_t *__restrict__ tkey,
                                                                       const int32_t *__restrict__ begin, int tiles,
                                                                       uint32_t tile, Digit g, int local_rows,
@@ -444,17 +456,18 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
                                                                       int32_t *__restrict__ key,
                                                                       int32_t *__restrict__ nvalid,
                                                                       uint8_t *__restrict__ used) {
+    static_assert(64 * NW >= kMostTiles, "a thread per tile");
     extern __shared__ __align__(16) uint32_t cnt[];                 // [local row][wave], and the end
     __shared__ uint32_t pre[kMostTiles + 1], src[kMostTiles];        // a tile's first entry; where it is
-    __shared__ uint32_t red[2][kBucketWaves];
+    __shared__ uint32_t red[2][NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int entries = local_rows * kBucketWaves;
+    const int entries = local_rows * NW;
     uint32_t s = 0, e = 0;
     if (tid < tiles) {
         s = (uint32_t)begin[(int64_t)tid * (kBuckets + 1) + blockIdx.x];
         e = (uint32_t)begin[(int64_t)tid * (kBuckets + 1) + blockIdx.x + 1];
     }
-    for (int q = tid; q < entries; q += kBucketThreads) cnt[q] = 0;
+    for (int q = tid; q < entries; q += (64 * NW)) cnt[q] = 0;
     uint32_t incl = e - s, before = s;
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t up = __shfl_up(incl, o, 64);
@@ -468,13 +481,15 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
     __syncthreads();
     uint32_t at = incl - (e - s), m = 0;
     before = 0;
-    for (int w = 0; w < kBucketWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
         if (w < wave) at += red[0][w];
         m += red[0][w];
         before += red[1][w];
     }
-    pre[tid] = at;
-    src[tid] = tid * tile + s;
+    if (tid < kMostTiles) {
+        pre[tid] = at;
+        src[tid] = tid * tile + s;
+    }
     if (tid == 0) pre[kMostTiles] = m;
     __syncthreads();
     // entry i of the bucket: in the last tile whose first is not behind it
@@ -485,7 +500,7 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
             if (pre[t + step] <= i) t += step;
         return src[t] + (i - pre[t]);
     };
-    const uint32_t per = ((m + kBucketWaves - 1) / kBucketWaves + 63) / 64 * 64;
+    const uint32_t per = ((m + NW - 1) / NW + 63) / 64 * 64;
     const uint32_t lo = min(m, wave * per), hi = min(m, lo + per);
     // entries that a lane has at hand, and fetches at a time; worked on four by four, side by side
     constexpr int KEEP = 16;
@@ -511,17 +526,17 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
             for (int q = q0; q < q0 + 4; ++q) {
                 uint32_t b, l;
                 g.place(id[q], b, l);
-                if (base + q * 64 + lane < hi) atomicAdd(&cnt[l * kBucketWaves + wave], 1u);
+                count_place(cnt, l * NW + wave, base + q * 64 + lane < hi, lane);
             }
         }
     }
     __syncthreads();
-    const uint32_t end = scan_counts<kBucketWaves>(cnt, entries, before, red[0]);
+    const uint32_t end = scan_counts<NW>(cnt, entries, before, red[0]);
     if (blockIdx.x == kBuckets - 1 && tid == 0) *nvalid = (int32_t)end;
     if (used != nullptr) {
-        for (int l = tid; l < local_rows; l += kBucketThreads) {
+        for (int l = tid; l < local_rows; l += (64 * NW)) {
             const uint32_t row = place_row(blockIdx.x, l, 0, 8);
-            if (row < g.rows) used[row] = cnt[l * kBucketWaves] != cnt[(l + 1) * kBucketWaves];
+            if (row < g.rows) used[row] = cnt[l * NW] != cnt[(l + 1) * NW];
         }
         __syncthreads();
     }
@@ -541,7 +556,7 @@ __global__ __launch_bounds__(kBucketThreads) void embed_bucket_kernel(const int3
                 same[q] = same_lanes<10>(l[q], local_bits, ok[q]);
             }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) p[q] = take_places(&cnt[l[q] * kBucketWaves + wave], same[q], ok[q], lane);
+            for (int q = 0; q < 4; ++q) p[q] = take_places(&cnt[l[q] * NW + wave], same[q], ok[q], lane);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 if (ok[q]) {
@@ -651,7 +666,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy
 // waves, a contiguous share each, joined in their order.  Workgroups from `joins` on clear a share of the
 // rows without tokens (used; null: none to clear) -- last in the operation, so that the sums' reads do not
 // wait behind the writes.
-constexpr int kJoinWaves = 8, kJoinThreads = 64 * kJoinWaves, kJoinAlone = 16, kClearRows = 256;
+constexpr int kJoinWaves = 16, kJoinThreads = 64 * kJoinWaves, kJoinAlone = 16, kClearRows = 256;
 
 template <int V>
 __device__ __forceinline__ void add_parts(const float *part, int64_t d, int64_t ch, int64_t i0, int64_t i1, float *acc) {
@@ -927,9 +942,13 @@ static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const in
         hipLaunchKernelGGL(embed_tile_kernel, dim3((unsigned)t.count), dim3(kTileThreads), 0, st, r == 0 ? ids : key,
                            r == 0 ? nullptr : order, (uint32_t)n, r == 0 ? nullptr : nvalid, g, (uint32_t)t.size, ttok, tkey,
                            begin);
-        hipLaunchKernelGGL(embed_bucket_kernel, dim3(kBuckets), dim3(kBucketThreads),
-                           ((size_t)s.local * kBucketWaves + 1) * 4, st, ttok, tkey, begin, (int)t.count, (uint32_t)t.size, g,
-                           s.local, bits, order, key, nvalid, used);
+        // (a frequent row's bucket is one workgroup's: 16 waves, where their counters fit)
+#define TFK_GO(NW)                                                                                                     \
+    hipLaunchKernelGGL((embed_bucket_kernel<NW>), dim3(kBuckets), dim3(64 * NW), ((size_t)s.local * NW + 1) * 4, st,   \
+                       ttok, tkey, begin, (int)t.count, (uint32_t)t.size, g, s.local, bits, order, key, nvalid, used)
+        if (s.local <= 512) TFK_GO(16);
+        else TFK_GO(8);
+#undef TFK_GO
     }
     const int chunk = sum_chunk(n, cblocks);
     const int64_t chunks = (n + chunk - 1) / chunk, groups = (chunks + kJoinWaves - 1) / kJoinWaves * cblocks;
