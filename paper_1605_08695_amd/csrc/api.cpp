@@ -1096,7 +1096,7 @@ tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n, int32_t
                 return fail(TFK_ERR_ALIAS, "dlogits or loss overlaps an operand");
     // (a hard term of weight 0 is left out: the labels are not read)
     const DistillArgs a{logits, logits_ld, bias, top, top_idx, top_lse, alpha < 1.f ? labels : nullptr, weight, loss,
-                        dlogits, dlogits_ld, c, k, temperature, alpha, scale, top_dt == TFK_F32 ? 0 : 1, false};
+                        dlogits, dlogits_ld, c, k, temperature, alpha, scale, top_dt == TFK_F32 ? 0 : 1};
     return hip_status(launch_distill(dt == TFK_F32 ? 0 : 1, n, a, (hipStream_t)stream), "distill_xent");
 }
 

@@ -693,8 +693,7 @@ __global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64
                 for (int e = 0; e < V; ++e) g[e] -= t.mr;
 #pragma unroll
             for (int e = 0; e < V; ++e) g[e] = slope_at<POW>(t, g[e]);
-            if (a.away) RowVec<T, V>::store_away(at32(dz, (i * NT + tid) * V), g);
-            else RowVec<T, V>::store(at32(dz, fresh((i * NT + tid) * V)), g);
+            RowVec<T, V>::store(at32(dz, (i * NT + tid) * V), g);
         }
         if (i % 2 == 1) __builtin_amdgcn_sched_barrier(0);
     }
@@ -880,8 +879,7 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
 #pragma unroll
             for (int e = 0; e < V; ++e) g[e] = slope_at<POW>(t, x[u][e]);
             if (j + u * NT * V >= whole) break;
-            if (a.away) RowVec<T, V>::store_away(dz + j + u * NT * V, g);
-            else RowVec<T, V>::store(dz + fresh(j + u * NT * V), g);
+            RowVec<T, V>::store(dz + j + u * NT * V, g);
         }
     });
     if (jt >= 0) Elem<T>::store(dz + jt, slope_at<POW>(t, xt));
@@ -937,10 +935,7 @@ static hipError_t launch_typed(const DistillArgs &a, int64_t n, hipStream_t st) 
     return hipGetLastError();
 }
 
-hipError_t launch_distill(int dt, int64_t n, const DistillArgs &args, hipStream_t st) {
-    DistillArgs a = args;
-    // a gradient that no cache could hold for the next operation goes past them
-    a.away = a.z != a.dz && n * a.c * (dt == 0 ? 4 : 2) > ((int64_t)512 << 20);
+hipError_t launch_distill(int dt, int64_t n, const DistillArgs &a, hipStream_t st) {
     return dt == 0 ? launch_typed<float>(a, n, st) : launch_typed<bf16_t>(a, n, st);
 }
 

@@ -16,7 +16,7 @@ namespace tfk {
 // A thread moves V consecutive elements of a row; the last piece of a row that is not a whole number of
 // them starts V before the row's end (the elements it shares with the piece before are written twice,
 // with the same values).  A workgroup has 256 * UNR consecutive pieces of the output.
-template <typename TI, typename TO, int V, int UNR>
+template <typename TI, typename TO, int V, int UNR, bool AWAY>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(const TI *__restrict__ table, int64_t rows, int64_t tld, int d,
                                                         const int32_t *__restrict__ ids, int64_t n, float scale,
                                                         TO *__restrict__ out, int64_t old_, uint32_t pieces,
@@ -52,7 +52,9 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const TI *__restrict__ t
 #pragma unroll
             for (int e = 0; e < V; ++e) f[e] *= scale;
         }
-        if (i[u] < n) RowVec<TO, V>::store(out + i[u] * old_ + k[u], f);
+        if (i[u] >= n) continue;
+        if (AWAY) RowVec<TO, V>::store_away(out + i[u] * old_ + k[u], f);
+        else RowVec<TO, V>::store(out + i[u] * old_ + k[u], f);
     }
 }
 
@@ -62,12 +64,13 @@ static hipError_t embed_fwd(const TI *table, int64_t rows, int64_t tld, int d, c
     const uint32_t pieces = (uint32_t)((d + V - 1) / V);
     const FastDiv by(pieces);
     const int64_t total = n * pieces;
-    if (total < 256 * 4 * 1024)
-        hipLaunchKernelGGL((embed_fwd_kernel<TI, TO, V, 1>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, table,
-                           rows, tld, d, ids, n, scale, out, old_, pieces, by);
-    else
-        hipLaunchKernelGGL((embed_fwd_kernel<TI, TO, V, 4>), dim3((unsigned)((total + 1023) / 1024)), dim3(256), 0, st,
-                           table, rows, tld, d, ids, n, scale, out, old_, pieces, by);
+#define TFK_GO(UNR, AWAY)                                                                                             \
+    hipLaunchKernelGGL((embed_fwd_kernel<TI, TO, V, UNR, AWAY>), dim3((unsigned)((total + 256 * UNR - 1) / (256 * UNR))), \
+                       dim3(256), 0, st, table, rows, tld, d, ids, n, scale, out, old_, pieces, by)
+    if (total < 256 * 4 * 1024) TFK_GO(1, false);     // (a workgroup per CU and more)
+    else if (n * d * (int64_t)sizeof(TO) < kPastCaches) TFK_GO(4, false);
+    else TFK_GO(4, true);
+#undef TFK_GO
     return hipGetLastError();
 }
 
@@ -628,15 +631,16 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy
         for (int e = 0; e < V; ++e)
             if (act && e >= skip) slot[(began ? d : 0) + e] = acc[e];
     };
-    // kAhead tokens at a time; with each that ends its row, what is there in the row
-    constexpr int kAhead = MODE == kStore ? 8 : 4;
+    // kAhead tokens at a time (dy is read past the caches: nothing reads a gradient after its sum); with each
+    // that ends its row, what is there in the row
+    constexpr int kAhead = 8;
     for (; i < end; i += kAhead) {
         typename RowVec<T, V>::raw buf[kAhead];
         typename RowVec<float, V>::raw old[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
             if (i + u < end && act) {
-                buf[u] = RowVec<T, V>::load(dy + __builtin_amdgcn_readlane(tok, i + u) * dld + c0);
+                buf[u] = RowVec<T, V>::load_last(dy + __builtin_amdgcn_readlane(tok, i + u) * dld + c0);
                 const int r = __builtin_amdgcn_readlane(row, i + u);
                 if (MODE != kStore && (i + u + 1 >= end || __builtin_amdgcn_readlane(row, i + u + 1) != r))
                     old[u] = row_old<MODE, V>(dst, (int64_t)r * d + c0);

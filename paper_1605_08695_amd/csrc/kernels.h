@@ -193,7 +193,6 @@ struct DistillArgs {
     int c, k;
     float temperature, alpha, scale;
     int top_dt;
-    bool away;             // (set by the launch)
 };
 hipError_t launch_distill(int dt, int64_t n, const DistillArgs &a, hipStream_t st);
 // Embedding table: lookup of n tokens; the dense gradient of the table (beta 0 or 1); the table's SGD

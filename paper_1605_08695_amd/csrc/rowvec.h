@@ -9,7 +9,13 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef u32x2_t u32x2_a2_t __attribute__((aligned(2)));
 typedef f32x4_t f32x4_a4_t __attribute__((aligned(4)));
 
-// V elements of T at p as fp32 and back; V = 1, 4 or 8.
+// A result of this size or more is stored past the caches: the last of them, 256 MB, could not hold it until
+// its reader comes.  (Lookup and the matrix product that reads it, 512 MB of bf16: 334 us through the caches,
+// 306 past them; 256 MB 156, 151; 128 MB 75, 78.)
+constexpr int64_t kPastCaches = (int64_t)256 << 20;
+
+// V elements of T at p as fp32 and back; V = 1, 4 or 8.  load_last and store_away: past the caches, for
+// what is not read again, or is too much for them.
 template <typename T, int V>
 struct RowVec;
 
@@ -17,8 +23,10 @@ template <typename T>
 struct RowVec<T, 1> {
     typedef float raw;
     __device__ static raw load(const T *p) { return Elem<T>::load(p); }
+    __device__ static raw load_last(const T *p) { return load(p); }
     __device__ static void unpack(raw r, float *v) { v[0] = r; }
     __device__ static void store(T *p, const float *v) { Elem<T>::store(p, v[0]); }
+    __device__ static void store_away(T *p, const float *v) { store(p, v); }
 };
 
 template <>
@@ -52,6 +60,10 @@ struct RowVec<float, 8> {
     __device__ static void store(float *p, const float *v) {
         RowVec<float, 4>::store(p, v);
         RowVec<float, 4>::store(p + 4, v + 4);
+    }
+    __device__ static void store_away(float *p, const float *v) {
+        RowVec<float, 4>::store_away(p, v);
+        RowVec<float, 4>::store_away(p + 4, v + 4);
     }
 };
 
