@@ -528,7 +528,8 @@ TFK_API tfk_status tfk_embedding_fwd(const void *table, tfk_dtype dt, int64_t ro
  * [0, rows) are left out; dtable: dense fp32 rows x d.  beta 0 writes every row (0 where no token
  * is); beta 1 adds to the rows that have tokens and leaves the others as they are.  The tokens are
  * grouped by row first and each row's sum is formed in fp32 in a fixed order.
- *   ws : at least tfk_embedding_workspace_bytes(n, d, rows) bytes, 16-byte aligned, apart from every operand.
+ *   ws : at least tfk_embedding_workspace_bytes(n, d, rows) bytes, 16-byte aligned, apart from every operand;
+ *        calls that may overlap in time need one each.  Nothing in it is kept from one call to the next.
  * Errors: n < 0, rows < 0, d < 1, dy_ld below d (SHAPE); scale not finite, beta not 0 or 1 (ARG); n or
  * rows > 2^31 - 1, or n dy_ld or rows d > 2^40 (OVERFLOW); NULL, misaligned or overlapping buffers (NULL, ALIGN, ALIAS);
  * WORKSPACE.  n == 0 writes zeros (beta 0) or nothing. */

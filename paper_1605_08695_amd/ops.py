@@ -678,6 +678,8 @@ def embedding_fwd(table, ids, scale=1.0, out=None, out_dtype=None, stream=None):
         if tuple(out.shape) != shape or (out_dtype is not None and out.dtype != out_dtype):
             raise ValueError("out must be %s%s, got %s of %s" % (shape, " of %s" % out_dtype if out_dtype else "",
                                                                 tuple(out.shape), out.dtype))
+        if len(shape) == 1 and not out.is_contiguous():
+            raise ValueError("out must be contiguous for a single id")
         old = d if len(shape) == 1 else _rows_of(out, "out")[2]
         st = _on_device(stream, table, ids, out)
     check(load().tfk_embedding_fwd(_ptr(table), dt, rows, tld, d, _ptr(ids), n, float(scale), _ptr(out), _dt(out), old,

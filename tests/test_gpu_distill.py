@@ -184,7 +184,7 @@ SHAPES = [(1, 1, 1), (1, 2, 1), (3, 2, 2), (5, 9, 9), (17, 63, 4), (4, 64, 64), 
 @gpu
 @pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("T,rest,alpha", [(1.0, False, 1.0), (2.0, True, 0.6), (1.0, True, 0.5), (4.0, False, 0.9),
-                                          (0.5, True, 1.0)])
+                                          (0.5, True, 1.0), (1.5, False, 0.3)])
 @pytest.mark.parametrize("n,c,k", SHAPES)
 def test_distill(dt, T, rest, alpha, n, c, k):
     say("distill", dt, T, rest, alpha, n, c, k)
@@ -223,7 +223,7 @@ def test_strided_rows(dt, n, c, zx, dx):
 @gpu
 @pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("c", [6, 300, 5000, 70000, 140000])
-@pytest.mark.parametrize("T,rest,alpha", [(1.0, False, 1.0), (2.0, True, 0.6), (1.0, True, 0.5)])
+@pytest.mark.parametrize("T,rest,alpha", [(1.0, False, 1.0), (2.0, True, 0.6), (1.0, True, 0.5), (1.5, True, 0.4)])
 def test_lists_and_masks(dt, c, T, rest, alpha):
     """Rows whose lists are short, empty, doubled or all -inf, whose logits are masked, far apart or
     not finite, whose labels are outside and whose weight is zero, one kind a row."""
@@ -282,6 +282,24 @@ def test_probabilities_of_the_rest():
     loss, dz = _run(v, 1.0, T, True, 1.0)
     torch.cuda.synchronize()
     assert float(loss.abs().max()) < 1e-4 and float(dz.abs().max()) < 1e-5
+
+
+@gpu
+def test_two_calls_at_once():
+    """Losses on two streams at a time, rows in registers and long ones."""
+    jobs = []
+    for c in (3000, 140000):
+        v = _case(c, 70, c, 9, BF16, F32, 2.0)
+        jobs.append((v, _run(v, 0.1, 2.0, True, 0.5), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for v, _, st in jobs:
+            st.wait_stream(torch.cuda.current_stream())
+            got.append(_run(v, 0.1, 2.0, True, 0.5, stream=st))
+    torch.cuda.synchronize()
+    for i, (loss, dz) in enumerate(got):
+        assert torch.equal(loss, jobs[i % 2][1][0]) and torch.equal(dz, jobs[i % 2][1][1])
 
 
 @gpu

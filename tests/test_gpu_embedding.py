@@ -28,6 +28,9 @@ def _tokens(rng, n, rows, kind):
         ids = np.full(n, rows // 2)
     elif kind == "distinct":
         ids = rng.permutation(rows)[:n] if n <= rows else rng.integers(0, rows, n)
+    elif kind == "half":                 # half of them one word
+        ids = rng.integers(0, rows, n)
+        ids[rng.random(n) < 0.5] = rows - 1
     elif kind == "stride":               # rows a power of two apart
         ids = rng.integers(0, max(1, rows // 256), n) * 256 % rows
     else:                                # padding and ids outside the table among the others
@@ -135,7 +138,8 @@ CASES = [
     (300, 33, 50, "zipf", 3), (1000, 64, 1, "same", 0), (2560, 512, 40000, "zipf", 0), (2049, 257, 700, "bad", 1),
     (4097, 96, 60000, "distinct", 0), (5000, 1000, 5000, "same", 0), (3000, 2056, 300, "zipf", 0), (777, 8200, 100, "zipf", 0),
     (20000, 40, 300000, "zipf", 0), (20011, 34, 1 << 20, "stride", 2), (70001, 64, 131072, "zipf", 0), (70000, 72, 9, "zipf", 8),
-    (66000, 16, 3, "same", 0), (33333, 520, 33333, "bad", 0)]
+    (66000, 16, 3, "same", 0), (33333, 520, 33333, "bad", 0), (8192, 36, 491520, "zipf", 0), (8193, 130, 262144, "half", 0),
+    (40000, 260, 262145, "half", 0), (300, 4, 3000000, "distinct", 0), (9000, 6, 2097152, "half", 0)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
@@ -241,6 +245,33 @@ def test_other_stream_and_workspace():
     torch.cuda.synchronize()
     assert torch.equal(got, ref)
     assert torch.all(ws[need:] == 0xA5)                       # nothing behind the workspace is written
+
+
+@pytest.mark.parametrize("n", [600, 30000])
+def test_two_calls_at_once(n):
+    """Two updates and their lookups on two streams, each with a workspace of its own."""
+    d, rows = 192, 5000
+    rng = np.random.default_rng(12)
+    jobs = []
+    for kind in ("zipf", "bad"):
+        ids = _tokens(rng, n, rows, kind)
+        W = torch.from_numpy(rng.standard_normal((rows, d)).astype(np.float32)).to(DEV)
+        dy = torch.from_numpy(rng.standard_normal((n, d)).astype(np.float32)).to(BF16).to(DEV)
+        want = W.clone()
+        ops.embedding_apply_sgd(want, ids, dy, 0.1)
+        jobs.append((ids, W, dy, want, ops.embedding_fwd(want, ids, 3.0), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for ids, W, dy, _, _, st in jobs:
+            W0 = W.clone()
+            st.wait_stream(torch.cuda.current_stream())
+            ops.embedding_apply_sgd(W0, ids, dy, 0.1, stream=st)
+            got.append((W0, ops.embedding_fwd(W0, ids, 3.0, stream=st)))
+            W0.record_stream(st)
+    torch.cuda.synchronize()
+    for i, (W0, y) in enumerate(got):
+        assert torch.equal(W0, jobs[i % 2][3]) and torch.equal(y, jobs[i % 2][4])
 
 
 @pytest.mark.parametrize("n,rows", [(700, 300), (50000, 3000)])

@@ -133,6 +133,9 @@ def test_binding_refuses_host_tensors():
     lambda: ops.embedding_fwd(_t(10, 4), _t(3, dtype=I32), out=_t(3, 5)),
     lambda: ops.embedding_fwd(_t(10, 4), _t(3, dtype=I32), out=_t(4, 3).t()),
     lambda: ops.embedding_fwd(_t(10, 4), _t(3, dtype=I32), out=_t(3, 4), out_dtype=torch.bfloat16),
+    lambda: ops.embedding_fwd(_t(10, 4), _t(1, dtype=I32)[0], out=_t(4, 2)[:, 0]),
+    lambda: ops.embedding_bwd(_t(4, 2)[:, 0], _t(1, dtype=I32)[0], 10),
+    lambda: ops.embedding_bwd(_t(3, 4), _t(3, dtype=I32), 10, ws=torch.zeros(64, 2, dtype=torch.uint8)[:, 0]),
     lambda: ops.embedding_bwd(_t(3, 4), _t(4, dtype=I32), 10),
     lambda: ops.embedding_bwd(_t(1, 4).expand(3, 4), _t(3, dtype=I32), 10),
     lambda: ops.embedding_bwd(_t(3, 4), _t(3, dtype=I32), 10, beta=1.0),
