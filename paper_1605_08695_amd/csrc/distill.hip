@@ -17,6 +17,16 @@
 // Exponentials are powers of two, exp(y / T) = 2^(y ct): 2^(x ct - R) by one fma and one exp instruction,
 // with R = m_r ct rounded once and used as it is wherever the sum is.  Rows whose maximum is beyond 1e30
 // (masks of the type's lowest value throughout, infinities, NaN) are shifted first, by exact differences.
+//
+// Bound by HBM: a row's logits are read once and its gradient written once, with everything between in
+// registers; what the loss needs besides (the list, the label, the bias) is small or comes from the caches.  A
+// workgroup has a row, so nothing is exchanged between workgroups and no workspace is needed.
+//   c <= 40960 in bf16, 20480 in fp32: x in fp32 registers, its exponential in the same ones; 2560 x 40000 bf16
+//     with bias 93 us (4.4 TB/s)
+//   c <= 131072, 65536: the logits as they were read; 1021 x 50021 with bias 54 us (3.8 TB/s); one workgroup per
+//     CU from 65536 on: 4096 x 131072 with labels at T = 2 590 us (3.6 TB/s; exponentials twice, VALU 60 % busy;
+//     read twice instead: 664 us)
+//   longer rows: read twice
 #include <type_traits>
 
 #include "common.h"
@@ -30,7 +40,8 @@
 namespace tfk {
 
 // Where the T = 1 exponentials of the hard term come from: those at T themselves (no hard term, or T = 1),
-// their square (T = 2), their fourth power (T = 4), or exponentials of their own.
+// their square (T = 2), their fourth power (T = 4), or exponentials of their own.  (4096 x 40000, T = 2, labels:
+// 159 us by squares, 179 with exponentials of their own.)
 enum { kSame = 0, kSquare = 1, kFourth = 2, kOwn = 3 };
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f, kHuge = 1e30f;
@@ -304,18 +315,38 @@ __device__ __forceinline__ float add_power(float e, float s) {
     return s + e;
 }
 
+// The gradient outside the list from the exponential at T (not kOwn).
+template <int POW>
+__device__ __forceinline__ float slope_of(const RowTotals &t, float y) {
+    if (POW == kSquare) return y * fmaf(t.ch, y, t.co);
+    if (POW == kFourth) return y * fmaf(t.ch * y, y * y, t.co);
+    return (t.co + t.ch) * y;                         // (one exponential for both)
+}
+
 // ------------------------------------------------------------------ rows in registers
 // A workgroup of NT threads has a row of up to NT * NCH * V classes in registers, in fp32: one read of the
-// logits and one write of the gradient.  Piece i of thread t is V classes from (i NT + t) V; the c % V
-// classes behind the last whole piece are one each in the first lanes of the last wave (xt).
+// logits and one write of the gradient.  Piece i of thread t is V classes from head + (i NT + t) V; the classes
+// before and behind the whole pieces are one each in the first lanes of the last wave (xt).
+//
+// A row of bf16 that begins between two words leaves its first class to them (head = 1): pieces at any word are
+// read as fast as aligned ones, pieces between two words are not (4096 x 50001: 244 us; 205 with a head).
+template <typename T>
+__device__ __forceinline__ int row_head(const T *z) {
+    return sizeof(T) == 2 ? (int)(((uintptr_t)z >> 1) & 1) : 0;
+}
+
+// The bits of V classes from j on.  (A piece's may lie in two words; what follows the last word is the list.)
+template <int V>
+__device__ __forceinline__ uint32_t bits_at(const uint32_t *bits, uint32_t j) {
+    const uint32_t lo = bits[j >> 5], hi = V == 8 ? bits[(j >> 5) + 1] : 0;
+    return __builtin_amdgcn_alignbit(hi, lo, j & 31) & ((1u << V) - 1u);
+}
+
 template <typename T>
 __device__ __forceinline__ T *at32(T *p, uint32_t i) {     // (a uniform base and a 32-bit offset)
     typedef typename std::conditional<std::is_const<T>::value, const char, char>::type C;
     return reinterpret_cast<T *>(reinterpret_cast<C *>(p) + i * (uint32_t)sizeof(T));
 }
-
-// Waves per SIMD that the registers have to leave room for.
-constexpr int row_waves(int nch) { return nch <= 2 ? 8 : nch <= 4 ? 6 : 4; }
 
 template <typename T, int NT, int NCH, int POW>
 __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t n, int bit_words) {
@@ -323,8 +354,7 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
     extern __shared__ __align__(16) uint32_t smem[];
     __shared__ RowShared sh;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c = a.c, k = a.k, whole = c / V;
-    const int jt = wave == NW - 1 && lane < c - whole * V ? whole * V + lane : -1;      // this lane's class past the pieces
+    const int c = a.c, k = a.k;
     RowList l;
     l.bits = smem;
     l.cls = (int32_t *)(smem + bit_words);
@@ -336,8 +366,14 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
     int tid = fresh(threadIdx.x);
     const T *z = (const T *)a.z + row * a.zld;
     T *dz = (T *)a.dz + row * a.dld;
-    ListHead head{};
-    if (wave == 0) head = list_head(a, row);
+    const int head = row_head(z), whole = (c - head) / V;
+    // this lane's class outside the pieces, which start at zp, dzp, bp
+    const int jt = wave == NW - 1 && lane < c - whole * V ? (lane < head ? lane : whole * V + lane) : -1;
+    const T *const zp = z + head;
+    T *const dzp = dz + head;
+    const float *const bp = a.bias ? a.bias + head : nullptr;
+    ListHead first{};
+    if (wave == 0) first = list_head(a, row);
     const float w = a.weight ? a.weight[row] : 1.f;
     const int lab = hard ? a.labels[row] : -1;
     const bool bad = hard && (lab < 0 || lab >= c);
@@ -350,12 +386,12 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
         if (read_last) {
 #pragma unroll
             for (int i = 0; i < NCH; ++i)
-                if (i * NT + tid < whole) raw[i] = RowVec<T, V>::load_last(at32(z, (i * NT + tid) * V));
+                if (i * NT + tid < whole) raw[i] = RowVec<T, V>::load_last(at32(zp, (i * NT + tid) * V));
         } else {
             const int tid_ = fresh(tid);              // (equal addresses would make one plain load of the two)
 #pragma unroll
             for (int i = 0; i < NCH; ++i)
-                if (i * NT + tid_ < whole) raw[i] = RowVec<T, V>::load(at32(z, (i * NT + tid_) * V));
+                if (i * NT + tid_ < whole) raw[i] = RowVec<T, V>::load(at32(zp, (i * NT + tid_) * V));
         }
     };
     if (NT == 64) read();                         // (short rows: not after the weight and the label)
@@ -364,7 +400,7 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
         if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
         if (wave == 0) {
             if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
-            read_list<T>(a, row, head, z, c, l, sh);
+            read_list<T>(a, row, first, z, c, l, sh);
         }
         __syncthreads();
         if (!sh.soft && !hard) {
@@ -376,7 +412,7 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
         float f[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) f[e] = fill;
-        for (int p = tid; p < whole; p += NT) RowVec<T, V>::store(at32(dz, p * V), f);
+        for (int p = tid; p < whole; p += NT) RowVec<T, V>::store(at32(dzp, p * V), f);
         if (jt >= 0) Elem<T>::store(dz + jt, fill);
         if (tid == 0) a.loss[row] = fill;
         return;
@@ -396,11 +432,11 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
             RowVec<T, V>::unpack(raw[i], x[i]);
             if (a.bias) {
                 float b[V];
-                RowVec<float, V>::unpack(RowVec<float, V>::load(at32(a.bias, j)), b);
+                RowVec<float, V>::unpack(RowVec<float, V>::load(at32(bp, j)), b);
 #pragma unroll
                 for (int e = 0; e < V; ++e) x[i][e] += b[e];
             }
-            const uint32_t on = (l.bits[j >> 5] >> (j & 31)) & ((1u << V) - 1u);
+            const uint32_t on = bits_at<V>(l.bits, j + head);
             if (on != 0) {
 #pragma unroll
                 for (int e = 0; e < V; ++e)
@@ -431,8 +467,12 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
     const auto add = [&](float &v) {
         const float y = ex2(fmaf(v, t.ct, -t.R));
         s += y;
-        if (POW == kOwn) s1 += ex2(fmaf(v, kLog2e, -t.R1));
-        else v = y;
+        if (POW == kOwn) {
+            s1 += ex2(fmaf(v, kLog2e, -t.R1));
+            return;
+        }
+        if (POW != kSame) s1 = add_power<POW>(POW == kFourth ? fresh(y) : y, s1);  // (its square is not kept for the slope)
+        v = y;
     };
     add(xt);
 #pragma unroll
@@ -459,11 +499,11 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
     if (POW == kSame) s1 = s;                     // (T = 1, or not used)
     const float pr = rest_of(a, sh);
     t.sums(a, w, s, s1, sh, hard, pr);
-    const float cs = t.co + t.ch;                 // (kSame: one exponential for both)
     tid = fresh(tid);
     const float R = fresh(t.R), R1 = fresh(t.R1);
     const auto slope = [&](float v) {
-        return POW == kOwn ? fmaf(t.ch, ex2(fmaf(v, kLog2e, -R1)), t.co * ex2(fmaf(v, t.ct, -R))) : cs * v;
+        if (POW == kOwn) return fmaf(t.ch, ex2(fmaf(v, kLog2e, -R1)), t.co * ex2(fmaf(v, t.ct, -R)));
+        return slope_of<POW>(t, v);
     };
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
@@ -471,7 +511,7 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
             float g[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) g[e] = slope(x[i][e]);
-            RowVec<T, V>::store(at32(dz, (i * NT + tid) * V), g);
+            RowVec<T, V>::store(at32(dzp, (i * NT + tid) * V), g);
             __builtin_amdgcn_sched_barrier(0);
         }
     if (jt >= 0) Elem<T>::store(dz + jt, slope(xt));
@@ -534,9 +574,7 @@ template <int POW>
 __device__ __forceinline__ float slope_at(const RowTotals &t, float x) {
     const float y = ex2(fmaf(x, t.ct, -t.R));
     if (POW == kOwn) return fmaf(t.ch, ex2(fmaf(x, kLog2e, -t.R1)), t.co * y);
-    if (POW == kSame) return (t.co + t.ch) * y;
-    if (POW == kSquare) return y * fmaf(t.ch, y, t.co);
-    return y * fmaf(t.ch * y, y * y, t.co);
+    return slope_of<POW>(t, y);
 }
 
 // Pieces of the logits as they were read, with the listed classes made -inf.
@@ -553,16 +591,16 @@ __device__ __forceinline__ void make_inf(f32x4_t &raw, uint32_t on) {
         if ((on >> e) & 1u) raw[e] = -INFINITY;
 }
 
-// As distill_row_kernel, with the logits in registers as they were read (half the registers in bf16): the
-// bias is added twice, and the maximum and the sums are formed in one pass, piece by piece.
+// As distill_row_kernel, with the logits in registers as they were read (half the registers in bf16, so twice the
+// classes, or two workgroups per CU where x in fp32 leaves one): the bias is added twice, and the maximum and
+// the sums are formed in one pass, piece by piece.
 template <typename T, int NT, int NCH, int POW>
-__global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64_t n, int bit_words) {
+__global__ __launch_bounds__(NT, NT / 256) void distill_raw_kernel(DistillArgs a, int64_t n, int bit_words) {
     constexpr int V = 16 / sizeof(T), NW = NT / 64;
     extern __shared__ __align__(16) uint32_t smem[];
     __shared__ RowShared sh;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c = a.c, k = a.k, whole = c / V;
-    const int jt = wave == NW - 1 && lane < c - whole * V ? whole * V + lane : -1;      // this lane's class past the pieces
+    const int c = a.c, k = a.k;
     RowList l;
     l.bits = smem;
     l.cls = (int32_t *)(smem + bit_words);
@@ -574,8 +612,14 @@ __global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64
     int tid = threadIdx.x;
     const T *z = (const T *)a.z + row * a.zld;
     T *dz = (T *)a.dz + row * a.dld;
-    ListHead head{};
-    if (wave == 0) head = list_head(a, row);
+    const int head = row_head(z), whole = (c - head) / V;
+    // this lane's class outside the pieces, which start at zp, dzp, bp
+    const int jt = wave == NW - 1 && lane < c - whole * V ? (lane < head ? lane : whole * V + lane) : -1;
+    const T *const zp = z + head;
+    T *const dzp = dz + head;
+    const float *const bp = a.bias ? a.bias + head : nullptr;
+    ListHead first{};
+    if (wave == 0) first = list_head(a, row);
     const float w = a.weight ? a.weight[row] : 1.f;
     const int lab = hard ? a.labels[row] : -1;
     const bool bad = hard && (lab < 0 || lab >= c);
@@ -587,17 +631,17 @@ __global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64
         if (a.z != a.dz) {                        // (in place, the lines are written again at once)
 #pragma unroll
             for (int i = 0; i < NCH; ++i)
-                if (i * NT + tid < whole) raw[i] = RowVec<T, V>::load_last(at32(z, (i * NT + tid) * V));
+                if (i * NT + tid < whole) raw[i] = RowVec<T, V>::load_last(at32(zp, (i * NT + tid) * V));
         } else {
             const int tid_ = fresh(tid);          // (equal addresses would make one plain load of the two)
 #pragma unroll
             for (int i = 0; i < NCH; ++i)
-                if (i * NT + tid_ < whole) raw[i] = RowVec<T, V>::load(at32(z, (i * NT + tid_) * V));
+                if (i * NT + tid_ < whole) raw[i] = RowVec<T, V>::load(at32(zp, (i * NT + tid_) * V));
         }
         if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
         if (wave == 0) {
             if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
-            read_list<T>(a, row, head, z, c, l, sh);
+            read_list<T>(a, row, first, z, c, l, sh);
         }
         __syncthreads();
         if (!sh.soft && !hard) {
@@ -609,7 +653,7 @@ __global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64
         float f[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) f[e] = fill;
-        for (int p = tid; p < whole; p += NT) RowVec<T, V>::store(at32(dz, p * V), f);
+        for (int p = tid; p < whole; p += NT) RowVec<T, V>::store(at32(dzp, p * V), f);
         if (jt >= 0) Elem<T>::store(dz + jt, fill);
         if (tid == 0) a.loss[row] = fill;
         return;
@@ -619,7 +663,7 @@ __global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64
         RowVec<T, V>::unpack(raw[i], x);
         if (a.bias) {
             float b[V];
-            RowVec<float, V>::unpack(RowVec<float, V>::load(at32(a.bias, (i * NT + tid) * V)), b);
+            RowVec<float, V>::unpack(RowVec<float, V>::load(at32(bp, (i * NT + tid) * V)), b);
 #pragma unroll
             for (int e = 0; e < V; ++e) x[e] += b[e];
         }
@@ -629,7 +673,7 @@ __global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
         if (i * NT + tid < whole) {
-            const uint32_t j = (i * NT + tid) * V, on = (l.bits[j >> 5] >> (j & 31)) & ((1u << V) - 1u);
+            const uint32_t on = bits_at<V>(l.bits, (i * NT + tid) * V + head);
             if (on != 0) make_inf(raw[i], on);
             float x[V];
             x_of(i, x);
@@ -693,7 +737,7 @@ __global__ __launch_bounds__(NT, 4) void distill_raw_kernel(DistillArgs a, int64
                 for (int e = 0; e < V; ++e) g[e] -= t.mr;
 #pragma unroll
             for (int e = 0; e < V; ++e) g[e] = slope_at<POW>(t, g[e]);
-            RowVec<T, V>::store(at32(dz, (i * NT + tid) * V), g);
+            RowVec<T, V>::store(at32(dzp, (i * NT + tid) * V), g);
         }
         if (i % 2 == 1) __builtin_amdgcn_sched_barrier(0);
     }
@@ -760,8 +804,8 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
     if (row >= n) return;
     const T *z = (const T *)a.z + row * a.zld;
     T *dz = (T *)a.dz + row * a.dld;
-    ListHead head{};
-    if (wave == 0) head = list_head(a, row);
+    ListHead first{};
+    if (wave == 0) first = list_head(a, row);
     const float w = a.weight ? a.weight[row] : 1.f;
     const int lab = hard ? a.labels[row] : -1;
     const bool bad = hard && (lab < 0 || lab >= c);
@@ -772,7 +816,7 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
         if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
         if (wave == 0) {
             if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
-            read_list<T>(a, row, head, z, min(c, kSeg), l, sh);
+            read_list<T>(a, row, first, z, min(c, kSeg), l, sh);
         }
         __syncthreads();
         if (!sh.soft && !hard) {
@@ -895,33 +939,48 @@ static dim3 row_grid(int64_t n) {
     return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
 }
 
+// (Short rows are bound by latencies: exponentials of their own cost them nothing.)
 template <typename T, int NT, int NCH>
-static void launch_rows(const DistillArgs &a, int64_t n, bool two, size_t lds, int words, hipStream_t st) {
+static void launch_rows(const DistillArgs &a, int64_t n, int kind, size_t lds, int words, hipStream_t st) {
     const dim3 g = row_grid(n);
-    if (two) hipLaunchKernelGGL((distill_row_kernel<T, NT, NCH, kOwn>), g, dim3(NT), lds, st, a, n, words);
-    else hipLaunchKernelGGL((distill_row_kernel<T, NT, NCH, kSame>), g, dim3(NT), lds, st, a, n, words);
+#define TFK_GO(POW) hipLaunchKernelGGL((distill_row_kernel<T, NT, NCH, POW>), g, dim3(NT), lds, st, a, n, words)
+    if (kind == kSame) TFK_GO(kSame);
+    else if (NT >= 512 && kind == kSquare) TFK_GO(NT >= 512 ? kSquare : kOwn);
+    else if (NT >= 512 && kind == kFourth) TFK_GO(NT >= 512 ? kFourth : kOwn);
+    else TFK_GO(kOwn);
+#undef TFK_GO
 }
+
+// The least threads that hold the row with two, three or more workgroups per CU: a wave for rows of up to 256
+// pieces (4096 x 1000 bf16: 14 us; 22 by 256 threads), then 256 (4096 x 4000: 27 us; 52 by 512) and 512, each
+// with the least pieces a thread that suffice (4096 x 32000: 152 us with 10; 238 in one workgroup of 1024).
+// From 5120 pieces on the row as it was read keeps two workgroups per CU (4096 x 50000 with labels: 208 us; x
+// in fp32 and one workgroup 290), unless there is a row per CU at most: then 1024 threads have it sooner
+// (256 x 50000: 17 us; 21.6).
+constexpr int kCUs = 256;
 
 template <typename T>
 static hipError_t launch_typed(const DistillArgs &a, int64_t n, hipStream_t st) {
     const int pieces = (a.c + (int)(16 / sizeof(T)) - 1) / (int)(16 / sizeof(T));
     const int words = (std::min(a.c, kSeg) + 127) / 128 * 4;
     const size_t lds = (size_t)words * 4 + (size_t)a.k * 12;
-    const bool two = a.labels != nullptr && a.temperature != 1.f;
-    if (pieces <= 64 * 2) launch_rows<T, 64, 2>(a, n, two, lds, words, st);
-    else if (pieces <= 64 * 4) launch_rows<T, 64, 4>(a, n, two, lds, words, st);
-    else if (pieces <= 256 * 2) launch_rows<T, 256, 2>(a, n, two, lds, words, st);
-    else if (pieces <= 256 * 4) launch_rows<T, 256, 4>(a, n, two, lds, words, st);
-    else if (pieces <= 512 * 4) launch_rows<T, 512, 4>(a, n, two, lds, words, st);
-    else if (pieces <= 512 * 7) launch_rows<T, 512, 7>(a, n, two, lds, words, st);
-    else if (pieces <= 512 * 10) launch_rows<T, 512, 10>(a, n, two, lds, words, st);
-    else if (pieces <= 1024 * 8) launch_rows<T, 1024, 8>(a, n, two, lds, words, st);
+    const int kind = a.labels == nullptr || a.temperature == 1.f ? kSame
+                     : a.temperature == 2.f ? kSquare : a.temperature == 4.f ? kFourth : kOwn;
+    if (pieces <= 64 * 2) launch_rows<T, 64, 2>(a, n, kind, lds, words, st);
+    else if (pieces <= 64 * 4) launch_rows<T, 64, 4>(a, n, kind, lds, words, st);
+    else if (pieces <= 256 * 2) launch_rows<T, 256, 2>(a, n, kind, lds, words, st);
+    else if (pieces <= 256 * 4) launch_rows<T, 256, 4>(a, n, kind, lds, words, st);
+    else if (pieces <= 512 * 4) launch_rows<T, 512, 4>(a, n, kind, lds, words, st);
+    else if (pieces <= 512 * 7) launch_rows<T, 512, 7>(a, n, kind, lds, words, st);
+    else if (pieces <= 512 * 10) launch_rows<T, 512, 10>(a, n, kind, lds, words, st);
+    else if (pieces <= 1024 * 8 && n <= kCUs) launch_rows<T, 1024, 8>(a, n, kind, lds, words, st);
     else {
         const dim3 g = row_grid(n);
-        const int kind = !two ? kSame : a.temperature == 2.f ? kSquare : a.temperature == 4.f ? kFourth : kOwn;
 #define TFK_GO(POW)                                                                                                   \
     do {                                                                                                              \
-        if (pieces <= 1024 * 16)                                                                                      \
+        if (pieces <= 512 * 16)                                                                                       \
+            hipLaunchKernelGGL((distill_raw_kernel<T, 512, 16, POW>), g, dim3(512), lds, st, a, n, words);            \
+        else if (pieces <= 1024 * 16)                                                                                 \
             hipLaunchKernelGGL((distill_raw_kernel<T, 1024, 16, POW>), g, dim3(1024), lds, st, a, n, words);          \
         else                                                                                                          \
             hipLaunchKernelGGL((distill_long_kernel<T, POW>), g, dim3(kLongThreads), lds, st, a, n, words);           \

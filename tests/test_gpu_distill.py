@@ -270,6 +270,47 @@ def test_lists_and_masks(dt, c, T, rest, alpha):
 
 
 @gpu
+@pytest.mark.parametrize("dt,n,c", [(BF16, 300, 41003), (BF16, 257, 65535), (F32, 300, 20490), (F32, 257, 32767), (BF16, 256, 50001)])
+@pytest.mark.parametrize("T,rest,alpha", [(1.0, False, 1.0), (2.0, True, 0.6), (4.0, True, 0.5), (1.5, True, 0.4)])
+def test_more_rows_than_compute_units(dt, n, c, T, rest, alpha):
+    say("distill rows", dt, n, c, T, rest, alpha)
+    v = _case(n + c, n, c, 9, dt, F32, T)
+    loss, dz = _run(v, 1.0 / n, T, rest, alpha)
+    torch.cuda.synchronize()
+    _ref(v, 1.0 / n, T, rest, alpha).check(loss, dz)
+
+
+@gpu
+@pytest.mark.parametrize("T,alpha", [(1.0, 1.0), (2.0, 0.5), (4.0, 0.5), (3.0, 0.5)])
+@pytest.mark.parametrize("c", [1, 2, 7, 8, 9, 16, 17, 31, 33, 64, 65, 127, 300, 1001, 2055, 8193, 20481, 70001, 140001])
+def test_rows_between_words(c, T, alpha):
+    """Rows of bf16 that begin at odd elements, with the classes at the ends of pieces and of words listed or
+    the label."""
+    say("distill odd rows", c, T, alpha)
+    n = 9
+    want = [j for j in (0, 1, 7, 8, 9, 24, 25, 31, 32, 33, 63, 64, c // 2, c - 9, c - 2, c - 1) if 0 <= j < c]
+    k = len(want)
+    v = _case(c, n, c, 1, BF16, F32, T)
+    v["weight"].fill_(1.0)
+    v["idx"] = torch.tensor(want, dtype=torch.int32, device=DEV).repeat(n, 1)
+    for i in range(k):                                 # row by row one more of them left out (doubles stay doubles)
+        v["idx"][i % n, i] = -1
+    v["t"] = torch.gather(v["z"].float(), 1, torch.tensor(want, device=DEV).repeat(n, 1)) + 0.5
+    v["lse"] = torch.logsumexp(v["t"].double() / T, 1).float() + 0.25
+    v["labels"] = torch.tensor([want[(3 * i) % k] for i in range(n)], dtype=torch.int32, device=DEV)
+    wide = torch.full((n, c + 4 + c % 2), float("nan"), dtype=BF16, device=DEV)
+    out = torch.full((n, c + 5 - c % 2), 3.0, dtype=BF16, device=DEV)
+    for at in (1, 2):
+        z = wide[:, at:at + c]
+        z.copy_(v["z"])
+        loss, dz = _run({**v, "z": z}, 0.5, T, True, alpha, dlogits=out[:, at:at + c])
+        torch.cuda.synchronize()
+        _ref(v, 0.5, T, True, alpha).check(loss, dz, "at %d" % at)
+        assert torch.all(out[:, :at] == 3.0) and torch.all(out[:, at + c:] == 3.0)
+        out.fill_(3.0)
+
+
+@gpu
 def test_probabilities_of_the_rest():
     """A student that agrees with the teacher has no loss and no gradient, whichever way the mass of the
     rest is spread."""
