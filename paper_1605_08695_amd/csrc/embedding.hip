@@ -5,7 +5,13 @@
 //   gradient  dtable[r] = beta * dtable[r] + scale * sum over the tokens i with ids[i] == r of dy[i]
 //   update    var[r] <- fma(-lr, scale * that sum, var[r])          (rows with tokens only)
 //
-// Sums are fp32, in an order fixed by n, d and the ids alone.
+// Sums are fp32, in an order fixed by n, d and the ids alone: no atomic touches a value.
+//
+// All three are bound by HBM (one addition per element read).  The lookup is one pass over what it reads and
+// writes.  A gradient needs a row's tokens together: the tokens are sorted by row, as indexes, and each row's
+// sum is formed in registers and written once, so the table's gradient is never read, and an update moves only
+// the rows that have tokens.  Rows of tables are not equal: a frequent word can have half the tokens, so nothing
+// below leaves a row's length to one wave.
 #include "common.h"
 #include "kernels.h"
 #include "rowvec.h"
@@ -15,7 +21,10 @@ namespace tfk {
 // ------------------------------------------------------------------ lookup
 // A thread moves V consecutive elements of a row; the last piece of a row that is not a whole number of
 // them starts V before the row's end (the elements it shares with the piece before are written twice,
-// with the same values).  A workgroup has 256 * UNR consecutive pieces of the output.
+// with the same values).  A workgroup has 256 * UNR consecutive pieces of the output, whatever the row's length:
+// the loads of UNR pieces, ids first, are in flight together.  Bound by HBM: 65536 x 2048 bf16, 350 MB, 59 us
+// (stores past the caches; 73 through them), 20011 x 771 fp32, 83 MB, 15.6 us.  Small outputs take one piece a
+// thread: 128 x 512 is 2.6 us, a launch and two dependent loads.
 template <typename TI, typename TO, int V, int UNR, bool AWAY>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(const TI *__restrict__ table, int64_t rows, int64_t tld, int d,
                                                         const int32_t *__restrict__ ids, int64_t n, float scale,
@@ -67,7 +76,7 @@ static hipError_t embed_fwd(const TI *table, int64_t rows, int64_t tld, int d, c
 #define TFK_GO(UNR, AWAY)                                                                                             \
     hipLaunchKernelGGL((embed_fwd_kernel<TI, TO, V, UNR, AWAY>), dim3((unsigned)((total + 256 * UNR - 1) / (256 * UNR))), \
                        dim3(256), 0, st, table, rows, tld, d, ids, n, scale, out, old_, pieces, by)
-    if (total < 256 * 4 * 1024) TFK_GO(1, false);     // (a workgroup per CU and more)
+    if (total < 256 * 4 * 1024) TFK_GO(1, false);     // (with four a thread, less than four workgroups per CU)
     else if (n * d * (int64_t)sizeof(TO) < kPastCaches) TFK_GO(4, false);
     else TFK_GO(4, true);
 #undef TFK_GO
@@ -187,9 +196,8 @@ __device__ __forceinline__ void zero_rows(float *dst, int d, int c0, int c1, uin
 // One bucket's part of a stable counting sort of the tokens by row: a workgroup of NW waves reads all n
 // ids (they stay in the caches), counts those of its bucket per row and wave (each wave has a contiguous
 // range of the tokens), which gives every (row, wave) its first place, and puts each token into its place:
-// by row, then by token.  Ids outside [0, rows) are in no bucket.  A lane keeps its first KEEP ids in
-// registers, and a bit for those of the bucket, between the two turns; further ones are read and placed
-// again (n > NW * 64 * KEEP).
+// by row, then by token.  Ids outside [0, rows) are in no bucket.  A lane keeps its ids (KEEP of them:
+// n <= NW * 64 * KEEP) in registers, and a bit for those of the bucket, between the two turns.
 template <int NW, int KEEP>
 struct BucketSort {
     static_assert(KEEP <= 64, "one bit per kept id");
@@ -214,9 +222,8 @@ struct BucketSort {
         return id < rows ? b : ~0u;
     }
 
-    // Counts into cnt[local row][wave]; returns this lane's ids of the buckets before.
-    __device__ __forceinline__ uint32_t count(uint32_t *cnt) {
-        uint32_t before = 0;
+    // Counts into cnt[local row][wave].
+    __device__ __forceinline__ void count(uint32_t *cnt) {
 #pragma unroll
         for (int e = 0; e < KEEP; ++e) {
             if (lo + e * 64 >= hi) break;
@@ -227,29 +234,11 @@ struct BucketSort {
         for (int e = 0; e < KEEP; ++e) {
             if (lo + e * 64 >= hi) break;
             uint32_t l;
-            const uint32_t b = place(v[e], l);
-            before += b < mine;
-            if (b == mine) {
+            if (place(v[e], l) == mine) {
                 atomicAdd(&cnt[l * NW + wave], 1u);
                 hits |= 1ull << e;
             }
         }
-        for (uint32_t base = lo + KEEP * 64; base < hi; base += 512) {
-            uint32_t x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t i = base + e * 64 + lane;
-                x[e] = i < hi ? (uint32_t)ids[i] : ~0u;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                uint32_t l;
-                const uint32_t b = place(x[e], l);
-                before += b < mine;
-                if (b == mine) atomicAdd(&cnt[l * NW + wave], 1u);
-            }
-        }
-        return before;
     }
 
     // One id a lane: put(place, token, row) for the lanes with ok, in the order of the lanes.
@@ -280,19 +269,6 @@ struct BucketSort {
         for (int e = 0; e < KEEP; ++e) {
             if (lo + e * 64 >= hi) break;
             step(cnt, lo + e * 64, v[e], (hits >> e) & 1, f);
-        }
-        for (uint32_t base = lo + KEEP * 64; base < hi; base += 512) {
-            uint32_t x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t i = base + e * 64 + lane;
-                x[e] = i < hi ? (uint32_t)ids[i] : ~0u;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                uint32_t l;
-                step(cnt, base + e * 64, x[e], place(x[e], l) == mine, f);
-            }
         }
     }
 };
@@ -341,6 +317,10 @@ __device__ __forceinline__ uint32_t scan_counts(uint32_t *cnt, int entries, uint
 //            256 buckets begins in it
 //   buckets  each workgroup takes its bucket's tokens out of every tile, in order, and sorts them by row;
 //            the tokens of the buckets before are the sum of the tiles' beginnings of its own
+// Bound by latency, not by the ids' few bytes: 65536 tokens 5 + 10 us (a sort in one launch, every bucket
+// reading all ids, took 41).  256 buckets are a workgroup per CU, each tile's beginnings one line of
+// 1 KB, and a table of 2^18 rows leaves 1024 rows to count per bucket, what the LDS holds for 8 waves.  By
+// the digits of the ids themselves two rounds are slower (65536 x 64 of 3M rows: 164 us, 63 by the spread ids).
 // Round two and the sums read the number of tokens left (those with ids in the table) from *nvalid.
 constexpr int kDigitBits = 18, kTileWaves = 4, kTileThreads = 64 * kTileWaves, kBuckets = 256, kMostTiles = 512;
 
@@ -571,10 +551,13 @@ __global__ __launch_bounds__(64 * NW) void embed_bucket_kernel(const int32_t *__
 }
 
 // ------------------------------------------------------------------ sums of the grouped tokens
+// Bound by HBM: 65536 x 1024 bf16 tokens of a 131072-row table, 237 MB with the rows written, 54 us (4.4 TB/s);
+// an update, which reads those rows too, 75 us (4.6 TB/s).
 // A wave sums the grouped tokens of `chunk` places over 64 * V columns, eight rows of dy in flight, and
 // finishes the rows of the table that begin there and end there or in the next chunk.  A row that goes on
 // beyond (it covers the whole of a chunk that it does not begin in) is left in parts: [chunk][1] in the chunk
-// where it begins, [chunk][0] in the others.
+// where it begins, [chunk][0] in the others.  A chunk and the next are one lane each of a wave's 64: kMaxChunk
+// is the most (with every row over a border in parts, 65536 x 1024 took 211 us in all, with these 184).
 constexpr int kMaxChunk = 32;
 
 template <typename T, int V, int MODE>
@@ -781,6 +764,8 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int64_t n, int
 }
 
 // ------------------------------------------------------------------ few tokens: one launch
+// The gradient of 2560 x 512 is 16.8 us, most of it the clearing of an 80 MB table; the update of as many is
+// 8.9 us, half of it the sort: a chain of LDS and cache latencies, which more waves lengthen (16: 13.3 us).
 // Workgroup (bucket, 64 * V columns) sorts the bucket's tokens into LDS and sums its rows itself.  A row of
 // more than kAlone tokens is summed by all waves, each a contiguous part of its tokens, joined in their
 // order; the others go to the waves in turn.
@@ -867,7 +852,10 @@ __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__r
     }
 }
 
-constexpr int kSmallTokens = 8192, kSmallKeep = 16;    // (further ids of a lane are read twice)
+constexpr int kSmallKeep = 16, kSmallTokens = kSmallThreads * kSmallKeep;
+// Buckets: 2^3 to 2^9 of them, eight tokens in each on average (2^9 where each clears its own rows; 256, 512
+// and 1024 for 2560 tokens: 10.6, 9.0 and 9.2 us), more only where a bucket's counters (kSmallLocal rows)
+// would not fit the LDS.
 constexpr int kSmallBits = 9, kSmallLocal = 960;
 
 static size_t list_bytes(int64_t n) { return ((size_t)n * 4 + 15) / 16 * 16; }
@@ -875,7 +863,7 @@ static size_t list_bytes(int64_t n) { return ((size_t)n * 4 + 15) / 16 * 16; }
 // a byte per row (gradients of one round that store)
 static size_t used_bytes(int64_t rows) { return rows > ((int64_t)1 << kDigitBits) ? 0 : ((size_t)rows + 15) / 16 * 16; }
 
-// tokens per wave: 32, or 16 where that makes less than 4096 waves
+// tokens per wave: 32, or 16 where that makes less than 4096 waves, half of what the chip holds
 static int sum_chunk(int64_t n, int cblocks) {
     return (n + kMaxChunk - 1) / kMaxChunk * cblocks < 4096 ? kMaxChunk / 2 : kMaxChunk;
 }
@@ -892,7 +880,10 @@ static Tiles tiles_of(int64_t n) {
     return t;
 }
 
-// Few tokens, and few enough buckets: each of them reads all ids.
+// Few tokens, and few enough buckets: each of them reads all ids.  One launch against the four of the sort in
+// two launches, update of a table of 32000 rows: 2560 x 512 9.4 us against 25.4, 7500 x 256 20 against 31,
+// 7500 x 1024 27 against 35; from 12000 tokens on the sort is as fast or faster (gradient 12000 x 1024: 71, 51),
+// and so it is with thousands of columns from 6000 on (7500 x 4096: 70, 63).
 static bool sum_small(int64_t n, int64_t rows) { return n <= kSmallTokens && rows <= ((int64_t)kSmallLocal << 10); }
 
 size_t embed_ws_bytes(int64_t n, int d, int64_t rows) {
@@ -913,7 +904,7 @@ static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const in
     if (sum_small(n, rows)) {
         int gs = 0, bb = mode == kStore ? kSmallBits : 3;
         while (mode == kStore && ((int64_t)d << gs) < 128) ++gs;
-        while (bb < kSmallBits && (8 << bb) < n) ++bb;                // (eight tokens a bucket)
+        while (bb < kSmallBits && (8 << bb) < n) ++bb;
         const RowSplit s = row_split(rows, gs, bb, kSmallLocal);
         const size_t lds = ((size_t)s.local * kSmallWaves + 1) * 4 + n * 2;
 #define TFK_GO(MODE, KEEP)                                                                                             \
