@@ -531,7 +531,7 @@ TFK_API tfk_status tfk_embedding_fwd(const void *table, tfk_dtype dt, int64_t ro
  *   ws : at least tfk_embedding_workspace_bytes(n, d, rows) bytes, 16-byte aligned, apart from every operand;
  *        calls that may overlap in time need one each.  Nothing in it is kept from one call to the next.
  * Errors: n < 0, rows < 0, d < 1, dy_ld below d (SHAPE); scale not finite, beta not 0 or 1 (ARG); n or
- * rows > 2^31 - 1, or n dy_ld or rows d > 2^40 (OVERFLOW); NULL, misaligned or overlapping buffers (NULL, ALIGN, ALIAS);
+ * rows > 2^31 - 1, d > 2^23, or n dy_ld or rows d > 2^40 (OVERFLOW); NULL, misaligned or overlapping buffers (NULL, ALIGN, ALIAS);
  * WORKSPACE.  n == 0 writes zeros (beta 0) or nothing. */
 TFK_API tfk_status tfk_embedding_bwd(const void *dy, tfk_dtype dt, int64_t n, int64_t dy_ld, int32_t d, const int32_t *ids,
                              int64_t rows, float scale, float beta, float *dtable, void *ws, size_t ws_bytes,

@@ -1126,9 +1126,12 @@ tfk_status tfk_embedding_fwd(const void *table, tfk_dtype dt, int64_t rows, int6
                       "embedding_fwd");
 }
 
+// The most columns whose sums one launch can spread over a grid dimension.
+static constexpr int32_t kEmbedColumns = 1 << 23;
+
 size_t tfk_embedding_workspace_bytes(int64_t n, int32_t d, int64_t rows) {
-    if (n <= 0 || rows <= 0 || d < 1 || n > INT32_MAX || rows > INT32_MAX || rows > ((int64_t)1 << 40) / d ||
-        n > ((int64_t)1 << 40) / d)
+    if (n <= 0 || rows <= 0 || d < 1 || d > kEmbedColumns || n > INT32_MAX || rows > INT32_MAX ||
+        rows > ((int64_t)1 << 40) / d || n > ((int64_t)1 << 40) / d)
         return 0;
     return embed_ws_bytes(n, d, rows);
 }
@@ -1140,6 +1143,7 @@ static tfk_status check_embed_sum(const void *dy, tfk_dtype dt, int64_t n, int64
                                   bool whole, const void *ws, size_t ws_bytes) {
     if (!valid_dt(dt)) return fail(TFK_ERR_DTYPE, "unknown dtype %d", (int)dt);
     if (n < 0 || rows < 0 || d < 1) return fail(TFK_ERR_SHAPE, "need n >= 0, rows >= 0 and d >= 1");
+    if (d > kEmbedColumns) return fail(TFK_ERR_OVERFLOW, "more than 2^23 columns");
     int64_t dld = d;
     TRY(check_rows("dy", n, d, dy_ld));
     TRY(check_rows(dname, rows, d, dld));

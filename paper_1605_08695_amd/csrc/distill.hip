@@ -750,7 +750,8 @@ __global__ __launch_bounds__(NT, NT / 256) void distill_raw_kernel(DistillArgs a
 // ------------------------------------------------------------------ long rows
 // Rows that do not fit the registers are read twice: once for the maximum and the sums together (each thread
 // keeps its own running maximum and sums relative to it), once for the gradient; the second read of a row
-// follows the first closely enough to come from the caches.  The bits are those of kSeg classes at a time.
+// follows the first closely enough to come from the caches (1024 x 262144 bf16 361 us, 3.0 TB/s).  The bits are
+// those of kSeg classes at a time.
 constexpr int kSeg = 262144, kLongThreads = 1024, kLongPieces = 4;
 
 // f(j, x) for the pieces of V classes from j0 on, j0 + NT V, ... below j1 (whole pieces), UN at a time; their

@@ -18,6 +18,14 @@
 
 namespace tfk {
 
+// A grid of so many workgroups in two dimensions (the threads of one have to stay below 2^32), and a
+// workgroup's place in it.
+static dim3 block_grid(int64_t blocks) {
+    const int64_t x = std::min<int64_t>(blocks, 1 << 22);
+    return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+__device__ __forceinline__ int64_t block_index() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // ------------------------------------------------------------------ lookup
 // A thread moves V consecutive elements of a row; the last piece of a row that is not a whole number of
 // them starts V before the row's end (the elements it shares with the piece before are written twice,
@@ -30,7 +38,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const TI *__restrict__ t
                                                         const int32_t *__restrict__ ids, int64_t n, float scale,
                                                         TO *__restrict__ out, int64_t old_, uint32_t pieces,
                                                         FastDiv by_pieces) {
-    const int64_t base = (int64_t)blockIdx.x * (256 * UNR);
+    const int64_t base = block_index() * (256 * UNR);
     const int64_t i0 = base / pieces;
     const uint32_t r0 = (uint32_t)(base - i0 * pieces);
     int64_t i[UNR];
@@ -74,7 +82,7 @@ static hipError_t embed_fwd(const TI *table, int64_t rows, int64_t tld, int d, c
     const FastDiv by(pieces);
     const int64_t total = n * pieces;
 #define TFK_GO(UNR, AWAY)                                                                                             \
-    hipLaunchKernelGGL((embed_fwd_kernel<TI, TO, V, UNR, AWAY>), dim3((unsigned)((total + 256 * UNR - 1) / (256 * UNR))), \
+    hipLaunchKernelGGL((embed_fwd_kernel<TI, TO, V, UNR, AWAY>), block_grid((total + 256 * UNR - 1) / (256 * UNR)),   \
                        dim3(256), 0, st, table, rows, tld, d, ids, n, scale, out, old_, pieces, by)
     if (total < 256 * 4 * 1024) TFK_GO(1, false);     // (with four a thread, less than four workgroups per CU)
     else if (n * d * (int64_t)sizeof(TO) < kPastCaches) TFK_GO(4, false);
@@ -568,7 +576,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T *__restrict__ dy
                                                         float *__restrict__ dst, bf16_t *__restrict__ sh,
                                                         float *__restrict__ part) {
     const int lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t id = block_index() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t ch = id / cblocks;
     const int cb = (int)(id - ch * cblocks);
     const int64_t p0 = ch * chunk, p1 = p0 + chunk, p2 = p1 + chunk;
@@ -948,7 +956,7 @@ static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const in
     const int chunk = sum_chunk(n, cblocks);
     const int64_t chunks = (n + chunk - 1) / chunk, groups = (chunks + kJoinWaves - 1) / kJoinWaves * cblocks;
     const unsigned joins = (unsigned)std::min<int64_t>(groups, 1 << 20);
-    const dim3 gs((unsigned)((chunks * cblocks + 3) / 4));
+    const dim3 gs = block_grid((chunks * cblocks + 3) / 4);
     const dim3 gj(joins + (used != nullptr ? (unsigned)((rows + kClearRows - 1) / kClearRows) : 0u));
 #define TFK_GO(MODE)                                                                                                   \
     do {                                                                                                               \

@@ -575,6 +575,13 @@ def scatter_apply_sgd(var, idx, grad_t, lr, shadow=None, stream=None):
 
 
 # ----------------------------------------------------------------------------- rows
+def _width(c, name) -> int:
+    """c, a number of columns that the library counts in 32 bits."""
+    if c > 0x7fffffff:
+        raise ValueError("%s has more than 2^31 - 1 columns" % name)
+    return c
+
+
 def _rows_of(t, name) -> Tuple[int, int, int]:
     """(n, c, elements between rows) of a tensor whose last dimension has unit stride and whose others
     together are n rows a fixed distance apart."""
@@ -594,7 +601,7 @@ def _rows_of(t, name) -> Tuple[int, int, int]:
     if c == 0 or (c > 1 and s1 != 1 and n > 0) or s < c:
         raise ValueError("%s must be rows of unit stride that do not overlap, got shape %s, strides %s" %
                          (name, tuple(t.shape), tuple(t.stride())))
-    return n, c, s
+    return n, _width(c, name), s
 
 
 def _vector(t, dtype, n, name):
@@ -634,6 +641,7 @@ def distill_xent(logits, top_idx, top, scale, temperature=1.0, top_lse=None, lab
                                                                                           tuple(top_idx.shape)))
     if top_idx.dtype != torch.int32 or not (top_idx.is_contiguous() and top.is_contiguous()):
         raise ValueError("top_idx must be int32, top and top_idx contiguous")
+    k = _width(top.shape[-1], "top")
     _vector(top_lse, torch.float32, n, "top_lse")
     _vector(labels, torch.int32, n, "labels")
     _vector(weight, torch.float32, n, "weight")
@@ -648,7 +656,7 @@ def distill_xent(logits, top_idx, top, scale, temperature=1.0, top_lse=None, lab
         loss = _empty(stream, n, dtype=torch.float32, device=logits.device)
     if dlogits is None:
         dlogits = _empty_like(stream, logits)
-    check(load().tfk_distill_xent(_ptr(logits), dt, n, c, ld, _ptr(bias), _ptr(top), tdt, _ptr(top_idx), top.shape[-1],
+    check(load().tfk_distill_xent(_ptr(logits), dt, n, c, ld, _ptr(bias), _ptr(top), tdt, _ptr(top_idx), k,
                                   _ptr(top_lse), _ptr(labels), _ptr(weight), float(temperature), float(alpha),
                                   float(scale), _ptr(loss), _ptr(dlogits), dld, st))
     return loss, dlogits
@@ -689,7 +697,7 @@ def embedding_fwd(table, ids, scale=1.0, out=None, out_dtype=None, stream=None):
 
 def embedding_workspace_bytes(n, d, rows) -> int:
     """Workspace of embedding_bwd and embedding_apply_sgd for n tokens of a rows x d table."""
-    return load().tfk_embedding_workspace_bytes(operator.index(n), operator.index(d), operator.index(rows))
+    return load().tfk_embedding_workspace_bytes(operator.index(n), _width(operator.index(d), "dy"), operator.index(rows))
 
 
 _embed_need = functools.lru_cache(_KEPT)(embedding_workspace_bytes)
@@ -714,7 +722,7 @@ def _embed_args(dy, ids, stream, ws, rows, d, *more):
 def embedding_bwd(dy, ids, rows, scale=1.0, dtable=None, beta=0.0, ws=None, stream=None):
     """The table's dense fp32 gradient: dtable (rows x d) = beta * dtable + scale * the sum of dy over
     each row's tokens (beta 0 or 1).  Returns dtable."""
-    d = dy.shape[-1] if dy.dim() else 0
+    d = _width(dy.shape[-1], "dy") if dy.dim() else 0
     rows = operator.index(rows)
     if dtable is None and beta != 0.0:
         raise ValueError("beta = 1 adds to a dtable that is given")
@@ -737,7 +745,7 @@ def embedding_apply_sgd(var, ids, dy, lr, scale=1.0, shadow=None, ws=None, strea
         raise ValueError("var must be a contiguous float32 tensor of rows x d")
     if shadow is not None and (shadow.dtype != torch.bfloat16 or shadow.shape != var.shape or not shadow.is_contiguous()):
         raise ValueError("shadow must be a contiguous bfloat16 tensor of var's shape")
-    rows, d = var.shape
+    rows, d = var.shape[0], _width(var.shape[1], "var")
     dt = _dt(dy)
     n, ld, ws, need, st = _embed_args(dy, ids, stream, ws, rows, d, var, shadow)
     check(load().tfk_embedding_apply_sgd(_ptr(var), _ptr(shadow), rows, d, _ptr(ids), n, _ptr(dy), dt, ld, float(scale),

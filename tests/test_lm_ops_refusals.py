@@ -192,3 +192,31 @@ def test_table_keeps_what_lookups_read():
     import numpy as np
     t = EmbeddingTable(np.linspace(-1, 1, 12).reshape(4, 3), lr=0.1, scale=2.0, device="cpu")
     assert t.W.dtype == torch.float32 and torch.equal(t.W, t.W_lp.float()) and (t.vocab, t.d) == (4, 3)
+
+
+def test_embedding_columns(lib):
+    """Sums of more columns than a launch's grid holds are refused; the lookup takes them."""
+    a = _sum_args(dict(n=1, rows=1, d=(1 << 23) + 1, dst=1 << 32, dy=1 << 33, wb=0))
+    assert lib.tfk_embedding_bwd(vp(a["dy"]), a["dt"], a["n"], a["ld"], a["d"], vp(a["ids"]), a["rows"], f(1.0), f(0.0),
+                                 vp(a["dst"]), vp(a["ws"]), a["wb"], None) == OVERFLOW
+    assert lib.tfk_embedding_apply_sgd(vp(a["dst"]), None, a["rows"], a["d"], vp(a["ids"]), a["n"], vp(a["dy"]), a["dt"],
+                                       a["ld"], f(1.0), f(0.1), vp(a["ws"]), a["wb"], None) == OVERFLOW
+    assert lib.tfk_embedding_workspace_bytes(100000, (1 << 23) + 1, 100) == 0
+    assert lib.tfk_embedding_workspace_bytes(100000, 1 << 20, 100) > 0
+
+
+def test_columns_past_32_bits():
+    """Column counts are 32 bits at the C ABI: wider tensors are refused, not cut off."""
+    c, one = (1 << 32) + 8, torch.zeros(1, dtype=torch.int32)
+    wide = torch.empty((1, c), dtype=torch.bfloat16, device="meta")
+    top = torch.zeros((1, 3))
+    for call in (lambda: ops.distill_xent(wide, torch.zeros((1, 3), dtype=torch.int32), top, 1.0),
+                 lambda: ops.distill_xent(torch.zeros(1, 8), torch.empty((1, c), dtype=torch.int32, device="meta"),
+                                          torch.empty((1, c), device="meta"), 1.0),
+                 lambda: ops.embedding_fwd(wide, one),
+                 lambda: ops.embedding_bwd(wide, one, 4),
+                 lambda: ops.embedding_bwd(wide[0], one[0], 4),
+                 lambda: ops.embedding_apply_sgd(torch.empty((1, c), device="meta"), one, wide, 0.1),
+                 lambda: ops.embedding_workspace_bytes(5, c, 4)):
+        with pytest.raises(ValueError, match="columns"):
+            call()
