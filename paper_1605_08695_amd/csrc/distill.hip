@@ -22,7 +22,7 @@
 // registers; what the loss needs besides (the list, the label, the bias) is small or comes from the caches.  A
 // workgroup has a row, so nothing is exchanged between workgroups and no workspace is needed.
 //   c <= 40960 in bf16, 20480 in fp32: x in fp32 registers, its exponential in the same ones; 2560 x 40000 bf16
-//     with bias 93 us (4.4 TB/s)
+//     with bias 90 us (4.5 TB/s)
 //   c <= 131072, 65536: the logits as they were read; 1021 x 50021 with bias 54 us (3.8 TB/s); one workgroup per
 //     CU from 65536 on: 4096 x 131072 with labels at T = 2 590 us (3.6 TB/s; exponentials twice, VALU 60 % busy;
 //     read twice instead: 664 us)
@@ -48,15 +48,29 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f, kHu
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Reductions of a wave, the same in all its lanes (which are all here): within 16 lanes by exchanges in the
+// operand's own read -- neighbours, pairs, mirrored eights and sixteens -- and the four sixteens by scalars.  (A
+// row's chain holds about ten of them: 128 rows of 1000 8.0 us by exchanges through the LDS, 7.2 so; 2560 x 40000 92.5, 90.)
+template <int CTRL>
+__device__ __forceinline__ float lane_swap(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_of(float v, int lane) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
 __device__ __forceinline__ float wave_maxf(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
+    v = fmaxf(v, lane_swap<0xb1>(v));
+    v = fmaxf(v, lane_swap<0x4e>(v));
+    v = fmaxf(v, lane_swap<0x141>(v));
+    v = fmaxf(v, lane_swap<0x140>(v));
+    return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
 }
 __device__ __forceinline__ float wave_sumf(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    v += lane_swap<0xb1>(v);
+    v += lane_swap<0x4e>(v);
+    v += lane_swap<0x141>(v);
+    v += lane_swap<0x140>(v);
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 
 // The same number, as one that nothing computed from it before is known for: what a later phase computes
