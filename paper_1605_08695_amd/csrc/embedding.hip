@@ -779,7 +779,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int64_t n, int
 // order; the others go to the waves in turn.
 constexpr int kSmallWaves = 8, kSmallThreads = 64 * kSmallWaves, kAlone = 8, kSmallAhead = 8;
 
-template <typename T, int V, int MODE, int KEEP>
+template <typename T, int V, int MODE, int KEEP, int BATCH>
 __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__restrict__ dy, int64_t dld, int d,
                                                                     const int32_t *__restrict__ ids, uint32_t n,
                                                                     uint32_t rows, int gs, int bb, int local_rows,
@@ -828,8 +828,22 @@ __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__r
             float acc[V];
 #pragma unroll
             for (int q = 0; q < V; ++q) acc[q] = 0.f;
-            if (skip < V)
-                for (int t = t0; t < t1; t += kSmallAhead) {
+            int t = t0;
+            if (skip < V) {
+                if (BATCH > kSmallAhead)
+                    for (; t + BATCH <= t1; t += BATCH) {
+                        typename RowVec<T, V>::raw buf[BATCH];
+#pragma unroll
+                        for (int u = 0; u < BATCH; ++u) buf[u] = RowVec<T, V>::load(dy + list[t + u] * dld + c0);
+#pragma unroll
+                        for (int u = 0; u < BATCH; ++u) {
+                            float f[V];
+                            RowVec<T, V>::unpack(buf[u], f);
+#pragma unroll
+                            for (int q = 0; q < V; ++q) acc[q] += f[q];
+                        }
+                    }
+                for (; t < t1; t += kSmallAhead) {
                     typename RowVec<T, V>::raw buf[kSmallAhead];
 #pragma unroll
                     for (int u = 0; u < kSmallAhead; ++u)
@@ -843,6 +857,7 @@ __global__ __launch_bounds__(kSmallThreads) void embed_small_kernel(const T *__r
                             for (int q = 0; q < V; ++q) acc[q] += f[q];
                         }
                 }
+            }
             if (all) {
                 if (wave > 0)
 #pragma unroll
@@ -865,6 +880,10 @@ constexpr int kSmallKeep = 16, kSmallTokens = kSmallThreads * kSmallKeep;
 // and 1024 for 2560 tokens: 10.6, 9.0 and 9.2 us), more only where a bucket's counters (kSmallLocal rows)
 // would not fit the LDS.
 constexpr int kSmallBits = 9, kSmallLocal = 960;
+// Up to so many workgroups, two per CU, 16 rows of dy are in flight in a wave: a frequent row's sum is a chain of such
+// rounds (8000 x 512 with half the tokens one word 78 us, 50 so; 2560 x 512 10.1, 9.1).  More workgroups need the
+// registers for one another (2560 x 2048: 18 us with 8 in flight, 23 with 16).
+constexpr int kSmallDeep = 512;
 
 static size_t list_bytes(int64_t n) { return ((size_t)n * 4 + 15) / 16 * 16; }
 
@@ -915,14 +934,20 @@ static hipError_t embed_bwd(const T *dy, int64_t n, int d, int64_t dld, const in
         while (bb < kSmallBits && (8 << bb) < n) ++bb;
         const RowSplit s = row_split(rows, gs, bb, kSmallLocal);
         const size_t lds = ((size_t)s.local * kSmallWaves + 1) * 4 + n * 2;
-#define TFK_GO(MODE, KEEP)                                                                                             \
-    hipLaunchKernelGGL((embed_small_kernel<T, V, MODE, KEEP>),                                                        \
-                       dim3(1u << s.bb, cblocks), dim3(kSmallThreads), lds, st, dy, dld, d, ids, (uint32_t)n, (uint32_t)rows, s.gs,      \
-                       s.bb, s.local, scale, lr, dst, sh)
-        if (mode == kStore) TFK_GO(kStore, kSmallKeep);
-        else if (mode == kAdd) TFK_GO(kAdd, kSmallKeep);
-        else TFK_GO(kSgd, kSmallKeep);
+#define TFK_BATCH(MODE, BATCH)                                                                                         \
+    hipLaunchKernelGGL((embed_small_kernel<T, V, MODE, kSmallKeep, BATCH>), dim3(1u << s.bb, cblocks),                \
+                       dim3(kSmallThreads), lds, st, dy, dld, d, ids, (uint32_t)n, (uint32_t)rows, s.gs, s.bb,        \
+                       s.local, scale, lr, dst, sh)
+#define TFK_GO(MODE)                                                                                                   \
+    do {                                                                                                               \
+        if ((int64_t)cblocks << s.bb <= kSmallDeep) TFK_BATCH(MODE, 16);                                               \
+        else TFK_BATCH(MODE, kSmallAhead);                                                                             \
+    } while (0)
+        if (mode == kStore) TFK_GO(kStore);
+        else if (mode == kAdd) TFK_GO(kAdd);
+        else TFK_GO(kSgd);
 #undef TFK_GO
+#undef TFK_BATCH
         return hipGetLastError();
     }
     const size_t list = list_bytes(n) / 4;

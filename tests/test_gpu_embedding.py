@@ -189,6 +189,44 @@ def test_update(dt, shadow, n, d, rows, kind, extra):
         assert torch.equal(sh[~none], W[~none].to(BF16)) and torch.all(sh[none] == 7.0)
 
 
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,d,rows,kind,extra", [(127, 512, 900, "same", 0), (129, 200, 900, "same", 1), (4000, 64, 700, "half", 0),
+                                                 (8192, 512, 30000, "same", 0), (8000, 250, 5000, "half", 3),
+                                                 (6001, 1030, 2000, "half", 0), (8191, 7, 40, "half", 0)])
+def test_frequent_rows_of_few_tokens(dt, n, d, rows, kind, extra):
+    test_gradient(dt, n, d, rows, kind, extra)
+    test_update(dt, True, n, d, rows, kind, extra)
+
+
+@pytest.mark.parametrize("n", [4096, 9000])
+def test_gradient_offsets_past_32_bits(n):
+    """dy's rows spread over more than 2^32 bytes and elements, and a table of more than 2^31 elements."""
+    d, rows, ld = 64, (1 << 25) + 9, (1 << 32) // n + 5
+    free = torch.cuda.mem_get_info()[0]
+    if free < n * ld * 2 + 3 * rows * d * 4:
+        pytest.skip("needs %d GB" % ((n * ld * 2 + 3 * rows * d * 4) >> 30))
+    rng = np.random.default_rng(n)
+    wide = torch.zeros(n, ld, dtype=BF16, device=DEV)
+    dy = wide[:, 3:3 + d]
+    dy.copy_(torch.from_numpy(rng.integers(-4, 5, (n, d)).astype(np.float32)))      # (sums of whole numbers are exact)
+    names = np.array([0, 1, 77, (1 << 25) - 1, 1 << 25, rows - 1])
+    ids = names[rng.integers(0, len(names), n)]
+    ids[n - 1], ids[0] = rows - 1, 0
+    ids_ = torch.from_numpy(ids.astype(np.int32)).to(DEV)
+    got = ops.embedding_bwd(dy, ids_, rows)
+    W = torch.ones(rows, d, device=DEV)
+    ops.embedding_apply_sgd(W, ids_, dy, 0.5)
+    torch.cuda.synchronize()
+    vals = dy.float().cpu().numpy().astype(np.float64)
+    for r in names:
+        s = vals[ids == r].sum(0)
+        assert np.array_equal(got[int(r)].cpu().numpy(), s.astype(np.float32))
+        assert np.array_equal(W[int(r)].cpu().numpy(), (1 - 0.5 * s).astype(np.float32))
+        got[int(r)] = 0
+        W[int(r)] = 1
+    assert not got.any() and bool((W == 1).all())
+
+
 @pytest.mark.parametrize("n", [500, 40000])
 def test_gradient_of_the_lookup(n):
     """<dy, lookup(W + E) - lookup(W)> = <gradient, E>: the lookup is linear in the table."""
