@@ -24,7 +24,7 @@
 //   c <= 40960 in bf16, 20480 in fp32: x in fp32 registers, its exponential in the same ones; 2560 x 40000 bf16
 //     with bias 90 us (4.5 TB/s)
 //   c <= 131072, 65536: the logits as they were read; 1021 x 50021 with bias 54 us (3.8 TB/s); one workgroup per
-//     CU from 65536 on: 4096 x 131072 with labels at T = 2 572 us (3.8 TB/s; exponentials twice, VALU 60 % busy;
+//     CU from 65536 on: 4096 x 131072 with labels at T = 2 580 us (3.7 TB/s; exponentials twice, VALU 60 % busy;
 //     read twice instead: 664 us)
 //   longer rows: read twice
 #include <type_traits>
