@@ -408,9 +408,17 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
                 if (i * NT + tid_ < whole) raw[i] = RowVec<T, V>::load(at32(zp, (i * NT + tid_) * V));
         }
     };
-    if (NT == 64) read();                         // (short rows: not after the weight and the label)
+    constexpr bool kShort = NT == 64;             // short rows: the reads, the bias's too, not after the weight and the label
+    typename RowVec<float, V>::raw braw[kShort ? NCH : 1];
+    if (kShort) {
+        read();
+        if (a.bias)
+#pragma unroll
+            for (int i = 0; i < (kShort ? NCH : 1); ++i)
+                if (i * NT + tid < whole) braw[i] = RowVec<float, V>::load(at32(bp, (i * NT + tid) * V));
+    }
     if (!done) {
-        if (NT != 64) read();
+        if (!kShort) read();
         if (jt >= 0) xt = Elem<T>::load(z + jt) + (a.bias ? a.bias[jt] : 0.f);
         if (wave == 0) {
             if (hard) xlab = Elem<T>::load(z + lab) + (a.bias ? a.bias[lab] : 0.f);
@@ -446,7 +454,7 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
             RowVec<T, V>::unpack(raw[i], x[i]);
             if (a.bias) {
                 float b[V];
-                RowVec<float, V>::unpack(RowVec<float, V>::load(at32(bp, j)), b);
+                RowVec<float, V>::unpack(kShort ? braw[kShort ? i : 0] : RowVec<float, V>::load(at32(bp, j)), b);
 #pragma unroll
                 for (int e = 0; e < V; ++e) x[i][e] += b[e];
             }

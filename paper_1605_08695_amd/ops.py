@@ -585,13 +585,14 @@ def _width(c, name) -> int:
 def _rows_of(t, name) -> Tuple[int, int, int]:
     """(n, c, elements between rows) of a tensor whose last dimension has unit stride and whose others
     together are n rows a fixed distance apart."""
-    if t.dim() == 2:
-        n, c = t.shape
-        s, s1 = t.stride()
+    shape = t.shape
+    if len(shape) == 2:
+        n, c = shape
+        s, s1 = (c, 1) if t.is_contiguous() else t.stride()
     else:
-        if t.dim() < 2:
-            raise ValueError("%s must have rows and columns, got shape %s" % (name, tuple(t.shape)))
-        c = t.shape[-1]
+        if len(shape) < 2:
+            raise ValueError("%s must have rows and columns, got shape %s" % (name, tuple(shape)))
+        c = shape[-1]
         n = t.numel() // c if c else 0
         if not t.is_contiguous():
             raise ValueError("%s with more than two dimensions must be contiguous" % name)
@@ -618,7 +619,7 @@ def _on_device(stream, first, *others) -> int:
             raise ValueError("operands must be on one GPU, got %s and %s" % (first.device, t.device))
     if at < 0:
         raise ValueError("operands must be on the GPU, got one on %s" % first.device)
-    if at != torch.cuda.current_device() or (stream is not None and stream.device.index != at):
+    if at != torch._C._cuda_getDevice() or (stream is not None and stream.device.index != at):
         raise ValueError("operands are on GPU %d, which is not the current device or the stream's" % at)
     return torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
 
@@ -636,21 +637,24 @@ def distill_xent(logits, top_idx, top, scale, temperature=1.0, top_lse=None, lab
     mass counts as one more class.  Rows of weight 0 give loss 0 and no gradient.  Not differentiated
     through the teacher."""
     n, c, ld = _rows_of(logits, "logits")
-    if top.dim() < 2 or top.shape != top_idx.shape or top.numel() != n * top.shape[-1]:
-        raise ValueError("top and top_idx must share one shape of n rows, got %s and %s" % (tuple(top.shape),
+    shape = top.shape
+    if len(shape) < 2 or shape != top_idx.shape or top.numel() != n * shape[-1]:
+        raise ValueError("top and top_idx must share one shape of n rows, got %s and %s" % (tuple(shape),
                                                                                           tuple(top_idx.shape)))
     if top_idx.dtype != torch.int32 or not (top_idx.is_contiguous() and top.is_contiguous()):
         raise ValueError("top_idx must be int32, top and top_idx contiguous")
-    k = _width(top.shape[-1], "top")
+    k = _width(shape[-1], "top")
     _vector(top_lse, torch.float32, n, "top_lse")
     _vector(labels, torch.int32, n, "labels")
     _vector(weight, torch.float32, n, "weight")
     _vector(bias, torch.float32, c, "bias")
     _vector(loss, torch.float32, n, "loss")
     dt, tdt = _dt(logits), _dt(top)
-    if dlogits is not None and (dlogits.shape != logits.shape or dlogits.dtype != logits.dtype):
-        raise ValueError("dlogits must have the logits' shape and type")
-    dld = ld if dlogits is logits else (c if dlogits is None else _rows_of(dlogits, "dlogits")[2])
+    dld = c if dlogits is None else ld
+    if dlogits is not None and dlogits is not logits:
+        if dlogits.shape != logits.shape or dlogits.dtype != logits.dtype:
+            raise ValueError("dlogits must have the logits' shape and type")
+        dld = _rows_of(dlogits, "dlogits")[2]
     st = _on_device(stream, logits, top, top_idx, top_lse, labels, weight, bias, loss, dlogits)
     if loss is None:
         loss = _empty(stream, n, dtype=torch.float32, device=logits.device)
