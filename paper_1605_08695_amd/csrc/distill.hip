@@ -15,8 +15,11 @@
 // gradients it stores after the bulk's.
 //
 // Exponentials are powers of two, exp(y / T) = 2^(y ct): 2^(x ct - R) by one fma and one exp instruction,
-// with R = m_r ct rounded once and used as it is wherever the sum is.  Rows whose maximum is beyond 1e30
-// (masks of the type's lowest value throughout, infinities, NaN) are shifted first, by exact differences.
+// with R = m_r ct rounded once and used as it is wherever the sum is.  R's rounding error is then a factor of
+// all of the sum's terms, and has to stay a small one: up to |R| = 2^24 it is at most half a power of two (two,
+// of the fourth powers below).  Rows whose maximum is further out (a mask throughout, -1e9 as well as the
+// type's lowest value, infinities, NaN) are shifted first, by exact differences; in a running sum classes that
+// far below count as 0 until a nearer one comes.
 //
 // Bound by HBM: a row's logits are read once and its gradient written once, with everything between in
 // registers; what the loss needs besides (the list, the label, the bias) is small or comes from the caches.  A
@@ -45,6 +48,9 @@ namespace tfk {
 enum { kSame = 0, kSquare = 1, kFourth = 2, kOwn = 3 };
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f, kHuge = 1e30f;
+
+// The largest |x| whose exponents, at T and at 1, stay within 2^24.
+__device__ __forceinline__ float far_of(float temperature) { return 0x1p24f * kLn2 * fminf(temperature, 1.f); }
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -226,7 +232,7 @@ struct RowTotals {
         m = fmaxf(outside, mtop);
         ct = kLog2e / temperature;
         mr = outside > -INFINITY ? outside : 0.f;
-        huge = !(fabsf(mr) < kHuge && !(m >= kHuge));
+        huge = !(fabsf(mr) < far_of(temperature) && !(m >= kHuge));        // (m ct itself could overflow)
         R = huge ? 0.f : mr * ct;
         R1 = huge ? 0.f : (kind == kOwn ? mr * kLog2e : R * temperature);   // (exact: T is 1, 2 or 4 otherwise)
         const bool none = !(outside > -INFINITY);
@@ -546,8 +552,9 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a, int64_t 
 // The running maximum and sums of a thread, relative to the maximum: exponents r at T, r1 at 1.
 template <int POW>
 struct Running {
-    float M, ct, r, r1, s, s1;
-    __device__ explicit Running(float ct_) : M(-INFINITY), ct(ct_), r(-kHuge * ct_), r1(-kHuge * kLog2e), s(0.f), s1(0.f) {}
+    float M, ct, far, r, r1, s, s1;
+    __device__ explicit Running(float temperature)
+        : M(-INFINITY), ct(kLog2e / temperature), far(far_of(temperature)), r(-far * ct), r1(-far * kLog2e), s(0.f), s1(0.f) {}
 
     template <int N>
     __device__ __forceinline__ void add(const float (&x)[N]) {
@@ -555,7 +562,7 @@ struct Running {
 #pragma unroll
         for (int e = 0; e < N; ++e) cm = fmaxf(cm, x[e]);
         M = cm;
-        const float at = fminf(fmaxf(cm, -kHuge), kHuge), rn = at * ct, f = ex2(r - rn);
+        const float at = fminf(fmaxf(cm, -far), far), rn = at * ct, f = ex2(r - rn);
         s *= f;
         if (POW == kOwn) {
             const float rn1 = at * kLog2e;
@@ -574,7 +581,7 @@ struct Running {
         }
     }
 
-    // x as an exact difference from the row's maximum, where that is beyond kHuge (t.huge)
+    // x as an exact difference from the row's maximum, where t.huge
     __device__ __forceinline__ void add_shifted(float d) {
         const float y = ex2(d * ct);
         s += y;
@@ -691,7 +698,7 @@ __global__ __launch_bounds__(NT, NT / 256) void distill_raw_kernel(DistillArgs a
         }
     };
     if (jt >= 0 && ((l.bits[jt >> 5] >> (jt & 31)) & 1u)) xt = -INFINITY;
-    Running<POW> run(kLog2e / a.temperature);
+    Running<POW> run(a.temperature);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
         if (i * NT + tid < whole) {
@@ -889,7 +896,7 @@ __global__ __launch_bounds__(kLongThreads) void distill_long_kernel(DistillArgs 
             if (s0 + kSeg >= c && jt >= 0 && ((l.bits[(jt - s0) >> 5] >> ((jt - s0) & 31)) & 1u)) xt = -INFINITY;
         }
     };
-    Running<POW> run(kLog2e / a.temperature);
+    Running<POW> run(a.temperature);
     outside(true, [&](float(&x)[UN][V]) { run.add(*reinterpret_cast<float(*)[UN * V]>(&x)); });
     {
         const float x[1] = {xt};

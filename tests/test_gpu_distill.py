@@ -269,6 +269,82 @@ def test_lists_and_masks(dt, c, T, rest, alpha):
     r.check(loss, dz)
 
 
+# ----------------------------------------------------------------------------- finite masks
+def _masks(T):
+    """Finite values that put a class out of play, from the ordinary ones to past 1e30, and both sides of
+    2^24 steps of the exponents."""
+    near = 2.0 ** 24 * math.log(2) * min(T, 1.0)
+    return [-0.99 * near, -1.02 * near, -1e8, -1e9, -1e10, -1e12, -1e15, -1e20, -1e25, -1e30, -1.5e30]
+
+
+REST, ALL, FIRST, MOST, LAST, HALF, HIGH, LIST = range(8)
+
+
+def _masked_rows(c, dt, T, rest, alpha, copies=1):
+    """Inputs with a row per mask and place of it, and their reference: the formula's values on logits with
+    the same probabilities that are small (a class that a mask puts out of play has less than e^-150, which
+    no bound can see, whatever the mask's size), and the loss by the masks themselves."""
+    masks, k = _masks(T), 6
+    n = len(masks) * 8 * copies
+    v = _case(c + 7, n, c, k, dt, F32, T)
+    v["weight"].fill_(1.0)
+    v["bias"][:] = 0.25
+    row = torch.arange(n, device=DEV)
+    kind, M = row % 8, torch.tensor(masks, device=DEV)[row // 8 % len(masks)][:, None]
+    idx, j = v["idx"].long(), torch.arange(c, device=DEV)[None]
+    K = torch.zeros(n, c, dtype=torch.bool, device=DEV).scatter_(1, idx, True)
+    is_ = lambda q: (kind == q)[:, None]                          # noqa: E731
+    hit = torch.rand(n, c, generator=torch.Generator(device=DEV).manual_seed(c), device=DEV) < 0.5
+    out = (is_(REST) | is_(HIGH) | (is_(FIRST) & (j < c // 2)) | (is_(MOST) & (j < c - 3)) | (is_(LAST) & (j >= c // 3)) |
+           (is_(HALF) & hit)) & ~K
+    out = out | is_(ALL) | (is_(LIST) & K)
+    # the label: listed, or (where the list is masked; where the rest is, every other row) the first class that is not
+    other = torch.argmax((~K).int(), 1)
+    masked_label = (kind == REST) & (row // 8 % 2 == 1)
+    v["labels"] = torch.where((kind == LIST) | masked_label, other, idx[:, 0]).to(torch.int32)
+    z = v["z"].float()
+    far = 150.0 * max(T, 1.0)
+    low = torch.where(is_(REST) | is_(LIST), z.amin(1, keepdim=True) - far,
+                      torch.where(is_(HIGH), z.amax(1, keepdim=True) + far, torch.where(is_(ALL), 0.0, -INF)))
+    args = (v["idx"], v["t"], 0.5, T, v["lse"] if rest else None, v["labels"], alpha, v["weight"], v["bias"])
+    r = Ref(torch.where(out, low, z), *args)
+    v["z"] = torch.where(out, torch.where(is_(HIGH), -M, M), z).to(dt)
+    true = Ref(v["z"], *args)
+    # the loss by the masks: a probability, off by eP, times a difference D / T that is rounded by less than 8 half
+    # steps (of the operands, the difference, the quotient, the sum with the logarithms and the product)
+    t = v["t"].double() / T
+    p = torch.exp(t - v["lse"].double()[:, None]).sum(1) if rest else torch.ones(n, dtype=torch.float64, device=DEV)
+    rp = U * (6 * t.abs().amax(1) + (v["lse"].double().abs() if rest else 2 * t.abs().amax(1)) + k + 16)
+    pr = torch.clamp(1 - p, min=0) if rest else torch.zeros_like(p)
+    epr = rp * p + (k + 2) * U if rest else torch.zeros_like(p)
+    D = v["z"].double().abs().amax(1) + 50.0
+    soft = torch.where(kind == REST, epr + 8 * U * pr, torch.where((kind == HIGH) | (kind == LIST), p * (rp + 8 * U), 0.0))
+    hard = torch.where(masked_label | (kind == HIGH), 4 * U, 0.0) if alpha < 1 else 0.0
+    by_mask = (kind == REST) | (kind == HIGH) | (kind == LIST)
+    r.loss = torch.where(by_mask, true.loss, r.loss)
+    r.eloss = r.eloss + torch.where(by_mask, D * (alpha * T * soft + (1 - alpha) * hard) + 16 * U * true.loss.abs(), 0.0)
+    return v, r
+
+
+@gpu
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("c,copies", [(40, 1), (300, 1), (5000, 1), (24001, 4), (41003, 4), (70001, 1), (140000, 1), (300007, 1)])
+@pytest.mark.parametrize("T,rest,alpha", [(1.0, False, 1.0), (1.0, True, 0.5), (2.0, True, 0.6), (4.0, True, 0.5),
+                                          (1.5, True, 0.4), (0.01, True, 1.0), (0.01, True, 0.5)])
+def test_finite_masks(dt, c, copies, T, rest, alpha):
+    """Classes masked by a finite value of any size: outside the list, throughout, in blocks and scattered; the
+    list itself; and logits as far above the others.  (copies: more rows than compute units.)"""
+    say("distill finite masks", dt, c, T, rest, alpha)
+    T = float(np.float32(T))
+    v, r = _masked_rows(c, dt, T, rest, alpha, copies)
+    loss, dz = _run(v, 0.5, T, rest, alpha)
+    z = v["z"].clone()
+    loss2, dz2 = _run({**v, "z": z}, 0.5, T, rest, alpha, dlogits=z)
+    torch.cuda.synchronize()
+    r.check(loss, dz)
+    assert torch.equal(loss, loss2) and torch.equal(dz, dz2)
+
+
 @gpu
 @pytest.mark.parametrize("dt,n,c", [(BF16, 300, 41003), (BF16, 257, 65535), (F32, 300, 20490), (F32, 257, 32767), (BF16, 256, 50001)])
 @pytest.mark.parametrize("T,rest,alpha", [(1.0, False, 1.0), (2.0, True, 0.6), (4.0, True, 0.5), (1.5, True, 0.4)])
