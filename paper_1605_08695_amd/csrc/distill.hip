@@ -212,6 +212,10 @@ __device__ __forceinline__ void read_list(const DistillArgs &a, int64_t row, con
     }
 }
 
+// What the divergence is formed times: next to a listed class of the type's lowest value x / T may have no fp32 value
+// (T < 1), nor the sum of its terms (the probabilities add up to one and a rounding), where alpha T^2 of it has.
+__device__ __forceinline__ float loss_unit(float temperature) { return 0.5f * fminf(temperature, 1.f); }
+
 // A row's sums and what follows from them, the same in every thread.
 struct RowTotals {
     float m, mr;           // maxima: of all, outside the list (0: none)
@@ -219,7 +223,7 @@ struct RowTotals {
     float ct;              // log2(e) / T
     float R, R1;           // exponents' references outside the list, at T and at 1 (0 where huge)
     float relt, rel1;      // 2^(those - m's)
-    float ln_rel;          // log relt
+    float ln_rel;          // log relt, times loss_unit
     float st, s1, logst, qr;
     float co, ch;          // gradients outside the list: co e + ch e1
     float gs, at, gb;      // scale w, alpha T, scale w (1 - alpha)
@@ -238,7 +242,7 @@ struct RowTotals {
         const bool none = !(outside > -INFINITY);
         relt = none ? 0.f : ex2(huge ? (mr - m) * ct : fmaf(-m, ct, R));
         rel1 = none ? 0.f : ex2(huge ? (mr - m) * kLog2e : fmaf(-m, kLog2e, R1));
-        ln_rel = none ? 0.f : huge ? (mr - m) / temperature : fmaf(-m, ct, R) * kLn2;
+        ln_rel = none ? 0.f : huge ? 0.5f * (mr - m) / fmaxf(temperature, 1.f) : fmaf(-m, ct, R) * (kLn2 * loss_unit(temperature));
     }
 
     __device__ __forceinline__ void sums(const DistillArgs &a, float w, float rest, float rest1, const RowShared &sh,
@@ -283,20 +287,20 @@ __device__ __forceinline__ void sum_list(const DistillArgs &a, const RowTotals &
 __device__ __forceinline__ void row_loss(const DistillArgs &a, int64_t row, const RowTotals &t, const RowList &l,
                                          const RowShared &sh, float rest, float pr, float w, bool hard, float xlab) {
     const int lane = threadIdx.x & 63;
-    const float invt = 1.f / a.temperature;
-    float kl = 0.f;
+    const float unit = loss_unit(a.temperature), invt = unit / a.temperature, logst = t.logst * unit;
+    float kl = 0.f;                                   // (times unit)
     if (sh.soft) {
 #pragma unroll 1
         for (int j = lane; j < a.k; j += 64)
             if (l.cls[j] >= 0) {
                 const float p = l.P[j];
-                if (p != 0.f) kl += p * (logf(p) - ((l.x[j] - t.m) * invt - t.logst));
+                if (p != 0.f) kl += p * (logf(p) * unit - ((l.x[j] - t.m) * invt - logst));
             }
         kl = wave_sumf(kl);
-        if (pr != 0.f) kl += pr * (logf(pr) - (logf(rest) + t.ln_rel - t.logst));
+        if (pr != 0.f) kl += pr * (logf(pr) * unit - (logf(rest) * unit + t.ln_rel - logst));
     }
     if (lane == 0) {
-        float loss = sh.soft ? a.alpha * a.temperature * a.temperature * kl : 0.f;
+        float loss = sh.soft ? a.alpha * a.temperature * (a.temperature / unit) * kl : 0.f;
         if (hard) loss += (1.f - a.alpha) * (t.m - xlab + logf(t.s1));
         a.loss[row] = w * loss;
     }

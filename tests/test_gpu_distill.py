@@ -280,11 +280,11 @@ def _masks(T):
 REST, ALL, FIRST, MOST, LAST, HALF, HIGH, LIST = range(8)
 
 
-def _masked_rows(c, dt, T, rest, alpha, copies=1):
+def _masked_rows(c, dt, T, rest, alpha, copies=1, masks=None):
     """Inputs with a row per mask and place of it, and their reference: the formula's values on logits with
     the same probabilities that are small (a class that a mask puts out of play has less than e^-150, which
     no bound can see, whatever the mask's size), and the loss by the masks themselves."""
-    masks, k = _masks(T), 6
+    masks, k = masks or _masks(T), 6
     n = len(masks) * 8 * copies
     v = _case(c + 7, n, c, k, dt, F32, T)
     v["weight"].fill_(1.0)
@@ -343,6 +343,20 @@ def test_finite_masks(dt, c, copies, T, rest, alpha):
     torch.cuda.synchronize()
     r.check(loss, dz)
     assert torch.equal(loss, loss2) and torch.equal(dz, dz2)
+
+
+@gpu
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("c", [40, 5000, 70001, 140000])
+@pytest.mark.parametrize("T,rest,alpha", [(0.5, True, 1.0), (0.5, False, 0.5), (0.01, True, 0.6), (1.0, False, 0.5)])
+def test_lowest_masks(dt, c, T, rest, alpha):
+    """The type's lowest (and largest) values where x / T, or a sum of their shares, has no fp32 value, but the loss has."""
+    say("distill lowest masks", dt, c, T, rest, alpha)
+    T = float(np.float32(T))
+    v, r = _masked_rows(c, dt, T, rest, alpha, masks=[torch.finfo(dt).min, torch.finfo(dt).min / 2])
+    loss, dz = _run(v, 0.5, T, rest, alpha)
+    torch.cuda.synchronize()
+    r.check(loss, dz)
 
 
 @gpu
