@@ -498,6 +498,8 @@ TFK_API tfk_status tfk_scatter_apply_sgd(float *var, uint16_t *var_bf16, int64_t
  * A row without a teacher (renormalised, and no entry or only entries of -inf) has no soft term.
  * Logits of -inf are classes without probability: a p_j > 0 there (or a p_r > 0 where all classes
  * outside K are) makes the loss infinite, and the gradient stays as above with q = 0 (0 outside K).
+ * Finite logits are numbers whatever their size (masks of -1e9, -1e30 or the type's lowest value): the
+ * loss is finite where fp32 holds it and the differences between the row's logits.
  * Logits that are NaN or +inf, or -inf throughout, make the row NaN where a term needs them.
  * Errors: n < 0, c < 1, k not in 1..1024, a row distance below c (SHAPE); scale not finite, temperature
  * not in [1e-4, 1e4], alpha not in (0, 1], alpha < 1 without labels (ARG); n > 2^31 - 1, c > 2^30 or n
@@ -649,7 +651,8 @@ TFK_API tfk_status tfk_program_run(tfk_program *prog);
 TFK_API const char *tfk_status_string(tfk_status s);
 /* Detail of the last non-OK status returned on the calling thread ("" if none). */
 TFK_API const char *tfk_last_error(void);
-/* Version of this interface (incremented when a declaration here changes or goes; a new one leaves it). */
+/* Version of this interface (incremented when a declaration here changes or goes; a new one leaves it:
+ * whether a library has the entry points added within a version is told by their symbols). */
 TFK_API int32_t tfk_abi_version(void);
 
 #ifdef __cplusplus

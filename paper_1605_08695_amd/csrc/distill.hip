@@ -25,10 +25,10 @@
 // registers; what the loss needs besides (the list, the label, the bias) is small or comes from the caches.  A
 // workgroup has a row, so nothing is exchanged between workgroups and no workspace is needed.
 //   c <= 40960 in bf16, 20480 in fp32: x in fp32 registers, its exponential in the same ones; 2560 x 40000 bf16
-//     with bias 90 us (4.5 TB/s)
-//   c <= 131072, 65536: the logits as they were read; 1021 x 50021 with bias 54 us (3.8 TB/s); one workgroup per
-//     CU from 65536 on: 4096 x 131072 with labels at T = 2 580 us (3.7 TB/s; exponentials twice, VALU 60 % busy;
-//     read twice instead: 664 us)
+//     with bias 99 us a call (4.2 TB/s; in place 100)
+//   c <= 131072, 65536: the logits as they were read; 1021 x 50021 with bias 55 us (3.7 TB/s; in place 63); one
+//     workgroup per CU from 65536 on: 4096 x 131072 with labels at T = 2 582 us (3.7 TB/s; in place 597;
+//     exponentials twice, VALU 60 % busy; read twice instead: 664 us)
 //   longer rows: read twice
 #include <type_traits>
 

@@ -909,8 +909,9 @@ static Tiles tiles_of(int64_t n) {
 
 // Few tokens, and few enough buckets: each of them reads all ids.  One launch against the four of the sort in
 // two launches, update of a table of 32000 rows: 2560 x 512 9.4 us against 25.4, 7500 x 256 20 against 31,
-// 7500 x 1024 27 against 35; from 12000 tokens on the sort is as fast or faster (gradient 12000 x 1024: 71, 51),
-// and so it is with thousands of columns from 6000 on (7500 x 4096: 70, 63).
+// 7500 x 1024 27 against 35; from 12000 tokens on the sort is as fast or faster (gradient 12000 x 1024: 71, 51).
+// The rule looks at n and rows alone, though with thousands of columns the sort is faster from 6000 tokens on
+// already (7500 x 4096: 70 us here, 63 there): d is left out of it.
 static bool sum_small(int64_t n, int64_t rows) { return n <= kSmallTokens && rows <= ((int64_t)kSmallLocal << 10); }
 
 size_t embed_ws_bytes(int64_t n, int d, int64_t rows) {
