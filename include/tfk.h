@@ -510,6 +510,109 @@ TFK_API tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n,
                             const float *top_lse, const int32_t *labels, const float *weight, float temperature,
                             float alpha, float scale, float *loss, void *dlogits, int64_t dlogits_ld, void *stream);
 
+/* ---------------------------------------------------------------- log-probabilities
+ * What a classifier's logits say about given classes, for scoring, for choosing the next token and for
+ * preparing a teacher's largest classes (Section 4.2's large-vocabulary heads).  For each row i < n, with
+ * x = logits + bias, u = x / T, p = softmax(u):
+ *   lse[i]     = log sum_j exp(u_j)
+ *   logp[i]    = u[tokens[i]] - lse[i]
+ *   entropy[i] = -sum_j p_j log p_j                        (a class with p = 0 adds nothing)
+ *   top_idx[i], top_logp[i] : the k classes of the largest x, largest first, of equal ones the lower class
+ *                first, and their u - lse; behind the last class that is not -inf: -1 and -inf
+ * Arithmetic is fp32.
+ *   logits   : n rows of c values, type dt, logits_ld elements apart (0 = c).
+ *   bias     : fp32 [c], or NULL for none.
+ *   tokens   : int32 [n], or NULL (logp must be NULL then).  A token outside [0, c) is padding: its row's
+ *              logits are not read, its logp, entropy and lse are 0 and its list is all -1 and -inf.
+ *   logp, entropy, lse : fp32 [n], each may be NULL.     top_idx, top_logp : n x k dense, int32 and fp32.
+ * Finite logits are numbers whatever their size (masks of -1e9, -1e30 or the type's lowest value), where
+ * fp32 holds the differences between the row's.  A row of -inf throughout has lse -inf, logp -inf, entropy
+ * 0 and no list.  A row with a NaN or +inf has NaN in logp, entropy, lse and top_logp, and -1 in top_idx.
+ * top_idx and top_logp are what tfk_distill_xent takes as top_idx and top at T = 1 (with top_lse = 0 the
+ * rest of the mass counts as one class); at another T the teacher's logits are T top_logp.
+ * Errors: n < 0, c < 1, k not in 0..128, a row distance below c (SHAPE); temperature not in [1e-4, 1e4] (ARG);
+ * n > 2^31 - 1, c > 2^30 or n times a row distance > 2^40 (OVERFLOW); NULL, misaligned (to the element) or
+ * overlapping buffers (NULL, ALIGN, ALIAS).  n == 0 is a no-op. */
+TFK_API tfk_status tfk_token_logprobs(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld,
+                              const float *bias, const int32_t *tokens, float temperature, int32_t k, float *logp,
+                              float *entropy, float *lse, int32_t *top_idx, float *top_logp, void *stream);
+
+/* Gradient of logp and entropy (Section 4.1's backpropagation, from what a loss makes of the two):
+ *   dlogits[i][j] = (dlogp[i] ([j == tokens[i]] - p_j) - dentropy[i] p_j (log p_j + entropy[i])) / T
+ * rounded to dt once; 0 for a padding row (whose logits are not read) and for a row of -inf throughout.
+ *   logits, bias, tokens, temperature, lse, entropy : as given to and returned by tfk_token_logprobs.
+ *   dlogp     : fp32 [n].     dentropy : fp32 [n], or NULL for none (entropy is not read then).
+ *   dlogits   : n rows of c values, type dt, dlogits_ld elements apart (0 = c); may equal logits with the same
+ *               row distance (in place).
+ * Classes of -inf get 0.  Errors as above. */
+TFK_API tfk_status tfk_token_logprobs_bwd(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld,
+                              const float *bias, const int32_t *tokens, float temperature, const float *lse,
+                              const float *entropy, const float *dlogp, const float *dentropy, void *dlogits,
+                              int64_t dlogits_ld, void *stream);
+
+/* ---------------------------------------------------------------- gated linear recurrence
+ * A recurrent layer between the embedding table and the softmax head of a language model (Section 6.4's
+ * model has one), whose state moves towards the input by a gate's share and is not fed back into the gates,
+ * so that all products of the layer are made before the recurrence and all its steps in one operation.
+ * For each sequence of a batch and each of d channels, with x, a, o the columns [0, d), [d, 2d) and, where
+ * gates is 3, [2d, 3d) of z + bias, and s the logistic function:
+ *   h_t = s(a_t) h_(t-1) + (1 - s(a_t)) x_t              h_(-1) = h0
+ *   y_t = h_t  (gates 2)     or  s(o_t) h_t  (gates 3)
+ * Arithmetic and states are fp32; y is rounded to dt once.
+ *   z        : b sequences of t rows of gates * d values, type dt; z_bs and z_ts elements lie between
+ *              sequences and between rows: either may be the outer one, rows may not overlap (0, 0: dense).
+ *   bias     : fp32 [gates * d], or NULL for none.
+ *   h0       : fp32 b x d dense, or NULL for zeros.
+ *   lengths  : int32 [b] on the device, or NULL for t: rows from lengths[b] on (at most t, at least 0) are
+ *              padding, which is not read; y is 0 there and the state stays as it is.
+ *   y        : b sequences of t rows of d values, type dt, y_bs and y_ts elements apart.
+ *   h_last   : fp32 b x d, the state after each sequence's last row; or NULL.
+ *   states   : fp32 b x ceil(t / TFK_SCAN_BLOCK) x d, or NULL: the state before each TFK_SCAN_BLOCK-th row, for
+ *              tfk_gated_scan_bwd (undefined for blocks of padding alone).
+ *   ws       : at least tfk_gated_scan_workspace_bytes(0, b, t, d) bytes (may be NULL when that is 0); calls
+ *              that may overlap in time need one each.
+ * A NaN in z makes its channel NaN from there on.
+ * Errors: b, t < 0, d < 1, rows that overlap (SHAPE); gates not 2 or 3 (ARG); b > 2^31 - 1, t > 2^30 - 1, d > 2^24,
+ * more than 2^40 elements, negative strides (OVERFLOW); NULL, misaligned or overlapping buffers (NULL, ALIGN,
+ * ALIAS); WORKSPACE.  b == 0 is a no-op; t == 0 sets h_last to h0. */
+#define TFK_SCAN_BLOCK 128
+TFK_API tfk_status tfk_gated_scan_fwd(const void *z, tfk_dtype dt, int64_t b, int64_t t, int32_t d, int32_t gates,
+                              int64_t z_bs, int64_t z_ts, const float *bias, const float *h0, const int32_t *lengths,
+                              void *y, int64_t y_bs, int64_t y_ts, float *h_last, float *states, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/* Gradient of the recurrence (Section 4.1's backpropagation) for dy and, if not NULL, dh_last (fp32 b x d): with
+ * g_t = s(o_t) dy_t + s(a_(t+1)) g_(t+1), where dh_last is added at a sequence's last row,
+ *   dz[x] = (1 - s(a)) g     dz[a] = s(a) (1 - s(a)) (h_(t-1) - x) g     dz[o] = s(o) (1 - s(o)) dy h
+ *   dh0 = s(a_0) g_0  (dh_last for a sequence without rows)
+ * rounded to dt once; 0 in padding rows, whose dy is not read.  The bias's gradient is dz's column sums
+ * (tfk_bias_relu_bwd without y).
+ *   z, bias, lengths : as in the forward call.   states : what it wrote.
+ *   dz       : like z, with strides of its own; may equal z with the same strides (in place).
+ *   dh0      : fp32 b x d, or NULL.
+ *   ws       : at least tfk_gated_scan_workspace_bytes(1, b, t, d) bytes.
+ * Errors as above; t == 0 sets dh0 to dh_last. */
+TFK_API tfk_status tfk_gated_scan_bwd(const void *z, tfk_dtype dt, int64_t b, int64_t t, int32_t d, int32_t gates,
+                              int64_t z_bs, int64_t z_ts, const float *bias, const int32_t *lengths, const void *dy,
+                              int64_t dy_bs, int64_t dy_ts, const float *states, const float *dh_last, void *dz,
+                              int64_t dz_bs, int64_t dz_ts, float *dh0, void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace of the two operations above (of Section 4.1 and 6.4): op 0 = forward, 1 = gradient; 0 for
+ * arguments they refuse and where they need none. */
+TFK_API size_t tfk_gated_scan_workspace_bytes(int32_t op, int64_t b, int64_t t, int32_t d);
+
+/* One token of each of n sequences being served (Section 6.4's model, asked token by token): row i moves the
+ * state of slot slots[i] (slot i where slots is NULL) by one step of the recurrence, in place, and y's row i is
+ * its output.  A slot outside [0, nslots) is none: y's row is 0.  Slots must be distinct (each state then has
+ * one writer).
+ *   z : n rows of gates * d values, type dt, z_ld elements apart (0: dense); y : n rows of d, y_ld apart.
+ *   state : fp32 nslots x d dense.   slots : int32 [n] on the device, or NULL (n <= nslots then).
+ * Errors: n, nslots < 0, d < 1, a row distance below the row, n > nslots without slots (SHAPE); the others
+ * as above.  n == 0 is a no-op. */
+TFK_API tfk_status tfk_gated_scan_step(const void *z, tfk_dtype dt, int64_t n, int32_t d, int32_t gates, int64_t z_ld,
+                              const float *bias, const int32_t *slots, float *state, int64_t nslots, void *y,
+                              int64_t y_ld, void *stream);
+
 /* ---------------------------------------------------------------- embedding table
  * The embedding layer of Section 4.2: a Gather of the table's rows that the batch names, and its
  * gradient, which touches only those rows (the sparse updates of Sections 4.2 and 6.2).
@@ -584,6 +687,33 @@ TFK_API tfk_status tfk_apply_adam(float *var, float *m, float *v, const float *g
                           float beta1, float beta2, float epsilon, int64_t t, uint16_t *var_bf16,
                           void *stream);
 
+/* AdamW (Loshchilov & Hutter 2019: Adam with the weight decay apart from the gradient) over `count` variables
+ * at once, in place, step t >= 1 (Section 4.1's optimizers; the update of every variable of a synchronous step,
+ * Section 4.4):
+ *   m <- beta1 m + (1 - beta1) grad        v <- beta2 v + (1 - beta2) grad^2
+ *   var <- var - lr weight_decay var - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + epsilon)
+ * and its bf16 copy, if any, as in tfk_apply_sgd.  Arithmetic is fp32; 1 - beta, the bias corrections
+ * and lr weight_decay are formed in fp64 (1 - 0.999f would be off by 1e-5) and rounded to fp32.
+ *   bits     : 32: ms and vs hold fp32 moments.  8: they hold one byte per value, the 8-bit floating-point format
+ *              e4m3 (1 sign, 4 exponent bits of bias 7, 3 mantissa bits, no infinities, largest 448), and
+ *              m_scales, v_scales one fp32 factor for each 256 values of a variable (the last block may be
+ *              shorter): m = value * factor, sqrt(v) = value * factor (8-bit optimizers in blocks: Dettmers et al.
+ *              2022).  A new factor is the block's largest magnitude / 448, values are rounded to nearest
+ *              even, and a second moment that is not 0 is at least 2^-9 of its block's factor.  The step is made
+ *              with the moments before they are rounded.  A block whose largest magnitude is below 2^-100
+ *              becomes 0; one with a NaN or an infinity becomes NaN throughout.  Zeros are the first state.
+ *   weight_decay : one value for each variable, or NULL for none.
+ *   shadows  : NULL, or one bf16 copy for each variable, entries may be NULL.
+ * The arrays are host memory, read during the call; ns[i] values in variable i (0: skipped).
+ * Errors: count < 0, bits not 8 or 32, the scalars of tfk_apply_adam, weight decay negative or not finite (ARG);
+ * ns < 0 (SHAPE); ns > 2^38 or a scalar that overflows (OVERFLOW); NULL, misaligned (NULL, ALIGN); buffers of a
+ * variable that overlap, or two variables that do (ALIAS).  Moments, copies and gradients of different variables
+ * must not overlap where one is written (not checked). */
+TFK_API tfk_status tfk_apply_adamw_multi(int32_t count, int32_t bits, float *const *vars, void *const *ms, void *const *vs,
+                              float *const *m_scales, float *const *v_scales, const float *const *grads,
+                              const int64_t *ns, const double *weight_decay, double lr, double beta1, double beta2,
+                              double epsilon, int64_t t, uint16_t *const *shadows, void *stream);
+
 /* ---------------------------------------------------------------- streams and programs
  * The dataflow executor runs independent kernels of a step on several GPU streams (Section 5);
  * a step's subgraph is pruned and placed once, cached, and run again for every later step from
@@ -627,7 +757,7 @@ TFK_API tfk_status tfk_program_create(tfk_program **prog);
 TFK_API void tfk_program_destroy(tfk_program *prog);
 /* Starts recording on the calling thread (previous contents are dropped).  Until
  * tfk_program_end, every tfk_* call on this thread that enqueues work (convolutions, bias/ReLU,
- * pooling, updates, losses, sampled-softmax and embedding ops, tfk_stream_wait, marks) runs as usual and, when it
+ * pooling, updates, losses, recurrences, sampled-softmax and embedding ops, tfk_stream_wait, marks) runs as usual and, when it
  * returns TFK_OK, is appended to the program with its arguments by value: the same pointers,
  * shapes, scalars and streams.  Calls that fail are not appended.  Queries
  * (*_workspace_bytes) are never recorded.  Errors: NULL; ARG (this thread already records). */
@@ -639,7 +769,7 @@ TFK_API int64_t tfk_program_length(const tfk_program *prog);
 /* Issues the recorded calls again, in order, each validated as when it was recorded.  Every
  * buffer a recorded call names must still be allocated, and each call's results depend only
  * on what its buffers hold when it runs: scalars are replayed as recorded (a recorded
- * tfk_apply_adam replays its step count t unchanged).  Stops at the first call that fails
+ * tfk_apply_adam or tfk_apply_adamw_multi replays its step count t unchanged).  Stops at the first call that fails
  * and returns its status.  Errors: NULL; ARG (a program is recording on this thread); any
  * status a recorded call returns. */
 TFK_API tfk_status tfk_program_run(tfk_program *prog);

@@ -25,7 +25,9 @@ EXPORTS = ["tfk_conv2d_fwd", "tfk_conv2d_fwd_bias_relu", "tfk_maxpool_bwd_relu_b
            "tfk_maxpool_bwd_relu_bwd_taps", "tfk_apply_sgd", "tfk_apply_sgd_multi",
            "tfk_apply_momentum", "tfk_apply_adam", "tfk_softmax_xent", "tfk_gather_rows_t",
            "tfk_sampled_softmax_xent", "tfk_scatter_apply_sgd", "tfk_distill_xent", "tfk_embedding_fwd",
-           "tfk_embedding_bwd", "tfk_embedding_apply_sgd", "tfk_embedding_workspace_bytes", "tfk_stream_wait", "tfk_mark_create", "tfk_mark_destroy",
+           "tfk_embedding_bwd", "tfk_embedding_apply_sgd", "tfk_embedding_workspace_bytes",
+           "tfk_token_logprobs", "tfk_token_logprobs_bwd", "tfk_gated_scan_fwd", "tfk_gated_scan_bwd", "tfk_gated_scan_step",
+           "tfk_gated_scan_workspace_bytes", "tfk_apply_adamw_multi", "tfk_stream_wait", "tfk_mark_create", "tfk_mark_destroy",
            "tfk_mark_record", "tfk_stream_wait_mark", "tfk_program_create",
            "tfk_program_destroy", "tfk_program_begin", "tfk_program_end", "tfk_program_length", "tfk_program_run",
            "tfk_status_string", "tfk_last_error", "tfk_abi_version"]
@@ -60,6 +62,7 @@ def load(path: str = LIB_PATH):
         raise RuntimeError("libtfk.so is not built (%s): run `python -m paper_1605_08695_amd.build`" % path)
     lib = ctypes.CDLL(path)
     vp, i32, i64, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+    f64 = ctypes.c_double
     st = ctypes.c_int
     lib.tfk_conv2d_fwd.argtypes = [vp, Nhwc, vp, i32, Window, st, vp, Nhwc, vp, sz, vp]
     lib.tfk_conv2d_fwd_bias_relu.argtypes = [vp, Nhwc, vp, i32, vp, Window, st, vp, Nhwc, vp, sz, vp]
@@ -97,6 +100,17 @@ def load(path: str = LIB_PATH):
     lib.tfk_embedding_apply_sgd.argtypes = [vp, vp, i64, i32, vp, i64, vp, st, i64, f32, f32, vp, sz, vp]
     lib.tfk_embedding_workspace_bytes.argtypes = [i64, i32, i64]
     lib.tfk_embedding_workspace_bytes.restype = sz
+    lib.tfk_token_logprobs.argtypes = [vp, st, i64, i32, i64, vp, vp, f32, i32, vp, vp, vp, vp, vp, vp]
+    lib.tfk_token_logprobs_bwd.argtypes = [vp, st, i64, i32, i64, vp, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    lib.tfk_gated_scan_fwd.argtypes = [vp, st, i64, i64, i32, i32, i64, i64, vp, vp, vp, vp, i64, i64, vp, vp, vp, sz, vp]
+    lib.tfk_gated_scan_bwd.argtypes = [vp, st, i64, i64, i32, i32, i64, i64, vp, vp, vp, i64, i64, vp, vp, vp, i64, i64, vp,
+                                       vp, sz, vp]
+    lib.tfk_gated_scan_step.argtypes = [vp, st, i64, i32, i32, i64, vp, vp, vp, i64, vp, i64, vp]
+    lib.tfk_gated_scan_workspace_bytes.argtypes = [i32, i64, i64, i32]
+    lib.tfk_gated_scan_workspace_bytes.restype = sz
+    pvp = ctypes.POINTER(vp)
+    lib.tfk_apply_adamw_multi.argtypes = [i32, i32, pvp, pvp, pvp, pvp, pvp, pvp, ctypes.POINTER(i64), ctypes.POINTER(f64),
+                                          f64, f64, f64, f64, i64, pvp, vp]
     for name in ("tfk_conv2d_fwd", "tfk_conv2d_fwd_bias_relu", "tfk_conv2d_fwd_bias_relu_maxpool", "tfk_conv2d_bwd_input", "tfk_conv2d_bwd_input_relu_bwd",
                  "tfk_conv2d_bwd_filter", "tfk_conv2d_bwd_filter_noalloc", "tfk_bias_relu_fwd",
                  "tfk_bias_relu_bwd", "tfk_maxpool_fwd", "tfk_maxpool_bwd", "tfk_maxpool_bwd_relu_bwd",

@@ -1100,6 +1100,221 @@ tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n, int32_t
     return hip_status(launch_distill(dt == TFK_F32 ? 0 : 1, n, a, (hipStream_t)stream), "distill_xent");
 }
 
+// ------------------------------------------------------------------ log-probabilities
+// Shared by the operation and its gradient: logits' rows, their temperature, bias and tokens.
+static tfk_status check_logits(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t &ld, const float *bias,
+                               const int32_t *tokens, float temperature) {
+    if (!valid_dt(dt)) return fail(TFK_ERR_DTYPE, "unknown dtype %d", (int)dt);
+    if (n < 0 || c < 1) return fail(TFK_ERR_SHAPE, "need n >= 0 and c >= 1 (n=%lld, c=%d)", (long long)n, c);
+    if (c > (1 << 30)) return fail(TFK_ERR_OVERFLOW, "more than 2^30 classes");
+    TRY(check_rows("logits", n, c, ld));
+    if (!(temperature >= 1e-4f && temperature <= 1e4f)) return fail(TFK_ERR_ARG, "temperature must be in [1e-4, 1e4]");
+    if (n == 0) return TFK_OK;
+    TRY(need_ptr(logits, "logits"));
+    TRY(need_align(logits, esize(dt), "logits"));
+    TRY(need_align(bias, 4, "bias"));
+    TRY(need_align(tokens, 4, "tokens"));
+    return TFK_OK;
+}
+
+tfk_status tfk_token_logprobs(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld, const float *bias,
+                              const int32_t *tokens, float temperature, int32_t k, float *logp, float *entropy, float *lse,
+                              int32_t *top_idx, float *top_logp, void *stream) {
+    RECORDED(tfk_token_logprobs, logits, dt, n, c, logits_ld, bias, tokens, temperature, k, logp, entropy, lse, top_idx,
+             top_logp, stream);
+    TRY(check_logits(logits, dt, n, c, logits_ld, bias, tokens, temperature));
+    if (k < 0 || k > 128) return fail(TFK_ERR_SHAPE, "k must be in 0..128 (got %d)", k);
+    if (n == 0) return ok();
+    if (logp) TRY(need_ptr(tokens, "tokens"));
+    if (k > 0) TRY(need_ptr(top_idx, "top_idx"));
+    if (k > 0) TRY(need_ptr(top_logp, "top_logp"));
+    const void *p[8] = {logp, entropy, lse, k ? top_idx : nullptr, k ? top_logp : nullptr, logits, bias, tokens};
+    const int64_t b[8] = {n * 4, n * 4, n * 4, n * k * 4, n * k * 4, rows_bytes(n, c, logits_ld, esize(dt)), (int64_t)c * 4,
+                          n * 4};
+    const char *const name[5] = {"logp", "entropy", "lse", "top_idx", "top_logp"};
+    for (int i = 0; i < 5; ++i) TRY(need_align(p[i], 4, name[i]));
+    for (int i = 0; i < 5; ++i)
+        for (int j = i + 1; j < 8; ++j)
+            if (overlap(p[i], b[i], p[j], b[j])) return fail(TFK_ERR_ALIAS, "%s overlaps an operand", name[i]);
+    const LogprobArgs a{logits, logits_ld, bias, tokens, logp, entropy, lse, top_idx, top_logp, n, c, k, temperature};
+    return hip_status(launch_logprob(dt == TFK_F32 ? 0 : 1, a, (hipStream_t)stream), "token_logprobs");
+}
+
+tfk_status tfk_token_logprobs_bwd(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld, const float *bias,
+                                  const int32_t *tokens, float temperature, const float *lse, const float *entropy,
+                                  const float *dlogp, const float *dentropy, void *dlogits, int64_t dlogits_ld,
+                                  void *stream) {
+    RECORDED(tfk_token_logprobs_bwd, logits, dt, n, c, logits_ld, bias, tokens, temperature, lse, entropy, dlogp, dentropy,
+             dlogits, dlogits_ld, stream);
+    TRY(check_logits(logits, dt, n, c, logits_ld, bias, tokens, temperature));
+    TRY(check_rows("dlogits", n, c, dlogits_ld));
+    if (n == 0) return ok();
+    TRY(need_ptr(tokens, "tokens"));
+    TRY(need_ptr(lse, "lse"));
+    TRY(need_ptr(dlogp, "dlogp"));
+    if (dentropy) TRY(need_ptr(entropy, "entropy"));
+    TRY(need_ptr(dlogits, "dlogits"));
+    const int64_t es = esize(dt);
+    TRY(need_align(dlogits, es, "dlogits"));
+    TRY(need_align(lse, 4, "lse"));
+    TRY(need_align(entropy, 4, "entropy"));
+    TRY(need_align(dlogp, 4, "dlogp"));
+    TRY(need_align(dentropy, 4, "dentropy"));
+    const bool in_place = dlogits == logits && dlogits_ld == logits_ld;
+    const int64_t db = rows_bytes(n, c, dlogits_ld, es);
+    const void *p[6] = {bias, tokens, lse, entropy, dlogp, dentropy};
+    const int64_t b[6] = {(int64_t)c * 4, n * 4, n * 4, n * 4, n * 4, n * 4};
+    if (!in_place && overlap(dlogits, db, logits, rows_bytes(n, c, logits_ld, es)))
+        return fail(TFK_ERR_ALIAS, "dlogits overlaps logits");
+    for (int i = 0; i < 6; ++i)
+        if (overlap(dlogits, db, p[i], b[i])) return fail(TFK_ERR_ALIAS, "dlogits overlaps an operand");
+    const LogprobBwdArgs a{logits, logits_ld, bias, tokens, lse, entropy, dlogp, dentropy, dlogits, dlogits_ld, n, c,
+                           temperature};
+    return hip_status(launch_logprob_bwd(dt == TFK_F32 ? 0 : 1, a, (hipStream_t)stream), "token_logprobs_bwd");
+}
+
+// ------------------------------------------------------------------ gated linear recurrence
+// The most channels whose columns of z stay well inside 32 bits.
+static constexpr int32_t kScanChannels = 1 << 24;
+
+// A batch of b sequences of t rows of `cols` elements, bs and ts elements between sequences and rows: either may be
+// the outer one, and rows do not overlap.  0: dense, sequence first.
+static tfk_status check_seqs(const char *name, int64_t b, int64_t t, int64_t cols, int64_t &bs, int64_t &ts) {
+    const int64_t most = (int64_t)1 << 40;
+    if (t <= 1 || ts == 0) ts = cols;
+    if (ts < 0 || bs < 0 || ts > most / std::max<int64_t>(t, 1))
+        return fail(TFK_ERR_OVERFLOW, "%s: negative strides or too large", name);
+    if (b <= 1 || bs == 0) bs = std::max(t * ts, cols);
+    if (bs > most / std::max<int64_t>(b, 1)) return fail(TFK_ERR_OVERFLOW, "%s: too large", name);
+    if (b == 0 || t == 0) return TFK_OK;
+    const bool rows = ts >= cols && (b == 1 || bs >= (t - 1) * ts + cols);
+    const bool cross = bs >= cols && (t == 1 || ts >= (b - 1) * bs + cols);
+    if (!rows && !cross)
+        return fail(TFK_ERR_SHAPE, "%s: strides %lld, %lld make rows of %lld overlap", name, (long long)bs, (long long)ts,
+                    (long long)cols);
+    return TFK_OK;
+}
+
+static int64_t seqs_bytes(int64_t b, int64_t t, int64_t cols, int64_t bs, int64_t ts, int64_t es) {
+    return b == 0 || t == 0 ? 0 : ((b - 1) * bs + (t - 1) * ts + cols) * es;
+}
+
+static tfk_status check_scan(tfk_dtype dt, int64_t b, int64_t t, int32_t d, int32_t gates) {
+    if (!valid_dt(dt)) return fail(TFK_ERR_DTYPE, "unknown dtype %d", (int)dt);
+    if (b < 0 || t < 0 || d < 1) return fail(TFK_ERR_SHAPE, "need b >= 0, t >= 0 and d >= 1");
+    if (gates != 2 && gates != 3) return fail(TFK_ERR_ARG, "gates must be 2 or 3 (got %d)", gates);
+    if (b > INT32_MAX || t > INT32_MAX / 2 || d > kScanChannels) return fail(TFK_ERR_OVERFLOW, "b, t or d too large");
+    if (b > 0 && (t + 1) * d > ((int64_t)1 << 40) / b) return fail(TFK_ERR_OVERFLOW, "b * t * d too large");
+    return TFK_OK;
+}
+
+size_t tfk_gated_scan_workspace_bytes(int32_t op, int64_t b, int64_t t, int32_t d) {
+    if (op < 0 || op > 1 || check_scan(TFK_F32, b, t, d, 2) != TFK_OK || b == 0 || t == 0) return 0;
+    return scan_ws_bytes(op == 1, b, t, d);
+}
+
+tfk_status tfk_gated_scan_fwd(const void *z, tfk_dtype dt, int64_t b, int64_t t, int32_t d, int32_t gates, int64_t z_bs,
+                              int64_t z_ts, const float *bias, const float *h0, const int32_t *lengths, void *y, int64_t y_bs,
+                              int64_t y_ts, float *h_last, float *states, void *ws, size_t ws_bytes, void *stream) {
+    RECORDED(tfk_gated_scan_fwd, z, dt, b, t, d, gates, z_bs, z_ts, bias, h0, lengths, y, y_bs, y_ts, h_last, states, ws,
+             ws_bytes, stream);
+    TRY(check_scan(dt, b, t, d, gates));
+    TRY(check_seqs("z", b, t, (int64_t)gates * d, z_bs, z_ts));
+    TRY(check_seqs("y", b, t, d, y_bs, y_ts));
+    if (b == 0) return ok();
+    if (t > 0) {
+        TRY(need_ptr(z, "z"));
+        TRY(need_ptr(y, "y"));
+    }
+    const int64_t es = esize(dt), hb = b * d * 4, sb = (t + kScanBlock - 1) / kScanBlock * hb;
+    const size_t need = t == 0 ? 0 : scan_ws_bytes(false, b, t, d);
+    TRY(check_ws(ws, ws_bytes, need));
+    TRY(need_align(z, es, "z"));
+    TRY(need_align(y, es, "y"));
+    const void *p[8] = {y, h_last, states, ws, z, bias, h0, lengths};
+    const int64_t n[8] = {seqs_bytes(b, t, d, y_bs, y_ts, es), hb, sb, (int64_t)need,
+                          seqs_bytes(b, t, (int64_t)gates * d, z_bs, z_ts, es), (int64_t)gates * d * 4, hb, b * 4};
+    const char *const name[8] = {"y", "h_last", "states", "ws", "z", "bias", "h0", "lengths"};
+    for (int i = 1; i < 8; ++i)
+        if (i != 3 && i != 4) TRY(need_align(p[i], 4, name[i]));
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 8; ++j)
+            if (overlap(p[i], n[i], p[j], n[j])) return fail(TFK_ERR_ALIAS, "%s overlaps %s", name[i], name[j]);
+    if (t == 0 && h_last == nullptr) return ok();
+    const ScanArgs a{z, z_bs, z_ts, bias, h0, lengths, y, y_bs, y_ts, h_last, states, b, (int)t, d};
+    return hip_status(launch_scan_fwd(dt == TFK_F32 ? 0 : 1, gates, a, ws, (hipStream_t)stream), "gated_scan_fwd");
+}
+
+tfk_status tfk_gated_scan_bwd(const void *z, tfk_dtype dt, int64_t b, int64_t t, int32_t d, int32_t gates, int64_t z_bs,
+                              int64_t z_ts, const float *bias, const int32_t *lengths, const void *dy, int64_t dy_bs,
+                              int64_t dy_ts, const float *states, const float *dh_last, void *dz, int64_t dz_bs,
+                              int64_t dz_ts, float *dh0, void *ws, size_t ws_bytes, void *stream) {
+    RECORDED(tfk_gated_scan_bwd, z, dt, b, t, d, gates, z_bs, z_ts, bias, lengths, dy, dy_bs, dy_ts, states, dh_last, dz,
+             dz_bs, dz_ts, dh0, ws, ws_bytes, stream);
+    TRY(check_scan(dt, b, t, d, gates));
+    TRY(check_seqs("z", b, t, (int64_t)gates * d, z_bs, z_ts));
+    TRY(check_seqs("dy", b, t, d, dy_bs, dy_ts));
+    TRY(check_seqs("dz", b, t, (int64_t)gates * d, dz_bs, dz_ts));
+    if (b == 0) return ok();
+    if (t > 0) {
+        TRY(need_ptr(z, "z"));
+        TRY(need_ptr(dy, "dy"));
+        TRY(need_ptr(states, "states"));
+        TRY(need_ptr(dz, "dz"));
+    }
+    const int64_t es = esize(dt), hb = b * d * 4, sb = (t + kScanBlock - 1) / kScanBlock * hb;
+    const size_t need = t == 0 ? 0 : scan_ws_bytes(true, b, t, d);
+    TRY(check_ws(ws, ws_bytes, need));
+    TRY(need_align(z, es, "z"));
+    TRY(need_align(dy, es, "dy"));
+    TRY(need_align(dz, es, "dz"));
+    const bool in_place = dz == z && dz_bs == z_bs && dz_ts == z_ts;
+    const void *p[9] = {dz, dh0, ws, z, dy, states, dh_last, bias, lengths};
+    const int64_t n[9] = {seqs_bytes(b, t, (int64_t)gates * d, dz_bs, dz_ts, es), hb, (int64_t)need,
+                          seqs_bytes(b, t, (int64_t)gates * d, z_bs, z_ts, es), seqs_bytes(b, t, d, dy_bs, dy_ts, es), sb, hb,
+                          (int64_t)gates * d * 4, b * 4};
+    const char *const name[9] = {"dz", "dh0", "ws", "z", "dy", "states", "dh_last", "bias", "lengths"};
+    for (int i : {1, 5, 6, 7, 8}) TRY(need_align(p[i], 4, name[i]));
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 9; ++j)
+            if (!(in_place && i == 0 && j == 3) && overlap(p[i], n[i], p[j], n[j]))
+                return fail(TFK_ERR_ALIAS, "%s overlaps %s", name[i], name[j]);
+    if (t == 0 && dh0 == nullptr) return ok();
+    const ScanBwdArgs a{z, z_bs, z_ts, bias, lengths, dy, dy_bs, dy_ts, states, dh_last, dz, dz_bs, dz_ts, dh0, b, (int)t, d};
+    return hip_status(launch_scan_bwd(dt == TFK_F32 ? 0 : 1, gates, a, ws, (hipStream_t)stream), "gated_scan_bwd");
+}
+
+tfk_status tfk_gated_scan_step(const void *z, tfk_dtype dt, int64_t n, int32_t d, int32_t gates, int64_t z_ld,
+                               const float *bias, const int32_t *slots, float *state, int64_t nslots, void *y, int64_t y_ld,
+                               void *stream) {
+    RECORDED(tfk_gated_scan_step, z, dt, n, d, gates, z_ld, bias, slots, state, nslots, y, y_ld, stream);
+    TRY(check_scan(dt, n, 1, d, gates));
+    if (nslots < 0) return fail(TFK_ERR_SHAPE, "nslots must be >= 0");
+    TRY(check_rows("z", n, (int64_t)gates * d, z_ld));
+    TRY(check_rows("y", n, d, y_ld));
+    int64_t sld = d;
+    TRY(check_rows("state", nslots, d, sld));
+    if (slots == nullptr && n > nslots) return fail(TFK_ERR_SHAPE, "n rows without slots need as many states");
+    if (n == 0) return ok();
+    TRY(need_ptr(z, "z"));
+    TRY(need_ptr(y, "y"));
+    if (nslots > 0) TRY(need_ptr(state, "state"));
+    const int64_t es = esize(dt);
+    TRY(need_align(z, es, "z"));
+    TRY(need_align(y, es, "y"));
+    TRY(need_align(state, 4, "state"));
+    TRY(need_align(bias, 4, "bias"));
+    TRY(need_align(slots, 4, "slots"));
+    const void *p[5] = {y, state, z, bias, slots};
+    const int64_t b[5] = {rows_bytes(n, d, y_ld, es), nslots * d * 4, rows_bytes(n, (int64_t)gates * d, z_ld, es),
+                          (int64_t)gates * d * 4, n * 4};
+    for (int i = 0; i < 2; ++i)
+        for (int j = i + 1; j < 5; ++j)
+            if (overlap(p[i], b[i], p[j], b[j])) return fail(TFK_ERR_ALIAS, "y or state overlaps an operand");
+    const ScanStepArgs a{z, z_ld, bias, slots, state, nslots, y, y_ld, n, d};
+    return hip_status(launch_scan_step(dt == TFK_F32 ? 0 : 1, gates, a, (hipStream_t)stream), "gated_scan_step");
+}
+
 // ------------------------------------------------------------------ embedding table
 tfk_status tfk_embedding_fwd(const void *table, tfk_dtype dt, int64_t rows, int64_t table_ld, int32_t d, const int32_t *ids,
                              int64_t n, float scale, void *out, tfk_dtype out_dt, int64_t out_ld, void *stream) {
@@ -1253,6 +1468,130 @@ tfk_status tfk_apply_adam(float *var, float *m, float *v, const float *grad, int
     p.eps = epsilon;
     if (!isfinite(p.lr) || !isfinite(p.rc2)) return fail(TFK_ERR_OVERFLOW, "bias-corrected step overflows fp32");
     return hip_status(launch_opt(2, var, m, v, grad, n, p, var_bf16, (hipStream_t)stream), "apply_adam");
+}
+
+// ------------------------------------------------------------------ AdamW
+// Variables that share memory would be updated by two workgroups at once.
+static tfk_status check_apart(int32_t count, float *const *vars, const int64_t *ns) {
+    try {
+        std::vector<std::pair<uintptr_t, int>> at;
+        at.reserve(count);
+        for (int i = 0; i < count; ++i)
+            if (ns[i] > 0) at.emplace_back((uintptr_t)vars[i], i);
+        std::sort(at.begin(), at.end());
+        for (size_t j = 1; j < at.size(); ++j)
+            if (at[j].first < at[j - 1].first + (uintptr_t)ns[at[j - 1].second] * 4)
+                return fail(TFK_ERR_ALIAS, "variables %d and %d overlap", at[j - 1].second, at[j].second);
+    } catch (...) {
+        return fail(TFK_ERR_ARG, "tfk_apply_adamw_multi: out of host memory");
+    }
+    return TFK_OK;
+}
+
+tfk_status tfk_apply_adamw_multi(int32_t count, int32_t bits, float *const *vars, void *const *ms, void *const *vs,
+                                 float *const *m_scales, float *const *v_scales, const float *const *grads, const int64_t *ns,
+                                 const double *weight_decay, double lr, double beta1, double beta2, double epsilon, int64_t t,
+                                 uint16_t *const *shadows, void *stream) {
+    if (g_rec != nullptr && count > 0 && vars && ms && vs && grads && ns) {
+        // the arrays belong to the caller: the recorded call keeps copies of them
+        tfk_program *const rec_ = g_rec;
+        g_rec = nullptr;
+        const tfk_status s_ = tfk_apply_adamw_multi(count, bits, vars, ms, vs, m_scales, v_scales, grads, ns, weight_decay, lr,
+                                                    beta1, beta2, epsilon, t, shadows, stream);
+        g_rec = rec_;
+        if (s_ != TFK_OK) return s_;
+        try {
+            std::vector<float *> x(vars, vars + count), mc, vc;
+            std::vector<void *> m(ms, ms + count), v(vs, vs + count);
+            std::vector<const float *> g(grads, grads + count);
+            std::vector<int64_t> n(ns, ns + count);
+            std::vector<double> wd;
+            std::vector<uint16_t *> sh;
+            if (bits == 8) mc.assign(m_scales, m_scales + count);
+            if (bits == 8) vc.assign(v_scales, v_scales + count);
+            if (weight_decay) wd.assign(weight_decay, weight_decay + count);
+            if (shadows) sh.assign(shadows, shadows + count);
+            rec_->calls.emplace_back([=]() {
+                return tfk_apply_adamw_multi(count, bits, x.data(), m.data(), v.data(), mc.empty() ? nullptr : mc.data(),
+                                             vc.empty() ? nullptr : vc.data(), g.data(), n.data(),
+                                             wd.empty() ? nullptr : wd.data(), lr, beta1, beta2, epsilon, t,
+                                             sh.empty() ? nullptr : sh.data(), stream);
+            });
+        } catch (...) {
+            return fail(TFK_ERR_ARG, "tfk_apply_adamw_multi: out of host memory while recording");
+        }
+        return s_;
+    }
+    if (count < 0) return fail(TFK_ERR_ARG, "count must be >= 0");
+    if (bits != 8 && bits != 32) return fail(TFK_ERR_ARG, "bits must be 8 or 32 (got %d)", bits);
+    if (!isfinite(lr)) return fail(TFK_ERR_ARG, "lr must be finite");
+    if (!(beta1 >= 0. && beta1 < 1.)) return fail(TFK_ERR_ARG, "beta1 must be in [0, 1)");
+    if (!(beta2 >= 0. && beta2 < 1.)) return fail(TFK_ERR_ARG, "beta2 must be in [0, 1)");
+    if (!(epsilon >= 0.) || !isfinite(epsilon)) return fail(TFK_ERR_ARG, "epsilon must be finite and >= 0");
+    if (t < 1) return fail(TFK_ERR_ARG, "t must be >= 1");
+    if (count == 0) return ok();
+    TRY(need_ptr(vars, "vars"));
+    TRY(need_ptr(ms, "ms"));
+    TRY(need_ptr(vs, "vs"));
+    TRY(need_ptr(grads, "grads"));
+    TRY(need_ptr(ns, "ns"));
+    if (bits == 8) TRY(need_ptr(m_scales, "m_scales"));
+    if (bits == 8) TRY(need_ptr(v_scales, "v_scales"));
+    const double c1 = 1.0 - pow(beta1, (double)t), c2 = 1.0 - pow(beta2, (double)t);
+    const AdamwParams q{(float)(lr / c1), (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2),
+                        (float)(1.0 / c2), (float)epsilon};
+    if (!isfinite(q.lr) || !isfinite(q.rc2) || !isfinite(q.eps)) return fail(TFK_ERR_OVERFLOW, "bias-corrected step overflows fp32");
+    for (int i = 0; i < count; ++i) {
+        const double wd = weight_decay ? weight_decay[i] : 0.;
+        const int64_t n = ns[i], blocks = (n + 255) / 256, mb = bits == 8 ? n : n * 4;
+        tfk_status s = TFK_OK;
+        if (!(wd >= 0.) || !isfinite((float)wd) || !isfinite((float)(lr * wd))) s = fail(TFK_ERR_ARG, "weight decay must be finite and >= 0");
+        else if (n < 0) s = fail(TFK_ERR_SHAPE, "n must be >= 0");
+        else if (n > ((int64_t)1 << 38)) s = fail(TFK_ERR_OVERFLOW, "n too large");
+        if (s == TFK_OK && n > 0) {
+            const void *p[7] = {vars[i], ms[i], vs[i], grads[i], bits == 8 ? m_scales[i] : nullptr,
+                                bits == 8 ? v_scales[i] : nullptr, shadows ? shadows[i] : nullptr};
+            const int64_t b[7] = {n * 4, mb, mb, n * 4, blocks * 4, blocks * 4, n * 2};
+            const int64_t al[7] = {4, bits == 8 ? 1 : 4, bits == 8 ? 1 : 4, 4, 4, 4, 2};
+            const char *const name[7] = {"var", "m", "v", "grad", "m_scale", "v_scale", "var_bf16"};
+            for (int j = 0; j < 7 && s == TFK_OK; ++j) {
+                if (j < (bits == 8 ? 6 : 4)) s = need_ptr(p[j], name[j]);
+                if (s == TFK_OK) s = need_align(p[j], al[j], name[j]);
+            }
+            for (int j = 0; j < 7 && s == TFK_OK; ++j)
+                for (int k = j + 1; k < 7 && s == TFK_OK; ++k)
+                    if (overlap(p[j], b[j], p[k], b[k])) s = fail(TFK_ERR_ALIAS, "%s overlaps %s", name[j], name[k]);
+        }
+        if (s != TFK_OK) return fail(s, "variable %d: %s", i, std::string(g_err).c_str());
+    }
+    TRY(check_apart(count, vars, ns));
+    int i = 0;
+    while (i < count) {
+        AdamwBatch b;
+        b.count = 0;
+        b.blk_start[0] = 0;
+        for (; i < count && b.count < kAdamwBatch; ++i) {
+            if (ns[i] == 0) continue;
+            const int64_t blocks = (ns[i] + 255) / 256;
+            const int k = b.count;
+            if (k > 0 && b.blk_start[k] + blocks > INT32_MAX / 2) break;
+            ++b.count;
+            b.var[k] = vars[i];
+            b.grad[k] = grads[i];
+            b.m[k] = ms[i];
+            b.v[k] = vs[i];
+            b.m_scale[k] = bits == 8 ? m_scales[i] : nullptr;
+            b.v_scale[k] = bits == 8 ? v_scales[i] : nullptr;
+            b.shadow[k] = shadows ? shadows[i] : nullptr;
+            b.n[k] = ns[i];
+            b.decay[k] = weight_decay ? (float)(lr * weight_decay[i]) : 0.f;
+            b.blk_start[k + 1] = (int)(b.blk_start[k] + blocks);
+        }
+        if (b.count == 0) continue;
+        const hipError_t e = launch_adamw(bits == 8, b, q, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_status(e, "apply_adamw_multi");
+    }
+    return ok();
 }
 
 // ------------------------------------------------------------------ streams and programs

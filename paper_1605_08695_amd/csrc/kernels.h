@@ -204,6 +204,101 @@ hipError_t launch_embed_bwd(int dt, const void *dy, int64_t n, int d, int64_t dl
                             float scale, float beta, float *dtable, void *ws, hipStream_t st);
 hipError_t launch_embed_sgd(int dt, float *var, uint16_t *sh, int64_t rows, int d, const int32_t *ids, int64_t n,
                             const void *dy, int64_t dld, float scale, float lr, void *ws, hipStream_t st);
+// A grid of at least n workgroups in two dimensions (a launch has fewer than 2^32 threads in each).
+inline dim3 grid_2d(int64_t n) {
+    const int64_t x = std::min<int64_t>(n, 1 << 20);
+    return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+
+// Gated linear recurrence (see tfk_gated_scan_fwd): b sequences of t tokens, d channels; element strides of
+// sequences (_bs) and tokens (_ts).  bias, h0, lengths, h_last, states, dh_last and dh0 may be null.
+constexpr int kScanBlock = 128;       // tokens between two saved states
+struct ScanArgs {
+    const void *z;
+    int64_t z_bs, z_ts;
+    const float *bias, *h0;
+    const int32_t *lengths;
+    void *y;
+    int64_t y_bs, y_ts;
+    float *h_last, *states;
+    int64_t b;
+    int t, d;
+};
+struct ScanBwdArgs {
+    const void *z;
+    int64_t z_bs, z_ts;
+    const float *bias;
+    const int32_t *lengths;
+    const void *dy;
+    int64_t dy_bs, dy_ts;
+    const float *states, *dh_last;
+    void *dz;
+    int64_t dz_bs, dz_ts;
+    float *dh0;
+    int64_t b;
+    int t, d;
+};
+struct ScanStepArgs {
+    const void *z;
+    int64_t z_ld;
+    const float *bias;
+    const int32_t *slots;
+    float *state;
+    int64_t nslots;
+    void *y;
+    int64_t y_ld;
+    int64_t n;
+    int d;
+};
+size_t scan_ws_bytes(bool bwd, int64_t b, int64_t t, int d);
+hipError_t launch_scan_fwd(int dt, int gates, const ScanArgs &a, void *ws, hipStream_t st);
+hipError_t launch_scan_bwd(int dt, int gates, const ScanBwdArgs &a, void *ws, hipStream_t st);
+hipError_t launch_scan_step(int dt, int gates, const ScanStepArgs &a, hipStream_t st);
+// Log-probabilities, entropy and the k largest classes of n rows, and their logits' gradient (see
+// tfk_token_logprobs; tokens, bias, logp, entropy, lse and dentropy may be null; dz may be z).
+struct LogprobArgs {
+    const void *z;
+    int64_t zld;
+    const float *bias;
+    const int32_t *tokens;
+    float *logp, *entropy, *lse;
+    int32_t *top_idx;
+    float *top_logp;
+    int64_t n;
+    int c, k;
+    float temperature;
+};
+struct LogprobBwdArgs {
+    const void *z;
+    int64_t zld;
+    const float *bias;
+    const int32_t *tokens;
+    const float *lse, *entropy, *dlogp, *dentropy;
+    void *dz;
+    int64_t dld, n;
+    int c;
+    float temperature;
+};
+hipError_t launch_logprob(int dt, const LogprobArgs &a, hipStream_t st);
+hipError_t launch_logprob_bwd(int dt, const LogprobBwdArgs &a, hipStream_t st);
+// AdamW over a batch of variables; blocks of 256 values, numbered through the batch.  m, v: fp32, or e4m3
+// values with a scale per block.
+constexpr int kAdamwBatch = 44;
+struct AdamwParams {
+    float lr, b1, omb1, b2, omb2, rc2, eps;      // lr and rc2 hold the bias corrections
+};
+struct AdamwBatch {
+    int count;
+    int blk_start[kAdamwBatch + 1];
+    float decay[kAdamwBatch];                    // lr times the weight decay
+    int64_t n[kAdamwBatch];
+    float *var[kAdamwBatch];
+    const float *grad[kAdamwBatch];
+    void *m[kAdamwBatch], *v[kAdamwBatch];
+    float *m_scale[kAdamwBatch], *v_scale[kAdamwBatch];
+    uint16_t *shadow[kAdamwBatch];
+};
+hipError_t launch_adamw(bool bits8, const AdamwBatch &b, const AdamwParams &p, hipStream_t st);
 // Momentum (kind 0, 1 = look-ahead form) and Adam (kind 2) in place over n fp32 elements.
 hipError_t launch_opt(int kind, float *var, float *s1, float *s2, const float *grad, int64_t n, const OptParams &p,
                       uint16_t *sh, hipStream_t st);

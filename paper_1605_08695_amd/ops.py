@@ -22,7 +22,9 @@ __all__ = ["conv2d_fwd", "conv2d_fwd_bias_relu", "conv2d_bwd_input", "conv2d_bwd
            "bias_relu_bwd", "bias_relu_bwd_workspace_bytes", "maxpool_fwd", "maxpool_bwd", "maxpool_bwd_relu_bwd", "apply_sgd",
            "apply_sgd_multi", "apply_momentum", "apply_adam", "softmax_xent",
            "gather_rows_t", "sampled_softmax_xent", "scatter_apply_sgd", "distill_xent", "embedding_fwd", "embedding_bwd",
-           "embedding_apply_sgd", "embedding_workspace_bytes", "stream_wait", "Program", "out_len", "nhwc",
+           "embedding_apply_sgd", "embedding_workspace_bytes", "token_logprobs", "token_logprobs_bwd", "TokenLogprobs",
+           "gated_scan_fwd", "gated_scan_bwd", "gated_scan_step", "gated_scan_workspace_bytes", "SCAN_BLOCK",
+           "apply_adamw_multi", "adamw_scales", "stream_wait", "Program", "out_len", "nhwc",
            "window", "TfkError", "abi_version", "DeferredBias", "bias_grad_finish"]
 
 
@@ -531,6 +533,72 @@ def apply_sgd_multi(vars_: Sequence[torch.Tensor], grads: Sequence[torch.Tensor]
     check(load().tfk_apply_sgd_multi(count, v, g, ns, float(lr), sh, _stream(stream)))
 
 
+def adamw_scales(n: int) -> int:
+    """How many factors the 8-bit moments of a variable of n values have: one for each 256."""
+    return (n + 255) // 256
+
+
+def _check_adamw(vars_, ms, vs, m_scales, v_scales, shadows, bits):
+    """Types, sizes and layout of the variables and of what is kept for each."""
+    if bits not in (8, 32):
+        raise ValueError("bits must be 8 or 32, got %r" % (bits,))
+    kinds = [("m", ms, torch.float32 if bits == 32 else torch.float8_e4m3fn), ("v", vs, torch.float32 if bits == 32 else
+                                                                              torch.float8_e4m3fn)]
+    if bits == 8:
+        if m_scales is None or v_scales is None:
+            raise ValueError("moments in 8 bits need m_scales and v_scales")
+        kinds += [("m_scales", m_scales, torch.float32), ("v_scales", v_scales, torch.float32)]
+    if shadows is not None:
+        kinds.append(("shadows", shadows, torch.bfloat16))
+    for name, ts, dtype in kinds:
+        if len(ts) != len(vars_):
+            raise ValueError("%s must have one entry for each variable" % name)
+        for i, (var, t) in enumerate(zip(vars_, ts)):
+            if t is None and name == "shadows":
+                continue
+            n = adamw_scales(var.numel()) if name.endswith("scales") else var.numel()
+            if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+                raise ValueError("%s of variable %d must be a contiguous %s tensor of %d values" %
+                                 (name, i, str(dtype).split(".")[-1], n))
+    for i, var in enumerate(vars_):
+        if var.dtype != torch.float32 or not var.is_contiguous():
+            raise ValueError("variable %d must be contiguous float32" % i)
+
+
+def _pointers(ts):
+    return (ctypes.c_void_p * max(len(ts), 1))(*[t.data_ptr() if t is not None else 0 for t in ts])
+
+
+def _check_grads(grads, sizes):
+    if len(grads) != len(sizes):
+        raise ValueError("one gradient for each variable")
+    for i, (g, n) in enumerate(zip(grads, sizes)):
+        if g.dtype != torch.float32 or g.numel() != n or not g.is_contiguous():
+            raise ValueError("the gradient of variable %d must be a contiguous float32 tensor of %d values" % (i, n))
+
+
+def apply_adamw_multi(vars_: Sequence[torch.Tensor], ms, vs, grads, lr, beta1, beta2, epsilon, t, weight_decay=None,
+                      shadows=None, m_scales=None, v_scales=None, bits=32, stream=None):
+    """In place, AdamW step t >= 1 over all variables at once: moments ms and vs in fp32, or with bits=8 as
+    float8_e4m3fn values (vs: the square root) with one fp32 factor for each 256 of them in m_scales and
+    v_scales; weight_decay one number for each variable; shadows bf16 copies (entries may be None).
+    optim.AdamW keeps all of this for a program."""
+    _check_adamw(vars_, ms, vs, m_scales, v_scales, shadows, bits)
+    sizes = [v.numel() for v in vars_]
+    _check_grads(grads, sizes)
+    n = len(vars_)
+    if weight_decay is not None and len(weight_decay) != n:
+        raise ValueError("weight_decay must have one entry for each variable")
+    if n == 0:
+        return
+    st = _on_device(stream, *vars_, *ms, *vs, *grads, *(shadows or ()), *((*m_scales, *v_scales) if bits == 8 else ()))
+    check(load().tfk_apply_adamw_multi(
+        n, bits, _pointers(vars_), _pointers(ms), _pointers(vs), _pointers(m_scales) if bits == 8 else None,
+        _pointers(v_scales) if bits == 8 else None, _pointers(grads), (ctypes.c_int64 * n)(*sizes),
+        None if weight_decay is None else (ctypes.c_double * n)(*weight_decay), float(lr), float(beta1), float(beta2),
+        float(epsilon), operator.index(t), None if shadows is None else _pointers(shadows), st))
+
+
 # ----------------------------------------------------------------------------- sampled softmax
 def gather_rows_t(table, idx, u_pad, out_t=None, stream=None):
     """out_t (d x u_pad) = table[idx]^T, zero past len(idx); table (rows x d) contiguous."""
@@ -755,6 +823,207 @@ def embedding_apply_sgd(var, ids, dy, lr, scale=1.0, shadow=None, ws=None, strea
     check(load().tfk_embedding_apply_sgd(_ptr(var), _ptr(shadow), rows, d, _ptr(ids), n, _ptr(dy), dt, ld, float(scale),
                                          float(lr), _ptr(ws), need, st))
     return var
+
+
+# ----------------------------------------------------------------------------- log-probabilities
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs found out about each row; logp without tokens and top_* with k = 0 are None."""
+    logp: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_idx: Optional[torch.Tensor]
+    top_logp: Optional[torch.Tensor]
+
+
+def token_logprobs(logits, tokens=None, k=0, temperature=1.0, bias=None, stream=None) -> TokenLogprobs:
+    """Of each row of (logits + bias) / temperature: the log-probability of its token (int32; one outside the
+    classes is padding), the entropy, the log-sum-exp and the k <= 128 largest classes with their
+    log-probabilities, largest first (n x k, -1 and -inf behind the last class that is not -inf)."""
+    n, c, ld = _rows_of(logits, "logits")
+    k = operator.index(k)
+    if not 0 <= k <= 128:
+        raise ValueError("k must be in 0..128, got %d" % k)
+    _vector(tokens, torch.int32, n, "tokens")
+    _vector(bias, torch.float32, c, "bias")
+    dt = _dt(logits)
+    st = _on_device(stream, logits, tokens, bias)
+    out = _empty(stream, (2 if tokens is None else 3, n), dtype=torch.float32, device=logits.device)
+    idx = top = None
+    if k:
+        idx = _empty(stream, (n, k), dtype=torch.int32, device=logits.device)
+        top = _empty(stream, (n, k), dtype=torch.float32, device=logits.device)
+    r = TokenLogprobs(None if tokens is None else out[2], out[0], out[1], idx, top)
+    check(load().tfk_token_logprobs(_ptr(logits), dt, n, c, ld, _ptr(bias), _ptr(tokens), float(temperature), k, _ptr(r.logp),
+                                    _ptr(r.entropy), _ptr(r.lse), _ptr(idx), _ptr(top), st))
+    return r
+
+
+def token_logprobs_bwd(logits, tokens, lse, dlogp, entropy=None, dentropy=None, temperature=1.0, bias=None, dlogits=None,
+                       stream=None):
+    """The logits' gradient for the gradients dlogp of token_logprobs' logp and, if given, dentropy of its entropy;
+    lse and entropy as that call returned them.  dlogits may be logits (in place).  Returns dlogits."""
+    n, c, ld = _rows_of(logits, "logits")
+    _vector(tokens, torch.int32, n, "tokens")
+    _vector(lse, torch.float32, n, "lse")
+    _vector(dlogp, torch.float32, n, "dlogp")
+    _vector(entropy, torch.float32, n, "entropy")
+    _vector(dentropy, torch.float32, n, "dentropy")
+    _vector(bias, torch.float32, c, "bias")
+    if dentropy is not None and entropy is None:
+        raise ValueError("dentropy needs the entropy")
+    dt, dld = _dt(logits), c if dlogits is None else ld
+    if dlogits is not None and dlogits is not logits:
+        if dlogits.shape != logits.shape or dlogits.dtype != logits.dtype:
+            raise ValueError("dlogits must have the logits' shape and type")
+        dld = _rows_of(dlogits, "dlogits")[2]
+    st = _on_device(stream, logits, tokens, lse, dlogp, entropy, dentropy, bias, dlogits)
+    if dlogits is None:
+        dlogits = _empty(stream, logits.shape, dtype=logits.dtype, device=logits.device)
+    check(load().tfk_token_logprobs_bwd(_ptr(logits), dt, n, c, ld, _ptr(bias), _ptr(tokens), float(temperature), _ptr(lse),
+                                        _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dlogits), dld, st))
+    return dlogits
+
+
+# ----------------------------------------------------------------------------- gated linear recurrence
+SCAN_BLOCK = 128       # tokens between two states that gated_scan_fwd saves
+
+
+def _seqs(t, name, cols=None) -> Tuple[int, int, int, int, int]:
+    """(b, t, columns, elements between sequences, between rows) of a b x t x columns tensor of either order."""
+    if t.dim() != 3:
+        raise ValueError("%s must be sequences x tokens x columns, got shape %s" % (name, tuple(t.shape)))
+    b, n, c = t.shape
+    if c == 0 or (cols is not None and c != cols):
+        raise ValueError("%s must have %s columns, got shape %s" % (name, cols or "some", tuple(t.shape)))
+    sb, st, sc = t.stride()
+    if b and n and c > 1 and sc != 1:
+        raise ValueError("%s must have unit stride within rows, got strides %s" % (name, t.stride()))
+    st = st if n > 1 else c
+    sb = sb if b > 1 else max(1, n) * st
+    if b and n and not ((st >= c and (b == 1 or sb >= (n - 1) * st + c)) or (sb >= c and st >= (b - 1) * sb + c)):
+        raise ValueError("%s must have rows that do not overlap, got shape %s, strides %s" % (name, tuple(t.shape), t.stride()))
+    return b, n, _width(c, name), sb, st
+
+
+def _scan_args(z, output_gate, bias, lengths):
+    gates = 3 if output_gate else 2
+    b, t, cols, zb, zt = _seqs(z, "z")
+    if cols % gates:
+        raise ValueError("z must have %d columns for each channel, got %d" % (gates, cols))
+    _vector(bias, torch.float32, cols, "bias")
+    _vector(lengths, torch.int32, b, "lengths")
+    return gates, b, t, cols // gates, zb, zt
+
+
+def _like_seqs(stream, z, cols):
+    """A dense b x t x cols tensor with z's order of sequences and tokens."""
+    b, t = z.shape[:2]
+    if b > 1 and t > 1 and z.stride(0) < z.stride(1):
+        return _empty(stream, (t, b, cols), dtype=z.dtype, device=z.device).transpose(0, 1)
+    return _empty(stream, (b, t, cols), dtype=z.dtype, device=z.device)
+
+
+def _states_of(h, b, d, name):
+    if h is not None and (h.dtype != torch.float32 or tuple(h.shape) != (b, d) or not h.is_contiguous()):
+        raise ValueError("%s must be a contiguous float32 tensor of %d x %d" % (name, b, d))
+
+
+def gated_scan_workspace_bytes(op, b, t, d) -> int:
+    """Workspace of gated_scan_fwd (op 0) or gated_scan_bwd (op 1)."""
+    return load().tfk_gated_scan_workspace_bytes(operator.index(op), operator.index(b), operator.index(t),
+                                                 _width(operator.index(d), "z"))
+
+
+_scan_need = functools.lru_cache(_KEPT)(gated_scan_workspace_bytes)
+
+
+def _scan_ws(op, b, t, d, ws, device, stream):
+    need = _scan_need(op, b, t, d)
+    if ws is not None and not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    if need and (ws is None or ws.numel() * ws.element_size() < need):
+        ws = _ws(need, device, stream)
+    return ws, need
+
+
+def gated_scan_fwd(z, output_gate=False, bias=None, h0=None, lengths=None, y=None, save=False, ws=None, stream=None):
+    """Gated linear recurrence over sequences: with x, a (and o, with output_gate) the column blocks of z + bias
+    (b x t x 2 d or 3 d; sequence or token first) and s the logistic function,
+    h_t = s(a_t) h_(t-1) + (1 - s(a_t)) x_t from h0 (b x d fp32, default 0), y_t = h_t or s(o_t) h_t.
+    lengths (int32): tokens of each sequence, the rest is padding (y is 0 there).
+    Returns (y, the last states, the saved states for gated_scan_bwd, or None without save)."""
+    gates, b, t, d, zb, zt = _scan_args(z, output_gate, bias, lengths)
+    _states_of(h0, b, d, "h0")
+    dt = _dt(z)
+    if y is not None and (tuple(y.shape) != (b, t, d) or y.dtype != z.dtype):
+        raise ValueError("y must be %s of z's type" % ((b, t, d),))
+    st = _on_device(stream, z, bias, h0, lengths, y, ws)
+    if y is None:
+        y = _like_seqs(stream, z, d)
+    _, _, _, yb, yt = _seqs(y, "y", d)
+    last = _empty(stream, (b, d), dtype=torch.float32, device=z.device)
+    states = None
+    if save:
+        states = _empty(stream, (b, (t + SCAN_BLOCK - 1) // SCAN_BLOCK, d), dtype=torch.float32, device=z.device)
+    ws, need = _scan_ws(0, b, t, d, ws, z.device, stream)
+    check(load().tfk_gated_scan_fwd(_ptr(z), dt, b, t, d, gates, zb, zt, _ptr(bias), _ptr(h0), _ptr(lengths), _ptr(y), yb, yt,
+                                    _ptr(last), _ptr(states), _ptr(ws), need, st))
+    return y, last, states
+
+
+def gated_scan_bwd(z, dy, states, output_gate=False, bias=None, lengths=None, dh_last=None, dz=None, ws=None, stream=None):
+    """Gradient of gated_scan_fwd for dy (of y) and dh_last (of the last states, default 0), with the states that
+    call saved.  dz may be z (in place).  Returns (dz, the gradient of h0); the bias's gradient is dz's
+    column sums (bias_relu_bwd without y)."""
+    gates, b, t, d, zb, zt = _scan_args(z, output_gate, bias, lengths)
+    dt = _dt(z)
+    if tuple(dy.shape) != (b, t, d) or dy.dtype != z.dtype:
+        raise ValueError("dy must be %s of z's type" % ((b, t, d),))
+    _, _, _, yb, yt = _seqs(dy, "dy", d)
+    _states_of(dh_last, b, d, "dh_last")
+    blocks = (t + SCAN_BLOCK - 1) // SCAN_BLOCK
+    if states.dtype != torch.float32 or tuple(states.shape) != (b, blocks, d) or not states.is_contiguous():
+        raise ValueError("states must be a contiguous float32 tensor of %d x %d x %d" % (b, blocks, d))
+    if dz is not None and (dz.shape != z.shape or dz.dtype != z.dtype):
+        raise ValueError("dz must have z's shape and type")
+    st = _on_device(stream, z, dy, states, bias, lengths, dh_last, dz, ws)
+    if dz is None:
+        dz = _like_seqs(stream, z, gates * d)
+    _, _, _, gb, gt = _seqs(dz, "dz")
+    dh0 = _empty(stream, (b, d), dtype=torch.float32, device=z.device)
+    ws, need = _scan_ws(1, b, t, d, ws, z.device, stream)
+    check(load().tfk_gated_scan_bwd(_ptr(z), dt, b, t, d, gates, zb, zt, _ptr(bias), _ptr(lengths), _ptr(dy), yb, yt,
+                                    _ptr(states), _ptr(dh_last), _ptr(dz), gb, gt, _ptr(dh0), _ptr(ws), need, st))
+    return dz, dh0
+
+
+def gated_scan_step(z, state, slots=None, output_gate=False, bias=None, y=None, stream=None):
+    """One token of each of n sequences: z (n x 2 d or 3 d) moves the states of their slots (int32, distinct; one
+    outside the states is none, and y's row 0; default row i has slot i) in state (slots x d fp32) in
+    place.  Returns y (n x d)."""
+    gates = 3 if output_gate else 2
+    if z.dim() != 2:
+        raise ValueError("z must be rows x columns, got shape %s" % (tuple(z.shape),))
+    n, cols, ld = _rows_of(z, "z")
+    if cols % gates:
+        raise ValueError("z must have %d columns for each channel, got %d" % (gates, cols))
+    d = cols // gates
+    if state.dim() != 2 or state.dtype != torch.float32 or state.shape[1] != d or not state.is_contiguous():
+        raise ValueError("state must be a contiguous float32 tensor of slots x %d" % d)
+    _vector(bias, torch.float32, cols, "bias")
+    _vector(slots, torch.int32, n, "slots")
+    dt = _dt(z)
+    yld = d
+    if y is not None:
+        if tuple(y.shape) != (n, d) or y.dtype != z.dtype:
+            raise ValueError("y must be %s of z's type" % ((n, d),))
+        yld = _rows_of(y, "y")[2]
+    st = _on_device(stream, z, state, slots, bias, y)
+    if y is None:
+        y = _empty(stream, (n, d), dtype=z.dtype, device=z.device)
+    check(load().tfk_gated_scan_step(_ptr(z), dt, n, d, gates, ld, _ptr(bias), _ptr(slots), _ptr(state), state.shape[0],
+                                     _ptr(y), yld, st))
+    return y
 
 
 # ----------------------------------------------------------------------------- streams and programs

@@ -114,8 +114,22 @@ class FullSoftmaxHead:
                                     alpha=alpha, weight=weight, bias=self.b, dlogits=z, stream=stream)
         return loss, self._apply(h, dz, stream)
 
-    def _apply(self, h: torch.Tensor, dz: torch.Tensor, stream):
-        """The gradients of h, W and b for the logits' gradient, and the update; returns dh."""
+    def score(self, h: torch.Tensor, tokens=None, k: int = 0, temperature: float = 1.0, stream=None):
+        """Log-probabilities of given tokens, entropy and the k largest classes of each row (ops.token_logprobs), and
+        the logits, which score_gradients needs."""
+        z = self._logits(h, stream).view(h.shape[0], self.vocab)
+        return ops.token_logprobs(z, tokens, k, temperature, self.b, stream=stream), z
+
+    def score_gradients(self, h: torch.Tensor, z: torch.Tensor, tokens, scores, dlogp, dentropy=None, temperature: float = 1.0,
+                        stream=None):
+        """The gradients (dh, dW, db) for the gradients dlogp and dentropy of score()'s results; the logits z are used
+        up (their gradient takes their place)."""
+        dz = ops.token_logprobs_bwd(z, tokens, scores.lse, dlogp, scores.entropy, dentropy, temperature, self.b, dlogits=z,
+                                    stream=stream)
+        return self._gradients(h, dz.view(h.shape[0], 1, 1, self.vocab), stream)
+
+    def _gradients(self, h: torch.Tensor, dz: torch.Tensor, stream):
+        """The gradients of h, W and b for the logits' gradient."""
         n, d = h.shape
         h4, w4 = h.view(n, 1, 1, d), self.W_lp.view(1, 1, d, self.vocab)
         _, db = ops.bias_relu_bwd(None, dz, dpre=dz, stream=stream)
@@ -123,6 +137,11 @@ class FullSoftmaxHead:
         ops.conv2d_bwd_filter(h4, dz, (1, 1), 1, (0, 0, 0, 0), dw=dw, stream=stream)
         dh = ops._empty_like(stream, h4)
         ops.conv2d_bwd_input(dz, w4, dh, 1, (0, 0, 0, 0), stream=stream)
+        return dh.view(n, d), dw.view(d, self.vocab), db
+
+    def _apply(self, h: torch.Tensor, dz: torch.Tensor, stream):
+        """The gradients of h, W and b for the logits' gradient, and the update; returns dh."""
+        dh, dw, db = self._gradients(h, dz, stream)
         ops.apply_sgd(self.W.view(-1), dw.view(-1), self.lr, shadow=self.W_lp.view(-1), stream=stream)
         ops.apply_sgd(self.b, db, self.lr, stream=stream)
-        return dh.view(n, d)
+        return dh

@@ -1,0 +1,327 @@
+"""Token log-probabilities, entropy, largest classes and their gradient on the GPU, against float64."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1605_08695_amd import ops
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F32, BF16 = torch.float32, torch.bfloat16
+U = 2.0 ** -24
+INF, NAN = float("inf"), float("nan")
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def half(dt):
+    return torch.finfo(dt).eps / 2
+
+
+def strided(v, extra):
+    if not extra:
+        return v.contiguous()
+    wide = torch.full((v.shape[0], v.shape[1] + extra), NAN, dtype=v.dtype, device=v.device)
+    wide[:, 1:1 + v.shape[1]] = v
+    return wide[:, 1:1 + v.shape[1]]
+
+
+def order(x):
+    """Classes of each row by x, largest first, then the lower class, in float64 on the host."""
+    v = x.double().cpu().numpy()
+    return np.stack([np.lexsort((np.arange(r.size), -r)) for r in v]) if v.size else np.zeros(v.shape, np.int64)
+
+
+# Bounds.  A term's exponent u = (x - m) / T has three roundings (difference, 1/T, product), the product with log2(e)
+# one more, and the exponential is good to its last place: (4 |u| + 4) U of the term.  Sums are of positive terms in
+# runs of up to c / 64 by one lane and then of 64 lanes and 16 waves, and follow the maximum, each rise of which costs
+# as one term's exponent over the whole range R of the row; so a sum is off by its terms' errors and (c / 64 + 100 +
+# 8 R) U of itself.  The logarithm is good to two last places.
+def reference(z, bias, tokens, T):
+    x32 = z.float() if bias is None else z.float() + bias
+    x = x32.double()
+    m = x.amax(1, keepdim=True)
+    u = (x - m) / T
+    p = torch.softmax(x / T, 1)
+    n, c = x.shape
+    fin = torch.where(p > 0, u, torch.zeros((), dtype=torch.float64, device=DEV))
+    R = fin.abs().amax(1).clamp(max=200.0)
+    run = (c / 64 + 100 + 8 * R) * U
+    ds = (p * (4 * fin.abs() + 4)).sum(1) * U + run
+    ls = torch.log(torch.exp(u).sum(1))
+    dls = ds + 4 * U * ls.abs() + 2 * U
+    lse = m[:, 0] / T + ls
+    dlse = dls + 4 * U * (m[:, 0] / T).abs() + 2 * U * lse.abs()
+    w = (p * fin.abs()).sum(1)
+    H = ls + w
+    dH = dls + (p * fin.abs() * (8 * fin.abs() + 8)).sum(1) * U + w * (run + ds + 6 * U) + 2 * U * H
+    logp = dlogp = None
+    if tokens is not None:
+        ut = u.gather(1, tokens.long()[:, None])[:, 0]
+        logp = ut - ls
+        dlogp = 4 * U * ut.abs() + dls + 2 * U * logp.abs()
+    return dict(x32=x32, u=u, p=p, ls=ls, lse=lse, dlse=dlse, H=H, dH=dH, logp=logp, dlogp=dlogp, dls=dls)
+
+
+def close(got, want, tol, what):
+    got = got.double()
+    both = torch.isinf(want) & (got == want)
+    off = torch.where(both, torch.zeros_like(want), (got - want).abs() - tol)
+    assert not off.isnan().any() and (off <= 1e-37).all(), (what, off.max().item())
+
+
+def check(z, bias, tokens, T, k):
+    r = ops.token_logprobs(z, tokens, k, T, bias)
+    torch.cuda.synchronize()
+    ref = reference(z, bias, None if tokens is None else tokens.clamp(min=0), T)
+    live = torch.ones(z.shape[0], dtype=torch.bool, device=DEV) if tokens is None else tokens >= 0
+    zero = torch.zeros((), dtype=torch.float64, device=DEV)
+    at = lambda v: torch.where(live, v, zero)  # noqa: E731
+    close(r.entropy, at(ref["H"]), at(ref["dH"]), "entropy")
+    close(r.lse, at(ref["lse"]), at(ref["dlse"]), "lse")
+    if tokens is None:
+        assert r.logp is None
+    else:
+        close(r.logp, at(ref["logp"]), at(ref["dlogp"]), "logp")
+    if k == 0:
+        assert r.top_idx is None and r.top_logp is None
+        return r, ref
+    want = torch.from_numpy(order(ref["x32"])[:, :k].copy()).to(DEV)
+    if want.shape[1] < k:
+        want = torch.cat([want, want.new_zeros(want.shape[0], k - want.shape[1])], 1)
+        there = torch.arange(k, device=DEV)[None, :] < z.shape[1]
+    else:
+        there = torch.ones(1, k, dtype=torch.bool, device=DEV)
+    there = there & (ref["x32"].gather(1, want) > -INF) & live[:, None]
+    assert torch.equal(r.top_idx.long(), torch.where(there, want, torch.full_like(want, -1)))
+    u = ref["u"].gather(1, want)
+    lp = torch.where(there, u - ref["ls"][:, None], torch.full((), -INF, dtype=torch.float64, device=DEV))
+    close(r.top_logp, lp, torch.where(there, 4 * U * u.abs() + ref["dls"][:, None] + 2 * U * lp.abs(), zero), "top_logp")
+    return r, ref
+
+
+def logits(n, c, dt, seed, scale=3.0):
+    rng = np.random.default_rng(seed)
+    return torch.from_numpy(rng.standard_normal((n, c)) * scale).to(dt).to(DEV)
+
+
+def toks(n, c, seed, pad=True):
+    t = np.random.default_rng(seed).integers(0, c, n).astype(np.int32)
+    if pad and n > 2:
+        t[2::7] = -1
+    return torch.from_numpy(t).to(DEV)
+
+
+CASES = [(1, 1, 1, 1.0, 0, True), (3, 2, 5, 0.7, 0, False), (5, 7, 7, 1.0, 1, True), (4, 63, 20, 2.0, 0, True),
+         (33, 1000, 5, 4.0, 0, True), (9, 1023, 128, 1.0, 3, False), (7, 2049, 1, 0.5, 0, True), (6, 4100, 100, 1.0, 8, True),
+         (3, 20011, 64, 1.3, 1, True), (2, 70001, 128, 1.0, 0, False), (2, 160000, 33, 0.9, 0, True), (1, 131072, 20, 0.8, 0, False),
+         (300, 40, 40, 1.0, 0, False), (2, 300001, 50, 1.0, 0, True)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("n,c,k,T,extra,bias", CASES)
+def test_scores(n, c, k, T, extra, bias, dt):
+    say("scores", n, c, k, T, extra, bias, dt)
+    z = strided(logits(n, c, dt, n + c), extra)
+    b = torch.from_numpy(np.random.default_rng(c).standard_normal(c)).float().to(DEV) if bias else None
+    tokens = toks(n, c, n)
+    r, _ = check(z, b, tokens, T, k)
+    # the same without tokens, and with no list: the same bits on the rows that are not padding
+    w, _ = check(z, b, None, T, 0)
+    live = tokens >= 0
+    assert torch.equal(w.entropy[live], r.entropy[live]) and torch.equal(w.lse[live], r.lse[live])
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("c", [1, 5, 300, 5000, 70001, 140000])
+@pytest.mark.parametrize("kind", ["equal", "rising", "falling", "few", "zeros", "last", "period", "one"])
+def test_largest_where_they_lie_badly(kind, c, dt):
+    say("largest", kind, c, dt)
+    rng = np.random.default_rng(c)
+    i = np.arange(c)
+    rows = {"equal": np.zeros(c), "rising": i / c * 20, "falling": -i / c * 20, "few": np.where(rng.random(c) < 0.01, 1.0, -1.0),
+            "zeros": np.where(i % 2 == 0, 0.0, -0.0), "last": np.where(i >= c - 40, 5.0 + i % 3, 0.0),
+            "period": np.where(i % 1024 // 8 == 5, 8.0 + rng.random(c), rng.random(c)),
+            "one": np.where(i < 600, 4.0 + rng.random(c), -3.0)}[kind]
+    z = torch.from_numpy(np.stack([rows, rows[::-1].copy(), np.roll(rows, 3)])).to(dt).to(DEV)
+    for k in (1, 17, 128):
+        check(z, None, None, 1.0, k)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("c", [9, 1000, 9000, 70000, 140001])
+def test_masks(c, dt):
+    """Classes ruled out by -inf or by numbers as low as the type has, rows with one class left and with none."""
+    say("masks", c, dt)
+    low = torch.finfo(dt).min
+    z = logits(8, c, dt, c)
+    keep = torch.from_numpy(np.random.default_rng(c).random((8, c)) < 0.3).to(DEV)
+    keep[:, 1] = True
+    for i, v in enumerate((-INF, -INF, -1e9, -1e30, low, low)):
+        z[i].masked_fill_(~keep[i], v)
+    z[1].fill_(-INF)
+    z[1, c - 1] = 2.5
+    z[5].fill_(low)
+    z[6].fill_(-1e9)
+    z[7].fill_(-INF)
+    tokens = torch.full((8,), 1, dtype=torch.int32, device=DEV)
+    k = 50
+    r = ops.token_logprobs(z, tokens, k, 1.0)
+    torch.cuda.synchronize()
+    part = [0, 2, 3, 4, 5, 6]
+    one = check(z[part].contiguous(), None, tokens[:6].contiguous(), 1.0, k)[0]
+    for a, b in zip(r, one):
+        assert torch.equal(a[part], b)
+    assert r.logp[1].item() == -INF and r.entropy[1].item() == 0 and abs(r.lse[1].item() - 2.5) <= 2 * U * 2.5
+    assert r.top_idx[1].tolist() == [c - 1] + [-1] * (k - 1) and r.top_logp[1, 0].item() == 0
+    assert r.logp[7].item() == -INF and r.entropy[7].item() == 0 and r.lse[7].item() == -INF
+    assert (r.top_idx[7] == -1).all() and (r.top_logp[7] == -INF).all()
+    d = ops.token_logprobs_bwd(z, tokens, r.lse, torch.ones(8, device=DEV), r.entropy, torch.ones(8, device=DEV))
+    torch.cuda.synchronize()
+    assert torch.isfinite(d[[0, 2, 3, 4, 5, 6, 7]]).all()
+    assert not d[7].any() and not d[0][~keep[0]].any()
+
+
+def test_nan_and_infinite_rows():
+    for c in (5, 3000, 70000, 140000):
+        z = logits(4, c, F32, c)
+        z[0, c - 2] = NAN
+        z[1, 3] = INF
+        z[2].fill_(NAN)
+        r = ops.token_logprobs(z, torch.zeros(4, dtype=torch.int32, device=DEV), 4)
+        torch.cuda.synchronize()
+        for v in (r.logp, r.entropy, r.lse, r.top_logp):
+            assert v[:3].isnan().all() and torch.isfinite(v[3]).all()
+        assert (r.top_idx[:3] == -1).all() and (r.top_idx[3] >= 0).all()
+
+
+def test_padding_is_not_read():
+    z = logits(4, 3000, BF16, 1)
+    tokens = torch.tensor([5, -1, 3000, 7], dtype=torch.int32, device=DEV)
+    want = ops.token_logprobs(z, tokens, 6)
+    wd = ops.token_logprobs_bwd(z, tokens, want.lse, torch.ones(4, device=DEV), want.entropy, torch.ones(4, device=DEV))
+    z[1:3] = NAN
+    nan = torch.tensor([1.0, NAN, NAN, 1.0], device=DEV)
+    got = ops.token_logprobs(z, tokens, 6)
+    gd = ops.token_logprobs_bwd(z, tokens, got.lse, nan, got.entropy, nan)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(gd, wd)
+    assert not gd[1:3].any() and not got.lse[1:3].any() and (got.top_idx[1:3] == -1).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("with_entropy", [False, True])
+@pytest.mark.parametrize("n,c,T,extra,bias", [(1, 1, 1.0, 0, True), (5, 7, 0.5, 1, False), (33, 1000, 2.0, 0, True),
+                                              (7, 2049, 1.0, 3, True), (3, 50021, 1.0, 0, True), (2, 160000, 1.3, 8, False)])
+def test_gradient(n, c, T, extra, bias, with_entropy, dt):
+    say("gradient", n, c, T, extra, bias, with_entropy, dt)
+    z = strided(logits(n, c, dt, c), extra)
+    b = torch.from_numpy(np.random.default_rng(c).standard_normal(c)).float().to(DEV) if bias else None
+    tokens = toks(n, c, n)
+    rng = np.random.default_rng(n)
+    a = torch.from_numpy(rng.standard_normal(n)).float().to(DEV)
+    e = torch.from_numpy(rng.standard_normal(n)).float().to(DEV) if with_entropy else None
+    r = ops.token_logprobs(z, tokens, 0, T, b)
+    d = ops.token_logprobs_bwd(z, tokens, r.lse, a, r.entropy, e, T, b)
+    torch.cuda.synchronize()
+    ref = reference(z, b, tokens.clamp(min=0), T)
+    live = (tokens >= 0)[:, None]
+    A, E = a.double()[:, None], (e.double()[:, None] if with_entropy else torch.zeros(n, 1, dtype=torch.float64, device=DEV))
+    lp = ref["u"] - ref["ls"][:, None]
+    one = torch.zeros(n, c, dtype=torch.float64, device=DEV).scatter_(1, tokens.clamp(min=0).long()[:, None], 1.0)
+    p, H = ref["p"], ref["H"][:, None]
+    want = (A * (one - p) - E * p * (lp + H)) / T
+    # log p = x / T - lse: roundings of numbers of the size of |x| / T and |lse|, and lse's own error; p is off by as
+    # much of itself and the exponential's last places
+    dlp = ref["dlse"][:, None] + 4 * U * ((ref["x32"].double() / T).abs() + ref["lse"][:, None].abs()) + 2 * U * lp.abs()
+    tol = (p * (dlp + (2 * lp.abs() + 8) * U) * (A.abs() + E.abs() * (lp + H).abs()) + E.abs() * p * (dlp + ref["dH"][:, None] +
+           4 * U * (lp.abs() + H)) + 6 * U * (A.abs() * (one + p) + E.abs() * p * (lp.abs() + H))) / T
+    want, tol = torch.where(live, want, torch.zeros_like(want)), torch.where(live, tol, torch.zeros_like(tol))
+    close(d, want, tol * (1 + half(dt)) + half(dt) * want.abs(), "gradient")
+    if extra == 0:
+        mine = z.clone()
+        assert torch.equal(ops.token_logprobs_bwd(mine, tokens, r.lse, a, r.entropy, e, T, b, dlogits=mine), d)
+    else:
+        room = strided(torch.zeros_like(d), extra)
+        assert torch.equal(ops.token_logprobs_bwd(z, tokens, r.lse, a, r.entropy, e, T, b, dlogits=room), d)
+        assert room._base.isnan().sum().item() == n * extra
+
+
+def test_gradient_against_differences():
+    n, c, T = 3, 50, 1.5
+    z = logits(n, c, F32, 1)
+    tokens = toks(n, c, 1, pad=False)
+    rng = np.random.default_rng(1)
+    a, e = (torch.from_numpy(rng.standard_normal(n)).float().to(DEV) for _ in range(2))
+    r = ops.token_logprobs(z, tokens, 0, T)
+    d = ops.token_logprobs_bwd(z, tokens, r.lse, a, r.entropy, e, T).double()
+    torch.cuda.synchronize()
+
+    def loss(x):
+        lp = torch.log_softmax(x / T, 1)
+        return (a.double() * lp.gather(1, tokens.long()[:, None])[:, 0]).sum() - (e.double() * (lp.exp() * lp).sum(1)).sum()
+
+    for _ in range(3):
+        v = torch.from_numpy(rng.standard_normal((n, c))).to(DEV)
+        h = 1e-4
+        diff = (loss(z.double() + h * v) - loss(z.double() - h * v)) / (2 * h)
+        wide = (loss(z.double() + 2 * h * v) - loss(z.double() - 2 * h * v)) / (4 * h)
+        # each gradient is good to some 200 roundings of numbers below 10
+        tol = (200 * U * 10 * v.abs()).sum() / T + abs(wide - diff) + 1e-7
+        assert abs((d * v).sum() - diff) <= tol
+
+
+def test_offsets_past_32_bits():
+    n, c = 40000, 60000
+    z = torch.zeros(n, c, dtype=BF16, device=DEV)
+    z[-1, -1] = 9.0
+    z[-1, 17] = 9.0
+    tokens = torch.full((n,), -1, dtype=torch.int32, device=DEV)
+    tokens[-1] = c - 1
+    tokens[0] = 3
+    r = ops.token_logprobs(z, tokens, 2)
+    assert r.top_idx[-1].tolist() == [17, c - 1] and r.top_idx[0].tolist() == [0, 1]
+    small = ops.token_logprobs(z[-1:].contiguous(), tokens[-1:].contiguous(), 2)
+    assert all(torch.equal(a[-1:], b) for a, b in zip(r, small))
+    want = ops.token_logprobs_bwd(z[-1:].clone(), tokens[-1:].contiguous(), small.lse, torch.ones(1, device=DEV))
+    d = ops.token_logprobs_bwd(z, tokens, r.lse, torch.ones(n, device=DEV), dlogits=z)
+    torch.cuda.synchronize()
+    assert torch.equal(d[-1:], want) and not d[1].any()
+
+
+def test_a_teacher_for_distillation():
+    """The list and distill_xent agree: a student that is its own teacher has no loss, and its gradient vanishes."""
+    z = logits(16, 3000, F32, 2)
+    r = ops.token_logprobs(z, k=64)
+    loss, dz = ops.distill_xent(z, r.top_idx, r.top_logp, 1.0, top_lse=torch.zeros(16, device=DEV))
+    torch.cuda.synchronize()
+    # both sides' log-probabilities are off by some 200 roundings each
+    assert loss.abs().max().item() < 400 * U * 10 and dz.abs().max().item() < 400 * U
+
+
+def test_two_streams_and_a_captured_graph():
+    zs = [logits(40, 30000, BF16, s) for s in (1, 2)]
+    tokens = toks(40, 30000, 1)
+    g = torch.randn(40, device=DEV)
+
+    def both(z, stream=None):
+        r = ops.token_logprobs(z, tokens, 20, stream=stream)
+        return tuple(r) + (ops.token_logprobs_bwd(z, tokens, r.lse, g, r.entropy, g, stream=stream),)
+
+    want = [both(z) for z in zs]
+    torch.cuda.synchronize()
+    got = [both(z, torch.cuda.Stream()) for z in zs]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+    z = zs[0].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both(z)
+    for k in range(4):
+        z.copy_(zs[k % 2])
+        graph.replay()
+        both(zs[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[k % 2]))
