@@ -4,18 +4,29 @@
 // With x = logits + bias, m = max x, u = (x - m) / T, s = sum e^u, W = sum u e^u:
 //   lse = m / T + log s     logp = u_token - log s     entropy = log s - W / s
 //   dx_j = (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)) / T,   p_j = e^(x_j / T - lse)
-// A class of -inf has p = 0 and no term.  The sums run with the maximum seen so far: where it rises by D, W
-// becomes (W - D s) e^-D.  The largest classes are ordered by x, then by the lower class.
+// A class of -inf has p = 0 and no term.  Exponentials are powers of two of exact differences, so that a row of
+// masks alone (-1e9, -1e30, the type's lowest value) is a row like any other.  The largest classes are ordered by x,
+// then by the lower class.
+//
+// A workgroup has a row and reads it once.  A lane's sums are relative to a value of its own, which it raises
+// only when one passes it by 2^kSlack: rescaling costs an exponential, and without the slack nearly every step
+// of a wave has a lane with a new maximum.  Each lane keeps the largest x it saw.  The k-th largest of these, tau, is
+// at most the row's k-th largest, so the classes on the list are in the few lanes whose largest is at least tau, and
+// only what those lanes read is read again (by whole waves, from the caches) to find the candidates, which then
+// count how many are before them.
 #include "common.h"
 #include "kernels.h"
+#include "rowvec.h"
 
 #pragma clang fp contract(off)
 
 namespace tfk {
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kSlack = 32.f, kFar = 1e4f;      // in powers of two
+constexpr int kCands = 1024;                     // candidates for the list in LDS
 
-__device__ __forceinline__ float exp_of(float u) { return __builtin_amdgcn_exp2f(u * kLog2e); }
+__device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // x's order as an unsigned number (+0 and -0 alike), 0 for -inf and below every finite x's.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -25,128 +36,427 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
-// Maximum, sum and weighted sum of a part of a row.
+typedef unsigned long long u64;
+__device__ __forceinline__ u64 key_of(uint32_t order, int j) { return (u64)order << 32 | (uint32_t)~j; }
+
+__device__ __forceinline__ float wave_maxf(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+__device__ __forceinline__ float wave_sumf(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// A lane's part of a row: sums relative to ref, and its largest x.
 struct Part {
-    float m, s, W;
-    // Terms further than 200 below the maximum are 0, and so is their share of W.
-    __device__ void add(float x, float invT) {
-        if (x > m) {
-            const float D = m == -INFINITY ? 0.f : (x - m) * invT, r = m == -INFINITY ? 0.f : exp_of(-D);
-            W = (W - fminf(D, 200.f) * s) * r;
-            s *= r;
-            m = x;
-        }
-        const float u = m == -INFINITY ? x : (x - m) * invT;
-        const float e = exp_of(u);
-        s += e;
-        W = __builtin_fmaf(u < -200.f ? 0.f : u, e, W);
+    float ref, s, W, top;
+    __device__ __forceinline__ void raise(float x, float ct) {
+        const float D = fminf((x - ref) * ct, kFar), r = ex2(-D);
+        W = (W - D * s) * r;
+        s *= r;
+        ref = x;
     }
-    __device__ void join(const Part &o, float invT) {
-        const float M = fmaxf(m, o.m);
-        const float D = m == -INFINITY ? 0.f : (M - m) * invT, E = o.m == -INFINITY ? 0.f : (M - o.m) * invT;
-        const float r = exp_of(-D), t = exp_of(-E);
-        W = (W - fminf(D, 200.f) * s) * r + (o.W - fminf(E, 200.f) * o.s) * t;
-        s = s * r + o.s * t;
-        m = M;
+    template <int V>
+    __device__ __forceinline__ void add(const float *x, float ct) {
+        float t = x[0];
+#pragma unroll
+        for (int e = 1; e < V; ++e) t = fmaxf(t, x[e]);
+        top = fmaxf(top, t);
+        if ((t - ref) * ct > kSlack) raise(t, ct);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float u = (x[e] - ref) * ct, p = ex2(u);
+            s += p;
+            W = __builtin_fmaf(p, fmaxf(u, -kFar), W);      // (p is 0 where the bound is reached)
+        }
+    }
+};
+
+// 16 bytes of a row and the bias beside them.
+template <typename T>
+struct Piece {
+    static constexpr int V = Elem<T>::kPerChunk;
+    typename RowVec<T, V>::raw z;
+    typename RowVec<float, V>::raw b;
+    __device__ __forceinline__ void load(const T *zp, const float *bias, int j) {
+        z = RowVec<T, V>::load(zp + j);
+        if (bias) b = RowVec<float, V>::load(bias + j);
+    }
+    __device__ __forceinline__ void values(const float *bias, float *x) const {
+        RowVec<T, V>::unpack(z, x);
+        if (bias) {
+            float y[V];
+            RowVec<float, V>::unpack(b, y);
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] += y[e];
+        }
     }
 };
 
 template <typename T>
-__global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a) {
-    __shared__ Part parts[4];
-    __shared__ unsigned long long best[4];
+__device__ __forceinline__ float logit(const T *z, const float *bias, int j) {
+    return Elem<T>::load(z + j) + (bias ? bias[j] : 0.f);
+}
+
+// All of the workgroup's NT lanes' parts of a row of c classes: pieces lane, lane + NT ..., and single classes behind
+// the last whole piece.
+template <typename T, int NT>
+__device__ __forceinline__ Part read_row(const T *z, const float *bias, int c, float ct) {
+    constexpr int V = Piece<T>::V, U = 4;
+    Part p{-__FLT_MAX__, 0.f, 0.f, -INFINITY};
+    const int n = c / V;
+    int q = threadIdx.x;
+    for (; q + (U - 1) * NT < n; q += U * NT) {
+        Piece<T> b[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) b[i].load(z, bias, (q + i * NT) * V);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            float x[V];
+            b[i].values(bias, x);
+            p.template add<V>(x, ct);
+        }
+    }
+    for (; q < n; q += NT) {
+        Piece<T> b;
+        b.load(z, bias, q * V);
+        float x[V];
+        b.values(bias, x);
+        p.template add<V>(x, ct);
+    }
+    if (threadIdx.x < c - n * V) {
+        const float x = logit(z, bias, n * V + threadIdx.x);
+        p.template add<1>(&x, ct);
+    }
+    return p;
+}
+
+template <int NT>
+struct RowStats {
+    float top[NT / 64], s[NT / 64], W[NT / 64];
+};
+
+// The row's maximum m, sum s and weighted sum W (in powers of two) relative to it, in all lanes, from the lanes' parts.
+template <int NT>
+__device__ __forceinline__ void join_row(const Part &p, float ct, RowStats<NT> &sh, float &m, float &s, float &W) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const float wm = wave_maxf(p.top);
+    if (lane == 0) sh.top[w] = wm;
+    __syncthreads();
+    m = sh.top[0];
+#pragma unroll
+    for (int v = 1; v < NT / 64; ++v) m = fmaxf(m, sh.top[v]);
+    // ref is at most kSlack below m's part of the lane, or far below it, or, without a class yet, the lowest number
+    const float D = m == -INFINITY ? 0.f : fminf((m - p.ref) * ct, kFar), r = ex2(-D);
+    s = wave_sumf(p.s * r);
+    W = wave_sumf((p.W - D * p.s) * r);
+    if (lane == 0) {
+        sh.s[w] = s;
+        sh.W[w] = W;
+    }
+    __syncthreads();
+    s = sh.s[0];
+    W = sh.W[0];
+#pragma unroll
+    for (int v = 1; v < NT / 64; ++v) {
+        s += sh.s[v];
+        W += sh.W[v];
+    }
+}
+
+// The largest number that at least k of the NT orders are not below (0: fewer than k are above 0), by one wave, from its
+// highest bit down; at most as many as k stop the search.
+template <int NT>
+__device__ __forceinline__ uint32_t kth_of(const uint32_t *orders, int k) {
+    uint32_t mine[NT / 64], t = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) mine[i] = orders[i * 64 + (threadIdx.x & 63)];
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t trial = t | 1u << bit;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) n += __popcll(__ballot(mine[i] >= trial));
+        if (n >= k) t = trial;
+        if (n == k) break;
+    }
+    return t;
+}
+
+template <int NT>
+struct ListShared {
+    uint32_t orders[NT];       // of each lane's largest class
+    int hot[128 + NT];         // lanes whose largest is on the list, at most k, or more of equal ones
+    uint32_t tau;
+    int nhot, n, above;
+    int counts[NT / 64];
+    u64 best[NT / 64];
+    u64 cand[kCands];
+};
+
+// Classes of the row whose order is at least tau (above tau alone: least = tau + 1) into sh.cand; sh.n counts them all.
+template <typename T, int NT>
+__device__ __forceinline__ void collect(const T *z, const float *bias, int c, ListShared<NT> &sh, uint32_t least) {
+    constexpr int V = Piece<T>::V;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = c / V;
+    for (int h = w; h < sh.nhot; h += NT / 64) {
+        const int at = sh.hot[h];
+        for (int q = at + lane * NT; q < n; q += 64 * NT) {
+            Piece<T> b;
+            b.load(z, bias, q * V);
+            float x[V];
+            b.values(bias, x);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const uint32_t o = order_of(x[e]);
+                if (o >= least) {
+                    const int i = atomicAdd(&sh.n, 1);
+                    if (i < kCands) sh.cand[i] = key_of(o, q * V + e);
+                }
+            }
+        }
+        if (lane == 0 && at < c - n * V) {
+            const uint32_t o = order_of(logit(z, bias, n * V + at));
+            if (o >= least) {
+                const int i = atomicAdd(&sh.n, 1);
+                if (i < kCands) sh.cand[i] = key_of(o, n * V + at);
+            }
+        }
+    }
+}
+
+// The first `want` classes of the row whose order is tau, in the row's order, behind the n candidates in sh.cand.
+template <typename T, int NT>
+__device__ __forceinline__ void first_equal(const T *z, const float *bias, int c, ListShared<NT> &sh, int n, int want) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (int base = 0; base < c && want > 0; base += NT) {
+        const int j = base + threadIdx.x;
+        const bool eq = j < c && order_of(logit(z, bias, j)) == sh.tau;
+        const u64 all = __ballot(eq);
+        __syncthreads();
+        if (lane == 0) sh.counts[w] = __popcll(all);
+        __syncthreads();
+        int before = 0, total = 0;
+#pragma unroll
+        for (int v = 0; v < NT / 64; ++v) {
+            before += v < w ? sh.counts[v] : 0;
+            total += sh.counts[v];
+        }
+        before += __popcll(all & ((1ull << lane) - 1));
+        if (eq && before < want) sh.cand[n + before] = key_of(sh.tau, j);
+        n += min(total, want);
+        want -= total;
+    }
+}
+
+// The row's largest class below key `last`, by all lanes.
+template <typename T, int NT>
+__device__ __forceinline__ u64 next_below(const T *z, const float *bias, int c, ListShared<NT> &sh, u64 last) {
+    u64 mine = 0;
+    for (int j = threadIdx.x; j < c; j += NT) {
+        const u64 key = key_of(order_of(logit(z, bias, j)), j);
+        if (key < last && key > mine) mine = key;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const u64 other = __shfl_xor(mine, o, 64);
+        mine = other > mine ? other : mine;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.best[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    for (int v = 0; v < NT / 64; ++v) mine = sh.best[v] > mine ? sh.best[v] : mine;
+    return mine;
+}
+
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
+    __shared__ RowStats<NT> st;
+    __shared__ ListShared<NT> sh;
     const int64_t r = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (r >= a.n) return;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const float invT = 1.f / a.temperature;
+    const float invT = 1.f / a.temperature, ct = kLog2e / a.temperature;
     const int token = a.tokens ? a.tokens[r] : 0;
-    if (a.tokens && (token < 0 || token >= a.c)) {       // padding: the logits are not looked at
+    int32_t *const out_idx = a.top_idx + r * a.k;
+    float *const out_logp = a.top_logp + r * a.k;
+    if (token < 0 || token >= a.c) {                 // padding: the logits are not looked at
         if (threadIdx.x == 0) {
             if (a.logp) a.logp[r] = 0.f;
             if (a.entropy) a.entropy[r] = 0.f;
             if (a.lse) a.lse[r] = 0.f;
         }
-        for (int q = threadIdx.x; q < a.k; q += 256) {
-            a.top_idx[r * a.k + q] = -1;
-            a.top_logp[r * a.k + q] = -INFINITY;
+        for (int q = threadIdx.x; q < a.k; q += NT) {
+            out_idx[q] = -1;
+            out_logp[q] = -INFINITY;
         }
         return;
     }
     const T *const z = (const T *)a.z + r * a.zld;
-    Part p{-INFINITY, 0.f, 0.f};
-    for (int j = threadIdx.x; j < a.c; j += 256) p.add(Elem<T>::load(z + j) + (a.bias ? a.bias[j] : 0.f), invT);
-    for (int o = 32; o > 0; o >>= 1) p.join(Part{__shfl_xor(p.m, o), __shfl_xor(p.s, o), __shfl_xor(p.W, o)}, invT);
-    if (lane == 0) parts[w] = p;
-    __syncthreads();
-    p = parts[0];
-    for (int v = 1; v < 4; ++v) p.join(parts[v], invT);
-    const bool empty = p.m == -INFINITY && p.s == 0.f, nan = !(p.s < INFINITY);
-    const float ls = __builtin_amdgcn_logf(p.s) * kLn2;
-    if (threadIdx.x == 0) {
-        if (a.logp) {
-            const float x = Elem<T>::load(z + token) + (a.bias ? a.bias[token] : 0.f);
-            a.logp[r] = empty ? -INFINITY : nan ? NAN : (x - p.m) * invT - ls;
-        }
-        if (a.entropy) a.entropy[r] = empty ? 0.f : nan ? NAN : fmaxf(ls - p.W / p.s, 0.f);
-        if (a.lse) a.lse[r] = empty ? -INFINITY : nan ? NAN : p.m * invT + ls;
+    const float xt = logit(z, a.bias, token);
+    const Part p = read_row<T, NT>(z, a.bias, a.c, ct);
+    const uint32_t mine = order_of(p.top);
+    if (a.k > 0) {
+        sh.orders[threadIdx.x] = mine;
+        if (threadIdx.x == 0) sh.nhot = sh.n = 0;
     }
-    unsigned long long last = ~0ull;
-    for (int q = 0; q < a.k; ++q) {
-        unsigned long long mine = 0;
-        if (!nan && !empty && last != 0)
-            for (int j = threadIdx.x; j < a.c; j += 256) {
-                const unsigned long long key =
-                    (unsigned long long)order_of(Elem<T>::load(z + j) + (a.bias ? a.bias[j] : 0.f)) << 32 | (uint32_t)~j;
-                if (key < last && key > mine) mine = key;
+    float m, s, W;
+    join_row<NT>(p, ct, st, m, s, W);
+    const bool empty = m == -INFINITY && s == 0.f, nan = !(s < INFINITY);
+    const float ls = __builtin_amdgcn_logf(s) * kLn2;
+    if (threadIdx.x == 0) {
+        if (a.logp) a.logp[r] = empty ? -INFINITY : nan ? NAN : (xt - m) * invT - ls;
+        if (a.entropy) a.entropy[r] = empty ? 0.f : nan ? NAN : fmaxf(ls - W / s * kLn2, 0.f);
+        if (a.lse) a.lse[r] = empty ? -INFINITY : nan ? NAN : m * invT + ls;
+    }
+    if (a.k == 0) return;
+    if (empty || nan) {
+        for (int q = threadIdx.x; q < a.k; q += NT) {
+            out_idx[q] = -1;
+            out_logp[q] = nan ? NAN : -INFINITY;
+        }
+        return;
+    }
+    if (w == 0) {
+        const uint32_t t = kth_of<NT>(sh.orders, a.k);
+        if (lane == 0) sh.tau = max(t, 1u);
+    }
+    __syncthreads();
+    if (mine >= sh.tau) sh.hot[atomicAdd(&sh.nhot, 1)] = threadIdx.x;
+    __syncthreads();
+    collect<T, NT>(z, a.bias, a.c, sh, sh.tau);
+    __syncthreads();
+    int n = sh.n;
+    if (n > kCands) {
+        // many classes of the same x (masks of a finite number): those above it, then the first of the equal ones
+        __syncthreads();
+        if (threadIdx.x == 0) sh.n = 0;
+        __syncthreads();
+        collect<T, NT>(z, a.bias, a.c, sh, sh.tau + 1);
+        __syncthreads();
+        n = sh.n;
+        if (n <= kCands - 128) {
+            const int want = max(a.k - n, 0);
+            first_equal<T, NT>(z, a.bias, a.c, sh, n, want);
+            n += want;
+            __syncthreads();
+        }
+    }
+    if (n <= kCands) {
+        for (int i = threadIdx.x; i < n; i += NT) {
+            const u64 key = sh.cand[i];
+            int rank = 0;
+            for (int q = 0; q < n; ++q) rank += sh.cand[q] > key;
+            if (rank < a.k) {
+                out_idx[rank] = (int32_t)~(uint32_t)key;
+                out_logp[rank] = (value_of((uint32_t)(key >> 32)) - m) * invT - ls;
             }
-        for (int o = 32; o > 0; o >>= 1) {
-            const unsigned long long other = __shfl_xor(mine, o);
-            mine = other > mine ? other : mine;
         }
-        __syncthreads();
-        if (lane == 0) best[w] = mine;
-        __syncthreads();
-        for (int v = 0; v < 4; ++v) mine = best[v] > mine ? best[v] : mine;
-        if ((mine >> 32) == 0) mine = 0;             // nothing but -inf is left
+        for (int q = n + threadIdx.x; q < a.k; q += NT) {
+            out_idx[q] = -1;
+            out_logp[q] = -INFINITY;
+        }
+        return;
+    }
+    // the largest classes crowd in few lanes: one after the other, each by a reading of the row
+    u64 last = ~0ull;
+    for (int q = 0; q < a.k; ++q) {
+        if (last != 0) last = next_below<T, NT>(z, a.bias, a.c, sh, last);
+        if ((last >> 32) == 0) last = 0;             // nothing but -inf is left
         if (threadIdx.x == 0) {
-            a.top_idx[r * a.k + q] = mine ? (int32_t)~(uint32_t)mine : -1;
-            a.top_logp[r * a.k + q] = nan ? NAN : mine ? (value_of((uint32_t)(mine >> 32)) - p.m) * invT - ls : -INFINITY;
+            out_idx[q] = last ? (int32_t)~(uint32_t)last : -1;
+            out_logp[q] = last ? (value_of((uint32_t)(last >> 32)) - m) * invT - ls : -INFINITY;
         }
-        last = mine;
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobBwdArgs a) {
-    const int64_t r = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
+// The gradient.  Where lse is so large that fp32 no longer tells x / T from it (a row of masks alone), its maximum
+// and sum are formed again from the row.
+constexpr float kFarLse = 128.f;
+
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int parts, int part_len) {
+    constexpr int V = Piece<T>::V, U = 4;
+    __shared__ RowStats<NT> st;
+    const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x, r = job / parts;
     if (r >= a.n) return;
+    const int j0 = (int)(job - r * parts) * part_len, j1 = min(a.c, j0 + part_len);
     const T *const z = (const T *)a.z + r * a.zld;
     T *const dz = (T *)a.dz + r * a.dld;
     const int token = a.tokens[r];
     const float lse = a.lse[r];
     const bool none = token < 0 || token >= a.c || lse == -INFINITY;
-    const float invT = 1.f / a.temperature, dl = a.dlogp[r] * invT, de = a.dentropy ? a.dentropy[r] * invT : 0.f;
-    const float H = a.dentropy ? a.entropy[r] : 0.f;
-    for (int j = threadIdx.x; j < a.c; j += 256) {
-        float g = 0.f;
-        if (!none) {
-            const float lp = (Elem<T>::load(z + j) + (a.bias ? a.bias[j] : 0.f)) * invT - lse;
-            const float p = exp_of(lp);
-            g = -p * (dl + de * ((lp < -200.f ? -200.f : lp) + H)) + (j == token ? dl : 0.f);
-        }
-        Elem<T>::store(dz + j, g);
+    const float invT = 1.f / a.temperature, ct = kLog2e / a.temperature;
+    const float dl = none ? 0.f : a.dlogp[r] * invT, de = none || !a.dentropy ? 0.f : a.dentropy[r] * invT;
+    const float H = none || !a.dentropy ? 0.f : a.entropy[r];
+    // log p = (x - m) / T - ls
+    float m = 0.f, ls = lse;
+    if (!none && __builtin_fabsf(lse) > kFarLse && __builtin_fabsf(lse) < INFINITY) {
+        float s, W;
+        join_row<NT>(read_row<T, NT>(z, a.bias, a.c, ct), ct, st, m, s, W);
+        ls = __builtin_amdgcn_logf(s) * kLn2;
     }
+    const float base = dl + de * H;
+    const auto grad = [&](float x) {
+        const float lp = (x - m) * invT - ls, p = ex2(lp * kLog2e);
+        return -p * __builtin_fmaf(de, fmaxf(lp, -kFar), base);
+    };
+    const int n = (j1 - j0) / V;
+    for (int q = threadIdx.x; q < n; q += U * NT) {
+        Piece<T> b[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (!none && q + i * NT < n) b[i].load(z, a.bias, j0 + (q + i * NT) * V);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int j = j0 + (q + i * NT) * V;
+            if (q + i * NT >= n) break;
+            float x[V];
+            if (none) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) x[e] = 0.f;
+            } else {
+                b[i].values(a.bias, x);
+#pragma unroll
+                for (int e = 0; e < V; ++e) x[e] = grad(x[e]);
+                if ((unsigned)(token - j) < (unsigned)V) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) x[e] += token == j + e ? dl : 0.f;
+                }
+            }
+            RowVec<T, V>::store(dz + j, x);
+        }
+    }
+    const int j = j0 + n * V + threadIdx.x;
+    if (j < j1) Elem<T>::store(dz + j, none ? 0.f : grad(logit(z, a.bias, j)) + (j == token ? dl : 0.f));
+}
+
+template <typename T>
+static void launch_rows(const LogprobArgs &a, hipStream_t st) {
+    if (a.c <= kCands) hipLaunchKernelGGL((logprob_kernel<T, 64>), grid_2d(a.n), dim3(64), 0, st, a);
+    else if (a.n > 256 || a.c <= 16384) hipLaunchKernelGGL((logprob_kernel<T, 256>), grid_2d(a.n), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((logprob_kernel<T, 1024>), grid_2d(a.n), dim3(1024), 0, st, a);
 }
 
 hipError_t launch_logprob(int dt, const LogprobArgs &a, hipStream_t st) {
-    if (dt == 0) hipLaunchKernelGGL(logprob_kernel<float>, grid_2d(a.n), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(logprob_kernel<bf16_t>, grid_2d(a.n), dim3(256), 0, st, a);
+    if (dt == 0) launch_rows<float>(a, st);
+    else launch_rows<bf16_t>(a, st);
     return hipGetLastError();
 }
 
+template <typename T>
+static void launch_bwd_rows(const LogprobBwdArgs &a, hipStream_t st) {
+    // parts of a row read the whole of it where lse is far out: in place a row is one workgroup's
+    const int len = a.dz == a.z ? a.c : 256 * 4 * 16 / (int)sizeof(T), parts = (a.c + len - 1) / len;
+    if (a.c <= 1024) hipLaunchKernelGGL((logprob_bwd_kernel<T, 64>), grid_2d(a.n), dim3(64), 0, st, a, 1, a.c);
+    else hipLaunchKernelGGL((logprob_bwd_kernel<T, 256>), grid_2d(a.n * parts), dim3(256), 0, st, a, parts, len);
+}
+
 hipError_t launch_logprob_bwd(int dt, const LogprobBwdArgs &a, hipStream_t st) {
-    if (dt == 0) hipLaunchKernelGGL(logprob_bwd_kernel<float>, grid_2d(a.n), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(logprob_bwd_kernel<bf16_t>, grid_2d(a.n), dim3(256), 0, st, a);
+    if (dt == 0) launch_bwd_rows<float>(a, st);
+    else launch_bwd_rows<bf16_t>(a, st);
     return hipGetLastError();
 }
 
