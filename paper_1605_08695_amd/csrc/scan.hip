@@ -11,9 +11,12 @@
 // and P = prod f, kept as 1 - P or P, whichever is smaller, in the same way.  Backwards, a span maps what comes from
 // behind, c, to R + P c.
 //
-// A workgroup has a strip of channels of one sequence, each wave a run of kSteps tokens of it in registers; the
-// waves' spans are joined through LDS, and the workgroup goes on to the next kWaves * kSteps tokens with the
-// state they leave.  Bound by HBM: z is read once and y written once; the backward pass reads z and dy and
+// A workgroup has a strip of 64 channels of one sequence and takes it in blocks of kScanBlock tokens, each wave (or half
+// wave, with two bf16 channels a lane) a run of kSteps tokens of the block in registers; the waves' spans are joined
+// through LDS, and the workgroup goes on to the next block with the state they leave.  Where there are too few strips
+// for the chip, the time axis is cut into segments: a first launch reads all segments but the last for what each makes
+// of the state before it (x and the gate; backwards the gate and dy), and in the second each workgroup joins those of the
+// segments before its own.  Bound by HBM: z is read once and y written once; the backward pass reads z and dy and
 // writes dz, with the states of each kScanBlock-th token from the forward pass.
 #include "common.h"
 #include "kernels.h"
@@ -23,8 +26,9 @@
 namespace tfk {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kSteps = 16;                         // tokens a wave has in registers
-constexpr int kWaves = kScanBlock / kSteps;        // waves of a workgroup
+constexpr int kWaves = 4;                          // waves of a workgroup
+constexpr int kStrip = 64;                         // channels of a workgroup
+constexpr int kSegments = 64;                      // the most a sequence is cut into
 
 // The smaller share of a gate, with the sign of its argument.
 __device__ __forceinline__ float gate(float a) {
@@ -50,142 +54,424 @@ __device__ __forceinline__ int span_of(const int32_t *lengths, int64_t b, int t)
     return lengths == nullptr ? t : min(max(lengths[b], 0), t);
 }
 
-template <typename T, bool OUT>
-__global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanArgs a) {
-    __shared__ float2 spans[2][kWaves][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int strips = (a.d + 63) / 64;
-    const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x, b = job / strips;
-    if (b >= a.b) return;
-    const int c = (int)(job - b * strips) * 64 + lane;
-    const bool live = c < a.d;
-    const int cc = live ? c : a.d - 1;
-    const int len = span_of(a.lengths, b, a.t);
-    const float bx = a.bias ? a.bias[cc] : 0.f, bf = a.bias ? a.bias[a.d + cc] : 0.f;
-    const float bo = OUT && a.bias ? a.bias[2 * a.d + cc] : 0.f;
-    const T *const z = (const T *)a.z + b * a.z_bs + cc;
-    T *const y = (T *)a.y + b * a.y_bs + cc;
-    const int blocks = (a.t + kScanBlock - 1) / kScanBlock;
-    float H = a.h0 ? a.h0[b * a.d + cc] : 0.f;
-    for (int blk = 0; blk < blocks; ++blk) {
-        const int t0 = blk * kScanBlock + w * kSteps;
-        if (blk * kScanBlock >= len) {             // padding from here on
-            for (int i = 0; i < kSteps; ++i)
-                if (live && t0 + i < a.t) Elem<T>::store(y + (t0 + i) * a.y_ts, 0.f);
-            continue;
-        }
-        float s[kSteps], x[kSteps], o[OUT ? kSteps : 1];
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const bool in = t0 + i < len;
-            const T *const p = z + (in ? t0 + i : 0) * a.z_ts;
-            x[i] = Elem<T>::load(p) + bx;
-            s[i] = gate(Elem<T>::load(p + a.d) + bf);
-            if (OUT) o[i] = keeps(gate(Elem<T>::load(p + 2 * a.d) + bo));
-            if (!in) s[i] = x[i] = 0.f;            // a state stays as it is
-        }
-        float S = 0.f, Q = 0.f, P = 1.f;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            S = move(S, s[i], x[i]);
-            Q = move(Q, s[i], 1.f);
-            P = kept(P, s[i]);
-        }
-        spans[blk & 1][w][lane] = make_float2(S, span(Q, P));
-        __syncthreads();
-        float h = H;
-        for (int v = 0; v < kWaves; ++v) {
-            if (v == w) h = H;
-            const float2 m = spans[blk & 1][v][lane];
-            H = join(H, m.y, m.x);
-        }
-        if (a.states && w == 0 && live) a.states[((int64_t)b * blocks + blk) * a.d + c] = h;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            h = move(h, s[i], x[i]);
-            if (live && t0 + i < a.t) Elem<T>::store(y + (t0 + i) * a.y_ts, t0 + i < len ? (OUT ? o[i] * h : h) : 0.f);
-        }
+// V neighbouring channels of a row of d (V <= d) from channel c on.  The last lanes of a row of an odd number of channels
+// read the pair that ends with it.
+template <typename T, int V>
+struct Chans;
+template <typename T>
+struct Chans<T, 1> {
+    typedef T raw;
+    int at, live;
+    __device__ __forceinline__ Chans(int c, int d) : at(min(c, d - 1)), live(c < d) {}
+    __device__ __forceinline__ raw load(const T *p) const { return p[at]; }
+    __device__ __forceinline__ void unpack(raw r, float *v) const { v[0] = Elem<T>::load(&r); }
+    __device__ __forceinline__ void store(T *p, const float *v) const {
+        if (live) Elem<T>::store(p + at, v[0]);
     }
-    if (a.h_last && w == 0 && live) a.h_last[b * a.d + c] = H;
+};
+template <>
+struct Chans<bf16_t, 2> {
+    typedef uint32_t raw;
+    typedef uint32_t __attribute__((aligned(2))) pair_t;
+    int at, live, shift;
+    __device__ __forceinline__ Chans(int c, int d)
+        : at(min(c, d - 2)), live(min(max(d - c, 0), 2)), shift(c > d - 2 ? 16 : 0) {}
+    __device__ __forceinline__ raw load(const bf16_t *p) const { return *reinterpret_cast<const pair_t *>(p + at); }
+    __device__ __forceinline__ void unpack(raw r, float *v) const {
+        v[0] = __uint_as_float(r >> shift << 16);
+        v[1] = __uint_as_float(r & 0xffff0000u);
+    }
+    __device__ __forceinline__ void store(bf16_t *p, const float *v) const {
+        if (live == 2) *reinterpret_cast<pair_t *>(p + at) = pack_bf16x2(v[0], v[1]);
+        else if (live == 1) p[at + 1] = (bf16_t)f32_to_bf16(v[0]);
+    }
+};
+
+// The strip, sequence and run of tokens of a lane.
+template <typename T, int V>
+struct Lane {
+    static constexpr int kRow = 64 / V;                       // lanes of a row of the strip
+    static constexpr int kRuns = kWaves * V;                  // runs of tokens of a block
+    static constexpr int kSteps = kScanBlock / kRuns;
+    int sub, w, c, segment;
+    int64_t b;
+    Chans<T, V> ch;
+    __device__ __forceinline__ Lane(int64_t job, int strips, int segments, int d)
+        : sub((threadIdx.x & 63) / kRow), w(threadIdx.x >> 6),
+          c((int)(job % strips) * kStrip + (threadIdx.x % kRow) * V), segment((int)(job / strips % segments)),
+          b(job / strips / segments), ch(c, d) {}
+    __device__ __forceinline__ int run() const { return w * V + sub; }
+};
+
+// What the runs of a block make of a channel's state: S + P h, s the smaller of 1 - P and P (see above).
+struct Span {
+    float S, Q, P;
+    __device__ __forceinline__ void add(float s, float x) {
+        S = move(S, s, x);
+        Q = move(Q, s, 1.f);
+        P = kept(P, s);
+    }
+    // This span, then o.
+    __device__ __forceinline__ Span then(const Span &o) const {
+        return {join(S, span(o.Q, o.P), o.S), Q + o.Q - Q * o.Q, P * o.P};
+    }
+    __device__ __forceinline__ Span other_half() const {
+        return {__shfl_xor(S, 32, 64), __shfl_xor(Q, 32, 64), __shfl_xor(P, 32, 64)};
+    }
+};
+
+// A strip's state (or what comes from behind) at the border of a segment: h0 (dh_last), then the segments between.
+template <int V>
+__device__ __forceinline__ void join_segments(const float2 *agg, int64_t at, int64_t step, int n, int c, int d, float *H) {
+    for (int g = 0; g < n; g += 8) {
+        float2 m[8][V];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+#pragma unroll
+            for (int e = 0; e < V; ++e) m[q][e] = agg[at + min(g + q, n - 1) * step + min(c + e, d - 1)];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+#pragma unroll
+            for (int e = 0; e < V; ++e) H[e] = g + q < n ? join(H[e], m[q][e].y, m[q][e].x) : H[e];
+    }
 }
 
-template <typename T, bool OUT>
-__global__ __launch_bounds__(64 * kWaves) void scan_bwd_kernel(ScanBwdArgs a) {
-    __shared__ float spans[2][kWaves][3][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int strips = (a.d + 63) / 64;
-    const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x, b = job / strips;
-    if (b >= a.b) return;
-    const int c = (int)(job - b * strips) * 64 + lane;
-    const bool live = c < a.d;
-    const int cc = live ? c : a.d - 1;
-    const int len = span_of(a.lengths, b, a.t);
-    const float bx = a.bias ? a.bias[cc] : 0.f, bf = a.bias ? a.bias[a.d + cc] : 0.f;
-    const float bo = OUT && a.bias ? a.bias[2 * a.d + cc] : 0.f;
-    const T *const z = (const T *)a.z + b * a.z_bs + cc;
-    const T *const dy = (const T *)a.dy + b * a.dy_bs + cc;
-    T *const dz = (T *)a.dz + b * a.dz_bs + cc;
-    const int blocks = (a.t + kScanBlock - 1) / kScanBlock;
-    float C = a.dh_last ? a.dh_last[b * a.d + cc] : 0.f;     // what comes from behind
-    for (int blk = blocks - 1; blk >= 0; --blk) {
-        const int t0 = blk * kScanBlock + w * kSteps;
-        if (blk * kScanBlock >= len) {
-            for (int i = 0; i < kSteps; ++i)
-                if (live && t0 + i < a.t)
-                    for (int k = 0; k < (OUT ? 3 : 2); ++k) Elem<T>::store(dz + (t0 + i) * a.dz_ts + k * a.d, 0.f);
-            continue;
-        }
-        float s[kSteps], x[kSteps], up[kSteps], so[OUT ? kSteps : 1], h1[kSteps];
+// What each segment but the last makes of the state before it (BWD: each but the first of what comes from behind it),
+// to agg[b][segment][channel].  A run is an eighth (a quarter) of the segment.
+template <typename T, int V, bool OUT, bool BWD>
+__global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(const T *z0, int64_t z_bs, int64_t z_ts, const float *bias,
+                                                                    const int32_t *lengths, const T *dy0, int64_t dy_bs,
+                                                                    int64_t dy_ts, float2 *agg, int64_t nb, int t, int d,
+                                                                    int segments, int seg_len) {
+    constexpr int U = 8;
+    __shared__ Span spans[kWaves][kStrip];
+    const int strips = (d + kStrip - 1) / kStrip;
+    const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
+    if (job >= nb * strips * (segments - 1)) return;
+    Lane<T, V> l(job, strips, segments - 1, d);
+    if (BWD) ++l.segment;
+    const int len = span_of(lengths, l.b, t);
+    const int per = seg_len / Lane<T, V>::kRuns;
+    const int begin = l.segment * seg_len + l.run() * per, end = min(begin + per, len);
+    const T *const z = z0 + l.b * z_bs, *const dy = BWD ? dy0 + l.b * dy_bs : nullptr;
+    float bx[V], bf[V], bo[V];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const bool in = t0 + i < len;
-            const int at = in ? t0 + i : 0;
-            const T *const p = z + at * a.z_ts;
-            x[i] = Elem<T>::load(p) + bx;
-            s[i] = gate(Elem<T>::load(p + a.d) + bf);
-            up[i] = Elem<T>::load(dy + at * a.dy_ts);
-            if (OUT) so[i] = gate(Elem<T>::load(p + 2 * a.d) + bo);
-            if (!in) s[i] = x[i] = up[i] = 0.f;
-        }
-        float S = 0.f, Q = 0.f, P = 1.f, R = 0.f;
+    for (int e = 0; e < V; ++e) {
+        const int c = min(l.c + e, d - 1);
+        bx[e] = bias ? bias[c] : 0.f;
+        bf[e] = bias ? bias[d + c] : 0.f;
+        bo[e] = OUT && bias ? bias[2 * d + c] : 0.f;
+    }
+    Span m[V];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            S = move(S, s[i], x[i]);
-            Q = move(Q, s[i], 1.f);
-            P = kept(P, s[i]);
+    for (int e = 0; e < V; ++e) m[e] = Span{0.f, 0.f, 1.f};
+    for (int i = 0; begin + i < end; i += U) {
+        typename Chans<T, V>::raw rx[U], rf[U], ro[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int at = BWD ? max(end - 1 - i - k, 0) : min(begin + i + k, t - 1);
+            const T *const p = z + at * z_ts;
+            rx[k] = l.ch.load(BWD ? dy + at * dy_ts : p);
+            rf[k] = l.ch.load(p + d);
+            if (OUT && BWD) ro[k] = l.ch.load(p + 2 * d);
         }
 #pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) R = kept(R + (OUT ? keeps(so[i]) * up[i] : up[i]), s[i]);
-        float(*const sp)[3][64] = spans[blk & 1];
-        sp[w][0][lane] = S;
-        sp[w][1][lane] = span(Q, P);
-        sp[w][2][lane] = R;
-        __syncthreads();
-        float h = a.states[((int64_t)b * blocks + blk) * a.d + cc], cin = C;
-        for (int v = 0; v < w; ++v) h = join(h, sp[v][1][lane], sp[v][0][lane]);
-        for (int v = kWaves - 1; v >= 0; --v) {
-            if (v == w) cin = C;
-            C = join(C, sp[v][1][lane], sp[v][2][lane]);
-        }
+        for (int k = 0; k < U; ++k) {
+            if (begin + i + k >= end) break;
+            float x[V], f[V], o[V];
+            l.ch.unpack(rx[k], x);
+            l.ch.unpack(rf[k], f);
+            if (OUT && BWD) l.ch.unpack(ro[k], o);
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            h1[i] = h;
-            h = move(h, s[i], x[i]);
-        }
-#pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) {
-            const float g = cin + (OUT ? keeps(so[i]) * up[i] : up[i]);
-            cin = kept(g, s[i]);
-            if (live && t0 + i < a.t) {
-                const bool in = t0 + i < len;
-                T *const p = dz + (t0 + i) * a.dz_ts;
-                Elem<T>::store(p, in ? takes(s[i]) * g : 0.f);
-                Elem<T>::store(p + a.d, in ? (h1[i] - x[i]) * (slope(s[i]) * g) : 0.f);
-                if (OUT) Elem<T>::store(p + 2 * a.d, in ? slope(so[i]) * up[i] * move(h1[i], s[i], x[i]) : 0.f);
+            for (int e = 0; e < V; ++e) {
+                const float s = gate(f[e] + bf[e]);
+                if (!BWD) {
+                    m[e].add(s, x[e] + bx[e]);
+                } else {
+                    m[e].S = kept(m[e].S + (OUT ? keeps(gate(o[e] + bo[e])) * x[e] : x[e]), s);
+                    m[e].Q = move(m[e].Q, s, 1.f);
+                    m[e].P = kept(m[e].P, s);
+                }
             }
         }
     }
-    if (a.dh0 && w == 0 && live) a.dh0[b * a.d + c] = C;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        if (V == 2) {
+            const Span o = m[e].other_half();
+            const bool first = BWD ? l.sub == 1 : l.sub == 0;
+            const Span a = first ? m[e] : o, b = first ? o : m[e];
+            m[e] = a.then(b);
+        }
+        if (V == 1 || l.sub == e) spans[l.w][threadIdx.x % Lane<T, V>::kRow * V + e] = m[e];
+    }
+    __syncthreads();
+    if (threadIdx.x >= kStrip) return;
+    Span a = spans[BWD ? kWaves - 1 : 0][threadIdx.x];
+#pragma unroll
+    for (int v = 1; v < kWaves; ++v) a = a.then(spans[BWD ? kWaves - 1 - v : v][threadIdx.x]);
+    const int c = (int)(job % strips) * kStrip + threadIdx.x;
+    if (c < d) agg[(l.b * segments + l.segment) * d + c] = make_float2(a.S, span(a.Q, a.P));
+}
+
+template <typename T, int V, bool OUT>
+__global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
+    typedef Lane<T, V> L;
+    constexpr int kSteps = L::kSteps;
+    __shared__ float2 spans[2][kWaves][kStrip];
+    const int d = a.d, strips = (d + kStrip - 1) / kStrip;
+    const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
+    if (job >= a.b * strips * segments) return;
+    const L l(job, strips, segments, d);
+    const int len = span_of(a.lengths, l.b, a.t);
+    float bx[V], bf[V], bo[V], H[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const int c = min(l.c + e, d - 1);
+        bx[e] = a.bias ? a.bias[c] : 0.f;
+        bf[e] = a.bias ? a.bias[d + c] : 0.f;
+        bo[e] = OUT && a.bias ? a.bias[2 * d + c] : 0.f;
+        H[e] = a.h0 ? a.h0[l.b * d + c] : 0.f;
+    }
+    if (l.segment > 0) join_segments<V>(agg, l.b * segments * d, d, l.segment, l.c, d, H);
+    const T *const z = (const T *)a.z + l.b * a.z_bs;
+    T *const y = (T *)a.y + l.b * a.y_bs;
+    const int blocks = (a.t + kScanBlock - 1) / kScanBlock;
+    const int col = threadIdx.x % L::kRow * V;
+    for (int blk = l.segment * (seg_len / kScanBlock); blk < min(blocks, (l.segment + 1) * (seg_len / kScanBlock)); ++blk) {
+        const int t0 = blk * kScanBlock + l.run() * kSteps;
+        if (blk * kScanBlock >= len) {             // padding from here on
+            const float none[2] = {0.f, 0.f};
+            for (int i = 0; i < kSteps; ++i)
+                if (t0 + i < a.t) l.ch.store(y + (t0 + i) * a.y_ts, none);
+            continue;
+        }
+        float s[kSteps][V], x[kSteps][V], o[OUT ? kSteps : 1][V];
+        {
+            typename Chans<T, V>::raw rx[kSteps], rf[kSteps], ro[OUT ? kSteps : 1];
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const T *const p = z + min(t0 + i, len - 1) * a.z_ts;
+                rx[i] = l.ch.load(p);
+                rf[i] = l.ch.load(p + d);
+                if (OUT) ro[i] = l.ch.load(p + 2 * d);
+            }
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                l.ch.unpack(rx[i], x[i]);
+                l.ch.unpack(rf[i], s[i]);
+                if (OUT) l.ch.unpack(ro[i], o[i]);
+            }
+        }
+        Span m[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) m[e] = Span{0.f, 0.f, 1.f};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                x[i][e] += bx[e];
+                s[i][e] = gate(s[i][e] + bf[e]);
+                if (OUT) o[i][e] = keeps(gate(o[i][e] + bo[e]));
+                if (t0 + i >= len) s[i][e] = x[i][e] = 0.f;            // a state stays as it is
+                m[e].add(s[i][e], x[i][e]);
+            }
+        float2 half[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if (V == 2) {
+                const Span other = m[e].other_half();
+                half[e] = make_float2(other.S, span(other.Q, other.P));
+                m[e] = l.sub == 0 ? m[e].then(other) : other.then(m[e]);
+            }
+            if (V == 1 || l.sub == e) spans[blk & 1][l.w][col + e] = make_float2(m[e].S, span(m[e].Q, m[e].P));
+        }
+        __syncthreads();
+        float h[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if (a.states && threadIdx.x < L::kRow && l.c + e < d) a.states[(l.b * blocks + blk) * d + l.c + e] = H[e];
+#pragma unroll
+            for (int v = 0; v < kWaves; ++v) {
+                if (v == l.w) h[e] = H[e];
+                const float2 q = spans[blk & 1][v][col + e];
+                H[e] = join(H[e], q.y, q.x);
+            }
+            if (V == 2 && l.sub == 1) h[e] = join(h[e], half[e].y, half[e].x);
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            float out[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                h[e] = move(h[e], s[i][e], x[i][e]);
+                out[e] = t0 + i < len ? (OUT ? o[i][e] * h[e] : h[e]) : 0.f;
+            }
+            if (t0 + i < a.t) l.ch.store(y + (t0 + i) * a.y_ts, out);
+        }
+    }
+    if (a.h_last && l.segment == segments - 1 && threadIdx.x < L::kRow)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (l.c + e < d) a.h_last[l.b * d + l.c + e] = H[e];
+}
+
+template <typename T, int V, bool OUT>
+__global__ __launch_bounds__(64 * kWaves) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
+    typedef Lane<T, V> L;
+    constexpr int kSteps = L::kSteps;
+    __shared__ float2 spans[2][kWaves][kStrip];
+    __shared__ float backs[2][kWaves][kStrip];
+    const int d = a.d, strips = (d + kStrip - 1) / kStrip;
+    const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
+    if (job >= a.b * strips * segments) return;
+    const L l(job, strips, segments, d);
+    const int len = span_of(a.lengths, l.b, a.t);
+    float bx[V], bf[V], bo[V], C[V];                             // C: what comes from behind
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const int c = min(l.c + e, d - 1);
+        bx[e] = a.bias ? a.bias[c] : 0.f;
+        bf[e] = a.bias ? a.bias[d + c] : 0.f;
+        bo[e] = OUT && a.bias ? a.bias[2 * d + c] : 0.f;
+        C[e] = a.dh_last ? a.dh_last[l.b * d + c] : 0.f;
+    }
+    if (l.segment < segments - 1)
+        join_segments<V>(agg, (l.b * segments + segments - 1) * d, -(int64_t)d, segments - 1 - l.segment, l.c, d, C);
+    const T *const z = (const T *)a.z + l.b * a.z_bs;
+    const T *const dy = (const T *)a.dy + l.b * a.dy_bs;
+    T *const dz = (T *)a.dz + l.b * a.dz_bs;
+    const int blocks = (a.t + kScanBlock - 1) / kScanBlock;
+    const int col = threadIdx.x % L::kRow * V;
+    const int first = l.segment * (seg_len / kScanBlock);
+    for (int blk = min(blocks, first + seg_len / kScanBlock) - 1; blk >= first; --blk) {
+        const int t0 = blk * kScanBlock + l.run() * kSteps;
+        if (blk * kScanBlock >= len) {
+            const float none[2] = {0.f, 0.f};
+            for (int i = 0; i < kSteps; ++i)
+                if (t0 + i < a.t)
+                    for (int k = 0; k < (OUT ? 3 : 2); ++k) l.ch.store(dz + (t0 + i) * a.dz_ts + k * d, none);
+            continue;
+        }
+        float s[kSteps][V], x[kSteps][V], up[kSteps][V], o[OUT ? kSteps : 1][V], h[V];
+        {
+            typename Chans<T, V>::raw rx[kSteps], rf[kSteps], ru[kSteps], ro[OUT ? kSteps : 1];
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int at = min(t0 + i, len - 1);
+                const T *const p = z + at * a.z_ts;
+                rx[i] = l.ch.load(p);
+                rf[i] = l.ch.load(p + d);
+                ru[i] = l.ch.load(dy + at * a.dy_ts);
+                if (OUT) ro[i] = l.ch.load(p + 2 * d);
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) h[e] = a.states[(l.b * blocks + blk) * d + min(l.c + e, d - 1)];
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                l.ch.unpack(rx[i], x[i]);
+                l.ch.unpack(rf[i], s[i]);
+                l.ch.unpack(ru[i], up[i]);
+                if (OUT) l.ch.unpack(ro[i], o[i]);
+            }
+        }
+        Span m[V];
+        float R[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            m[e] = Span{0.f, 0.f, 1.f};
+            R[e] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                x[i][e] += bx[e];
+                s[i][e] = gate(s[i][e] + bf[e]);
+                if (OUT) o[i][e] = gate(o[i][e] + bo[e]);
+                if (t0 + i >= len) s[i][e] = x[i][e] = up[i][e] = 0.f;
+                m[e].add(s[i][e], x[i][e]);
+            }
+#pragma unroll
+        for (int i = kSteps - 1; i >= 0; --i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) R[e] = kept(R[e] + (OUT ? keeps(o[i][e]) * up[i][e] : up[i][e]), s[i][e]);
+        float half_S[V], half_s[V], half_R[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float back = R[e];
+            if (V == 2) {
+                const Span other = m[e].other_half();
+                half_S[e] = other.S;
+                half_s[e] = span(other.Q, other.P);
+                half_R[e] = __shfl_xor(R[e], 32, 64);
+                // the earlier half is the later one of the way back
+                back = l.sub == 0 ? join(half_R[e], span(m[e].Q, m[e].P), R[e]) : join(R[e], half_s[e], half_R[e]);
+                m[e] = l.sub == 0 ? m[e].then(other) : other.then(m[e]);
+            }
+            if (V == 1 || l.sub == e) {
+                spans[blk & 1][l.w][col + e] = make_float2(m[e].S, span(m[e].Q, m[e].P));
+                backs[blk & 1][l.w][col + e] = back;
+            }
+        }
+        __syncthreads();
+        float c[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+#pragma unroll
+            for (int v = 0; v < kWaves - 1; ++v) {
+                const float2 q = spans[blk & 1][v][col + e];
+                if (v < l.w) h[e] = join(h[e], q.y, q.x);
+            }
+#pragma unroll
+            for (int v = kWaves - 1; v >= 0; --v) {
+                if (v == l.w) c[e] = C[e];
+                C[e] = join(C[e], spans[blk & 1][v][col + e].y, backs[blk & 1][v][col + e]);
+            }
+            if (V == 2) {
+                if (l.sub == 1) h[e] = join(h[e], half_s[e], half_S[e]);
+                else c[e] = join(c[e], half_s[e], half_R[e]);
+            }
+        }
+        // forwards: x becomes h_(t-1) - x, dy becomes what reaches h_t, and the output gate's gradient is done
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            float out[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float before = h[e];
+                h[e] = move(before, s[i][e], x[i][e]);
+                x[i][e] = before - x[i][e];
+                if (OUT) {
+                    out[e] = slope(o[i][e]) * up[i][e] * h[e];
+                    up[i][e] *= keeps(o[i][e]);
+                    if (t0 + i >= len) out[e] = 0.f;
+                }
+            }
+            if (OUT && t0 + i < a.t) l.ch.store(dz + (t0 + i) * a.dz_ts + 2 * d, out);
+        }
+#pragma unroll
+        for (int i = kSteps - 1; i >= 0; --i) {
+            float dx[V], df[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float g = c[e] + up[i][e];
+                c[e] = kept(g, s[i][e]);
+                const bool in = t0 + i < len;
+                dx[e] = in ? takes(s[i][e]) * g : 0.f;
+                df[e] = in ? x[i][e] * (slope(s[i][e]) * g) : 0.f;
+            }
+            if (t0 + i < a.t) {
+                T *const p = dz + (t0 + i) * a.dz_ts;
+                l.ch.store(p, dx);
+                l.ch.store(p + d, df);
+            }
+        }
+    }
+    if (a.dh0 && l.segment == 0 && threadIdx.x < L::kRow)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (l.c + e < d) a.dh0[l.b * d + l.c + e] = C[e];
 }
 
 // One token of each row: the row's state, in its slot, moves on.  A row whose slot is none gets zeros.
@@ -210,29 +496,83 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStepArgs a) {
     Elem<T>::store(y, OUT ? o * h : h);
 }
 
-#define SCAN_LAUNCH(kernel, grid, threads, a)                                                               \
-    do {                                                                                                    \
-        if (dt == 0 && gates == 2) hipLaunchKernelGGL((kernel<float, false>), grid, dim3(threads), 0, st, a); \
-        if (dt == 0 && gates == 3) hipLaunchKernelGGL((kernel<float, true>), grid, dim3(threads), 0, st, a);  \
-        if (dt == 1 && gates == 2) hipLaunchKernelGGL((kernel<bf16_t, false>), grid, dim3(threads), 0, st, a); \
-        if (dt == 1 && gates == 3) hipLaunchKernelGGL((kernel<bf16_t, true>), grid, dim3(threads), 0, st, a);  \
+// How the time axis is cut: segments of seg_len tokens, a whole number of blocks.
+static void scan_plan(int64_t b, int64_t t, int d, int *segments, int *seg_len) {
+    const int64_t strips = b * ((d + kStrip - 1) / kStrip), blocks = std::max<int64_t>((t + kScanBlock - 1) / kScanBlock, 1);
+    int64_t want = 1;
+    if (strips < 512) want = std::min<int64_t>({kSegments, blocks / 2, (1024 + strips - 1) / strips});
+    want = std::max<int64_t>(want, 1);
+    const int64_t per = (blocks + want - 1) / want;
+    *segments = (int)((blocks + per - 1) / per);
+    *seg_len = (int)(per * kScanBlock);
+}
+
+size_t scan_ws_bytes(bool, int64_t b, int64_t t, int d) {
+    int segments, seg_len;
+    scan_plan(b, t, d, &segments, &seg_len);
+    return segments > 1 ? (size_t)b * segments * d * sizeof(float2) : 0;
+}
+
+// Two channels a lane in bf16, but for a single channel.
+template <typename T, int V, bool OUT>
+static void launch_fwd(const ScanArgs &a, float2 *ws, hipStream_t st) {
+    int segments, seg_len;
+    scan_plan(a.b, a.t, a.d, &segments, &seg_len);
+    const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
+    if (segments > 1)
+        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, false>), grid_2d(strips * (segments - 1)), dim3(64 * kWaves), 0, st,
+                           (const T *)a.z, a.z_bs, a.z_ts, a.bias, a.lengths, (const T *)nullptr, 0, 0, ws, a.b, a.t, a.d,
+                           segments, seg_len);
+    hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT>), grid_2d(strips * segments), dim3(64 * kWaves), 0, st, a, ws, segments,
+                       seg_len);
+}
+
+template <typename T, int V, bool OUT>
+static void launch_bwd(const ScanBwdArgs &a, float2 *ws, hipStream_t st) {
+    int segments, seg_len;
+    scan_plan(a.b, a.t, a.d, &segments, &seg_len);
+    const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
+    if (segments > 1)
+        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, true>), grid_2d(strips * (segments - 1)), dim3(64 * kWaves), 0, st,
+                           (const T *)a.z, a.z_bs, a.z_ts, a.bias, a.lengths, (const T *)a.dy, a.dy_bs, a.dy_ts, ws, a.b, a.t,
+                           a.d, segments, seg_len);
+    hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT>), grid_2d(strips * segments), dim3(64 * kWaves), 0, st, a, ws, segments,
+                       seg_len);
+}
+
+#define SCAN_CASES(fn, ...)                                                         \
+    do {                                                                            \
+        if (dt == 0) {                                                              \
+            if (gates == 2) fn<float, 1, false>(__VA_ARGS__);                       \
+            else fn<float, 1, true>(__VA_ARGS__);                                   \
+        } else if (a.d == 1) {                                                      \
+            if (gates == 2) fn<bf16_t, 1, false>(__VA_ARGS__);                      \
+            else fn<bf16_t, 1, true>(__VA_ARGS__);                                  \
+        } else {                                                                    \
+            if (gates == 2) fn<bf16_t, 2, false>(__VA_ARGS__);                      \
+            else fn<bf16_t, 2, true>(__VA_ARGS__);                                  \
+        }                                                                           \
     } while (0)
 
-size_t scan_ws_bytes(bool bwd, int64_t b, int64_t t, int d) { return 0; }
-
 hipError_t launch_scan_fwd(int dt, int gates, const ScanArgs &a, void *ws, hipStream_t st) {
-    SCAN_LAUNCH(scan_fwd_kernel, grid_2d(a.b * ((a.d + 63) / 64)), 64 * kWaves, a);
+    SCAN_CASES(launch_fwd, a, (float2 *)ws, st);
     return hipGetLastError();
 }
 
 hipError_t launch_scan_bwd(int dt, int gates, const ScanBwdArgs &a, void *ws, hipStream_t st) {
-    SCAN_LAUNCH(scan_bwd_kernel, grid_2d(a.b * ((a.d + 63) / 64)), 64 * kWaves, a);
+    SCAN_CASES(launch_bwd, a, (float2 *)ws, st);
     return hipGetLastError();
 }
 
-hipError_t launch_scan_step(int dt, int gates, const ScanStepArgs &a, hipStream_t st) {
+template <typename T, int V, bool OUT>
+static void launch_step(const ScanStepArgs &a, hipStream_t st) {
     const unsigned gy = (unsigned)std::min<int64_t>(a.n, 32768);
-    SCAN_LAUNCH(scan_step_kernel, dim3((a.d + 255) / 256, gy, (unsigned)((a.n + gy - 1) / gy)), 256, a);
+    hipLaunchKernelGGL((scan_step_kernel<T, OUT>), dim3((a.d + 255) / 256, gy, (unsigned)((a.n + gy - 1) / gy)), dim3(256), 0, st,
+                       a);
+}
+
+hipError_t launch_scan_step(int dt, int gates, const ScanStepArgs &a, hipStream_t st) {
+    SCAN_CASES(launch_step, a, st);
     return hipGetLastError();
 }
 
