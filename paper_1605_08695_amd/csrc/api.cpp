@@ -1187,6 +1187,7 @@ static tfk_status check_seqs(const char *name, int64_t b, int64_t t, int64_t col
     if (b <= 1 || bs == 0) bs = std::max(t * ts, cols);
     if (bs > most / std::max<int64_t>(b, 1)) return fail(TFK_ERR_OVERFLOW, "%s: too large", name);
     if (b == 0 || t == 0) return TFK_OK;
+    if (ts > kScanRowStep) return fail(TFK_ERR_OVERFLOW, "%s: rows more than 2^25 elements apart", name);
     const bool rows = ts >= cols && (b == 1 || bs >= (t - 1) * ts + cols);
     const bool cross = bs >= cols && (t == 1 || ts >= (b - 1) * bs + cols);
     if (!rows && !cross)

@@ -18,6 +18,8 @@
 // of the state before it (x and the gate; backwards the gate and dy), and in the second each workgroup joins those of the
 // segments before its own.  Bound by HBM: z is read once and y written once; the backward pass reads z and dy and
 // writes dz, with the states of each kScanBlock-th token from the forward pass.
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -57,37 +59,32 @@ __device__ __forceinline__ int span_of(const int32_t *lengths, int64_t b, int t)
 // V neighbouring channels of a row of d (V <= d) from channel c on.  The last lanes of a row of an odd number of channels
 // read the pair that ends with it.
 template <typename T, int V>
-struct Chans;
-template <typename T>
-struct Chans<T, 1> {
+struct Chans {
     typedef T raw;
     int at, live;
-    __device__ __forceinline__ Chans(int c, int d) : at(min(c, d - 1)), live(c < d) {}
-    __device__ __forceinline__ raw load(const T *p) const { return p[at]; }
+    __device__ __forceinline__ Chans(int c, int d) : at(min(c, d - 1)), live(c < d ? 1 : 0) {}
+    __device__ __forceinline__ static raw load(const T *p) { return *p; }
     __device__ __forceinline__ void unpack(raw r, float *v) const { v[0] = Elem<T>::load(&r); }
-    __device__ __forceinline__ void store(T *p, const float *v) const {
-        if (live) Elem<T>::store(p + at, v[0]);
-    }
 };
 template <>
 struct Chans<bf16_t, 2> {
     typedef uint32_t raw;
-    typedef uint32_t __attribute__((aligned(2))) pair_t;
-    int at, live, shift;
+    int at, live;
+    uint32_t low;                      // where the first channel's two bytes are in a pair
     __device__ __forceinline__ Chans(int c, int d)
-        : at(min(c, d - 2)), live(min(max(d - c, 0), 2)), shift(c > d - 2 ? 16 : 0) {}
-    __device__ __forceinline__ raw load(const bf16_t *p) const { return *reinterpret_cast<const pair_t *>(p + at); }
-    __device__ __forceinline__ void unpack(raw r, float *v) const {
-        v[0] = __uint_as_float(r >> shift << 16);
-        v[1] = __uint_as_float(r & 0xffff0000u);
+        : at(min(c, d - 2)), live(min(max(d - c, 0), 2)), low(c > d - 2 ? 0x03020c0c : 0x01000c0c) {}
+    __device__ __forceinline__ static raw load(const bf16_t *p) {
+        typedef uint32_t __attribute__((aligned(2))) pair_t;
+        return *reinterpret_cast<const pair_t *>(p);
     }
-    __device__ __forceinline__ void store(bf16_t *p, const float *v) const {
-        if (live == 2) *reinterpret_cast<pair_t *>(p + at) = pack_bf16x2(v[0], v[1]);
-        else if (live == 1) p[at + 1] = (bf16_t)f32_to_bf16(v[0]);
+    __device__ __forceinline__ void unpack(raw r, float *v) const {
+        v[0] = __uint_as_float(__builtin_amdgcn_perm(r, r, low));
+        v[1] = __uint_as_float(r & 0xffff0000u);
     }
 };
 
-// The strip, sequence and run of tokens of a lane.
+// The strip, sequence and run of tokens of a lane.  w, segment, b and whole (whether the strip has all its channels)
+// are the same for a wave.
 template <typename T, int V>
 struct Lane {
     static constexpr int kRow = 64 / V;                       // lanes of a row of the strip
@@ -95,12 +92,57 @@ struct Lane {
     static constexpr int kSteps = kScanBlock / kRuns;
     int sub, w, c, segment;
     int64_t b;
+    bool whole;
     Chans<T, V> ch;
     __device__ __forceinline__ Lane(int64_t job, int strips, int segments, int d)
-        : sub((threadIdx.x & 63) / kRow), w(threadIdx.x >> 6),
+        : sub((threadIdx.x & 63) / kRow), w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
           c((int)(job % strips) * kStrip + (threadIdx.x % kRow) * V), segment((int)(job / strips % segments)),
-          b(job / strips / segments), ch(c, d) {}
+          b(job / strips / segments), whole((int)(job % strips) * kStrip + kStrip <= d), ch(c, d) {}
     __device__ __forceinline__ int run() const { return w * V + sub; }
+};
+
+// Rows of a sequence, read and written through buffer descriptors: an address that the wave's lanes share, in scalar
+// registers, and an offset of 32 bits of each lane (rows are at most kScanRowStep elements apart).  A lane whose token or
+// channel is not there gives kNowhere, past the descriptor's end: it reads 0 and writes nothing, without a branch.
+constexpr uint32_t kNowhere = 0x80000000u;
+
+template <typename T, int V>
+struct Rows {
+    typedef std::remove_const_t<T> E;
+    typedef Lane<E, V> L;
+    T *p;
+    int64_t ts;
+    uint32_t off, off_all, off_half;   // where a lane reads, writes all of its channels, and the first one alone
+    __device__ __forceinline__ Rows(T *base, int64_t ts, const L &l)
+        : p(base), ts(ts), off((uint32_t)((l.sub * L::kSteps * ts + l.ch.at) * sizeof(T))) {
+        off_all = l.ch.live == V ? off : kNowhere;
+        off_half = V == 2 && l.ch.live == 1 ? off + (uint32_t)sizeof(T) : kNowhere;
+    }
+    // Token t of the wave's first run.
+    __device__ __forceinline__ T *row(int t) const { return p + t * ts; }
+    __device__ __forceinline__ static __amdgpu_buffer_rsrc_t desc(T *r) {
+        return __builtin_amdgcn_make_buffer_rsrc((void *)const_cast<E *>(r), 0, 0x7fffffff, 0x00027000);
+    }
+    // The lane's channels in the columns that begin at r, of the wave's first run's row or the same one of the lane's.
+    __device__ __forceinline__ typename Chans<E, V>::raw load(T *r, bool there) const {
+        const uint32_t o = there ? off : kNowhere;
+        if constexpr (sizeof(E) * V == 4) {
+            return __builtin_bit_cast(typename Chans<E, V>::raw, __builtin_amdgcn_raw_buffer_load_b32(desc(r), o, 0, 0));
+        } else {
+            return (E)__builtin_amdgcn_raw_buffer_load_b16(desc(r), o, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void store(T *r, const float *v, bool there, bool whole) const {
+        const uint32_t o = there ? off_all : kNowhere;
+        if constexpr (sizeof(E) == 4) {
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[0]), desc(r), o, 0, 0);
+        } else if constexpr (V == 2) {
+            __builtin_amdgcn_raw_buffer_store_b32(pack_bf16x2(v[0], v[1]), desc(r), o, 0, 0);
+            if (!whole) __builtin_amdgcn_raw_buffer_store_b16((short)f32_to_bf16(v[0]), desc(r), there ? off_half : kNowhere, 0, 0);
+        } else {
+            __builtin_amdgcn_raw_buffer_store_b16((short)f32_to_bf16(v[0]), desc(r), o, 0, 0);
+        }
+    }
 };
 
 // What the runs of a block make of a channel's state: S + P h, s the smaller of 1 - P and P (see above).
@@ -170,8 +212,8 @@ __global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(const T *z0,
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             const int at = BWD ? max(end - 1 - i - k, 0) : min(begin + i + k, t - 1);
-            const T *const p = z + at * z_ts;
-            rx[k] = l.ch.load(BWD ? dy + at * dy_ts : p);
+            const T *const p = z + at * z_ts + l.ch.at;
+            rx[k] = l.ch.load(BWD ? dy + at * dy_ts + l.ch.at : p);
             rf[k] = l.ch.load(p + d);
             if (OUT && BWD) ro[k] = l.ch.load(p + 2 * d);
         }
@@ -215,7 +257,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(const T *z0,
 }
 
 template <typename T, int V, bool OUT>
-__global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
+__global__ __launch_bounds__(64 * kWaves, OUT ? 3 : 4) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V> L;
     constexpr int kSteps = L::kSteps;
     __shared__ float2 spans[2][kWaves][kStrip];
@@ -234,27 +276,24 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanArgs a, const
         H[e] = a.h0 ? a.h0[l.b * d + c] : 0.f;
     }
     if (l.segment > 0) join_segments<V>(agg, l.b * segments * d, d, l.segment, l.c, d, H);
-    const T *const z = (const T *)a.z + l.b * a.z_bs;
-    T *const y = (T *)a.y + l.b * a.y_bs;
+    const Rows<const T, V> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l);
+    const Rows<T, V> y((T *)a.y + l.b * a.y_bs, a.y_ts, l);
     const int blocks = (a.t + kScanBlock - 1) / kScanBlock;
     const int col = threadIdx.x % L::kRow * V;
-    for (int blk = l.segment * (seg_len / kScanBlock); blk < min(blocks, (l.segment + 1) * (seg_len / kScanBlock)); ++blk) {
-        const int t0 = blk * kScanBlock + l.run() * kSteps;
-        if (blk * kScanBlock >= len) {             // padding from here on
-            const float none[2] = {0.f, 0.f};
-            for (int i = 0; i < kSteps; ++i)
-                if (t0 + i < a.t) l.ch.store(y + (t0 + i) * a.y_ts, none);
-            continue;
-        }
+    // INSIDE: all of the block's tokens and channels are there
+    const auto block = [&](int blk, auto inside) {
+        constexpr bool INSIDE = decltype(inside)::value;
+        const int t0 = blk * kScanBlock + l.run() * kSteps, tw = blk * kScanBlock + l.w * V * kSteps;
         float s[kSteps][V], x[kSteps][V], o[OUT ? kSteps : 1][V];
         {
             typename Chans<T, V>::raw rx[kSteps], rf[kSteps], ro[OUT ? kSteps : 1];
+            const T *r = z.row(tw);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const T *const p = z + min(t0 + i, len - 1) * a.z_ts;
-                rx[i] = l.ch.load(p);
-                rf[i] = l.ch.load(p + d);
-                if (OUT) ro[i] = l.ch.load(p + 2 * d);
+            for (int i = 0; i < kSteps; ++i, r += z.ts) {
+                const bool in = INSIDE || t0 + i < len;
+                rx[i] = z.load(r, in);
+                rf[i] = z.load(r + d, in);
+                if (OUT) ro[i] = z.load(r + 2 * d, in);
             }
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
@@ -273,7 +312,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanArgs a, const
                 x[i][e] += bx[e];
                 s[i][e] = gate(s[i][e] + bf[e]);
                 if (OUT) o[i][e] = keeps(gate(o[i][e] + bo[e]));
-                if (t0 + i >= len) s[i][e] = x[i][e] = 0.f;            // a state stays as it is
+                if (!INSIDE && t0 + i >= len) s[i][e] = x[i][e] = 0.f;            // a state stays as it is
                 m[e].add(s[i][e], x[i][e]);
             }
         float2 half[V];
@@ -297,17 +336,31 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanArgs a, const
                 const float2 q = spans[blk & 1][v][col + e];
                 H[e] = join(H[e], q.y, q.x);
             }
-            if (V == 2 && l.sub == 1) h[e] = join(h[e], half[e].y, half[e].x);
+            if (V == 2) h[e] = l.sub == 1 ? join(h[e], half[e].y, half[e].x) : h[e];
         }
+        T *r = y.row(tw);
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
+        for (int i = 0; i < kSteps; ++i, r += y.ts) {
             float out[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 h[e] = move(h[e], s[i][e], x[i][e]);
-                out[e] = t0 + i < len ? (OUT ? o[i][e] * h[e] : h[e]) : 0.f;
+                out[e] = OUT ? o[i][e] * h[e] : h[e];
+                if (!INSIDE && t0 + i >= len) out[e] = 0.f;
             }
-            if (t0 + i < a.t) l.ch.store(y + (t0 + i) * a.y_ts, out);
+            y.store(r, out, INSIDE || t0 + i < a.t, INSIDE || l.whole);
+        }
+    };
+    for (int blk = l.segment * (seg_len / kScanBlock); blk < min(blocks, (l.segment + 1) * (seg_len / kScanBlock)); ++blk) {
+        if (l.whole && (blk + 1) * kScanBlock <= len) {
+            block(blk, std::true_type{});
+        } else if (blk * kScanBlock < len) {
+            block(blk, std::false_type{});
+        } else {                                   // padding from here on
+            const int t0 = blk * kScanBlock + l.run() * kSteps, tw = blk * kScanBlock + l.w * V * kSteps;
+            const float none[2] = {0.f, 0.f};
+            for (int i = 0; i < kSteps; ++i)
+                y.store(y.row(tw + i), none, t0 + i < a.t, l.whole);
         }
     }
     if (a.h_last && l.segment == segments - 1 && threadIdx.x < L::kRow)
@@ -317,7 +370,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanArgs a, const
 }
 
 template <typename T, int V, bool OUT>
-__global__ __launch_bounds__(64 * kWaves) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
+__global__ __launch_bounds__(64 * kWaves, OUT ? 2 : 3) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V> L;
     constexpr int kSteps = L::kSteps;
     __shared__ float2 spans[2][kWaves][kStrip];
@@ -338,32 +391,24 @@ __global__ __launch_bounds__(64 * kWaves) void scan_bwd_kernel(ScanBwdArgs a, co
     }
     if (l.segment < segments - 1)
         join_segments<V>(agg, (l.b * segments + segments - 1) * d, -(int64_t)d, segments - 1 - l.segment, l.c, d, C);
-    const T *const z = (const T *)a.z + l.b * a.z_bs;
-    const T *const dy = (const T *)a.dy + l.b * a.dy_bs;
-    T *const dz = (T *)a.dz + l.b * a.dz_bs;
+    const Rows<const T, V> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
+    const Rows<T, V> dz((T *)a.dz + l.b * a.dz_bs, a.dz_ts, l);
     const int blocks = (a.t + kScanBlock - 1) / kScanBlock;
     const int col = threadIdx.x % L::kRow * V;
-    const int first = l.segment * (seg_len / kScanBlock);
-    for (int blk = min(blocks, first + seg_len / kScanBlock) - 1; blk >= first; --blk) {
-        const int t0 = blk * kScanBlock + l.run() * kSteps;
-        if (blk * kScanBlock >= len) {
-            const float none[2] = {0.f, 0.f};
-            for (int i = 0; i < kSteps; ++i)
-                if (t0 + i < a.t)
-                    for (int k = 0; k < (OUT ? 3 : 2); ++k) l.ch.store(dz + (t0 + i) * a.dz_ts + k * d, none);
-            continue;
-        }
+    const auto block = [&](int blk, auto inside) {
+        constexpr bool INSIDE = decltype(inside)::value;
+        const int t0 = blk * kScanBlock + l.run() * kSteps, tw = blk * kScanBlock + l.w * V * kSteps;
         float s[kSteps][V], x[kSteps][V], up[kSteps][V], o[OUT ? kSteps : 1][V], h[V];
         {
             typename Chans<T, V>::raw rx[kSteps], rf[kSteps], ru[kSteps], ro[OUT ? kSteps : 1];
+            const T *r = z.row(tw), *ry = dy.row(tw);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const int at = min(t0 + i, len - 1);
-                const T *const p = z + at * a.z_ts;
-                rx[i] = l.ch.load(p);
-                rf[i] = l.ch.load(p + d);
-                ru[i] = l.ch.load(dy + at * a.dy_ts);
-                if (OUT) ro[i] = l.ch.load(p + 2 * d);
+            for (int i = 0; i < kSteps; ++i, r += z.ts, ry += dy.ts) {
+                const bool in = INSIDE || t0 + i < len;
+                rx[i] = z.load(r, in);
+                rf[i] = z.load(r + d, in);
+                ru[i] = dy.load(ry, in);
+                if (OUT) ro[i] = z.load(r + 2 * d, in);
             }
 #pragma unroll
             for (int e = 0; e < V; ++e) h[e] = a.states[(l.b * blocks + blk) * d + min(l.c + e, d - 1)];
@@ -389,7 +434,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_bwd_kernel(ScanBwdArgs a, co
                 x[i][e] += bx[e];
                 s[i][e] = gate(s[i][e] + bf[e]);
                 if (OUT) o[i][e] = gate(o[i][e] + bo[e]);
-                if (t0 + i >= len) s[i][e] = x[i][e] = up[i][e] = 0.f;
+                if (!INSIDE && t0 + i >= len) s[i][e] = x[i][e] = up[i][e] = 0.f;
                 m[e].add(s[i][e], x[i][e]);
             }
 #pragma unroll
@@ -429,13 +474,14 @@ __global__ __launch_bounds__(64 * kWaves) void scan_bwd_kernel(ScanBwdArgs a, co
                 C[e] = join(C[e], spans[blk & 1][v][col + e].y, backs[blk & 1][v][col + e]);
             }
             if (V == 2) {
-                if (l.sub == 1) h[e] = join(h[e], half_s[e], half_S[e]);
-                else c[e] = join(c[e], half_s[e], half_R[e]);
+                h[e] = l.sub == 1 ? join(h[e], half_s[e], half_S[e]) : h[e];
+                c[e] = l.sub == 0 ? join(c[e], half_s[e], half_R[e]) : c[e];
             }
         }
         // forwards: x becomes h_(t-1) - x, dy becomes what reaches h_t, and the output gate's gradient is done
+        T *r = dz.row(tw);
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
+        for (int i = 0; i < kSteps; ++i, r += dz.ts) {
             float out[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -445,27 +491,38 @@ __global__ __launch_bounds__(64 * kWaves) void scan_bwd_kernel(ScanBwdArgs a, co
                 if (OUT) {
                     out[e] = slope(o[i][e]) * up[i][e] * h[e];
                     up[i][e] *= keeps(o[i][e]);
-                    if (t0 + i >= len) out[e] = 0.f;
+                    if (!INSIDE && t0 + i >= len) out[e] = 0.f;
                 }
             }
-            if (OUT && t0 + i < a.t) l.ch.store(dz + (t0 + i) * a.dz_ts + 2 * d, out);
+            if (OUT) dz.store(r + 2 * d, out, INSIDE || t0 + i < a.t, INSIDE || l.whole);
         }
 #pragma unroll
         for (int i = kSteps - 1; i >= 0; --i) {
+            r -= dz.ts;
             float dx[V], df[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float g = c[e] + up[i][e];
                 c[e] = kept(g, s[i][e]);
-                const bool in = t0 + i < len;
+                const bool in = INSIDE || t0 + i < len;
                 dx[e] = in ? takes(s[i][e]) * g : 0.f;
                 df[e] = in ? x[i][e] * (slope(s[i][e]) * g) : 0.f;
             }
-            if (t0 + i < a.t) {
-                T *const p = dz + (t0 + i) * a.dz_ts;
-                l.ch.store(p, dx);
-                l.ch.store(p + d, df);
-            }
+            dz.store(r, dx, INSIDE || t0 + i < a.t, INSIDE || l.whole);
+            dz.store(r + d, df, INSIDE || t0 + i < a.t, INSIDE || l.whole);
+        }
+    };
+    const int first = l.segment * (seg_len / kScanBlock);
+    for (int blk = min(blocks, first + seg_len / kScanBlock) - 1; blk >= first; --blk) {
+        if (l.whole && (blk + 1) * kScanBlock <= len) {
+            block(blk, std::true_type{});
+        } else if (blk * kScanBlock < len) {
+            block(blk, std::false_type{});
+        } else {                                   // padding
+            const int t0 = blk * kScanBlock + l.run() * kSteps, tw = blk * kScanBlock + l.w * V * kSteps;
+            const float none[2] = {0.f, 0.f};
+            for (int i = 0; i < kSteps; ++i)
+                for (int k = 0; k < (OUT ? 3 : 2); ++k) dz.store(dz.row(tw + i) + k * d, none, t0 + i < a.t, l.whole);
         }
     }
     if (a.dh0 && l.segment == 0 && threadIdx.x < L::kRow)

@@ -67,7 +67,7 @@ def test_token_logprobs_bwd(lib, kw, status):
 # ----------------------------------------------------------------------------- recurrence
 _SCAN = [(dict(dt=7), DTYPE), (dict(b=-1), SHAPE), (dict(t=-1), SHAPE), (dict(d=0), SHAPE), (dict(gates=1), ARG),
          (dict(gates=4), ARG), (dict(b=1 << 31), OVERFLOW), (dict(t=1 << 30), OVERFLOW), (dict(d=(1 << 24) + 1), OVERFLOW),
-         (dict(b=1 << 20, t=1 << 20, d=8), OVERFLOW), (dict(zt=-8), OVERFLOW), (dict(zb=-8, zt=0), OVERFLOW),
+         (dict(b=1 << 20, t=1 << 20, d=8), OVERFLOW), (dict(zt=-8), OVERFLOW), (dict(zt=(1 << 25) + 1), OVERFLOW), (dict(yt=1 << 27), OVERFLOW), (dict(zb=-8, zt=0), OVERFLOW),
          (dict(zt=23, zb=24), SHAPE), (dict(zt=24, zb=30), SHAPE), (dict(zb=24, zt=24), SHAPE), (dict(yt=7, yb=100), SHAPE),
          (dict(z=0), NULL), (dict(z=P + 2), ALIGN), (dict(bias=P + 2 * M + 2), ALIGN), (dict(lengths=P + 3 * M + 1), ALIGN)]
 
