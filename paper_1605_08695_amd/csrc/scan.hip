@@ -11,8 +11,8 @@
 // and P = prod f, kept as 1 - P or P, whichever is smaller, in the same way.  Backwards, a span maps what comes from
 // behind, c, to R + P c.
 //
-// A workgroup has a strip of 64 channels of one sequence and takes it in blocks of kScanBlock tokens, each wave (or half
-// wave, with two bf16 channels a lane) a run of kSteps tokens of the block in registers; the waves' spans are joined
+// A workgroup of W waves has a strip of 64 channels of one sequence and takes it in blocks of W runs of 32 tokens, each
+// wave one run in registers (with two bf16 channels a lane each half wave half of it); the waves' spans are joined
 // through LDS, and the workgroup goes on to the next block with the state they leave.  Where there are too few strips
 // for the chip, the time axis is cut into segments: a first launch reads all segments but the last for what each makes
 // of the state before it (x and the gate; backwards the gate and dy), and in the second each workgroup joins those of the
@@ -28,7 +28,7 @@
 namespace tfk {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kWaves = 4;                          // waves of a workgroup
+constexpr int kRun = 32;                           // tokens of a wave's run, or of its half waves' two
 constexpr int kStrip = 64;                         // channels of a workgroup
 constexpr int kSegments = 64;                      // the most a sequence is cut into
 
@@ -42,6 +42,13 @@ __device__ __forceinline__ bool shut(float s) { return __float_as_int(s) < 0; }
 __device__ __forceinline__ float keeps(float s) { return shut(s) ? -s : 1.f - s; }          // f
 __device__ __forceinline__ float takes(float s) { return shut(s) ? 1.f + s : s; }           // 1 - f
 __device__ __forceinline__ float slope(float s) { return __builtin_fabsf(s) * (1.f - __builtin_fabsf(s)); }
+
+// The same number, as one that nothing computed from it before is known for: each pass over a run's gates then looks at
+// their signs anew, where the compiler else keeps them all, a pair of scalar registers each, and runs out of those.
+__device__ __forceinline__ float fresh(float s) {
+    asm volatile("" : "+v"(s));
+    return s;
+}
 
 // f h + (1 - f) x
 __device__ __forceinline__ float move(float h, float s, float x) { return __builtin_fmaf(s, x - h, shut(s) ? x : h); }
@@ -88,8 +95,7 @@ struct Chans<bf16_t, 2> {
 template <typename T, int V>
 struct Lane {
     static constexpr int kRow = 64 / V;                       // lanes of a row of the strip
-    static constexpr int kRuns = kWaves * V;                  // runs of tokens of a block
-    static constexpr int kSteps = kScanBlock / kRuns;
+    static constexpr int kSteps = kRun / V;                   // tokens a lane has in registers
     int sub, w, c, segment;
     int64_t b;
     bool whole;
@@ -98,7 +104,6 @@ struct Lane {
         : sub((threadIdx.x & 63) / kRow), w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
           c((int)(job % strips) * kStrip + (threadIdx.x % kRow) * V), segment((int)(job / strips % segments)),
           b(job / strips / segments), whole((int)(job % strips) * kStrip + kStrip <= d), ch(c, d) {}
-    __device__ __forceinline__ int run() const { return w * V + sub; }
 };
 
 // Rows of a sequence, read and written through buffer descriptors: an address that the wave's lanes share, in scalar
@@ -162,6 +167,16 @@ struct Span {
     }
 };
 
+struct ScanSegArgs {
+    const void *z;
+    int64_t z_bs, z_ts;
+    const float *bias;
+    const int32_t *lengths;
+    const void *dy;
+    int64_t dy_bs, dy_ts, b;
+    int t, d;
+};
+
 // A strip's state (or what comes from behind) at the border of a segment: h0 (dh_last), then the segments between.
 template <int V>
 __device__ __forceinline__ void join_segments(const float2 *agg, int64_t at, int64_t step, int n, int c, int d, float *H) {
@@ -179,88 +194,98 @@ __device__ __forceinline__ void join_segments(const float2 *agg, int64_t at, int
 }
 
 // What each segment but the last makes of the state before it (BWD: each but the first of what comes from behind it),
-// to agg[b][segment][channel].  A run is an eighth (a quarter) of the segment.
+// to agg[b][segment][channel].  Each of four waves takes a quarter of the segment, run by run.
 template <typename T, int V, bool OUT, bool BWD>
-__global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(const T *z0, int64_t z_bs, int64_t z_ts, const float *bias,
-                                                                    const int32_t *lengths, const T *dy0, int64_t dy_bs,
-                                                                    int64_t dy_ts, float2 *agg, int64_t nb, int t, int d,
-                                                                    int segments, int seg_len) {
-    constexpr int U = 8;
-    __shared__ Span spans[kWaves][kStrip];
-    const int strips = (d + kStrip - 1) / kStrip;
+__global__ __launch_bounds__(256) void scan_segments_kernel(ScanSegArgs a, float2 *agg, int segments, int seg_len) {
+    typedef Lane<T, V> L;
+    constexpr int kSteps = L::kSteps;
+    __shared__ Span spans[4][kStrip];
+    const int d = a.d, strips = (d + kStrip - 1) / kStrip;
     const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
-    if (job >= nb * strips * (segments - 1)) return;
-    Lane<T, V> l(job, strips, segments - 1, d);
+    if (job >= a.b * strips * (segments - 1)) return;
+    L l(job, strips, segments - 1, d);
     if (BWD) ++l.segment;
-    const int len = span_of(lengths, l.b, t);
-    const int per = seg_len / Lane<T, V>::kRuns;
-    const int begin = l.segment * seg_len + l.run() * per, end = min(begin + per, len);
-    const T *const z = z0 + l.b * z_bs, *const dy = BWD ? dy0 + l.b * dy_bs : nullptr;
+    const int len = span_of(a.lengths, l.b, a.t);
     float bx[V], bf[V], bo[V];
+    Span m[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         const int c = min(l.c + e, d - 1);
-        bx[e] = bias ? bias[c] : 0.f;
-        bf[e] = bias ? bias[d + c] : 0.f;
-        bo[e] = OUT && bias ? bias[2 * d + c] : 0.f;
+        bx[e] = a.bias ? a.bias[c] : 0.f;
+        bf[e] = a.bias ? a.bias[d + c] : 0.f;
+        bo[e] = OUT && a.bias ? a.bias[2 * d + c] : 0.f;
+        m[e] = Span{0.f, 0.f, 1.f};
     }
-    Span m[V];
+    const Rows<const T, V> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
+    const int quarter = l.segment * seg_len + l.w * (seg_len / 4);
+    const auto run = [&](int tw, auto inside) {
+        constexpr bool INSIDE = decltype(inside)::value;
+        const int t0 = tw + l.sub * kSteps;
+        typename Chans<T, V>::raw rx[kSteps], rf[kSteps], ro[OUT && BWD ? kSteps : 1];
+        const T *r = z.row(tw), *ry = BWD ? dy.row(tw) : nullptr;
 #pragma unroll
-    for (int e = 0; e < V; ++e) m[e] = Span{0.f, 0.f, 1.f};
-    for (int i = 0; begin + i < end; i += U) {
-        typename Chans<T, V>::raw rx[U], rf[U], ro[U];
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int at = BWD ? max(end - 1 - i - k, 0) : min(begin + i + k, t - 1);
-            const T *const p = z + at * z_ts + l.ch.at;
-            rx[k] = l.ch.load(BWD ? dy + at * dy_ts + l.ch.at : p);
-            rf[k] = l.ch.load(p + d);
-            if (OUT && BWD) ro[k] = l.ch.load(p + 2 * d);
+        for (int i = 0; i < kSteps; ++i) {
+            const bool in = INSIDE || t0 + i < len;
+            rx[i] = BWD ? dy.load(ry, in) : z.load(r, in);
+            rf[i] = z.load(r + d, in);
+            if (OUT && BWD) ro[i] = z.load(r + 2 * d, in);
+            r += z.ts;
+            if (BWD) ry += dy.ts;
         }
+        Span n[V];
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            if (begin + i + k >= end) break;
+        for (int e = 0; e < V; ++e) n[e] = Span{0.f, 0.f, 1.f};
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const int i = BWD ? kSteps - 1 - k : k;
             float x[V], f[V], o[V];
-            l.ch.unpack(rx[k], x);
-            l.ch.unpack(rf[k], f);
-            if (OUT && BWD) l.ch.unpack(ro[k], o);
+            l.ch.unpack(rx[i], x);
+            l.ch.unpack(rf[i], f);
+            if (OUT && BWD) l.ch.unpack(ro[i], o);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float s = gate(f[e] + bf[e]);
-                if (!BWD) {
-                    m[e].add(s, x[e] + bx[e]);
-                } else {
-                    m[e].S = kept(m[e].S + (OUT ? keeps(gate(o[e] + bo[e])) * x[e] : x[e]), s);
-                    m[e].Q = move(m[e].Q, s, 1.f);
-                    m[e].P = kept(m[e].P, s);
-                }
+                float s = gate(f[e] + bf[e]), v = BWD ? x[e] : x[e] + bx[e];
+                if (OUT && BWD) v *= keeps(gate(o[e] + bo[e]));
+                if (!INSIDE && t0 + i >= len) s = v = 0.f;
+                if (BWD) n[e].S = kept(n[e].S + v, s);
+                else n[e].S = move(n[e].S, s, v);
+                n[e].Q = move(n[e].Q, s, 1.f);
+                n[e].P = kept(n[e].P, s);
             }
         }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if (V == 2) {
+                const Span o = n[e].other_half();
+                const bool first = (l.sub == 0) != BWD;
+                n[e] = (first ? n[e] : o).then(first ? o : n[e]);
+            }
+            m[e] = m[e].then(n[e]);
+        }
+    };
+    const int runs = seg_len / 4 / kRun;
+    for (int k = 0; k < runs; ++k) {
+        const int tw = quarter + (BWD ? runs - 1 - k : k) * kRun;
+        if (tw + kRun <= len) run(tw, std::true_type{});
+        else if (tw < len) run(tw, std::false_type{});
     }
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        if (V == 2) {
-            const Span o = m[e].other_half();
-            const bool first = BWD ? l.sub == 1 : l.sub == 0;
-            const Span a = first ? m[e] : o, b = first ? o : m[e];
-            m[e] = a.then(b);
-        }
-        if (V == 1 || l.sub == e) spans[l.w][threadIdx.x % Lane<T, V>::kRow * V + e] = m[e];
-    }
+    for (int e = 0; e < V; ++e)
+        if (V == 1 || l.sub == e) spans[l.w][threadIdx.x % L::kRow * V + e] = m[e];
     __syncthreads();
     if (threadIdx.x >= kStrip) return;
-    Span a = spans[BWD ? kWaves - 1 : 0][threadIdx.x];
+    Span n = spans[BWD ? 3 : 0][threadIdx.x];
 #pragma unroll
-    for (int v = 1; v < kWaves; ++v) a = a.then(spans[BWD ? kWaves - 1 - v : v][threadIdx.x]);
+    for (int v = 1; v < 4; ++v) n = n.then(spans[BWD ? 3 - v : v][threadIdx.x]);
     const int c = (int)(job % strips) * kStrip + threadIdx.x;
-    if (c < d) agg[(l.b * segments + l.segment) * d + c] = make_float2(a.S, span(a.Q, a.P));
+    if (c < d) agg[(l.b * segments + l.segment) * d + c] = make_float2(n.S, span(n.Q, n.P));
 }
 
-template <typename T, int V, bool OUT>
-__global__ __launch_bounds__(64 * kWaves, OUT ? 3 : 4) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
+template <typename T, int V, bool OUT, int W>
+__global__ __launch_bounds__(64 * W, OUT ? 3 : 4) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V> L;
-    constexpr int kSteps = L::kSteps;
-    __shared__ float2 spans[2][kWaves][kStrip];
+    constexpr int kSteps = L::kSteps, kBlock = W * kRun;
+    __shared__ float2 spans[2][W][kStrip];
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
     const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (job >= a.b * strips * segments) return;
@@ -278,12 +303,12 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 3 : 4) void scan_fwd_kernel(Scan
     if (l.segment > 0) join_segments<V>(agg, l.b * segments * d, d, l.segment, l.c, d, H);
     const Rows<const T, V> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l);
     const Rows<T, V> y((T *)a.y + l.b * a.y_bs, a.y_ts, l);
-    const int blocks = (a.t + kScanBlock - 1) / kScanBlock;
+    const int blocks = (a.t + kBlock - 1) / kBlock, saved = (a.t + kScanBlock - 1) / kScanBlock;
     const int col = threadIdx.x % L::kRow * V;
     // INSIDE: all of the block's tokens and channels are there
     const auto block = [&](int blk, auto inside) {
         constexpr bool INSIDE = decltype(inside)::value;
-        const int t0 = blk * kScanBlock + l.run() * kSteps, tw = blk * kScanBlock + l.w * V * kSteps;
+        const int tw = blk * kBlock + l.w * kRun, t0 = tw + l.sub * kSteps;
         float s[kSteps][V], x[kSteps][V], o[OUT ? kSteps : 1][V];
         {
             typename Chans<T, V>::raw rx[kSteps], rf[kSteps], ro[OUT ? kSteps : 1];
@@ -329,9 +354,9 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 3 : 4) void scan_fwd_kernel(Scan
         float h[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            if (a.states && threadIdx.x < L::kRow && l.c + e < d) a.states[(l.b * blocks + blk) * d + l.c + e] = H[e];
+            if (a.states && threadIdx.x < L::kRow && l.c + e < d) a.states[(l.b * saved + blk) * d + l.c + e] = H[e];
 #pragma unroll
-            for (int v = 0; v < kWaves; ++v) {
+            for (int v = 0; v < W; ++v) {
                 if (v == l.w) h[e] = H[e];
                 const float2 q = spans[blk & 1][v][col + e];
                 H[e] = join(H[e], q.y, q.x);
@@ -344,20 +369,20 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 3 : 4) void scan_fwd_kernel(Scan
             float out[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                h[e] = move(h[e], s[i][e], x[i][e]);
+                h[e] = move(h[e], fresh(s[i][e]), x[i][e]);
                 out[e] = OUT ? o[i][e] * h[e] : h[e];
                 if (!INSIDE && t0 + i >= len) out[e] = 0.f;
             }
             y.store(r, out, INSIDE || t0 + i < a.t, INSIDE || l.whole);
         }
     };
-    for (int blk = l.segment * (seg_len / kScanBlock); blk < min(blocks, (l.segment + 1) * (seg_len / kScanBlock)); ++blk) {
-        if (l.whole && (blk + 1) * kScanBlock <= len) {
+    for (int blk = l.segment * (seg_len / kBlock); blk < min(blocks, (l.segment + 1) * (seg_len / kBlock)); ++blk) {
+        if (l.whole && (blk + 1) * kBlock <= len) {
             block(blk, std::true_type{});
-        } else if (blk * kScanBlock < len) {
+        } else if (blk * kBlock < len) {
             block(blk, std::false_type{});
         } else {                                   // padding from here on
-            const int t0 = blk * kScanBlock + l.run() * kSteps, tw = blk * kScanBlock + l.w * V * kSteps;
+            const int tw = blk * kBlock + l.w * kRun, t0 = tw + l.sub * kSteps;
             const float none[2] = {0.f, 0.f};
             for (int i = 0; i < kSteps; ++i)
                 y.store(y.row(tw + i), none, t0 + i < a.t, l.whole);
@@ -369,12 +394,12 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 3 : 4) void scan_fwd_kernel(Scan
             if (l.c + e < d) a.h_last[l.b * d + l.c + e] = H[e];
 }
 
-template <typename T, int V, bool OUT>
-__global__ __launch_bounds__(64 * kWaves, OUT ? 2 : 3) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
+template <typename T, int V, bool OUT, int W>
+__global__ __launch_bounds__(64 * W, OUT ? 2 : 3) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V> L;
-    constexpr int kSteps = L::kSteps;
-    __shared__ float2 spans[2][kWaves][kStrip];
-    __shared__ float backs[2][kWaves][kStrip];
+    constexpr int kSteps = L::kSteps, kBlock = W * kRun;
+    __shared__ float2 spans[2][W][kStrip];
+    __shared__ float backs[2][W][kStrip];
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
     const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (job >= a.b * strips * segments) return;
@@ -393,11 +418,11 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 2 : 3) void scan_bwd_kernel(Scan
         join_segments<V>(agg, (l.b * segments + segments - 1) * d, -(int64_t)d, segments - 1 - l.segment, l.c, d, C);
     const Rows<const T, V> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
     const Rows<T, V> dz((T *)a.dz + l.b * a.dz_bs, a.dz_ts, l);
-    const int blocks = (a.t + kScanBlock - 1) / kScanBlock;
+    const int blocks = (a.t + kBlock - 1) / kBlock, saved = (a.t + kScanBlock - 1) / kScanBlock;
     const int col = threadIdx.x % L::kRow * V;
     const auto block = [&](int blk, auto inside) {
         constexpr bool INSIDE = decltype(inside)::value;
-        const int t0 = blk * kScanBlock + l.run() * kSteps, tw = blk * kScanBlock + l.w * V * kSteps;
+        const int tw = blk * kBlock + l.w * kRun, t0 = tw + l.sub * kSteps;
         float s[kSteps][V], x[kSteps][V], up[kSteps][V], o[OUT ? kSteps : 1][V], h[V];
         {
             typename Chans<T, V>::raw rx[kSteps], rf[kSteps], ru[kSteps], ro[OUT ? kSteps : 1];
@@ -411,7 +436,7 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 2 : 3) void scan_bwd_kernel(Scan
                 if (OUT) ro[i] = z.load(r + 2 * d, in);
             }
 #pragma unroll
-            for (int e = 0; e < V; ++e) h[e] = a.states[(l.b * blocks + blk) * d + min(l.c + e, d - 1)];
+            for (int e = 0; e < V; ++e) h[e] = a.states[(l.b * saved + blk) * d + min(l.c + e, d - 1)];
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 l.ch.unpack(rx[i], x[i]);
@@ -440,7 +465,7 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 2 : 3) void scan_bwd_kernel(Scan
 #pragma unroll
         for (int i = kSteps - 1; i >= 0; --i)
 #pragma unroll
-            for (int e = 0; e < V; ++e) R[e] = kept(R[e] + (OUT ? keeps(o[i][e]) * up[i][e] : up[i][e]), s[i][e]);
+            for (int e = 0; e < V; ++e) R[e] = kept(R[e] + (OUT ? keeps(fresh(o[i][e])) * up[i][e] : up[i][e]), fresh(s[i][e]));
         float half_S[V], half_s[V], half_R[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -464,12 +489,12 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 2 : 3) void scan_bwd_kernel(Scan
 #pragma unroll
         for (int e = 0; e < V; ++e) {
 #pragma unroll
-            for (int v = 0; v < kWaves - 1; ++v) {
+            for (int v = 0; v < W - 1; ++v) {
                 const float2 q = spans[blk & 1][v][col + e];
                 if (v < l.w) h[e] = join(h[e], q.y, q.x);
             }
 #pragma unroll
-            for (int v = kWaves - 1; v >= 0; --v) {
+            for (int v = W - 1; v >= 0; --v) {
                 if (v == l.w) c[e] = C[e];
                 C[e] = join(C[e], spans[blk & 1][v][col + e].y, backs[blk & 1][v][col + e]);
             }
@@ -486,11 +511,12 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 2 : 3) void scan_bwd_kernel(Scan
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float before = h[e];
-                h[e] = move(before, s[i][e], x[i][e]);
+                h[e] = move(before, fresh(s[i][e]), x[i][e]);
                 x[i][e] = before - x[i][e];
                 if (OUT) {
-                    out[e] = slope(o[i][e]) * up[i][e] * h[e];
-                    up[i][e] *= keeps(o[i][e]);
+                    const float so = fresh(o[i][e]);
+                    out[e] = slope(so) * up[i][e] * h[e];
+                    up[i][e] *= keeps(so);
                     if (!INSIDE && t0 + i >= len) out[e] = 0.f;
                 }
             }
@@ -502,24 +528,24 @@ __global__ __launch_bounds__(64 * kWaves, OUT ? 2 : 3) void scan_bwd_kernel(Scan
             float dx[V], df[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float g = c[e] + up[i][e];
-                c[e] = kept(g, s[i][e]);
+                const float g = c[e] + up[i][e], si = fresh(s[i][e]);
+                c[e] = kept(g, si);
                 const bool in = INSIDE || t0 + i < len;
-                dx[e] = in ? takes(s[i][e]) * g : 0.f;
-                df[e] = in ? x[i][e] * (slope(s[i][e]) * g) : 0.f;
+                dx[e] = in ? takes(si) * g : 0.f;
+                df[e] = in ? x[i][e] * (slope(si) * g) : 0.f;
             }
             dz.store(r, dx, INSIDE || t0 + i < a.t, INSIDE || l.whole);
             dz.store(r + d, df, INSIDE || t0 + i < a.t, INSIDE || l.whole);
         }
     };
-    const int first = l.segment * (seg_len / kScanBlock);
-    for (int blk = min(blocks, first + seg_len / kScanBlock) - 1; blk >= first; --blk) {
-        if (l.whole && (blk + 1) * kScanBlock <= len) {
+    const int first = l.segment * (seg_len / kBlock);
+    for (int blk = min(blocks, first + seg_len / kBlock) - 1; blk >= first; --blk) {
+        if (l.whole && (blk + 1) * kBlock <= len) {
             block(blk, std::true_type{});
-        } else if (blk * kScanBlock < len) {
+        } else if (blk * kBlock < len) {
             block(blk, std::false_type{});
         } else {                                   // padding
-            const int t0 = blk * kScanBlock + l.run() * kSteps, tw = blk * kScanBlock + l.w * V * kSteps;
+            const int tw = blk * kBlock + l.w * kRun, t0 = tw + l.sub * kSteps;
             const float none[2] = {0.f, 0.f};
             for (int i = 0; i < kSteps; ++i)
                 for (int k = 0; k < (OUT ? 3 : 2); ++k) dz.store(dz.row(tw + i) + k * d, none, t0 + i < a.t, l.whole);
@@ -576,12 +602,16 @@ static void launch_fwd(const ScanArgs &a, float2 *ws, hipStream_t st) {
     int segments, seg_len;
     scan_plan(a.b, a.t, a.d, &segments, &seg_len);
     const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
-    if (segments > 1)
-        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, false>), grid_2d(strips * (segments - 1)), dim3(64 * kWaves), 0, st,
-                           (const T *)a.z, a.z_bs, a.z_ts, a.bias, a.lengths, (const T *)nullptr, 0, 0, ws, a.b, a.t, a.d,
+    if (a.t <= kRun) {
+        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 1>), grid_2d(strips), dim3(64), 0, st, a, ws, 1, kRun);
+        return;
+    }
+    if (segments > 1) {
+        const ScanSegArgs g{a.z, a.z_bs, a.z_ts, a.bias, a.lengths, nullptr, 0, 0, a.b, a.t, a.d};
+        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, false>), grid_2d(strips * (segments - 1)), dim3(256), 0, st, g, ws,
                            segments, seg_len);
-    hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT>), grid_2d(strips * segments), dim3(64 * kWaves), 0, st, a, ws, segments,
-                       seg_len);
+    }
+    hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 4>), grid_2d(strips * segments), dim3(256), 0, st, a, ws, segments, seg_len);
 }
 
 template <typename T, int V, bool OUT>
@@ -589,12 +619,16 @@ static void launch_bwd(const ScanBwdArgs &a, float2 *ws, hipStream_t st) {
     int segments, seg_len;
     scan_plan(a.b, a.t, a.d, &segments, &seg_len);
     const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
-    if (segments > 1)
-        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, true>), grid_2d(strips * (segments - 1)), dim3(64 * kWaves), 0, st,
-                           (const T *)a.z, a.z_bs, a.z_ts, a.bias, a.lengths, (const T *)a.dy, a.dy_bs, a.dy_ts, ws, a.b, a.t,
-                           a.d, segments, seg_len);
-    hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT>), grid_2d(strips * segments), dim3(64 * kWaves), 0, st, a, ws, segments,
-                       seg_len);
+    if (a.t <= kRun) {
+        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 1>), grid_2d(strips), dim3(64), 0, st, a, ws, 1, kRun);
+        return;
+    }
+    if (segments > 1) {
+        const ScanSegArgs g{a.z, a.z_bs, a.z_ts, a.bias, a.lengths, a.dy, a.dy_bs, a.dy_ts, a.b, a.t, a.d};
+        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, true>), grid_2d(strips * (segments - 1)), dim3(256), 0, st, g, ws,
+                           segments, seg_len);
+    }
+    hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 4>), grid_2d(strips * segments), dim3(256), 0, st, a, ws, segments, seg_len);
 }
 
 #define SCAN_CASES(fn, ...)                                                         \
