@@ -9,6 +9,7 @@
 // not larger.  The step itself is made with the moments before they are rounded.
 #include "common.h"
 #include "kernels.h"
+#include "rowvec.h"
 
 #pragma clang fp contract(off)
 
@@ -16,87 +17,166 @@ namespace tfk {
 
 constexpr float kTop = 448.f, kLeast = 0x1p-9f, kNothing = 0x1p-100f;
 
-__device__ __forceinline__ float wave_max_bits(float v) {
-    uint32_t b = __float_as_uint(v) & 0x7fffffffu;        // as whole numbers NaN is the largest
-    for (int o = 32; o > 0; o >>= 1) b = max(b, (uint32_t)__shfl_xor((int)b, o));
-    return __uint_as_float(b);
+// The largest magnitude of a wave's values, by whole numbers: NaN is the largest of all.
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_swap(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ float wave_top(const float *x) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b = max(b, __float_as_uint(x[e]) & 0x7fffffffu);
+    b = max(b, lane_swap<0xb1>(b));                       // neighbours, pairs, mirrored eights and sixteens
+    b = max(b, lane_swap<0x4e>(b));
+    b = max(b, lane_swap<0x141>(b));
+    b = max(b, lane_swap<0x140>(b));
+    const uint32_t lo = max((uint32_t)__builtin_amdgcn_readlane((int)b, 0), (uint32_t)__builtin_amdgcn_readlane((int)b, 16));
+    const uint32_t hi = max((uint32_t)__builtin_amdgcn_readlane((int)b, 32), (uint32_t)__builtin_amdgcn_readlane((int)b, 48));
+    return __uint_as_float(max(lo, hi));
 }
 
-__device__ __forceinline__ float step_of(float m, float v, const AdamwParams &p) {
-    return p.lr * m / (__builtin_sqrtf(v * p.rc2) + p.eps);
+// One value's step.  The moments are rounded operation by operation, as they are written: an e4m3 value then does not
+// depend on how a compiler joins a product and a sum.
+__device__ __forceinline__ void step_of(float &var, float g, float &m, float &v, float &root, float decay, const AdamwParams &p) {
+    m = p.b1 * m + p.omb1 * g;
+    v = p.b2 * v + p.omb2 * g * g;
+    root = __builtin_sqrtf(v);
+    const float den = __builtin_fmaf(root, p.rrc2, p.eps);
+    var = __builtin_fmaf(-decay, var, var) - p.lr * m * __builtin_amdgcn_rcpf(den);
 }
 
-// One wave has one block of 256 values, four a lane.
-template <bool BITS8>
+// The factor of a block whose largest magnitude is top, and what its values are multiplied by.
+__device__ __forceinline__ float factor(float top, float &inv) {
+    const bool none = top < kNothing;
+    inv = none ? 0.f : kTop / top;
+    return none ? 0.f : top < INFINITY ? top / kTop : NAN;
+}
+__device__ __forceinline__ float code_m(float m, float inv) { return __builtin_amdgcn_fmed3f(m * inv, -kTop, kTop); }
+__device__ __forceinline__ float code_v(float root, float inv) {
+    return root > 0.f && inv > 0.f ? __builtin_amdgcn_fmed3f(root * inv, kLeast, kTop) : 0.f;
+}
+
+template <bool AWAY>
+__device__ __forceinline__ f32x4_t get4(const float *p) {
+    return AWAY ? RowVec<float, 4>::load_last(p) : RowVec<float, 4>::load(p);
+}
+template <bool AWAY>
+__device__ __forceinline__ void put4(float *p, const float *v) {
+    if (AWAY) RowVec<float, 4>::store_away(p, v);
+    else RowVec<float, 4>::store(p, v);
+}
+typedef uint32_t u32_a1_t __attribute__((aligned(1)));
+
+// One wave has one block of 256 values, four neighbouring ones a lane.  AWAY: past the caches, which the whole is too
+// much for.
+template <bool BITS8, bool AWAY>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch b, AdamwParams p) {
-    const int64_t blk0 = (blockIdx.x + (int64_t)blockIdx.y * gridDim.x) * 4 + (threadIdx.x >> 6);
+    const int64_t blk0 = (blockIdx.x + (int64_t)blockIdx.y * gridDim.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (blk0 >= b.blk_start[b.count]) return;
     int i = 0;
-    while (blk0 >= b.blk_start[i + 1]) ++i;
-    const int64_t blk = blk0 - b.blk_start[i], n = b.n[i];
-    float m[4], v[4];
+    for (int half = 32; half > 0; half >>= 1)             // the last variable that begins at or before blk0
+        if (i + half < b.count && blk0 >= b.blk_start[i + half]) i += half;
+    const int64_t blk = blk0 - b.blk_start[i];
+    const int64_t at = blk * 256 + 4 * lane;
+    const int there = (int)min((int64_t)4, max((int64_t)0, b.n[i] - at));      // of the lane's four
+    const bool whole = b.n[i] - blk * 256 >= 256;
+    const float decay = b.decay[i];
+    float *const pv = b.var[i] + at;
+    const float *const pg = b.grad[i] + at;
+    uint16_t *const ps = b.shadow[i] ? b.shadow[i] + at : nullptr;
+    float var[4], g[4], m[4], v[4], root[4];
     float ms = 0.f, vs = 0.f;
     if (BITS8) {
         ms = b.m_scale[i][blk];
         vs = b.v_scale[i][blk];
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int64_t at = blk * 256 + lane + 64 * e;
-        m[e] = v[e] = 0.f;
-        if (at >= n) continue;
-        const float g = b.grad[i][at];
-        float var = b.var[i][at];
+    if (whole) {
+        RowVec<float, 4>::unpack(get4<AWAY>(pv), var);
+        RowVec<float, 4>::unpack(get4<AWAY>(pg), g);
         if (BITS8) {
-            m[e] = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)b.m[i])[at], 0) * ms;
-            const float root = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)b.v[i])[at], 0) * vs;
-            v[e] = root * root;
+            const uint32_t cm = *reinterpret_cast<const u32_a1_t *>((const uint8_t *)b.m[i] + at);
+            const uint32_t cv = *reinterpret_cast<const u32_a1_t *>((const uint8_t *)b.v[i] + at);
+            m[0] = __builtin_amdgcn_cvt_f32_fp8(cm, 0), m[1] = __builtin_amdgcn_cvt_f32_fp8(cm, 1);
+            m[2] = __builtin_amdgcn_cvt_f32_fp8(cm, 2), m[3] = __builtin_amdgcn_cvt_f32_fp8(cm, 3);
+            v[0] = __builtin_amdgcn_cvt_f32_fp8(cv, 0), v[1] = __builtin_amdgcn_cvt_f32_fp8(cv, 1);
+            v[2] = __builtin_amdgcn_cvt_f32_fp8(cv, 2), v[3] = __builtin_amdgcn_cvt_f32_fp8(cv, 3);
         } else {
-            m[e] = ((const float *)b.m[i])[at];
-            v[e] = ((const float *)b.v[i])[at];
+            RowVec<float, 4>::unpack(get4<AWAY>((const float *)b.m[i] + at), m);
+            RowVec<float, 4>::unpack(get4<AWAY>((const float *)b.v[i] + at), v);
         }
-        m[e] = p.b1 * m[e] + p.omb1 * g;
-        v[e] = p.b2 * v[e] + p.omb2 * g * g;
-        var = __builtin_fmaf(-b.decay[i], var, var) - step_of(m[e], v[e], p);
-        b.var[i][at] = var;
-        if (b.shadow[i]) b.shadow[i][at] = (uint16_t)f32_to_bf16(var);
-        if (!BITS8) {
-            ((float *)b.m[i])[at] = m[e];
-            ((float *)b.v[i])[at] = v[e];
-        }
-    }
-    if (!BITS8) return;
-    float root[4], mt = 0.f, vt = 0.f;
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        root[e] = __builtin_sqrtf(v[e]);
-        mt = __uint_as_float(max(__float_as_uint(mt), __float_as_uint(m[e]) & 0x7fffffffu));
-        vt = __uint_as_float(max(__float_as_uint(vt), __float_as_uint(root[e]) & 0x7fffffffu));
-    }
-    mt = wave_max_bits(mt);
-    vt = wave_max_bits(vt);
-    const float mi = mt < kNothing ? 0.f : kTop / mt, vi = vt < kNothing ? 0.f : kTop / vt;
-    if (lane == 0) {
-        b.m_scale[i][blk] = mt < kNothing ? 0.f : mt < INFINITY ? mt / kTop : NAN;
-        b.v_scale[i][blk] = vt < kNothing ? 0.f : vt < INFINITY ? vt / kTop : NAN;
+        for (int e = 0; e < 4; ++e) {
+            var[e] = g[e] = m[e] = v[e] = 0.f;
+            if (e >= there) continue;
+            var[e] = pv[e];
+            g[e] = pg[e];
+            if (BITS8) {
+                m[e] = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)b.m[i])[at + e], 0);
+                v[e] = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)b.v[i])[at + e], 0);
+            } else {
+                m[e] = ((const float *)b.m[i])[at + e];
+                v[e] = ((const float *)b.v[i])[at + e];
+            }
+        }
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int64_t at = blk * 256 + lane + 64 * e;
-        if (at >= n) continue;
-        const float x = fminf(fmaxf(m[e] * mi, -kTop), kTop);
-        const float r = root[e] > 0.f && vi > 0.f ? fminf(fmaxf(root[e] * vi, kLeast), kTop) : 0.f;
-        const int two = __builtin_amdgcn_cvt_pk_fp8_f32(x, r, 0, false);
-        ((uint8_t *)b.m[i])[at] = (uint8_t)(two & 0xff);
-        ((uint8_t *)b.v[i])[at] = (uint8_t)(two >> 8 & 0xff);
+        if (BITS8) {
+            m[e] *= ms;
+            v[e] *= vs;
+            v[e] *= v[e];
+        }
+        step_of(var[e], g[e], m[e], v[e], root[e], decay, p);
+        if (!whole && e >= there) m[e] = root[e] = 0.f;     // beyond the variable, whatever its block's factors are
+    }
+    uint32_t cm = 0, cv = 0;
+    if (BITS8) {
+        float mi, vi;
+        const float fm = factor(wave_top(m), mi), fv = factor(wave_top(root), vi);
+        if (lane == 0) {
+            b.m_scale[i][blk] = fm;
+            b.v_scale[i][blk] = fv;
+        }
+        cm = __builtin_amdgcn_cvt_pk_fp8_f32(code_m(m[0], mi), code_m(m[1], mi), 0, false);
+        cm = __builtin_amdgcn_cvt_pk_fp8_f32(code_m(m[2], mi), code_m(m[3], mi), cm, true);
+        cv = __builtin_amdgcn_cvt_pk_fp8_f32(code_v(root[0], vi), code_v(root[1], vi), 0, false);
+        cv = __builtin_amdgcn_cvt_pk_fp8_f32(code_v(root[2], vi), code_v(root[3], vi), cv, true);
+    }
+    if (whole) {
+        put4<AWAY>(pv, var);
+        if (ps) RowVec<bf16_t, 4>::store(ps, var);
+        if (BITS8) {
+            *reinterpret_cast<u32_a1_t *>((uint8_t *)b.m[i] + at) = cm;
+            *reinterpret_cast<u32_a1_t *>((uint8_t *)b.v[i] + at) = cv;
+        } else {
+            put4<AWAY>((float *)b.m[i] + at, m);
+            put4<AWAY>((float *)b.v[i] + at, v);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (e >= there) break;
+        pv[e] = var[e];
+        if (ps) ps[e] = (uint16_t)f32_to_bf16(var[e]);
+        if (BITS8) {
+            ((uint8_t *)b.m[i])[at + e] = (uint8_t)(cm >> 8 * e);
+            ((uint8_t *)b.v[i])[at + e] = (uint8_t)(cv >> 8 * e);
+        } else {
+            ((float *)b.m[i])[at + e] = m[e];
+            ((float *)b.v[i])[at + e] = v[e];
+        }
     }
 }
 
-hipError_t launch_adamw(bool bits8, const AdamwBatch &b, const AdamwParams &p, hipStream_t st) {
-    const int64_t blocks = (b.blk_start[b.count] + 3) / 4;
-    if (bits8) hipLaunchKernelGGL(adamw_kernel<true>, grid_2d(blocks), dim3(256), 0, st, b, p);
-    else hipLaunchKernelGGL(adamw_kernel<false>, grid_2d(blocks), dim3(256), 0, st, b, p);
+hipError_t launch_adamw(bool bits8, const AdamwBatch &b, const AdamwParams &p, bool away, hipStream_t st) {
+    const dim3 grid = grid_2d((b.blk_start[b.count] + 3) / 4);
+    if (bits8 && away) hipLaunchKernelGGL((adamw_kernel<true, true>), grid, dim3(256), 0, st, b, p);
+    else if (bits8) hipLaunchKernelGGL((adamw_kernel<true, false>), grid, dim3(256), 0, st, b, p);
+    else if (away) hipLaunchKernelGGL((adamw_kernel<false, true>), grid, dim3(256), 0, st, b, p);
+    else hipLaunchKernelGGL((adamw_kernel<false, false>), grid, dim3(256), 0, st, b, p);
     return hipGetLastError();
 }
 

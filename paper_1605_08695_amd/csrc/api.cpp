@@ -1540,8 +1540,8 @@ tfk_status tfk_apply_adamw_multi(int32_t count, int32_t bits, float *const *vars
     if (bits == 8) TRY(need_ptr(v_scales, "v_scales"));
     const double c1 = 1.0 - pow(beta1, (double)t), c2 = 1.0 - pow(beta2, (double)t);
     const AdamwParams q{(float)(lr / c1), (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2),
-                        (float)(1.0 / c2), (float)epsilon};
-    if (!isfinite(q.lr) || !isfinite(q.rc2) || !isfinite(q.eps)) return fail(TFK_ERR_OVERFLOW, "bias-corrected step overflows fp32");
+                        (float)(1.0 / sqrt(c2)), (float)epsilon};
+    if (!isfinite(q.lr) || !isfinite(q.rrc2) || !isfinite(q.eps)) return fail(TFK_ERR_OVERFLOW, "bias-corrected step overflows fp32");
     for (int i = 0; i < count; ++i) {
         const double wd = weight_decay ? weight_decay[i] : 0.;
         const int64_t n = ns[i], blocks = (n + 255) / 256, mb = bits == 8 ? n : n * 4;
@@ -1566,6 +1566,10 @@ tfk_status tfk_apply_adamw_multi(int32_t count, int32_t bits, float *const *vars
         if (s != TFK_OK) return fail(s, "variable %d: %s", i, std::string(g_err).c_str());
     }
     TRY(check_apart(count, vars, ns));
+    int64_t values = 0;
+    for (int j = 0; j < count; ++j) values += ns[j];
+    // what a step moves is read again in the next one: past the caches where they could not hold it until then
+    const bool away = values > kAdamwAway;
     int i = 0;
     while (i < count) {
         AdamwBatch b;
@@ -1589,7 +1593,7 @@ tfk_status tfk_apply_adamw_multi(int32_t count, int32_t bits, float *const *vars
             b.blk_start[k + 1] = (int)(b.blk_start[k] + blocks);
         }
         if (b.count == 0) continue;
-        const hipError_t e = launch_adamw(bits == 8, b, q, (hipStream_t)stream);
+        const hipError_t e = launch_adamw(bits == 8, b, q, away, (hipStream_t)stream);
         if (e != hipSuccess) return hip_status(e, "apply_adamw_multi");
     }
     return ok();

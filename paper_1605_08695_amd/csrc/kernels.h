@@ -284,9 +284,10 @@ hipError_t launch_logprob(int dt, const LogprobArgs &a, hipStream_t st);
 hipError_t launch_logprob_bwd(int dt, const LogprobBwdArgs &a, hipStream_t st);
 // AdamW over a batch of variables; blocks of 256 values, numbered through the batch.  m, v: fp32, or e4m3
 // values with a scale per block.
-constexpr int kAdamwBatch = 44;
+constexpr int kAdamwBatch = 55;               // (a batch is an argument of the kernel: below 4 KB)
+constexpr int64_t kAdamwAway = (int64_t)12 << 20;   // values of a step past the caches
 struct AdamwParams {
-    float lr, b1, omb1, b2, omb2, rc2, eps;      // lr and rc2 hold the bias corrections
+    float lr, b1, omb1, b2, omb2, rrc2, eps;     // lr = lr / (1 - b1^t), rrc2 = 1 / sqrt(1 - b2^t)
 };
 struct AdamwBatch {
     int count;
@@ -299,7 +300,7 @@ struct AdamwBatch {
     float *m_scale[kAdamwBatch], *v_scale[kAdamwBatch];
     uint16_t *shadow[kAdamwBatch];
 };
-hipError_t launch_adamw(bool bits8, const AdamwBatch &b, const AdamwParams &p, hipStream_t st);
+hipError_t launch_adamw(bool bits8, const AdamwBatch &b, const AdamwParams &p, bool away, hipStream_t st);
 // Momentum (kind 0, 1 = look-ahead form) and Adam (kind 2) in place over n fp32 elements.
 hipError_t launch_opt(int kind, float *var, float *s1, float *s2, const float *grad, int64_t n, const OptParams &p,
                       uint16_t *sh, hipStream_t st);
