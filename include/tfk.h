@@ -525,6 +525,8 @@ TFK_API tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n,
  *   tokens   : int32 [n], or NULL (logp must be NULL then).  A token outside [0, c) is padding: its row's
  *              logits are not read, its logp, entropy and lse are 0 and its list is all -1 and -inf.
  *   logp, entropy, lse : fp32 [n], each may be NULL.     top_idx, top_logp : n x k dense, int32 and fp32.
+ *   ws       : at least tfk_token_logprobs_workspace_bytes(n, c, k) bytes (may be NULL when that is 0), 16-byte
+ *              aligned; calls that may overlap in time need one each.
  * Finite logits are numbers whatever their size (masks of -1e9, -1e30 or the type's lowest value), where
  * fp32 holds the differences between the row's.  A row of -inf throughout has lse -inf, logp -inf, entropy
  * 0 and no list.  A row with a NaN or +inf has NaN in logp, entropy, lse and top_logp, and -1 in top_idx.
@@ -532,10 +534,15 @@ TFK_API tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n,
  * rest of the mass counts as one class); at another T the teacher's logits are T top_logp.
  * Errors: n < 0, c < 1, k not in 0..128, a row distance below c (SHAPE); temperature not in [1e-4, 1e4] (ARG);
  * n > 2^31 - 1, c > 2^30 or n times a row distance > 2^40 (OVERFLOW); NULL, misaligned (to the element) or
- * overlapping buffers (NULL, ALIGN, ALIAS).  n == 0 is a no-op. */
+ * overlapping buffers (NULL, ALIGN, ALIAS); WORKSPACE.  n == 0 is a no-op. */
 TFK_API tfk_status tfk_token_logprobs(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld,
                               const float *bias, const int32_t *tokens, float temperature, int32_t k, float *logp,
-                              float *entropy, float *lse, int32_t *top_idx, float *top_logp, void *stream);
+                              float *entropy, float *lse, int32_t *top_idx, float *top_logp, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/* Workspace of tfk_token_logprobs (of Section 4.2's heads) for n rows of c classes; 0 for arguments it refuses and
+ * where it needs none (all but few long rows). */
+TFK_API size_t tfk_token_logprobs_workspace_bytes(int64_t n, int32_t c, int32_t k);
 
 /* Gradient of logp and entropy (Section 4.1's backpropagation, from what a loss makes of the two):
  *   dlogits[i][j] = (dlogp[i] ([j == tokens[i]] - p_j) - dentropy[i] p_j (log p_j + entropy[i])) / T

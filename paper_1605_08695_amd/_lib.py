@@ -26,7 +26,7 @@ EXPORTS = ["tfk_conv2d_fwd", "tfk_conv2d_fwd_bias_relu", "tfk_maxpool_bwd_relu_b
            "tfk_apply_momentum", "tfk_apply_adam", "tfk_softmax_xent", "tfk_gather_rows_t",
            "tfk_sampled_softmax_xent", "tfk_scatter_apply_sgd", "tfk_distill_xent", "tfk_embedding_fwd",
            "tfk_embedding_bwd", "tfk_embedding_apply_sgd", "tfk_embedding_workspace_bytes",
-           "tfk_token_logprobs", "tfk_token_logprobs_bwd", "tfk_gated_scan_fwd", "tfk_gated_scan_bwd", "tfk_gated_scan_step",
+           "tfk_token_logprobs", "tfk_token_logprobs_workspace_bytes", "tfk_token_logprobs_bwd", "tfk_gated_scan_fwd", "tfk_gated_scan_bwd", "tfk_gated_scan_step",
            "tfk_gated_scan_workspace_bytes", "tfk_apply_adamw_multi", "tfk_stream_wait", "tfk_mark_create", "tfk_mark_destroy",
            "tfk_mark_record", "tfk_stream_wait_mark", "tfk_program_create",
            "tfk_program_destroy", "tfk_program_begin", "tfk_program_end", "tfk_program_length", "tfk_program_run",
@@ -100,7 +100,9 @@ def load(path: str = LIB_PATH):
     lib.tfk_embedding_apply_sgd.argtypes = [vp, vp, i64, i32, vp, i64, vp, st, i64, f32, f32, vp, sz, vp]
     lib.tfk_embedding_workspace_bytes.argtypes = [i64, i32, i64]
     lib.tfk_embedding_workspace_bytes.restype = sz
-    lib.tfk_token_logprobs.argtypes = [vp, st, i64, i32, i64, vp, vp, f32, i32, vp, vp, vp, vp, vp, vp]
+    lib.tfk_token_logprobs.argtypes = [vp, st, i64, i32, i64, vp, vp, f32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.tfk_token_logprobs_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.tfk_token_logprobs_workspace_bytes.restype = sz
     lib.tfk_token_logprobs_bwd.argtypes = [vp, st, i64, i32, i64, vp, vp, f32, vp, vp, vp, vp, vp, i64, vp]
     lib.tfk_gated_scan_fwd.argtypes = [vp, st, i64, i64, i32, i32, i64, i64, vp, vp, vp, vp, i64, i64, vp, vp, vp, sz, vp]
     lib.tfk_gated_scan_bwd.argtypes = [vp, st, i64, i64, i32, i32, i64, i64, vp, vp, vp, i64, i64, vp, vp, vp, i64, i64, vp,

@@ -1119,25 +1119,32 @@ static tfk_status check_logits(const void *logits, tfk_dtype dt, int64_t n, int3
 
 tfk_status tfk_token_logprobs(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld, const float *bias,
                               const int32_t *tokens, float temperature, int32_t k, float *logp, float *entropy, float *lse,
-                              int32_t *top_idx, float *top_logp, void *stream) {
+                              int32_t *top_idx, float *top_logp, void *ws, size_t ws_bytes, void *stream) {
     RECORDED(tfk_token_logprobs, logits, dt, n, c, logits_ld, bias, tokens, temperature, k, logp, entropy, lse, top_idx,
-             top_logp, stream);
+             top_logp, ws, ws_bytes, stream);
     TRY(check_logits(logits, dt, n, c, logits_ld, bias, tokens, temperature));
     if (k < 0 || k > 128) return fail(TFK_ERR_SHAPE, "k must be in 0..128 (got %d)", k);
     if (n == 0) return ok();
     if (logp) TRY(need_ptr(tokens, "tokens"));
     if (k > 0) TRY(need_ptr(top_idx, "top_idx"));
     if (k > 0) TRY(need_ptr(top_logp, "top_logp"));
-    const void *p[8] = {logp, entropy, lse, k ? top_idx : nullptr, k ? top_logp : nullptr, logits, bias, tokens};
-    const int64_t b[8] = {n * 4, n * 4, n * 4, n * k * 4, n * k * 4, rows_bytes(n, c, logits_ld, esize(dt)), (int64_t)c * 4,
-                          n * 4};
-    const char *const name[5] = {"logp", "entropy", "lse", "top_idx", "top_logp"};
+    const size_t need = logprob_ws_bytes(n, c, k);
+    TRY(check_ws(ws, ws_bytes, need));
+    const void *p[9] = {logp, entropy, lse, k ? top_idx : nullptr, k ? top_logp : nullptr, ws, logits, bias, tokens};
+    const int64_t b[9] = {n * 4, n * 4, n * 4, n * k * 4, n * k * 4, (int64_t)need, rows_bytes(n, c, logits_ld, esize(dt)),
+                          (int64_t)c * 4, n * 4};
+    const char *const name[6] = {"logp", "entropy", "lse", "top_idx", "top_logp", "ws"};
     for (int i = 0; i < 5; ++i) TRY(need_align(p[i], 4, name[i]));
-    for (int i = 0; i < 5; ++i)
-        for (int j = i + 1; j < 8; ++j)
+    for (int i = 0; i < 6; ++i)
+        for (int j = i + 1; j < 9; ++j)
             if (overlap(p[i], b[i], p[j], b[j])) return fail(TFK_ERR_ALIAS, "%s overlaps an operand", name[i]);
     const LogprobArgs a{logits, logits_ld, bias, tokens, logp, entropy, lse, top_idx, top_logp, n, c, k, temperature};
-    return hip_status(launch_logprob(dt == TFK_F32 ? 0 : 1, a, (hipStream_t)stream), "token_logprobs");
+    return hip_status(launch_logprob(dt == TFK_F32 ? 0 : 1, a, ws, (hipStream_t)stream), "token_logprobs");
+}
+
+size_t tfk_token_logprobs_workspace_bytes(int64_t n, int32_t c, int32_t k) {
+    if (n <= 0 || n > INT32_MAX || c < 1 || c > (1 << 30) || k < 0 || k > 128) return 0;
+    return logprob_ws_bytes(n, c, k);
 }
 
 tfk_status tfk_token_logprobs_bwd(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld, const float *bias,

@@ -280,7 +280,8 @@ struct LogprobBwdArgs {
     int c;
     float temperature;
 };
-hipError_t launch_logprob(int dt, const LogprobArgs &a, hipStream_t st);
+size_t logprob_ws_bytes(int64_t n, int c, int k);
+hipError_t launch_logprob(int dt, const LogprobArgs &a, void *ws, hipStream_t st);
 hipError_t launch_logprob_bwd(int dt, const LogprobBwdArgs &a, hipStream_t st);
 // AdamW over a batch of variables; blocks of 256 values, numbered through the batch.  m, v: fp32, or e4m3
 // values with a scale per block.

@@ -196,35 +196,38 @@ struct ListShared {
     u64 cand[kCands];
 };
 
-// Classes of the row whose order is at least tau (above tau alone: least = tau + 1) into sh.cand; sh.n counts them all.
+// Classes of the row whose order is at least `least` into sh.cand; sh.n counts them all.  The pieces that the hot lanes
+// read are shared out to all lanes, four in flight each.
 template <typename T, int NT>
 __device__ __forceinline__ void collect(const T *z, const float *bias, int c, ListShared<NT> &sh, uint32_t least) {
-    constexpr int V = Piece<T>::V;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = c / V;
-    for (int h = w; h < sh.nhot; h += NT / 64) {
-        const int at = sh.hot[h];
-        for (int q = at + lane * NT; q < n; q += 64 * NT) {
-            Piece<T> b;
-            b.load(z, bias, q * V);
-            float x[V];
-            b.values(bias, x);
+    constexpr int V = Piece<T>::V, U = 4;
+    const int n = c / V, per = (n + NT - 1) / NT, all = sh.nhot * per;
+    const auto take = [&](float x, int j) {
+        const uint32_t o = order_of(x);
+        if (o < least) return;
+        const int i = atomicAdd(&sh.n, 1);
+        if (i < kCands) sh.cand[i] = key_of(o, j);
+    };
+    for (int q0 = threadIdx.x; q0 < all; q0 += U * NT) {
+        Piece<T> b[U];
+        int at[U];
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const uint32_t o = order_of(x[e]);
-                if (o >= least) {
-                    const int i = atomicAdd(&sh.n, 1);
-                    if (i < kCands) sh.cand[i] = key_of(o, q * V + e);
-                }
-            }
+        for (int i = 0; i < U; ++i) {
+            const int q = q0 + i * NT, h = q / per;
+            at[i] = q < all ? sh.hot[h] + (q - h * per) * NT : n;
+            if (at[i] < n) b[i].load(z, bias, at[i] * V);
         }
-        if (lane == 0 && at < c - n * V) {
-            const uint32_t o = order_of(logit(z, bias, n * V + at));
-            if (o >= least) {
-                const int i = atomicAdd(&sh.n, 1);
-                if (i < kCands) sh.cand[i] = key_of(o, n * V + at);
-            }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (at[i] >= n) continue;
+            float x[V];
+            b[i].values(bias, x);
+#pragma unroll
+            for (int e = 0; e < V; ++e) take(x[e], at[i] * V + e);
         }
     }
+    // single classes behind the last piece
+    if (threadIdx.x < c - n * V) take(logit(z, bias, n * V + threadIdx.x), n * V + threadIdx.x);
 }
 
 // The first `want` classes of the row whose order is tau, in the row's order, behind the n candidates in sh.cand.
@@ -271,62 +274,19 @@ __device__ __forceinline__ u64 next_below(const T *z, const float *bias, int c, 
     return mine;
 }
 
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
-    __shared__ RowStats<NT> st;
-    __shared__ ListShared<NT> sh;
-    const int64_t r = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
-    if (r >= a.n) return;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const float invT = 1.f / a.temperature, ct = kLog2e / a.temperature;
-    const int token = a.tokens ? a.tokens[r] : 0;
-    int32_t *const out_idx = a.top_idx + r * a.k;
-    float *const out_logp = a.top_logp + r * a.k;
-    if (token < 0 || token >= a.c) {                 // padding: the logits are not looked at
-        if (threadIdx.x == 0) {
-            if (a.logp) a.logp[r] = 0.f;
-            if (a.entropy) a.entropy[r] = 0.f;
-            if (a.lse) a.lse[r] = 0.f;
-        }
-        for (int q = threadIdx.x; q < a.k; q += NT) {
-            out_idx[q] = -1;
-            out_logp[q] = -INFINITY;
-        }
-        return;
-    }
-    const T *const z = (const T *)a.z + r * a.zld;
-    const float xt = logit(z, a.bias, token);
-    const Part p = read_row<T, NT>(z, a.bias, a.c, ct);
-    const uint32_t mine = order_of(p.top);
-    if (a.k > 0) {
-        sh.orders[threadIdx.x] = mine;
-        if (threadIdx.x == 0) sh.nhot = sh.n = 0;
-    }
-    float m, s, W;
-    join_row<NT>(p, ct, st, m, s, W);
-    const bool empty = m == -INFINITY && s == 0.f, nan = !(s < INFINITY);
-    const float ls = __builtin_amdgcn_logf(s) * kLn2;
-    if (threadIdx.x == 0) {
-        if (a.logp) a.logp[r] = empty ? -INFINITY : nan ? NAN : (xt - m) * invT - ls;
-        if (a.entropy) a.entropy[r] = empty ? 0.f : nan ? NAN : fmaxf(ls - W / s * kLn2, 0.f);
-        if (a.lse) a.lse[r] = empty ? -INFINITY : nan ? NAN : m * invT + ls;
-    }
-    if (a.k == 0) return;
-    if (empty || nan) {
-        for (int q = threadIdx.x; q < a.k; q += NT) {
-            out_idx[q] = -1;
-            out_logp[q] = nan ? NAN : -INFINITY;
-        }
-        return;
-    }
-    if (w == 0) {
-        const uint32_t t = kth_of<NT>(sh.orders, a.k);
+// The k largest classes of a row (or of a part of one) that has one, largest first, to emit(rank, key); behind the
+// last class that is not -inf emit(rank, 0).  orders, nhot and n of sh are set, and a barrier has been passed since.
+template <typename T, int NT, typename Emit>
+__device__ __forceinline__ void largest(const T *z, const float *bias, int c, int k, ListShared<NT> &sh, const Emit &emit) {
+    const int lane = threadIdx.x & 63;
+    if (threadIdx.x < 64) {
+        const uint32_t t = kth_of<NT>(sh.orders, k);
         if (lane == 0) sh.tau = max(t, 1u);
     }
     __syncthreads();
-    if (mine >= sh.tau) sh.hot[atomicAdd(&sh.nhot, 1)] = threadIdx.x;
+    if (sh.orders[threadIdx.x] >= sh.tau) sh.hot[atomicAdd(&sh.nhot, 1)] = threadIdx.x;
     __syncthreads();
-    collect<T, NT>(z, a.bias, a.c, sh, sh.tau);
+    collect<T, NT>(z, bias, c, sh, sh.tau);
     __syncthreads();
     int n = sh.n;
     if (n > kCands) {
@@ -334,12 +294,12 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
         __syncthreads();
         if (threadIdx.x == 0) sh.n = 0;
         __syncthreads();
-        collect<T, NT>(z, a.bias, a.c, sh, sh.tau + 1);
+        collect<T, NT>(z, bias, c, sh, sh.tau + 1);
         __syncthreads();
         n = sh.n;
         if (n <= kCands - 128) {
-            const int want = max(a.k - n, 0);
-            first_equal<T, NT>(z, a.bias, a.c, sh, n, want);
+            const int want = max(k - n, 0);
+            first_equal<T, NT>(z, bias, c, sh, n, want);
             n += want;
             __syncthreads();
         }
@@ -349,27 +309,165 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
             const u64 key = sh.cand[i];
             int rank = 0;
             for (int q = 0; q < n; ++q) rank += sh.cand[q] > key;
-            if (rank < a.k) {
-                out_idx[rank] = (int32_t)~(uint32_t)key;
-                out_logp[rank] = (value_of((uint32_t)(key >> 32)) - m) * invT - ls;
-            }
+            if (rank < k) emit(rank, key);
         }
-        for (int q = n + threadIdx.x; q < a.k; q += NT) {
-            out_idx[q] = -1;
-            out_logp[q] = -INFINITY;
-        }
+        for (int q = n + threadIdx.x; q < k; q += NT) emit(q, 0ull);
         return;
     }
     // the largest classes crowd in few lanes: one after the other, each by a reading of the row
     u64 last = ~0ull;
-    for (int q = 0; q < a.k; ++q) {
-        if (last != 0) last = next_below<T, NT>(z, a.bias, a.c, sh, last);
+    for (int q = 0; q < k; ++q) {
+        if (last != 0) last = next_below<T, NT>(z, bias, c, sh, last);
         if ((last >> 32) == 0) last = 0;             // nothing but -inf is left
-        if (threadIdx.x == 0) {
-            out_idx[q] = last ? (int32_t)~(uint32_t)last : -1;
-            out_logp[q] = last ? (value_of((uint32_t)(last >> 32)) - m) * invT - ls : -INFINITY;
-        }
+        if (threadIdx.x == 0) emit(q, last);
     }
+}
+
+// A row that is padding: its logits are not looked at.
+template <int NT>
+__device__ __forceinline__ bool padding(const LogprobArgs &a, int64_t r, int token) {
+    if (token >= 0 && token < a.c) return false;
+    if (threadIdx.x == 0) {
+        if (a.logp) a.logp[r] = 0.f;
+        if (a.entropy) a.entropy[r] = 0.f;
+        if (a.lse) a.lse[r] = 0.f;
+    }
+    for (int q = threadIdx.x; q < a.k; q += NT) {
+        a.top_idx[r * a.k + q] = -1;
+        a.top_logp[r * a.k + q] = -INFINITY;
+    }
+    return true;
+}
+
+// What a row's maximum and sums say, and whether it has a list (else that is written, too).
+template <int NT>
+__device__ __forceinline__ bool finish_row(const LogprobArgs &a, int64_t r, float xt, float m, float s, float W, float &ls) {
+    const bool empty = m == -INFINITY && s == 0.f, nan = !(s < INFINITY);
+    const float invT = 1.f / a.temperature;
+    ls = __builtin_amdgcn_logf(s) * kLn2;
+    if (threadIdx.x == 0) {
+        if (a.logp) a.logp[r] = empty ? -INFINITY : nan ? NAN : (xt - m) * invT - ls;
+        if (a.entropy) a.entropy[r] = empty ? 0.f : nan ? NAN : fmaxf(ls - W / s * kLn2, 0.f);
+        if (a.lse) a.lse[r] = empty ? -INFINITY : nan ? NAN : m * invT + ls;
+    }
+    if (!empty && !nan) return a.k > 0;
+    for (int q = threadIdx.x; q < a.k; q += NT) {
+        a.top_idx[r * a.k + q] = -1;
+        a.top_logp[r * a.k + q] = nan ? NAN : -INFINITY;
+    }
+    return false;
+}
+
+__device__ __forceinline__ void put_class(const LogprobArgs &a, int64_t r, int rank, u64 key, float m, float ls) {
+    a.top_idx[r * a.k + rank] = key ? (int32_t)~(uint32_t)key : -1;
+    a.top_logp[r * a.k + rank] = key ? (value_of((uint32_t)(key >> 32)) - m) * (1.f / a.temperature) - ls : -INFINITY;
+}
+
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
+    __shared__ RowStats<NT> st;
+    __shared__ ListShared<NT> sh;
+    const int64_t r = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
+    if (r >= a.n) return;
+    const float ct = kLog2e / a.temperature;
+    const int token = a.tokens ? a.tokens[r] : 0;
+    if (padding<NT>(a, r, token)) return;
+    const T *const z = (const T *)a.z + r * a.zld;
+    const float xt = logit(z, a.bias, token);
+    const Part p = read_row<T, NT>(z, a.bias, a.c, ct);
+    if (a.k > 0) {
+        sh.orders[threadIdx.x] = order_of(p.top);
+        if (threadIdx.x == 0) sh.nhot = sh.n = 0;
+    }
+    float m, s, W, ls;
+    join_row<NT>(p, ct, st, m, s, W);
+    if (finish_row<NT>(a, r, xt, m, s, W, ls))
+        largest<T, NT>(z, a.bias, a.c, a.k, sh, [&](int rank, u64 key) { put_class(a, r, rank, key, m, ls); });
+}
+
+// Few long rows: each cut into parts, a workgroup each, which leave their maximum, sums and k largest classes in the
+// workspace; then a workgroup joins each row's parts.
+struct PartStats {
+    float m, s, W;
+};
+constexpr int kPartLeast = 8192, kPartMost = 32;
+
+template <typename T>
+__global__ __launch_bounds__(256) void logprob_part_kernel(LogprobArgs a, PartStats *stats, u64 *lists, int parts, int part_len) {
+    constexpr int NT = 256;
+    __shared__ RowStats<NT> st;
+    __shared__ ListShared<NT> sh;
+    const int64_t r = blockIdx.y;
+    const int part = blockIdx.x, j0 = part * part_len, c = min(part_len, a.c - j0);
+    const float ct = kLog2e / a.temperature;
+    if (a.tokens && (a.tokens[r] < 0 || a.tokens[r] >= a.c)) return;
+    const T *const z = (const T *)a.z + r * a.zld + j0;
+    const float *const bias = a.bias ? a.bias + j0 : nullptr;
+    const Part p = read_row<T, NT>(z, bias, c, ct);
+    if (a.k > 0) {
+        sh.orders[threadIdx.x] = order_of(p.top);
+        if (threadIdx.x == 0) sh.nhot = sh.n = 0;
+    }
+    float m, s, W;
+    join_row<NT>(p, ct, st, m, s, W);
+    if (threadIdx.x == 0) stats[r * parts + part] = PartStats{m, s, W};
+    if (a.k == 0 || !(s < INFINITY)) return;         // (a NaN row has no list)
+    u64 *const list = lists + (r * parts + part) * a.k;
+    largest<T, NT>(z, bias, c, a.k, sh, [&](int rank, u64 key) { list[rank] = key ? key - (u64)j0 : 0ull; });
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, const PartStats *stats, const u64 *lists, int parts) {
+    constexpr int NT = 256, U = 4;
+    __shared__ u64 cand[kPartMost * 128];
+    __shared__ u64 least[NT / 64];
+    __shared__ int count;
+    const int64_t r = blockIdx.x;
+    const int lane = threadIdx.x & 63, total = parts * a.k;
+    const int token = a.tokens ? a.tokens[r] : 0;
+    // what is to be known about the row is asked for at once
+    const PartStats own = lane < parts ? stats[r * parts + lane] : PartStats{-INFINITY, 0.f, 0.f};
+    const u64 *const list = lists + r * total;
+    u64 key[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) key[i] = (int)threadIdx.x + i * NT < total ? list[threadIdx.x + i * NT] : 0;
+    if (padding<NT>(a, r, token)) return;
+    const float ct = kLog2e / a.temperature;
+    const float xt = logit((const T *)a.z + r * a.zld, a.bias, token);
+    const float m = wave_maxf(own.m);
+    const float D = own.m == -INFINITY ? 0.f : fminf((m - own.m) * ct, kFar), e = ex2(-D);
+    const float s = wave_sumf(own.s * e), W = wave_sumf((own.W - D * own.s) * e);
+    float ls;
+    if (!finish_row<NT>(a, r, xt, m, s, W, ls)) return;
+    // the row's k-th largest is at least each part's own k-th
+    u64 t = 0;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+        if ((threadIdx.x + i * NT) % a.k == a.k - 1) t = max(t, key[i]);
+    for (int q = threadIdx.x + U * NT; q < total; q += NT)
+        if (q % a.k == a.k - 1) t = max(t, list[q]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) t = max(t, (u64)__shfl_xor(t, o, 64));
+    if (lane == 0) least[threadIdx.x >> 6] = t;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    t = max(max(least[0], least[1]), max(max(least[2], least[3]), (u64)1));
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+        if (key[i] >= t) cand[atomicAdd(&count, 1)] = key[i];
+    for (int q = threadIdx.x + U * NT; q < total; q += NT) {
+        const u64 x = list[q];
+        if (x >= t) cand[atomicAdd(&count, 1)] = x;
+    }
+    __syncthreads();
+    const int n = count;
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const u64 x = cand[i];
+        int rank = 0;
+        for (int q = 0; q < n; ++q) rank += cand[q] > x;
+        if (rank < a.k) put_class(a, r, rank, x, m, ls);
+    }
+    for (int q = n + threadIdx.x; q < a.k; q += NT) put_class(a, r, q, 0ull, m, ls);
 }
 
 // The gradient.  Where lse is so large that fp32 no longer tells x / T from it (a row of masks alone), its maximum
@@ -433,16 +531,41 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int p
     if (j < j1) Elem<T>::store(dz + j, none ? 0.f : grad(logit(z, a.bias, j)) + (j == token ? dl : 0.f));
 }
 
-template <typename T>
-static void launch_rows(const LogprobArgs &a, hipStream_t st) {
-    if (a.c <= kCands) hipLaunchKernelGGL((logprob_kernel<T, 64>), grid_2d(a.n), dim3(64), 0, st, a);
-    else if (a.n > 256 || a.c <= 16384) hipLaunchKernelGGL((logprob_kernel<T, 256>), grid_2d(a.n), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((logprob_kernel<T, 1024>), grid_2d(a.n), dim3(1024), 0, st, a);
+// Parts of a row, 0 for rows that one workgroup reads: enough for two workgroups a CU, of at least kPartLeast classes.
+// (The list asked for has no say in it, and so none in the sums' order.)
+static int row_parts(int64_t n, int c) {
+    if (n > 256 || c < 4 * kPartLeast) return 0;
+    return (int)std::min<int64_t>({kPartMost, c / kPartLeast, (512 + n - 1) / n});
 }
 
-hipError_t launch_logprob(int dt, const LogprobArgs &a, hipStream_t st) {
-    if (dt == 0) launch_rows<float>(a, st);
-    else launch_rows<bf16_t>(a, st);
+size_t logprob_ws_bytes(int64_t n, int c, int k) {
+    const int64_t parts = n > 0 ? row_parts(n, c) : 0;
+    return (size_t)(n * parts * (sizeof(u64) * k + sizeof(PartStats)));
+}
+
+template <typename T>
+static void launch_rows(const LogprobArgs &a, void *ws, hipStream_t st) {
+    const int parts = row_parts(a.n, a.c);
+    if (parts) {
+        // parts begin at whole pieces of 16 bytes of the row
+        const int len = ((a.c + parts - 1) / parts + 63) / 64 * 64;
+        u64 *const lists = (u64 *)ws;
+        PartStats *const stats = (PartStats *)(lists + a.n * parts * a.k);
+        const int used = (a.c + len - 1) / len;
+        hipLaunchKernelGGL((logprob_part_kernel<T>), dim3(used, (unsigned)a.n), dim3(256), 0, st, a, stats, lists, used, len);
+        hipLaunchKernelGGL((logprob_join_kernel<T>), dim3((unsigned)a.n), dim3(256), 0, st, a, stats, lists, used);
+    } else if (a.c <= kCands) {
+        hipLaunchKernelGGL((logprob_kernel<T, 64>), grid_2d(a.n), dim3(64), 0, st, a);
+    } else if (a.n > 256 || a.c <= 16384) {
+        hipLaunchKernelGGL((logprob_kernel<T, 256>), grid_2d(a.n), dim3(256), 0, st, a);
+    } else {
+        hipLaunchKernelGGL((logprob_kernel<T, 1024>), grid_2d(a.n), dim3(1024), 0, st, a);
+    }
+}
+
+hipError_t launch_logprob(int dt, const LogprobArgs &a, void *ws, hipStream_t st) {
+    if (dt == 0) launch_rows<float>(a, ws, st);
+    else launch_rows<bf16_t>(a, ws, st);
     return hipGetLastError();
 }
 

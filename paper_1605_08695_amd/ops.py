@@ -22,7 +22,8 @@ __all__ = ["conv2d_fwd", "conv2d_fwd_bias_relu", "conv2d_bwd_input", "conv2d_bwd
            "bias_relu_bwd", "bias_relu_bwd_workspace_bytes", "maxpool_fwd", "maxpool_bwd", "maxpool_bwd_relu_bwd", "apply_sgd",
            "apply_sgd_multi", "apply_momentum", "apply_adam", "softmax_xent",
            "gather_rows_t", "sampled_softmax_xent", "scatter_apply_sgd", "distill_xent", "embedding_fwd", "embedding_bwd",
-           "embedding_apply_sgd", "embedding_workspace_bytes", "token_logprobs", "token_logprobs_bwd", "TokenLogprobs",
+           "embedding_apply_sgd", "embedding_workspace_bytes", "token_logprobs", "token_logprobs_bwd", "token_logprobs_workspace_bytes",
+           "TokenLogprobs",
            "gated_scan_fwd", "gated_scan_bwd", "gated_scan_step", "gated_scan_workspace_bytes", "SCAN_BLOCK",
            "apply_adamw_multi", "adamw_scales", "stream_wait", "Program", "out_len", "nhwc",
            "window", "TfkError", "abi_version", "DeferredBias", "bias_grad_finish"]
@@ -835,7 +836,15 @@ class TokenLogprobs(NamedTuple):
     top_logp: Optional[torch.Tensor]
 
 
-def token_logprobs(logits, tokens=None, k=0, temperature=1.0, bias=None, stream=None) -> TokenLogprobs:
+def token_logprobs_workspace_bytes(n, c, k) -> int:
+    """Workspace of token_logprobs for n rows of c classes and the k largest of them."""
+    return load().tfk_token_logprobs_workspace_bytes(operator.index(n), _width(operator.index(c), "logits"), operator.index(k))
+
+
+_logprob_need = functools.lru_cache(_KEPT)(token_logprobs_workspace_bytes)
+
+
+def token_logprobs(logits, tokens=None, k=0, temperature=1.0, bias=None, ws=None, stream=None) -> TokenLogprobs:
     """Of each row of (logits + bias) / temperature: the log-probability of its token (int32; one outside the
     classes is padding), the entropy, the log-sum-exp and the k <= 128 largest classes with their
     log-probabilities, largest first (n x k, -1 and -inf behind the last class that is not -inf)."""
@@ -846,7 +855,12 @@ def token_logprobs(logits, tokens=None, k=0, temperature=1.0, bias=None, stream=
     _vector(tokens, torch.int32, n, "tokens")
     _vector(bias, torch.float32, c, "bias")
     dt = _dt(logits)
-    st = _on_device(stream, logits, tokens, bias)
+    if ws is not None and not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    st = _on_device(stream, logits, tokens, bias, ws)
+    need = _logprob_need(n, c, k)
+    if need and (ws is None or ws.numel() * ws.element_size() < need):
+        ws = _ws(need, logits.device, stream)
     out = _empty(stream, (2 if tokens is None else 3, n), dtype=torch.float32, device=logits.device)
     idx = top = None
     if k:
@@ -854,7 +868,7 @@ def token_logprobs(logits, tokens=None, k=0, temperature=1.0, bias=None, stream=
         top = _empty(stream, (n, k), dtype=torch.float32, device=logits.device)
     r = TokenLogprobs(None if tokens is None else out[2], out[0], out[1], idx, top)
     check(load().tfk_token_logprobs(_ptr(logits), dt, n, c, ld, _ptr(bias), _ptr(tokens), float(temperature), k, _ptr(r.logp),
-                                    _ptr(r.entropy), _ptr(r.lse), _ptr(idx), _ptr(top), st))
+                                    _ptr(r.entropy), _ptr(r.lse), _ptr(idx), _ptr(top), _ptr(ws), need, st))
     return r
 
 

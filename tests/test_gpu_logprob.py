@@ -151,6 +151,25 @@ def test_largest_where_they_lie_badly(kind, c, dt):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("c", [2000, 70001])
+def test_long_rows_of_large_batches(c, dt):
+    """Many rows, which one workgroup each reads: equal classes, classes crowded in few places, masks, NaN."""
+    i = np.arange(c)
+    rng = np.random.default_rng(c)
+    one = [np.zeros(c), np.where(i % 2048 // 8 == 5, 8.0 + rng.random(c), rng.random(c)), rng.standard_normal(c) * 3,
+           np.where(i % 97 == 3, rng.random(c), -1e9), np.where(i < 5, 1.0, -np.inf)]
+    z = torch.from_numpy(np.stack(one * 55)).to(dt).to(DEV)
+    tokens = toks(z.shape[0], c, 3)
+    tokens[tokens > 0] = 3
+    for k in (4, 128):
+        check(z, None, tokens, 1.0, k)
+    z[7, c // 2] = NAN
+    r = ops.token_logprobs(z, tokens, 3)
+    torch.cuda.synchronize()
+    assert r.lse[7].isnan() and (r.top_idx[7] == -1).all() and torch.isfinite(r.lse[8:]).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
 @pytest.mark.parametrize("c", [9, 1000, 9000, 70000, 140001])
 def test_masks(c, dt):
     """Classes ruled out by -inf or by numbers as low as the type has, rows with one class left and with none."""

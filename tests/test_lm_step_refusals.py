@@ -39,14 +39,18 @@ _ROWS = [(dict(dt=7), DTYPE), (dict(n=-1), SHAPE), (dict(c=0), SHAPE), (dict(ld=
     (dict(logp=P + 3 * M + 2), ALIGN), (dict(ent=P + 4 * M + 1), ALIGN), (dict(lse=P + 5 * M + 2), ALIGN),
     (dict(idx=P + 6 * M + 2), ALIGN), (dict(top=P + 7 * M + 1), ALIGN), (dict(logp=P), ALIAS), (dict(ent=P + M), ALIAS),
     (dict(lse=P + 2 * M), ALIAS), (dict(idx=P + 7 * M), ALIAS), (dict(ent=P + 5 * M), ALIAS),
+    (dict(c=1 << 17, n=2, ws=0), WORKSPACE), (dict(c=1 << 17, n=2, wb=64), WORKSPACE), (dict(c=1 << 17, n=2, ws=P + 9 * M + 8), ALIGN),
+    (dict(c=1 << 17, n=2, ws=P + 16 * M), ALIAS), (dict(c=1 << 17, n=2, ws=P + 7 * M), ALIAS),
     (dict(n=0, z=0, tokens=0, logp=0, ent=0, lse=0, idx=0, top=0), OK)], ids=str)
 def test_token_logprobs(lib, kw, status):
     a = dict(z=P, dt=F32, n=4, c=100, ld=0, bias=P + M, tokens=P + 2 * M, T=1.0, k=5, logp=P + 3 * M, ent=P + 4 * M,
-             lse=P + 5 * M, idx=P + 6 * M, top=P + 7 * M)
+             lse=P + 5 * M, idx=P + 6 * M, top=P + 7 * M, ws=P + 9 * M, wb=M)
+    if kw.get("c", 0) > 100:
+        a.update(z=P + 16 * M, bias=P + 11 * M)
     a.update(kw)
     assert lib.tfk_token_logprobs(vp(a["z"]), a["dt"], a["n"], a["c"], a["ld"], vp(a["bias"]), vp(a["tokens"]), f(a["T"]),
                                   a["k"], vp(a["logp"]), vp(a["ent"]), vp(a["lse"]), vp(a["idx"]), vp(a["top"]),
-                                  None) == status
+                                  vp(a["ws"]), a["wb"], None) == status
 
 
 @pytest.mark.parametrize("kw,status", _ROWS + [
@@ -113,6 +117,12 @@ def test_gated_scan_step(lib, kw, status):
     a.update(kw)
     assert lib.tfk_gated_scan_step(vp(a["z"]), a["dt"], a["n"], a["d"], a["gates"], a["ld"], vp(a["bias"]), vp(a["slots"]),
                                    vp(a["state"]), a["slots_n"], vp(a["y"]), a["yld"], None) == status
+
+
+def test_logprob_workspace(lib):
+    q = lib.tfk_token_logprobs_workspace_bytes
+    assert q(0, 10, 1) == q(-1, 10, 1) == q(5, 0, 1) == q(5, 10, 129) == q(5, 10, -1) == q(1 << 31, 10, 1) == q(4, 1000, 5) == 0
+    assert q(5000, 1 << 17, 20) == 0 and q(2, 1 << 17, 20) >= 2 * 2 * (20 * 8 + 12)
 
 
 def test_gated_scan_workspace(lib):
