@@ -23,7 +23,8 @@
 namespace tfk {
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
-constexpr float kSlack = 32.f, kFar = 1e4f;      // in powers of two
+constexpr float kSlack = 32.f, kFar = 1e4f, kEdge = 0x1p28f;      // in powers of two
+constexpr int kBatch = 4, kGroups = 16;          // pieces in flight of a lane; groups of them that a lane's maxima are kept for
 constexpr int kCands = 1024;                     // candidates for the list in LDS
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -50,28 +51,37 @@ __device__ __forceinline__ float wave_sumf(float v) {
     return v;
 }
 
-// A lane's part of a row: sums relative to ref, and its largest x.
+// A lane's part of a row: sums relative to a power of two, and its largest x.  EXACT false: x ct - R by one fma, R a number
+// near the largest x ct, rounded once and used as it is; rows that this cannot hold (s is not a positive number
+// then: the largest class beyond +-2^28, infinite or NaN) are read again with EXACT, relative to a ref by exact
+// differences.
+template <bool EXACT>
 struct Part {
-    float ref, s, W, top;
+    float ref, s, W, top;              // ref: R, or an x
+    __device__ __forceinline__ static Part none() { return {EXACT ? -__FLT_MAX__ : -kEdge, 0.f, 0.f, -INFINITY}; }
+    __device__ __forceinline__ float power(float x, float ct) const {
+        return EXACT ? (x - ref) * ct : __builtin_fmaf(x, ct, -ref);
+    }
     __device__ __forceinline__ void raise(float x, float ct) {
-        const float D = fminf((x - ref) * ct, kFar), r = ex2(-D);
+        const float to = EXACT ? x : __builtin_amdgcn_fmed3f(x * ct, -kEdge, kEdge);
+        const float D = fminf(EXACT ? (x - ref) * ct : to - ref, kFar), r = ex2(-D);
         W = (W - D * s) * r;
         s *= r;
-        ref = x;
+        ref = to;
     }
     template <int V>
-    __device__ __forceinline__ void add(const float *x, float ct) {
+    __device__ __forceinline__ float add(const float *x, float ct) {
         float t = x[0];
 #pragma unroll
         for (int e = 1; e < V; ++e) t = fmaxf(t, x[e]);
-        top = fmaxf(top, t);
-        if ((t - ref) * ct > kSlack) raise(t, ct);
+        if (power(t, ct) > kSlack) raise(t, ct);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float u = (x[e] - ref) * ct, p = ex2(u);
+            const float u = power(x[e], ct), p = ex2(u);
             s += p;
             W = __builtin_fmaf(p, fmaxf(u, -kFar), W);      // (p is 0 where the bound is reached)
         }
+        return t;
     }
 };
 
@@ -101,35 +111,52 @@ __device__ __forceinline__ float logit(const T *z, const float *bias, int j) {
     return Elem<T>::load(z + j) + (bias ? bias[j] : 0.f);
 }
 
-// All of the workgroup's NT lanes' parts of a row of c classes: pieces lane, lane + NT ..., and single classes behind
-// the last whole piece.
-template <typename T, int NT>
-__device__ __forceinline__ Part read_row(const T *z, const float *bias, int c, float ct) {
-    constexpr int V = Piece<T>::V, U = 4;
-    Part p{-__FLT_MAX__, 0.f, 0.f, -INFINITY};
+// All of the workgroup's NT lanes' parts of a row of c classes: pieces lane, lane + NT ..., in batches of kBatch, and
+// single classes behind the last whole piece.  groups, if given: the upper halves of the orders of each lane's largest in
+// each kGroups-th batch.
+template <bool EXACT, typename T, int NT>
+__device__ __forceinline__ Part<EXACT> read_row(const T *z, const float *bias, int c, float ct, uint16_t (*groups)[NT]) {
+    constexpr int V = Piece<T>::V;
+    Part<EXACT> p = Part<EXACT>::none();
     const int n = c / V;
+    int g = 0;
+    const auto note = [&](float t) {
+        p.top = fmaxf(p.top, t);
+        if (groups) {
+            const uint16_t o = (uint16_t)(order_of(t) >> 16);
+            uint16_t *const at = &groups[g % kGroups][threadIdx.x];
+            *at = g < kGroups ? o : max(*at, o);
+            ++g;
+        }
+    };
     int q = threadIdx.x;
-    for (; q + (U - 1) * NT < n; q += U * NT) {
-        Piece<T> b[U];
+    for (; q + (kBatch - 1) * NT < n; q += kBatch * NT) {
+        Piece<T> b[kBatch];
 #pragma unroll
-        for (int i = 0; i < U; ++i) b[i].load(z, bias, (q + i * NT) * V);
+        for (int i = 0; i < kBatch; ++i) b[i].load(z, bias, (q + i * NT) * V);
+        float t = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
+        for (int i = 0; i < kBatch; ++i) {
             float x[V];
             b[i].values(bias, x);
-            p.template add<V>(x, ct);
+            t = fmaxf(t, p.template add<V>(x, ct));
         }
+        note(t);
     }
-    for (; q < n; q += NT) {
-        Piece<T> b;
-        b.load(z, bias, q * V);
-        float x[V];
-        b.values(bias, x);
-        p.template add<V>(x, ct);
+    if (q < n) {
+        float t = -INFINITY;
+        for (; q < n; q += NT) {
+            Piece<T> b;
+            b.load(z, bias, q * V);
+            float x[V];
+            b.values(bias, x);
+            t = fmaxf(t, p.template add<V>(x, ct));
+        }
+        note(t);
     }
     if (threadIdx.x < c - n * V) {
         const float x = logit(z, bias, n * V + threadIdx.x);
-        p.template add<1>(&x, ct);
+        p.top = fmaxf(p.top, p.template add<1>(&x, ct));
     }
     return p;
 }
@@ -140,17 +167,18 @@ struct RowStats {
 };
 
 // The row's maximum m, sum s and weighted sum W (in powers of two) relative to it, in all lanes, from the lanes' parts.
-template <int NT>
-__device__ __forceinline__ void join_row(const Part &p, float ct, RowStats<NT> &sh, float &m, float &s, float &W) {
+template <bool EXACT, int NT>
+__device__ __forceinline__ void join_row(const Part<EXACT> &p, float ct, RowStats<NT> &sh, float &m, float &s, float &W) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const float wm = wave_maxf(p.top);
+    __syncthreads();
     if (lane == 0) sh.top[w] = wm;
     __syncthreads();
     m = sh.top[0];
 #pragma unroll
     for (int v = 1; v < NT / 64; ++v) m = fmaxf(m, sh.top[v]);
-    // ref is at most kSlack below m's part of the lane, or far below it, or, without a class yet, the lowest number
-    const float D = m == -INFINITY ? 0.f : fminf((m - p.ref) * ct, kFar), r = ex2(-D);
+    // what the lane's sums are relative to is at most kSlack below its largest class, or far below m
+    const float D = m == -INFINITY ? 0.f : fminf(p.power(m, ct), kFar), r = ex2(-D);
     s = wave_sumf(p.s * r);
     W = wave_sumf((p.W - D * p.s) * r);
     if (lane == 0) {
@@ -165,6 +193,18 @@ __device__ __forceinline__ void join_row(const Part &p, float ct, RowStats<NT> &
         s += sh.s[v];
         W += sh.W[v];
     }
+}
+
+// Both, and again with exact differences where the row needs them.  top: the lane's largest class.
+template <typename T, int NT>
+__device__ __forceinline__ void row_sums(const T *z, const float *bias, int c, float ct, uint16_t (*groups)[NT], RowStats<NT> &sh,
+                                         float &top, float &m, float &s, float &W) {
+    {
+        const Part<false> p = read_row<false, T, NT>(z, bias, c, ct, groups);
+        top = p.top;
+        join_row<false, NT>(p, ct, sh, m, s, W);
+    }
+    if (!(s > 0.f && s < INFINITY)) join_row<true, NT>(read_row<true, T, NT>(z, bias, c, ct, nullptr), ct, sh, m, s, W);
 }
 
 // The largest number that at least k of the NT orders are not below (0: fewer than k are above 0), by one wave, from its
@@ -188,7 +228,8 @@ __device__ __forceinline__ uint32_t kth_of(const uint32_t *orders, int k) {
 template <int NT>
 struct ListShared {
     uint32_t orders[NT];       // of each lane's largest class
-    int hot[128 + NT];         // lanes whose largest is on the list, at most k, or more of equal ones
+    uint16_t groups[kGroups][NT];
+    int hot[NT];               // lanes whose largest is on the list, at most k, or more of equal ones
     uint32_t tau;
     int nhot, n, above;
     int counts[NT / 64];
@@ -196,34 +237,34 @@ struct ListShared {
     u64 cand[kCands];
 };
 
-// Classes of the row whose order is at least `least` into sh.cand; sh.n counts them all.  The pieces that the hot lanes
-// read are shared out to all lanes, four in flight each.
+// Classes of the row whose order is at least `least` into sh.cand; sh.n counts them all.  The batches of the hot lanes in
+// which such a class can be are shared out to all lanes.  (A hot lane's pieces lie NT pieces apart, so reading all of them
+// again would fetch as many lines as the row has.)
 template <typename T, int NT>
 __device__ __forceinline__ void collect(const T *z, const float *bias, int c, ListShared<NT> &sh, uint32_t least) {
-    constexpr int V = Piece<T>::V, U = 4;
-    const int n = c / V, per = (n + NT - 1) / NT, all = sh.nhot * per;
+    constexpr int V = Piece<T>::V;
+    const int n = c / V, per = (n + kBatch * NT - 1) / (kBatch * NT), all = sh.nhot * per;
     const auto take = [&](float x, int j) {
         const uint32_t o = order_of(x);
         if (o < least) return;
         const int i = atomicAdd(&sh.n, 1);
         if (i < kCands) sh.cand[i] = key_of(o, j);
     };
-    for (int q0 = threadIdx.x; q0 < all; q0 += U * NT) {
-        Piece<T> b[U];
-        int at[U];
+    for (int q = threadIdx.x; q < all; q += NT) {
+        const int h = q / per, g = q - h * per, lane = sh.hot[h];
+        if (sh.groups[g % kGroups][lane] < (uint16_t)(least >> 16)) continue;
+        const int at = g * kBatch * NT + lane;
+        Piece<T> b[kBatch];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int q = q0 + i * NT, h = q / per;
-            at[i] = q < all ? sh.hot[h] + (q - h * per) * NT : n;
-            if (at[i] < n) b[i].load(z, bias, at[i] * V);
-        }
+        for (int i = 0; i < kBatch; ++i)
+            if (at + i * NT < n) b[i].load(z, bias, (at + i * NT) * V);
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            if (at[i] >= n) continue;
+        for (int i = 0; i < kBatch; ++i) {
+            if (at + i * NT >= n) continue;
             float x[V];
             b[i].values(bias, x);
 #pragma unroll
-            for (int e = 0; e < V; ++e) take(x[e], at[i] * V + e);
+            for (int e = 0; e < V; ++e) take(x[e], (at + i * NT) * V + e);
         }
     }
     // single classes behind the last piece
@@ -275,10 +316,13 @@ __device__ __forceinline__ u64 next_below(const T *z, const float *bias, int c, 
 }
 
 // The k largest classes of a row (or of a part of one) that has one, largest first, to emit(rank, key); behind the
-// last class that is not -inf emit(rank, 0).  orders, nhot and n of sh are set, and a barrier has been passed since.
+// last class that is not -inf emit(rank, 0).  top: each lane's largest.
 template <typename T, int NT, typename Emit>
-__device__ __forceinline__ void largest(const T *z, const float *bias, int c, int k, ListShared<NT> &sh, const Emit &emit) {
+__device__ __forceinline__ void largest(const T *z, const float *bias, int c, int k, float top, ListShared<NT> &sh, const Emit &emit) {
     const int lane = threadIdx.x & 63;
+    sh.orders[threadIdx.x] = order_of(top);
+    if (threadIdx.x == 0) sh.nhot = sh.n = 0;
+    __syncthreads();
     if (threadIdx.x < 64) {
         const uint32_t t = kth_of<NT>(sh.orders, k);
         if (lane == 0) sh.tau = max(t, 1u);
@@ -344,7 +388,7 @@ template <int NT>
 __device__ __forceinline__ bool finish_row(const LogprobArgs &a, int64_t r, float xt, float m, float s, float W, float &ls) {
     const bool empty = m == -INFINITY && s == 0.f, nan = !(s < INFINITY);
     const float invT = 1.f / a.temperature;
-    ls = __builtin_amdgcn_logf(s) * kLn2;
+    ls = __builtin_amdgcn_logf(fmaxf(s, 1.f)) * kLn2;       // (the largest class alone adds 1, but for a rounding)
     if (threadIdx.x == 0) {
         if (a.logp) a.logp[r] = empty ? -INFINITY : nan ? NAN : (xt - m) * invT - ls;
         if (a.entropy) a.entropy[r] = empty ? 0.f : nan ? NAN : fmaxf(ls - W / s * kLn2, 0.f);
@@ -374,15 +418,10 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
     if (padding<NT>(a, r, token)) return;
     const T *const z = (const T *)a.z + r * a.zld;
     const float xt = logit(z, a.bias, token);
-    const Part p = read_row<T, NT>(z, a.bias, a.c, ct);
-    if (a.k > 0) {
-        sh.orders[threadIdx.x] = order_of(p.top);
-        if (threadIdx.x == 0) sh.nhot = sh.n = 0;
-    }
-    float m, s, W, ls;
-    join_row<NT>(p, ct, st, m, s, W);
+    float m, s, W, ls, top;
+    row_sums<T, NT>(z, a.bias, a.c, ct, a.k > 0 ? sh.groups : nullptr, st, top, m, s, W);
     if (finish_row<NT>(a, r, xt, m, s, W, ls))
-        largest<T, NT>(z, a.bias, a.c, a.k, sh, [&](int rank, u64 key) { put_class(a, r, rank, key, m, ls); });
+        largest<T, NT>(z, a.bias, a.c, a.k, top, sh, [&](int rank, u64 key) { put_class(a, r, rank, key, m, ls); });
 }
 
 // Few long rows: each cut into parts, a workgroup each, which leave their maximum, sums and k largest classes in the
@@ -403,17 +442,12 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobArgs a, PartSt
     if (a.tokens && (a.tokens[r] < 0 || a.tokens[r] >= a.c)) return;
     const T *const z = (const T *)a.z + r * a.zld + j0;
     const float *const bias = a.bias ? a.bias + j0 : nullptr;
-    const Part p = read_row<T, NT>(z, bias, c, ct);
-    if (a.k > 0) {
-        sh.orders[threadIdx.x] = order_of(p.top);
-        if (threadIdx.x == 0) sh.nhot = sh.n = 0;
-    }
-    float m, s, W;
-    join_row<NT>(p, ct, st, m, s, W);
+    float m, s, W, top;
+    row_sums<T, NT>(z, bias, c, ct, a.k > 0 ? sh.groups : nullptr, st, top, m, s, W);
     if (threadIdx.x == 0) stats[r * parts + part] = PartStats{m, s, W};
     if (a.k == 0 || !(s < INFINITY)) return;         // (a NaN row has no list)
     u64 *const list = lists + (r * parts + part) * a.k;
-    largest<T, NT>(z, bias, c, a.k, sh, [&](int rank, u64 key) { list[rank] = key ? key - (u64)j0 : 0ull; });
+    largest<T, NT>(z, bias, c, a.k, top, sh, [&](int rank, u64 key) { list[rank] = key ? key - (u64)j0 : 0ull; });
 }
 
 template <typename T>
@@ -493,8 +527,8 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int p
     float m = 0.f, ls = lse;
     if (!none && __builtin_fabsf(lse) > kFarLse && __builtin_fabsf(lse) < INFINITY) {
         float s, W;
-        join_row<NT>(read_row<T, NT>(z, a.bias, a.c, ct), ct, st, m, s, W);
-        ls = __builtin_amdgcn_logf(s) * kLn2;
+        join_row<true, NT>(read_row<true, T, NT>(z, a.bias, a.c, ct, nullptr), ct, st, m, s, W);
+        ls = __builtin_amdgcn_logf(fmaxf(s, 1.f)) * kLn2;
     }
     const float base = dl + de * H;
     const auto grad = [&](float x) {
