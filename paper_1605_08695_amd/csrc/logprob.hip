@@ -24,8 +24,7 @@ namespace tfk {
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kSlack = 32.f, kFar = 1e4f, kEdge = 0x1p28f;      // in powers of two
-constexpr int kBatch = 4, kGroups = 16;          // pieces in flight of a lane; groups of them that a lane's maxima are kept for
-constexpr int kCands = 1024;                     // candidates for the list in LDS
+constexpr int kBatch = 2, kGroups = 16;          // pieces in flight of a lane; groups of them that a lane's maxima are kept for
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -207,14 +206,14 @@ __device__ __forceinline__ void row_sums(const T *z, const float *bias, int c, f
     if (!(s > 0.f && s < INFINITY)) join_row<true, NT>(read_row<true, T, NT>(z, bias, c, ct, nullptr), ct, sh, m, s, W);
 }
 
-// The largest number that at least k of the NT orders are not below (0: fewer than k are above 0), by one wave, from its
-// highest bit down; at most as many as k stop the search.
+// The largest number, of those whose bits below `low` are 0, that at least k of the NT orders are not below (0: fewer than k
+// are above 0), by one wave, from its highest bit down; at most as many as k stop the search.
 template <int NT>
-__device__ __forceinline__ uint32_t kth_of(const uint32_t *orders, int k) {
+__device__ __forceinline__ uint32_t kth_of(const uint32_t *orders, int k, int low) {
     uint32_t mine[NT / 64], t = 0;
 #pragma unroll
     for (int i = 0; i < NT / 64; ++i) mine[i] = orders[i * 64 + (threadIdx.x & 63)];
-    for (int bit = 31; bit >= 0; --bit) {
+    for (int bit = 31; bit >= low; --bit) {
         const uint32_t trial = t | 1u << bit;
         int n = 0;
 #pragma unroll
@@ -225,8 +224,9 @@ __device__ __forceinline__ uint32_t kth_of(const uint32_t *orders, int k) {
     return t;
 }
 
-template <int NT>
+template <int NT, int CANDS>
 struct ListShared {
+    static constexpr int kCands = CANDS;       // candidates for the list
     uint32_t orders[NT];       // of each lane's largest class
     uint16_t groups[kGroups][NT];
     int hot[NT];               // lanes whose largest is on the list, at most k, or more of equal ones
@@ -240,9 +240,9 @@ struct ListShared {
 // Classes of the row whose order is at least `least` into sh.cand; sh.n counts them all.  The batches of the hot lanes in
 // which such a class can be are shared out to all lanes.  (A hot lane's pieces lie NT pieces apart, so reading all of them
 // again would fetch as many lines as the row has.)
-template <typename T, int NT>
-__device__ __forceinline__ void collect(const T *z, const float *bias, int c, ListShared<NT> &sh, uint32_t least) {
-    constexpr int V = Piece<T>::V;
+template <typename T, int NT, int CANDS>
+__device__ __forceinline__ void collect(const T *z, const float *bias, int c, ListShared<NT, CANDS> &sh, uint32_t least) {
+    constexpr int V = Piece<T>::V, kCands = CANDS;
     const int n = c / V, per = (n + kBatch * NT - 1) / (kBatch * NT), all = sh.nhot * per;
     const auto take = [&](float x, int j) {
         const uint32_t o = order_of(x);
@@ -272,8 +272,8 @@ __device__ __forceinline__ void collect(const T *z, const float *bias, int c, Li
 }
 
 // The first `want` classes of the row whose order is tau, in the row's order, behind the n candidates in sh.cand.
-template <typename T, int NT>
-__device__ __forceinline__ void first_equal(const T *z, const float *bias, int c, ListShared<NT> &sh, int n, int want) {
+template <typename T, int NT, int CANDS>
+__device__ __forceinline__ void first_equal(const T *z, const float *bias, int c, ListShared<NT, CANDS> &sh, int n, int want) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     for (int base = 0; base < c && want > 0; base += NT) {
         const int j = base + threadIdx.x;
@@ -296,8 +296,8 @@ __device__ __forceinline__ void first_equal(const T *z, const float *bias, int c
 }
 
 // The row's largest class below key `last`, by all lanes.
-template <typename T, int NT>
-__device__ __forceinline__ u64 next_below(const T *z, const float *bias, int c, ListShared<NT> &sh, u64 last) {
+template <typename T, int NT, int CANDS>
+__device__ __forceinline__ u64 next_below(const T *z, const float *bias, int c, ListShared<NT, CANDS> &sh, u64 last) {
     u64 mine = 0;
     for (int j = threadIdx.x; j < c; j += NT) {
         const u64 key = key_of(order_of(logit(z, bias, j)), j);
@@ -317,33 +317,39 @@ __device__ __forceinline__ u64 next_below(const T *z, const float *bias, int c, 
 
 // The k largest classes of a row (or of a part of one) that has one, largest first, to emit(rank, key); behind the
 // last class that is not -inf emit(rank, 0).  top: each lane's largest.
-template <typename T, int NT, typename Emit>
-__device__ __forceinline__ void largest(const T *z, const float *bias, int c, int k, float top, ListShared<NT> &sh, const Emit &emit) {
+template <typename T, int NT, int CANDS, typename Emit>
+__device__ __forceinline__ void largest(const T *z, const float *bias, int c, int k, float top, ListShared<NT, CANDS> &sh, const Emit &emit) {
+    constexpr int kCands = CANDS;
     const int lane = threadIdx.x & 63;
     sh.orders[threadIdx.x] = order_of(top);
-    if (threadIdx.x == 0) sh.nhot = sh.n = 0;
     __syncthreads();
-    if (threadIdx.x < 64) {
-        const uint32_t t = kth_of<NT>(sh.orders, k);
-        if (lane == 0) sh.tau = max(t, 1u);
-    }
-    __syncthreads();
-    if (sh.orders[threadIdx.x] >= sh.tau) sh.hot[atomicAdd(&sh.nhot, 1)] = threadIdx.x;
-    __syncthreads();
-    collect<T, NT>(z, bias, c, sh, sh.tau);
+    // sixteen bits of it will do, but where too many classes have the same ones: then all, the classes above it, and the
+    // first of those equal to it (masks of a finite number)
+    const auto set_tau = [&](int low) {
+        if (threadIdx.x < 64) {
+            const uint32_t t = kth_of<NT>(sh.orders, k, low);
+            if (lane == 0) {
+                sh.tau = max(t, 1u);
+                sh.nhot = sh.n = 0;
+            }
+        }
+        __syncthreads();
+        if (sh.orders[threadIdx.x] >= sh.tau) sh.hot[atomicAdd(&sh.nhot, 1)] = threadIdx.x;
+        __syncthreads();
+    };
+    set_tau(16);
+    collect<T, NT, CANDS>(z, bias, c, sh, sh.tau);
     __syncthreads();
     int n = sh.n;
     if (n > kCands) {
-        // many classes of the same x (masks of a finite number): those above it, then the first of the equal ones
         __syncthreads();
-        if (threadIdx.x == 0) sh.n = 0;
-        __syncthreads();
-        collect<T, NT>(z, bias, c, sh, sh.tau + 1);
+        set_tau(0);
+        collect<T, NT, CANDS>(z, bias, c, sh, sh.tau + 1);
         __syncthreads();
         n = sh.n;
         if (n <= kCands - 128) {
             const int want = max(k - n, 0);
-            first_equal<T, NT>(z, bias, c, sh, n, want);
+            first_equal<T, NT, CANDS>(z, bias, c, sh, n, want);
             n += want;
             __syncthreads();
         }
@@ -361,7 +367,7 @@ __device__ __forceinline__ void largest(const T *z, const float *bias, int c, in
     // the largest classes crowd in few lanes: one after the other, each by a reading of the row
     u64 last = ~0ull;
     for (int q = 0; q < k; ++q) {
-        if (last != 0) last = next_below<T, NT>(z, bias, c, sh, last);
+        if (last != 0) last = next_below<T, NT, CANDS>(z, bias, c, sh, last);
         if ((last >> 32) == 0) last = 0;             // nothing but -inf is left
         if (threadIdx.x == 0) emit(q, last);
     }
@@ -407,10 +413,10 @@ __device__ __forceinline__ void put_class(const LogprobArgs &a, int64_t r, int r
     a.top_logp[r * a.k + rank] = key ? (value_of((uint32_t)(key >> 32)) - m) * (1.f / a.temperature) - ls : -INFINITY;
 }
 
-template <typename T, int NT>
+template <typename T, int NT, int CANDS>
 __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
     __shared__ RowStats<NT> st;
-    __shared__ ListShared<NT> sh;
+    __shared__ ListShared<NT, CANDS> sh;
     const int64_t r = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (r >= a.n) return;
     const float ct = kLog2e / a.temperature;
@@ -421,7 +427,7 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
     float m, s, W, ls, top;
     row_sums<T, NT>(z, a.bias, a.c, ct, a.k > 0 ? sh.groups : nullptr, st, top, m, s, W);
     if (finish_row<NT>(a, r, xt, m, s, W, ls))
-        largest<T, NT>(z, a.bias, a.c, a.k, top, sh, [&](int rank, u64 key) { put_class(a, r, rank, key, m, ls); });
+        largest<T, NT, CANDS>(z, a.bias, a.c, a.k, top, sh, [&](int rank, u64 key) { put_class(a, r, rank, key, m, ls); });
 }
 
 // Few long rows: each cut into parts, a workgroup each, which leave their maximum, sums and k largest classes in the
@@ -435,7 +441,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobArgs a, PartStats *stats, u64 *lists, int parts, int part_len) {
     constexpr int NT = 256;
     __shared__ RowStats<NT> st;
-    __shared__ ListShared<NT> sh;
+    __shared__ ListShared<NT, 1024> sh;
     const int64_t r = blockIdx.y;
     const int part = blockIdx.x, j0 = part * part_len, c = min(part_len, a.c - j0);
     const float ct = kLog2e / a.temperature;
@@ -447,7 +453,7 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobArgs a, PartSt
     if (threadIdx.x == 0) stats[r * parts + part] = PartStats{m, s, W};
     if (a.k == 0 || !(s < INFINITY)) return;         // (a NaN row has no list)
     u64 *const list = lists + (r * parts + part) * a.k;
-    largest<T, NT>(z, bias, c, a.k, top, sh, [&](int rank, u64 key) { list[rank] = key ? key - (u64)j0 : 0ull; });
+    largest<T, NT, 1024>(z, bias, c, a.k, top, sh, [&](int rank, u64 key) { list[rank] = key ? key - (u64)j0 : 0ull; });
 }
 
 template <typename T>
@@ -588,12 +594,13 @@ static void launch_rows(const LogprobArgs &a, void *ws, hipStream_t st) {
         const int used = (a.c + len - 1) / len;
         hipLaunchKernelGGL((logprob_part_kernel<T>), dim3(used, (unsigned)a.n), dim3(256), 0, st, a, stats, lists, used, len);
         hipLaunchKernelGGL((logprob_join_kernel<T>), dim3((unsigned)a.n), dim3(256), 0, st, a, stats, lists, used);
-    } else if (a.c <= kCands) {
-        hipLaunchKernelGGL((logprob_kernel<T, 64>), grid_2d(a.n), dim3(64), 0, st, a);
+    } else if (a.c <= 1024) {
+        if (a.k <= 32) hipLaunchKernelGGL((logprob_kernel<T, 64, 320>), grid_2d(a.n), dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((logprob_kernel<T, 64, 1024>), grid_2d(a.n), dim3(64), 0, st, a);
     } else if (a.n > 256 || a.c <= 16384) {
-        hipLaunchKernelGGL((logprob_kernel<T, 256>), grid_2d(a.n), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((logprob_kernel<T, 256, 1024>), grid_2d(a.n), dim3(256), 0, st, a);
     } else {
-        hipLaunchKernelGGL((logprob_kernel<T, 1024>), grid_2d(a.n), dim3(1024), 0, st, a);
+        hipLaunchKernelGGL((logprob_kernel<T, 1024, 1024>), grid_2d(a.n), dim3(1024), 0, st, a);
     }
 }
 

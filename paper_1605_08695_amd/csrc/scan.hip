@@ -28,7 +28,7 @@
 namespace tfk {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kRun = 32;                           // tokens of a wave's run, or of its half waves' two
+constexpr int kRun = 32, kShort = 8;               // tokens of a wave's run, or of its half waves' two
 constexpr int kStrip = 64;                         // channels of a workgroup
 constexpr int kSegments = 64;                      // the most a sequence is cut into
 
@@ -92,10 +92,10 @@ struct Chans<bf16_t, 2> {
 
 // The strip, sequence and run of tokens of a lane.  w, segment, b and whole (whether the strip has all its channels)
 // are the same for a wave.
-template <typename T, int V>
+template <typename T, int V, int RUN>
 struct Lane {
     static constexpr int kRow = 64 / V;                       // lanes of a row of the strip
-    static constexpr int kSteps = kRun / V;                   // tokens a lane has in registers
+    static constexpr int kSteps = RUN / V;                      // tokens a lane has in registers
     int sub, w, c, segment;
     int64_t b;
     bool whole;
@@ -111,10 +111,10 @@ struct Lane {
 // channel is not there gives kNowhere, past the descriptor's end: it reads 0 and writes nothing, without a branch.
 constexpr uint32_t kNowhere = 0x80000000u;
 
-template <typename T, int V>
+template <typename T, int V, int RUN>
 struct Rows {
     typedef std::remove_const_t<T> E;
-    typedef Lane<E, V> L;
+    typedef Lane<E, V, RUN> L;
     T *p;
     int64_t ts;
     uint32_t off, off_all, off_half;   // where a lane reads, writes all of its channels, and the first one alone
@@ -197,7 +197,7 @@ __device__ __forceinline__ void join_segments(const float2 *agg, int64_t at, int
 // to agg[b][segment][channel].  Each of four waves takes a quarter of the segment, run by run.
 template <typename T, int V, bool OUT, bool BWD>
 __global__ __launch_bounds__(256) void scan_segments_kernel(ScanSegArgs a, float2 *agg, int segments, int seg_len) {
-    typedef Lane<T, V> L;
+    typedef Lane<T, V, kRun> L;
     constexpr int kSteps = L::kSteps;
     __shared__ Span spans[4][kStrip];
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(256) void scan_segments_kernel(ScanSegArgs a, float
         bo[e] = OUT && a.bias ? a.bias[2 * d + c] : 0.f;
         m[e] = Span{0.f, 0.f, 1.f};
     }
-    const Rows<const T, V> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
+    const Rows<const T, V, kRun> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
     const int quarter = l.segment * seg_len + l.w * (seg_len / 4);
     const auto run = [&](int tw, auto inside) {
         constexpr bool INSIDE = decltype(inside)::value;
@@ -281,10 +281,10 @@ __global__ __launch_bounds__(256) void scan_segments_kernel(ScanSegArgs a, float
     if (c < d) agg[(l.b * segments + l.segment) * d + c] = make_float2(n.S, span(n.Q, n.P));
 }
 
-template <typename T, int V, bool OUT, int W>
-__global__ __launch_bounds__(64 * W, OUT ? 3 : 4) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
-    typedef Lane<T, V> L;
-    constexpr int kSteps = L::kSteps, kBlock = W * kRun;
+template <typename T, int V, bool OUT, int W, int RUN>
+__global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : OUT ? 3 : 4) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
+    typedef Lane<T, V, RUN> L;
+    constexpr int kSteps = L::kSteps, kBlock = W * RUN;
     __shared__ float2 spans[2][W][kStrip];
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
     const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
@@ -301,14 +301,14 @@ __global__ __launch_bounds__(64 * W, OUT ? 3 : 4) void scan_fwd_kernel(ScanArgs 
         H[e] = a.h0 ? a.h0[l.b * d + c] : 0.f;
     }
     if (l.segment > 0) join_segments<V>(agg, l.b * segments * d, d, l.segment, l.c, d, H);
-    const Rows<const T, V> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l);
-    const Rows<T, V> y((T *)a.y + l.b * a.y_bs, a.y_ts, l);
+    const Rows<const T, V, RUN> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l);
+    const Rows<T, V, RUN> y((T *)a.y + l.b * a.y_bs, a.y_ts, l);
     const int blocks = (a.t + kBlock - 1) / kBlock, saved = (a.t + kScanBlock - 1) / kScanBlock;
     const int col = threadIdx.x % L::kRow * V;
     // INSIDE: all of the block's tokens and channels are there
     const auto block = [&](int blk, auto inside) {
         constexpr bool INSIDE = decltype(inside)::value;
-        const int tw = blk * kBlock + l.w * kRun, t0 = tw + l.sub * kSteps;
+        const int tw = blk * kBlock + l.w * RUN, t0 = tw + l.sub * kSteps;
         float s[kSteps][V], x[kSteps][V], o[OUT ? kSteps : 1][V];
         {
             typename Chans<T, V>::raw rx[kSteps], rf[kSteps], ro[OUT ? kSteps : 1];
@@ -382,7 +382,7 @@ __global__ __launch_bounds__(64 * W, OUT ? 3 : 4) void scan_fwd_kernel(ScanArgs 
         } else if (blk * kBlock < len) {
             block(blk, std::false_type{});
         } else {                                   // padding from here on
-            const int tw = blk * kBlock + l.w * kRun, t0 = tw + l.sub * kSteps;
+            const int tw = blk * kBlock + l.w * RUN, t0 = tw + l.sub * kSteps;
             const float none[2] = {0.f, 0.f};
             for (int i = 0; i < kSteps; ++i)
                 y.store(y.row(tw + i), none, t0 + i < a.t, l.whole);
@@ -394,10 +394,10 @@ __global__ __launch_bounds__(64 * W, OUT ? 3 : 4) void scan_fwd_kernel(ScanArgs 
             if (l.c + e < d) a.h_last[l.b * d + l.c + e] = H[e];
 }
 
-template <typename T, int V, bool OUT, int W>
-__global__ __launch_bounds__(64 * W, OUT ? 2 : 3) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
-    typedef Lane<T, V> L;
-    constexpr int kSteps = L::kSteps, kBlock = W * kRun;
+template <typename T, int V, bool OUT, int W, int RUN>
+__global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : OUT ? 2 : 3) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
+    typedef Lane<T, V, RUN> L;
+    constexpr int kSteps = L::kSteps, kBlock = W * RUN;
     __shared__ float2 spans[2][W][kStrip];
     __shared__ float backs[2][W][kStrip];
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
@@ -416,13 +416,13 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 3) void scan_bwd_kernel(ScanBwdAr
     }
     if (l.segment < segments - 1)
         join_segments<V>(agg, (l.b * segments + segments - 1) * d, -(int64_t)d, segments - 1 - l.segment, l.c, d, C);
-    const Rows<const T, V> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
-    const Rows<T, V> dz((T *)a.dz + l.b * a.dz_bs, a.dz_ts, l);
+    const Rows<const T, V, RUN> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
+    const Rows<T, V, RUN> dz((T *)a.dz + l.b * a.dz_bs, a.dz_ts, l);
     const int blocks = (a.t + kBlock - 1) / kBlock, saved = (a.t + kScanBlock - 1) / kScanBlock;
     const int col = threadIdx.x % L::kRow * V;
     const auto block = [&](int blk, auto inside) {
         constexpr bool INSIDE = decltype(inside)::value;
-        const int tw = blk * kBlock + l.w * kRun, t0 = tw + l.sub * kSteps;
+        const int tw = blk * kBlock + l.w * RUN, t0 = tw + l.sub * kSteps;
         float s[kSteps][V], x[kSteps][V], up[kSteps][V], o[OUT ? kSteps : 1][V], h[V];
         {
             typename Chans<T, V>::raw rx[kSteps], rf[kSteps], ru[kSteps], ro[OUT ? kSteps : 1];
@@ -545,7 +545,7 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 3) void scan_bwd_kernel(ScanBwdAr
         } else if (blk * kBlock < len) {
             block(blk, std::false_type{});
         } else {                                   // padding
-            const int tw = blk * kBlock + l.w * kRun, t0 = tw + l.sub * kSteps;
+            const int tw = blk * kBlock + l.w * RUN, t0 = tw + l.sub * kSteps;
             const float none[2] = {0.f, 0.f};
             for (int i = 0; i < kSteps; ++i)
                 for (int k = 0; k < (OUT ? 3 : 2); ++k) dz.store(dz.row(tw + i) + k * d, none, t0 + i < a.t, l.whole);
@@ -596,14 +596,17 @@ size_t scan_ws_bytes(bool, int64_t b, int64_t t, int d) {
     return segments > 1 ? (size_t)b * segments * d * sizeof(float2) : 0;
 }
 
+// So few workgroups leave the chip's lanes idle: each is given four times the waves, with a quarter of a run each.
+constexpr int kFewBlocks = 256;
+
 // Two channels a lane in bf16, but for a single channel.
 template <typename T, int V, bool OUT>
 static void launch_fwd(const ScanArgs &a, float2 *ws, hipStream_t st) {
     int segments, seg_len;
     scan_plan(a.b, a.t, a.d, &segments, &seg_len);
     const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
-    if (a.t <= kRun) {
-        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 1>), grid_2d(strips), dim3(64), 0, st, a, ws, 1, kRun);
+    if (a.t <= 4 * kShort) {
+        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 4, kShort>), grid_2d(strips), dim3(256), 0, st, a, ws, 1, 4 * kShort);
         return;
     }
     if (segments > 1) {
@@ -611,7 +614,12 @@ static void launch_fwd(const ScanArgs &a, float2 *ws, hipStream_t st) {
         hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, false>), grid_2d(strips * (segments - 1)), dim3(256), 0, st, g, ws,
                            segments, seg_len);
     }
-    hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 4>), grid_2d(strips * segments), dim3(256), 0, st, a, ws, segments, seg_len);
+    if (strips * segments < kFewBlocks)
+        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 16, kShort>), grid_2d(strips * segments), dim3(1024), 0, st, a, ws, segments,
+                           seg_len);
+    else
+        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 4, kRun>), grid_2d(strips * segments), dim3(256), 0, st, a, ws, segments,
+                           seg_len);
 }
 
 template <typename T, int V, bool OUT>
@@ -619,8 +627,8 @@ static void launch_bwd(const ScanBwdArgs &a, float2 *ws, hipStream_t st) {
     int segments, seg_len;
     scan_plan(a.b, a.t, a.d, &segments, &seg_len);
     const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
-    if (a.t <= kRun) {
-        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 1>), grid_2d(strips), dim3(64), 0, st, a, ws, 1, kRun);
+    if (a.t <= 4 * kShort) {
+        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 4, kShort>), grid_2d(strips), dim3(256), 0, st, a, ws, 1, 4 * kShort);
         return;
     }
     if (segments > 1) {
@@ -628,7 +636,12 @@ static void launch_bwd(const ScanBwdArgs &a, float2 *ws, hipStream_t st) {
         hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, true>), grid_2d(strips * (segments - 1)), dim3(256), 0, st, g, ws,
                            segments, seg_len);
     }
-    hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 4>), grid_2d(strips * segments), dim3(256), 0, st, a, ws, segments, seg_len);
+    if (strips * segments < kFewBlocks)
+        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 16, kShort>), grid_2d(strips * segments), dim3(1024), 0, st, a, ws, segments,
+                           seg_len);
+    else
+        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 4, kRun>), grid_2d(strips * segments), dim3(256), 0, st, a, ws, segments,
+                           seg_len);
 }
 
 #define SCAN_CASES(fn, ...)                                                         \

@@ -902,21 +902,26 @@ def token_logprobs_bwd(logits, tokens, lse, dlogp, entropy=None, dentropy=None, 
 SCAN_BLOCK = 128       # tokens between two states that gated_scan_fwd saves
 
 
-def _seqs(t, name, cols=None) -> Tuple[int, int, int, int, int]:
-    """(b, t, columns, elements between sequences, between rows) of a b x t x columns tensor of either order."""
-    if t.dim() != 3:
-        raise ValueError("%s must be sequences x tokens x columns, got shape %s" % (name, tuple(t.shape)))
-    b, n, c = t.shape
+@functools.lru_cache(_KEPT)
+def _seq_layout(shape, strides, name, cols) -> Tuple[int, int, int, int, int]:
+    if len(shape) != 3:
+        raise ValueError("%s must be sequences x tokens x columns, got shape %s" % (name, tuple(shape)))
+    b, n, c = shape
     if c == 0 or (cols is not None and c != cols):
-        raise ValueError("%s must have %s columns, got shape %s" % (name, cols or "some", tuple(t.shape)))
-    sb, st, sc = t.stride()
+        raise ValueError("%s must have %s columns, got shape %s" % (name, cols or "some", tuple(shape)))
+    sb, st, sc = strides
     if b and n and c > 1 and sc != 1:
-        raise ValueError("%s must have unit stride within rows, got strides %s" % (name, t.stride()))
+        raise ValueError("%s must have unit stride within rows, got strides %s" % (name, tuple(strides)))
     st = st if n > 1 else c
     sb = sb if b > 1 else max(1, n) * st
     if b and n and not ((st >= c and (b == 1 or sb >= (n - 1) * st + c)) or (sb >= c and st >= (b - 1) * sb + c)):
-        raise ValueError("%s must have rows that do not overlap, got shape %s, strides %s" % (name, tuple(t.shape), t.stride()))
+        raise ValueError("%s must have rows that do not overlap, got shape %s, strides %s" % (name, tuple(shape), tuple(strides)))
     return b, n, _width(c, name), sb, st
+
+
+def _seqs(t, name, cols=None) -> Tuple[int, int, int, int, int]:
+    """(b, t, columns, elements between sequences, between rows) of a b x t x columns tensor of either order."""
+    return _seq_layout(t.shape, t.stride(), name, cols)
 
 
 def _scan_args(z, output_gate, bias, lengths):
