@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256) void scan_segments_kernel(ScanSegArgs a, float
 }
 
 template <typename T, int V, bool OUT, int W, int RUN>
-__global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : OUT ? 3 : 4) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
+__global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : 3) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V, RUN> L;
     constexpr int kSteps = L::kSteps, kBlock = W * RUN;
     __shared__ float2 spans[2][W][kStrip];
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : OUT ? 3 : 4) void scan_
 }
 
 template <typename T, int V, bool OUT, int W, int RUN>
-__global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : OUT ? 2 : 3) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
+__global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : 2) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V, RUN> L;
     constexpr int kSteps = L::kSteps, kBlock = W * RUN;
     __shared__ float2 spans[2][W][kStrip];
@@ -583,7 +583,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStepArgs a) {
 static void scan_plan(int64_t b, int64_t t, int d, int *segments, int *seg_len) {
     const int64_t strips = b * ((d + kStrip - 1) / kStrip), blocks = std::max<int64_t>((t + kScanBlock - 1) / kScanBlock, 1);
     int64_t want = 1;
-    if (strips < 512) want = std::min<int64_t>({kSegments, blocks / 2, (1024 + strips - 1) / strips});
+    if (strips < 512) want = std::min<int64_t>({kSegments, blocks / 2, (2048 + strips - 1) / strips});
     want = std::max<int64_t>(want, 1);
     const int64_t per = (blocks + want - 1) / want;
     *segments = (int)((blocks + per - 1) / per);
