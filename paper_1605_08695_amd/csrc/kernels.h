@@ -286,7 +286,6 @@ hipError_t launch_logprob_bwd(int dt, const LogprobBwdArgs &a, hipStream_t st);
 // AdamW over a batch of variables; blocks of 256 values, numbered through the batch.  m, v: fp32, or e4m3
 // values with a scale per block.
 constexpr int kAdamwBatch = 55;               // (a batch is an argument of the kernel: below 4 KB)
-constexpr int64_t kAdamwAway = (int64_t)12 << 20;   // values of a step past the caches
 struct AdamwParams {
     float lr, b1, omb1, b2, omb2, rrc2, eps;     // lr = lr / (1 - b1^t), rrc2 = 1 / sqrt(1 - b2^t)
 };

@@ -574,7 +574,7 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int p
 // Parts of a row, 0 for rows that one workgroup reads: enough for two workgroups a CU, of at least kPartLeast classes.
 // (The list asked for has no say in it, and so none in the sums' order.)
 static int row_parts(int64_t n, int c) {
-    if (n > 256 || c < 4 * kPartLeast) return 0;
+    if (n > 128 || c < 4 * kPartLeast) return 0;
     return (int)std::min<int64_t>({kPartMost, c / kPartLeast, (512 + n - 1) / n});
 }
 

@@ -11,7 +11,7 @@
 // and P = prod f, kept as 1 - P or P, whichever is smaller, in the same way.  Backwards, a span maps what comes from
 // behind, c, to R + P c.
 //
-// A workgroup of W waves has a strip of 64 channels of one sequence and takes it in blocks of W runs of 32 tokens, each
+// A workgroup has a strip of 64 channels of one sequence and takes it in blocks of four runs of 32 tokens, each
 // wave one run in registers (with two bf16 channels a lane each half wave half of it); the waves' spans are joined
 // through LDS, and the workgroup goes on to the next block with the state they leave.  Where there are too few strips
 // for the chip, the time axis is cut into segments: a first launch reads all segments but the last for what each makes
@@ -28,6 +28,7 @@
 namespace tfk {
 
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kWaves = 4;                          // waves of a workgroup
 constexpr int kRun = 32, kShort = 8;               // tokens of a wave's run, or of its half waves' two
 constexpr int kStrip = 64;                         // channels of a workgroup
 constexpr int kSegments = 64;                      // the most a sequence is cut into
@@ -194,12 +195,12 @@ __device__ __forceinline__ void join_segments(const float2 *agg, int64_t at, int
 }
 
 // What each segment but the last makes of the state before it (BWD: each but the first of what comes from behind it),
-// to agg[b][segment][channel].  Each of four waves takes a quarter of the segment, run by run.
+// to agg[b][segment][channel].  Each wave takes a part of the segment, run by run.
 template <typename T, int V, bool OUT, bool BWD>
-__global__ __launch_bounds__(256) void scan_segments_kernel(ScanSegArgs a, float2 *agg, int segments, int seg_len) {
+__global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(ScanSegArgs a, float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V, kRun> L;
     constexpr int kSteps = L::kSteps;
-    __shared__ Span spans[4][kStrip];
+    __shared__ Span spans[kWaves][kStrip];
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
     const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (job >= a.b * strips * (segments - 1)) return;
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(256) void scan_segments_kernel(ScanSegArgs a, float
         m[e] = Span{0.f, 0.f, 1.f};
     }
     const Rows<const T, V, kRun> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
-    const int quarter = l.segment * seg_len + l.w * (seg_len / 4);
+    const int part = l.segment * seg_len + l.w * (seg_len / kWaves);
     const auto run = [&](int tw, auto inside) {
         constexpr bool INSIDE = decltype(inside)::value;
         const int t0 = tw + l.sub * kSteps;
@@ -263,9 +264,9 @@ __global__ __launch_bounds__(256) void scan_segments_kernel(ScanSegArgs a, float
             m[e] = m[e].then(n[e]);
         }
     };
-    const int runs = seg_len / 4 / kRun;
+    const int runs = seg_len / kWaves / kRun;
     for (int k = 0; k < runs; ++k) {
-        const int tw = quarter + (BWD ? runs - 1 - k : k) * kRun;
+        const int tw = part + (BWD ? runs - 1 - k : k) * kRun;
         if (tw + kRun <= len) run(tw, std::true_type{});
         else if (tw < len) run(tw, std::false_type{});
     }
@@ -274,18 +275,18 @@ __global__ __launch_bounds__(256) void scan_segments_kernel(ScanSegArgs a, float
         if (V == 1 || l.sub == e) spans[l.w][threadIdx.x % L::kRow * V + e] = m[e];
     __syncthreads();
     if (threadIdx.x >= kStrip) return;
-    Span n = spans[BWD ? 3 : 0][threadIdx.x];
+    Span n = spans[BWD ? kWaves - 1 : 0][threadIdx.x];
 #pragma unroll
-    for (int v = 1; v < 4; ++v) n = n.then(spans[BWD ? 3 - v : v][threadIdx.x]);
+    for (int v = 1; v < kWaves; ++v) n = n.then(spans[BWD ? kWaves - 1 - v : v][threadIdx.x]);
     const int c = (int)(job % strips) * kStrip + threadIdx.x;
     if (c < d) agg[(l.b * segments + l.segment) * d + c] = make_float2(n.S, span(n.Q, n.P));
 }
 
-template <typename T, int V, bool OUT, int W, int RUN>
-__global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : 3) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
+template <typename T, int V, bool OUT, int RUN>
+__global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 3) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V, RUN> L;
-    constexpr int kSteps = L::kSteps, kBlock = W * RUN;
-    __shared__ float2 spans[2][W][kStrip];
+    constexpr int kSteps = L::kSteps, kBlock = kWaves * RUN;
+    __shared__ float2 spans[2][kWaves][kStrip];
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
     const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (job >= a.b * strips * segments) return;
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : 3) void scan_fwd_kernel
         for (int e = 0; e < V; ++e) {
             if (a.states && threadIdx.x < L::kRow && l.c + e < d) a.states[(l.b * saved + blk) * d + l.c + e] = H[e];
 #pragma unroll
-            for (int v = 0; v < W; ++v) {
+            for (int v = 0; v < kWaves; ++v) {
                 if (v == l.w) h[e] = H[e];
                 const float2 q = spans[blk & 1][v][col + e];
                 H[e] = join(H[e], q.y, q.x);
@@ -394,12 +395,12 @@ __global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : 3) void scan_fwd_kernel
             if (l.c + e < d) a.h_last[l.b * d + l.c + e] = H[e];
 }
 
-template <typename T, int V, bool OUT, int W, int RUN>
-__global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : 2) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
+template <typename T, int V, bool OUT, int RUN>
+__global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V, RUN> L;
-    constexpr int kSteps = L::kSteps, kBlock = W * RUN;
-    __shared__ float2 spans[2][W][kStrip];
-    __shared__ float backs[2][W][kStrip];
+    constexpr int kSteps = L::kSteps, kBlock = kWaves * RUN;
+    __shared__ float2 spans[2][kWaves][kStrip];
+    __shared__ float backs[2][kWaves][kStrip];
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
     const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (job >= a.b * strips * segments) return;
@@ -489,12 +490,12 @@ __global__ __launch_bounds__(64 * W, RUN == kShort ? 4 : 2) void scan_bwd_kernel
 #pragma unroll
         for (int e = 0; e < V; ++e) {
 #pragma unroll
-            for (int v = 0; v < W - 1; ++v) {
+            for (int v = 0; v < kWaves - 1; ++v) {
                 const float2 q = spans[blk & 1][v][col + e];
                 if (v < l.w) h[e] = join(h[e], q.y, q.x);
             }
 #pragma unroll
-            for (int v = W - 1; v >= 0; --v) {
+            for (int v = kWaves - 1; v >= 0; --v) {
                 if (v == l.w) c[e] = C[e];
                 C[e] = join(C[e], spans[blk & 1][v][col + e].y, backs[blk & 1][v][col + e]);
             }
@@ -596,30 +597,23 @@ size_t scan_ws_bytes(bool, int64_t b, int64_t t, int d) {
     return segments > 1 ? (size_t)b * segments * d * sizeof(float2) : 0;
 }
 
-// So few workgroups leave the chip's lanes idle: each is given four times the waves, with a quarter of a run each.
-constexpr int kFewBlocks = 256;
-
 // Two channels a lane in bf16, but for a single channel.
 template <typename T, int V, bool OUT>
 static void launch_fwd(const ScanArgs &a, float2 *ws, hipStream_t st) {
     int segments, seg_len;
     scan_plan(a.b, a.t, a.d, &segments, &seg_len);
     const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
-    if (a.t <= 4 * kShort) {
-        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 4, kShort>), grid_2d(strips), dim3(256), 0, st, a, ws, 1, 4 * kShort);
+    if (a.t <= kWaves * kShort) {
+        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, kShort>), grid_2d(strips), dim3(64 * kWaves), 0, st, a, ws, 1, kWaves * kShort);
         return;
     }
     if (segments > 1) {
         const ScanSegArgs g{a.z, a.z_bs, a.z_ts, a.bias, a.lengths, nullptr, 0, 0, a.b, a.t, a.d};
-        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, false>), grid_2d(strips * (segments - 1)), dim3(256), 0, st, g, ws,
+        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, false>), grid_2d(strips * (segments - 1)), dim3(64 * kWaves), 0, st, g, ws,
                            segments, seg_len);
     }
-    if (strips * segments < kFewBlocks)
-        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 16, kShort>), grid_2d(strips * segments), dim3(1024), 0, st, a, ws, segments,
-                           seg_len);
-    else
-        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, 4, kRun>), grid_2d(strips * segments), dim3(256), 0, st, a, ws, segments,
-                           seg_len);
+    hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, kRun>), grid_2d(strips * segments), dim3(64 * kWaves), 0, st, a, ws, segments,
+                       seg_len);
 }
 
 template <typename T, int V, bool OUT>
@@ -627,21 +621,17 @@ static void launch_bwd(const ScanBwdArgs &a, float2 *ws, hipStream_t st) {
     int segments, seg_len;
     scan_plan(a.b, a.t, a.d, &segments, &seg_len);
     const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
-    if (a.t <= 4 * kShort) {
-        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 4, kShort>), grid_2d(strips), dim3(256), 0, st, a, ws, 1, 4 * kShort);
+    if (a.t <= kWaves * kShort) {
+        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, kShort>), grid_2d(strips), dim3(64 * kWaves), 0, st, a, ws, 1, kWaves * kShort);
         return;
     }
     if (segments > 1) {
         const ScanSegArgs g{a.z, a.z_bs, a.z_ts, a.bias, a.lengths, a.dy, a.dy_bs, a.dy_ts, a.b, a.t, a.d};
-        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, true>), grid_2d(strips * (segments - 1)), dim3(256), 0, st, g, ws,
+        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, true>), grid_2d(strips * (segments - 1)), dim3(64 * kWaves), 0, st, g, ws,
                            segments, seg_len);
     }
-    if (strips * segments < kFewBlocks)
-        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 16, kShort>), grid_2d(strips * segments), dim3(1024), 0, st, a, ws, segments,
-                           seg_len);
-    else
-        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, 4, kRun>), grid_2d(strips * segments), dim3(256), 0, st, a, ws, segments,
-                           seg_len);
+    hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, kRun>), grid_2d(strips * segments), dim3(64 * kWaves), 0, st, a, ws, segments,
+                       seg_len);
 }
 
 #define SCAN_CASES(fn, ...)                                                         \
