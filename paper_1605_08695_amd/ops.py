@@ -934,12 +934,12 @@ def _scan_args(z, output_gate, bias, lengths):
     return gates, b, t, cols // gates, zb, zt
 
 
-def _like_seqs(stream, z, cols):
-    """A dense b x t x cols tensor with z's order of sequences and tokens."""
+def _like_seqs(stream, z, cols, zb, zt):
+    """A dense b x t x cols tensor with z's order of sequences and tokens, and its two distances."""
     b, t = z.shape[:2]
-    if b > 1 and t > 1 and z.stride(0) < z.stride(1):
-        return _empty(stream, (t, b, cols), dtype=z.dtype, device=z.device).transpose(0, 1)
-    return _empty(stream, (b, t, cols), dtype=z.dtype, device=z.device)
+    if b > 1 and t > 1 and zb < zt:
+        return _empty(stream, (t, b, cols), dtype=z.dtype, device=z.device).transpose(0, 1), cols, b * cols
+    return _empty(stream, (b, t, cols), dtype=z.dtype, device=z.device), t * cols, cols
 
 
 def _states_of(h, b, d, name):
@@ -978,8 +978,9 @@ def gated_scan_fwd(z, output_gate=False, bias=None, h0=None, lengths=None, y=Non
         raise ValueError("y must be %s of z's type" % ((b, t, d),))
     st = _on_device(stream, z, bias, h0, lengths, y, ws)
     if y is None:
-        y = _like_seqs(stream, z, d)
-    _, _, _, yb, yt = _seqs(y, "y", d)
+        y, yb, yt = _like_seqs(stream, z, d, zb, zt)
+    else:
+        yb, yt = _seqs(y, "y", d)[3:]
     last = _empty(stream, (b, d), dtype=torch.float32, device=z.device)
     states = None
     if save:
@@ -998,7 +999,7 @@ def gated_scan_bwd(z, dy, states, output_gate=False, bias=None, lengths=None, dh
     dt = _dt(z)
     if tuple(dy.shape) != (b, t, d) or dy.dtype != z.dtype:
         raise ValueError("dy must be %s of z's type" % ((b, t, d),))
-    _, _, _, yb, yt = _seqs(dy, "dy", d)
+    yb, yt = _seqs(dy, "dy", d)[3:]
     _states_of(dh_last, b, d, "dh_last")
     blocks = (t + SCAN_BLOCK - 1) // SCAN_BLOCK
     if states.dtype != torch.float32 or tuple(states.shape) != (b, blocks, d) or not states.is_contiguous():
@@ -1007,8 +1008,9 @@ def gated_scan_bwd(z, dy, states, output_gate=False, bias=None, lengths=None, dh
         raise ValueError("dz must have z's shape and type")
     st = _on_device(stream, z, dy, states, bias, lengths, dh_last, dz, ws)
     if dz is None:
-        dz = _like_seqs(stream, z, gates * d)
-    _, _, _, gb, gt = _seqs(dz, "dz")
+        dz, gb, gt = _like_seqs(stream, z, gates * d, zb, zt)
+    else:
+        gb, gt = (zb, zt) if dz is z else _seqs(dz, "dz")[3:]
     dh0 = _empty(stream, (b, d), dtype=torch.float32, device=z.device)
     ws, need = _scan_ws(1, b, t, d, ws, z.device, stream)
     check(load().tfk_gated_scan_bwd(_ptr(z), dt, b, t, d, gates, zb, zt, _ptr(bias), _ptr(lengths), _ptr(dy), yb, yt,

@@ -36,8 +36,10 @@ class GatedRecurrence:
         self.b = torch.from_numpy(np.asarray(b, np.float32)).to(dev)
 
     def _product(self, x: torch.Tensor, stream) -> torch.Tensor:
+        if not x.is_contiguous():
+            raise ValueError("the layer's input must be contiguous")
         n = x.numel() // self.d_in
-        z = ops.conv2d_fwd(x.reshape(n, 1, 1, self.d_in), self.W_lp.view(1, 1, self.d_in, -1), 1, (0, 0, 0, 0), stream=stream)
+        z = ops.conv2d_fwd(x.view(n, 1, 1, self.d_in), self.W_lp.view(1, 1, self.d_in, -1), 1, (0, 0, 0, 0), stream=stream)
         return z.view(*x.shape[:-1], z.shape[-1])
 
     def forward(self, x: torch.Tensor, h0=None, lengths=None, save: bool = True, stream=None):

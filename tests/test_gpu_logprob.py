@@ -203,6 +203,17 @@ def test_masks(c, dt):
     assert not d[7].any() and not d[0][~keep[0]].any()
 
 
+@pytest.mark.parametrize("T", [1e-4, 0.01, 100.0, 1e4])
+def test_temperatures(T):
+    for c in (700, 5000, 70001):
+        z = logits(5, c, F32, c)
+        check(z, None, toks(5, c, 1), T, 20)
+        r = ops.token_logprobs(z, toks(5, c, 1, pad=False), 0, T)
+        d = ops.token_logprobs_bwd(z, toks(5, c, 1, pad=False), r.lse, torch.ones(5, device=DEV), r.entropy, torch.ones(5, device=DEV), T)
+        torch.cuda.synchronize()
+        assert torch.isfinite(d).all()
+
+
 def test_nan_and_infinite_rows():
     for c in (5, 3000, 70000, 140000):
         z = logits(4, c, F32, c)

@@ -171,6 +171,7 @@ def _t(*shape, dtype=torch.float32):
 
 
 I32, F8 = torch.int32, torch.float8_e4m3fn
+_S = torch.zeros(8)
 
 
 def test_binding_refuses_host_tensors():
@@ -207,7 +208,8 @@ def test_binding_refuses_host_tensors():
     lambda: AdamW([_t(4)], 0.1, bits=16), lambda: AdamW([_t(4, dtype=torch.bfloat16)], 0.1), lambda: AdamW([_t(4)], 0.1, weight_decay=[0.1, 0.2]),
     lambda: AdamW([_t(4)], 0.1, shadows=[_t(4)]), lambda: AdamW([_t(4, 4).t()], 0.1), lambda: AdamW([_t(4)], 0.1, bits=8, moments=([_t(4)], [_t(4)], None, None)),
     lambda: AdamW([_t(400)], 0.1, bits=8, moments=([_t(400, dtype=F8)], [_t(400, dtype=F8)], [_t(1)], [_t(2)])),
-    lambda: AdamW([_t(4)], 0.1).step([]), lambda: AdamW([_t(4)], 0.1).step([_t(5)]), lambda: AdamW([_t(4)], 0.1).step([_t(4, dtype=torch.bfloat16)]),
+    lambda: AdamW([_S, _S], 0.1), lambda: AdamW([_S[:3], _S[2:]], 0.1), lambda: AdamW([_t(8)], 0.1, moments=([_S], [_S], None, None)),
+    lambda: AdamW([_t(8), _t(8)], 0.1, moments=([_S, _t(8)], [_t(8), _S], None, None)), lambda: AdamW([_t(4)], 0.1).step([]), lambda: AdamW([_t(4)], 0.1).step([_t(5)]), lambda: AdamW([_t(4)], 0.1).step([_t(4, dtype=torch.bfloat16)]),
     lambda: ops.apply_adamw_multi([_t(4)], [_t(4)], [], [_t(4)], 0.1, 0.9, 0.99, 0.0, 1),
     lambda: GatedRecurrence(np.zeros((4, 7)), np.zeros(7), device="cpu"), lambda: GatedRecurrence(np.zeros((4, 6)), np.zeros(5), device="cpu"),
 ])
