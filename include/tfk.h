@@ -582,7 +582,7 @@ TFK_API tfk_status tfk_token_logprobs_bwd(const void *logits, tfk_dtype dt, int6
  * Errors: b, t < 0, d < 1, rows that overlap (SHAPE); gates not 2 or 3 (ARG); b > 2^31 - 1, t > 2^30 - 1, d > 2^24,
  * more than 2^40 elements, rows of a sequence more than 2^25 elements apart, negative strides (OVERFLOW); NULL,
  * misaligned or overlapping buffers (NULL, ALIGN, ALIAS); WORKSPACE.  b == 0 is a no-op; t == 0 sets h_last to h0. */
-#define TFK_SCAN_BLOCK 128
+#define TFK_SCAN_BLOCK 16
 TFK_API tfk_status tfk_gated_scan_fwd(const void *z, tfk_dtype dt, int64_t b, int64_t t, int32_t d, int32_t gates,
                               int64_t z_bs, int64_t z_ts, const float *bias, const float *h0, const int32_t *lengths,
                               void *y, int64_t y_bs, int64_t y_ts, float *h_last, float *states, void *ws,

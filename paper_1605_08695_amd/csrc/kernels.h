@@ -212,7 +212,7 @@ inline dim3 grid_2d(int64_t n) {
 
 // Gated linear recurrence (see tfk_gated_scan_fwd): b sequences of t tokens, d channels; element strides of
 // sequences (_bs) and tokens (_ts).  bias, h0, lengths, h_last, states, dh_last and dh0 may be null.
-constexpr int kScanBlock = 128;       // tokens between two saved states
+constexpr int kScanBlock = 16;        // tokens between two saved states
 constexpr int64_t kScanRowStep = (int64_t)1 << 25;
 struct ScanArgs {
     const void *z;

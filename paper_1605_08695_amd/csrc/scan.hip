@@ -196,9 +196,9 @@ __device__ __forceinline__ void join_segments(const float2 *agg, int64_t at, int
 
 // What each segment but the last makes of the state before it (BWD: each but the first of what comes from behind it),
 // to agg[b][segment][channel].  Each wave takes a part of the segment, run by run.
-template <typename T, int V, bool OUT, bool BWD>
+template <typename T, int V, bool OUT, bool BWD, int RUN>
 __global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(ScanSegArgs a, float2 *agg, int segments, int seg_len) {
-    typedef Lane<T, V, kRun> L;
+    typedef Lane<T, V, RUN> L;
     constexpr int kSteps = L::kSteps;
     __shared__ Span spans[kWaves][kStrip];
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(ScanSegArgs 
         bo[e] = OUT && a.bias ? a.bias[2 * d + c] : 0.f;
         m[e] = Span{0.f, 0.f, 1.f};
     }
-    const Rows<const T, V, kRun> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
+    const Rows<const T, V, RUN> z((const T *)a.z + l.b * a.z_bs, a.z_ts, l), dy((const T *)a.dy + l.b * a.dy_bs, a.dy_ts, l);
     const int part = l.segment * seg_len + l.w * (seg_len / kWaves);
     const auto run = [&](int tw, auto inside) {
         constexpr bool INSIDE = decltype(inside)::value;
@@ -264,10 +264,10 @@ __global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(ScanSegArgs 
             m[e] = m[e].then(n[e]);
         }
     };
-    const int runs = seg_len / kWaves / kRun;
+    const int runs = seg_len / kWaves / RUN;
     for (int k = 0; k < runs; ++k) {
-        const int tw = part + (BWD ? runs - 1 - k : k) * kRun;
-        if (tw + kRun <= len) run(tw, std::true_type{});
+        const int tw = part + (BWD ? runs - 1 - k : k) * RUN;
+        if (tw + RUN <= len) run(tw, std::true_type{});
         else if (tw < len) run(tw, std::false_type{});
     }
 #pragma unroll
@@ -355,7 +355,6 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 3) void scan_fwd_k
         float h[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            if (a.states && threadIdx.x < L::kRow && l.c + e < d) a.states[(l.b * saved + blk) * d + l.c + e] = H[e];
 #pragma unroll
             for (int v = 0; v < kWaves; ++v) {
                 if (v == l.w) h[e] = H[e];
@@ -367,6 +366,12 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 3) void scan_fwd_k
         T *r = y.row(tw);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i, r += y.ts) {
+            if (i % kScanBlock == 0 && a.states && (kSteps >= kScanBlock || t0 % kScanBlock == 0) && (INSIDE || t0 + i < a.t)) {
+                float *const st = a.states + (l.b * saved + (t0 + i) / kScanBlock) * d + l.c;
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (INSIDE || l.c + e < d) st[e] = h[e];
+            }
             float out[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -398,9 +403,12 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 3) void scan_fwd_k
 template <typename T, int V, bool OUT, int RUN>
 __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
     typedef Lane<T, V, RUN> L;
+    // DIRECT: a state was saved for each lane's first token; else the runs since the last one are joined
     constexpr int kSteps = L::kSteps, kBlock = kWaves * RUN;
-    __shared__ float2 spans[2][kWaves][kStrip];
-    __shared__ float backs[2][kWaves][kStrip];
+    constexpr bool DIRECT = kSteps >= kScanBlock;
+    constexpr int kSince = DIRECT ? 1 : kScanBlock / RUN;          // waves since a saved state
+    __shared__ float2 spans[2][kWaves][kStrip];                    // backwards: R, and the smaller of 1 - P and P
+    __shared__ float fronts[2][DIRECT ? 1 : kWaves][kStrip];       // forwards: S
     const int d = a.d, strips = (d + kStrip - 1) / kStrip;
     const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (job >= a.b * strips * segments) return;
@@ -436,8 +444,9 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_k
                 ru[i] = dy.load(ry, in);
                 if (OUT) ro[i] = z.load(r + 2 * d, in);
             }
+            const int at = min((t0 - (DIRECT ? 0 : (l.w % kSince) * RUN + l.sub * kSteps)) / kScanBlock, saved - 1);
 #pragma unroll
-            for (int e = 0; e < V; ++e) h[e] = a.states[(l.b * saved + blk) * d + min(l.c + e, d - 1)];
+            for (int e = 0; e < V; ++e) h[e] = a.states[(l.b * saved + at) * d + min(l.c + e, d - 1)];
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 l.ch.unpack(rx[i], x[i]);
@@ -446,6 +455,24 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_k
                 if (OUT) l.ch.unpack(ro[i], o[i]);
             }
         }
+        // Forwards with the states: x becomes h_(t-1) - x, dy becomes what reaches h_t, and the output gate's gradient
+        // is done.
+        T *r = dz.row(tw);
+        const auto forward = [&](int i, float(&out)[V]) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float before = h[e];
+                h[e] = move(before, fresh(s[i][e]), x[i][e]);
+                x[i][e] = before - x[i][e];
+                if (OUT) {
+                    const float so = fresh(o[i][e]);
+                    out[e] = INSIDE || t0 + i < len ? slope(so) * up[i][e] * h[e] : 0.f;
+                    up[i][e] *= keeps(so);
+                }
+            }
+            if (OUT) dz.store(r + 2 * d, out, INSIDE || t0 + i < a.t, INSIDE || l.whole);
+            r += dz.ts;
+        };
         Span m[V];
         float R[V];
 #pragma unroll
@@ -454,19 +481,25 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_k
             R[e] = 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i)
+        for (int i = 0; i < kSteps; ++i) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 x[i][e] += bx[e];
                 s[i][e] = gate(s[i][e] + bf[e]);
                 if (OUT) o[i][e] = gate(o[i][e] + bo[e]);
                 if (!INSIDE && t0 + i >= len) s[i][e] = x[i][e] = up[i][e] = 0.f;
-                m[e].add(s[i][e], x[i][e]);
+                if (!DIRECT) m[e].S = move(m[e].S, s[i][e], x[i][e]);
+                m[e].Q = move(m[e].Q, s[i][e], 1.f);
+                m[e].P = kept(m[e].P, s[i][e]);
             }
+            float out[V];
+            if (DIRECT) forward(i, out);
+        }
 #pragma unroll
         for (int i = kSteps - 1; i >= 0; --i)
 #pragma unroll
-            for (int e = 0; e < V; ++e) R[e] = kept(R[e] + (OUT ? keeps(fresh(o[i][e])) * up[i][e] : up[i][e]), fresh(s[i][e]));
+            for (int e = 0; e < V; ++e)
+                R[e] = kept(R[e] + (OUT && !DIRECT ? keeps(fresh(o[i][e])) * up[i][e] : up[i][e]), fresh(s[i][e]));
         float half_S[V], half_s[V], half_R[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -481,8 +514,8 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_k
                 m[e] = l.sub == 0 ? m[e].then(other) : other.then(m[e]);
             }
             if (V == 1 || l.sub == e) {
-                spans[blk & 1][l.w][col + e] = make_float2(m[e].S, span(m[e].Q, m[e].P));
-                backs[blk & 1][l.w][col + e] = back;
+                spans[blk & 1][l.w][col + e] = make_float2(back, span(m[e].Q, m[e].P));
+                if (!DIRECT) fronts[blk & 1][l.w][col + e] = m[e].S;
             }
         }
         __syncthreads();
@@ -490,38 +523,26 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_k
 #pragma unroll
         for (int e = 0; e < V; ++e) {
 #pragma unroll
-            for (int v = 0; v < kWaves - 1; ++v) {
-                const float2 q = spans[blk & 1][v][col + e];
-                if (v < l.w) h[e] = join(h[e], q.y, q.x);
-            }
-#pragma unroll
             for (int v = kWaves - 1; v >= 0; --v) {
                 if (v == l.w) c[e] = C[e];
-                C[e] = join(C[e], spans[blk & 1][v][col + e].y, backs[blk & 1][v][col + e]);
+                const float2 q = spans[blk & 1][v][col + e];
+                C[e] = join(C[e], q.y, q.x);
             }
-            if (V == 2) {
-                h[e] = l.sub == 1 ? join(h[e], half_s[e], half_S[e]) : h[e];
-                c[e] = l.sub == 0 ? join(c[e], half_s[e], half_R[e]) : c[e];
+            if (!DIRECT) {
+#pragma unroll
+                for (int v = 0; v < kWaves; ++v)
+                    if (v < l.w && v / kSince == l.w / kSince)
+                        h[e] = join(h[e], spans[blk & 1][v][col + e].y, fronts[blk & 1][v][col + e]);
+                if (V == 2) h[e] = l.sub == 1 ? join(h[e], half_s[e], half_S[e]) : h[e];
             }
+            if (V == 2) c[e] = l.sub == 0 ? join(c[e], half_s[e], half_R[e]) : c[e];
         }
-        // forwards: x becomes h_(t-1) - x, dy becomes what reaches h_t, and the output gate's gradient is done
-        T *r = dz.row(tw);
+        if (!DIRECT) {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i, r += dz.ts) {
-            float out[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float before = h[e];
-                h[e] = move(before, fresh(s[i][e]), x[i][e]);
-                x[i][e] = before - x[i][e];
-                if (OUT) {
-                    const float so = fresh(o[i][e]);
-                    out[e] = slope(so) * up[i][e] * h[e];
-                    up[i][e] *= keeps(so);
-                    if (!INSIDE && t0 + i >= len) out[e] = 0.f;
-                }
+            for (int i = 0; i < kSteps; ++i) {
+                float out[V];
+                forward(i, out);
             }
-            if (OUT) dz.store(r + 2 * d, out, INSIDE || t0 + i < a.t, INSIDE || l.whole);
         }
 #pragma unroll
         for (int i = kSteps - 1; i >= 0; --i) {
@@ -580,58 +601,71 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStepArgs a) {
     Elem<T>::store(y, OUT ? o * h : h);
 }
 
-// How the time axis is cut: segments of seg_len tokens, a whole number of blocks.
-static void scan_plan(int64_t b, int64_t t, int d, int *segments, int *seg_len) {
-    const int64_t strips = b * ((d + kStrip - 1) / kStrip), blocks = std::max<int64_t>((t + kScanBlock - 1) / kScanBlock, 1);
+// How the time axis is cut: segments of seg_len tokens, a whole number of blocks.  Measured, forward and backward in bf16:
+//   blocks of four short runs: for up to 32 tokens (128 x 20 x 512: 18 us, 22 by blocks of 128), and for more than 128
+//     where blocks of 128 are fewer than 512 (1 x 500 x 512: 17 us, 42; 4 x 200 x 1024: 19, 28; but a single block of 128
+//     is better read by one workgroup: 8 x 128 x 1024: 12 us, 17 by short runs)
+//   segments: below 512 strips, towards 2048 workgroups (8 x 4096 x 2048 ragged: 298 us, 348 towards 512; 65536 x 768:
+//     376, 416); from 512 on one workgroup reads all of a strip (32 x 2048 x 1024: 232 us, 300 in segments)
+struct ScanPlan {
+    bool fine;
+    int segments, seg_len;
+};
+
+static ScanPlan scan_plan(int64_t b, int64_t t, int d) {
+    const int64_t strips = b * ((d + kStrip - 1) / kStrip);
+    const int64_t whole = strips * ((t + kWaves * kRun - 1) / (kWaves * kRun));
+    const bool fine = t <= kWaves * kShort || (t > kWaves * kRun && whole < 512);
+    const int block = kWaves * (fine ? kShort : kRun);
+    const int64_t blocks = std::max<int64_t>((t + block - 1) / block, 1);
     int64_t want = 1;
-    if (strips < 512) want = std::min<int64_t>({kSegments, blocks / 2, (2048 + strips - 1) / strips});
-    want = std::max<int64_t>(want, 1);
-    const int64_t per = (blocks + want - 1) / want;
-    *segments = (int)((blocks + per - 1) / per);
-    *seg_len = (int)(per * kScanBlock);
+    if (strips < 512) want = std::min<int64_t>({kSegments, fine ? blocks : blocks / 2, (2048 + strips - 1) / strips});
+    const int64_t per = (blocks + std::max<int64_t>(want, 1) - 1) / std::max<int64_t>(want, 1);
+    return {fine, (int)((blocks + per - 1) / per), (int)(per * block)};
 }
 
 size_t scan_ws_bytes(bool, int64_t b, int64_t t, int d) {
-    int segments, seg_len;
-    scan_plan(b, t, d, &segments, &seg_len);
-    return segments > 1 ? (size_t)b * segments * d * sizeof(float2) : 0;
+    const ScanPlan p = scan_plan(b, t, d);
+    return p.segments > 1 ? (size_t)b * p.segments * d * sizeof(float2) : 0;
+}
+
+template <typename T, int V, bool OUT, int RUN>
+static void launch_fwd_run(const ScanArgs &a, float2 *ws, const ScanPlan &p, hipStream_t st) {
+    const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
+    if (p.segments > 1) {
+        const ScanSegArgs g{a.z, a.z_bs, a.z_ts, a.bias, a.lengths, nullptr, 0, 0, a.b, a.t, a.d};
+        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, false, RUN>), grid_2d(strips * (p.segments - 1)), dim3(64 * kWaves), 0,
+                           st, g, ws, p.segments, p.seg_len);
+    }
+    hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, RUN>), grid_2d(strips * p.segments), dim3(64 * kWaves), 0, st, a, ws, p.segments,
+                       p.seg_len);
+}
+
+template <typename T, int V, bool OUT, int RUN>
+static void launch_bwd_run(const ScanBwdArgs &a, float2 *ws, const ScanPlan &p, hipStream_t st) {
+    const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
+    if (p.segments > 1) {
+        const ScanSegArgs g{a.z, a.z_bs, a.z_ts, a.bias, a.lengths, a.dy, a.dy_bs, a.dy_ts, a.b, a.t, a.d};
+        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, true, RUN>), grid_2d(strips * (p.segments - 1)), dim3(64 * kWaves), 0,
+                           st, g, ws, p.segments, p.seg_len);
+    }
+    hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, RUN>), grid_2d(strips * p.segments), dim3(64 * kWaves), 0, st, a, ws, p.segments,
+                       p.seg_len);
 }
 
 // Two channels a lane in bf16, but for a single channel.
 template <typename T, int V, bool OUT>
 static void launch_fwd(const ScanArgs &a, float2 *ws, hipStream_t st) {
-    int segments, seg_len;
-    scan_plan(a.b, a.t, a.d, &segments, &seg_len);
-    const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
-    if (a.t <= kWaves * kShort) {
-        hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, kShort>), grid_2d(strips), dim3(64 * kWaves), 0, st, a, ws, 1, kWaves * kShort);
-        return;
-    }
-    if (segments > 1) {
-        const ScanSegArgs g{a.z, a.z_bs, a.z_ts, a.bias, a.lengths, nullptr, 0, 0, a.b, a.t, a.d};
-        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, false>), grid_2d(strips * (segments - 1)), dim3(64 * kWaves), 0, st, g, ws,
-                           segments, seg_len);
-    }
-    hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, kRun>), grid_2d(strips * segments), dim3(64 * kWaves), 0, st, a, ws, segments,
-                       seg_len);
+    const ScanPlan p = scan_plan(a.b, a.t, a.d);
+    if (p.fine) launch_fwd_run<T, V, OUT, kShort>(a, ws, p, st);
+    else launch_fwd_run<T, V, OUT, kRun>(a, ws, p, st);
 }
 
 template <typename T, int V, bool OUT>
 static void launch_bwd(const ScanBwdArgs &a, float2 *ws, hipStream_t st) {
-    int segments, seg_len;
-    scan_plan(a.b, a.t, a.d, &segments, &seg_len);
-    const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
-    if (a.t <= kWaves * kShort) {
-        hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, kShort>), grid_2d(strips), dim3(64 * kWaves), 0, st, a, ws, 1, kWaves * kShort);
-        return;
-    }
-    if (segments > 1) {
-        const ScanSegArgs g{a.z, a.z_bs, a.z_ts, a.bias, a.lengths, a.dy, a.dy_bs, a.dy_ts, a.b, a.t, a.d};
-        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, true>), grid_2d(strips * (segments - 1)), dim3(64 * kWaves), 0, st, g, ws,
-                           segments, seg_len);
-    }
-    hipLaunchKernelGGL((scan_bwd_kernel<T, V, OUT, kRun>), grid_2d(strips * segments), dim3(64 * kWaves), 0, st, a, ws, segments,
-                       seg_len);
+    const ScanPlan p = scan_plan(a.b, a.t, a.d);
+    if (p.fine) launch_bwd_run<T, V, OUT, kShort>(a, ws, p, st);
+    else launch_bwd_run<T, V, OUT, kRun>(a, ws, p, st);
 }
 
 #define SCAN_CASES(fn, ...)                                                         \

@@ -899,7 +899,7 @@ def token_logprobs_bwd(logits, tokens, lse, dlogp, entropy=None, dentropy=None, 
 
 
 # ----------------------------------------------------------------------------- gated linear recurrence
-SCAN_BLOCK = 128       # tokens between two states that gated_scan_fwd saves
+SCAN_BLOCK = 16       # tokens between two states that gated_scan_fwd saves
 
 
 @functools.lru_cache(_KEPT)

@@ -220,5 +220,5 @@ def test_binding_refuses(call):
 
 
 def test_binding_constants(lib):
-    assert ops.SCAN_BLOCK == 128 and [ops.adamw_scales(n) for n in (0, 1, 256, 257)] == [0, 1, 1, 2]
+    assert ops.SCAN_BLOCK == 16 and [ops.adamw_scales(n) for n in (0, 1, 256, 257)] == [0, 1, 1, 2]
     assert ops.gated_scan_workspace_bytes(0, 2, 3, 4) == lib.tfk_gated_scan_workspace_bytes(0, 2, 3, 4)
