@@ -45,11 +45,13 @@ __device__ __forceinline__ void step_of(float &var, float g, float &m, float &v,
     var = __builtin_fmaf(-decay, var, var) - p.lr * m * __builtin_amdgcn_rcpf(den);
 }
 
-// The factor of a block whose largest magnitude is top, and what its values are multiplied by.
+// The factor of a block whose largest magnitude is top, and what its values are multiplied by: by the reciprocals, as
+// elementary tensor operations divide by one number, so that values next to a border between two codes go to the same
+// side there and here (each product is within an ulp of the quotient, 2^-20 of a code's step).
 __device__ __forceinline__ float factor(float top, float &inv) {
     const bool none = top < kNothing;
-    inv = none ? 0.f : kTop / top;
-    return none ? 0.f : top < INFINITY ? top / kTop : NAN;
+    inv = none ? 0.f : 1.f / top * kTop;
+    return none ? 0.f : top < INFINITY ? top * (1.f / kTop) : NAN;
 }
 __device__ __forceinline__ float code_m(float m, float inv) { return __builtin_amdgcn_fmed3f(m * inv, -kTop, kTop); }
 __device__ __forceinline__ float code_v(float root, float inv) {
