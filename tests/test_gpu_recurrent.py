@@ -129,7 +129,10 @@ def strided(v, order, pad):
 
 CASES = [(1, 1, 1, "b", 0, None), (3, 1, 7, "t", 0, None), (2, 2, 64, "b", 0, None), (2, 127, 65, "b", 3, None),
          (2, 128, 64, "t", 0, None), (3, 129, 130, "b", 0, "mixed"), (1, 700, 33, "b", 1, None), (7, 260, 24, "t", 5, "mixed"),
-         (5, 40, 200, "b", 8, "short"), (2, 300, 512, "b", 0, "none"), (1, 5000, 3, "b", 0, None), (70, 3, 10, "t", 0, "mixed")]
+         (5, 40, 200, "b", 8, "short"), (2, 300, 512, "b", 0, "none"), (1, 5000, 3, "b", 0, None), (70, 3, 10, "t", 0, "mixed"),
+         # long runs in segments, short runs of several strips, and strips enough to be read by a workgroup each
+         (4, 2100, 600, "b", 0, None), (6, 4200, 131, "t", 2, "mixed"), (2, 1000, 512, "t", 0, None),
+         (520, 140, 40, "b", 0, "mixed")]
 
 
 def _lengths(kind, b, t):
