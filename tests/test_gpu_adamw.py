@@ -262,3 +262,23 @@ def test_captured_and_recorded():
         ref.step(want.grads, t=2)
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(md.vars, want.vars))
+
+
+def test_codes_agree_with_elementary_operations():
+    """Each operation on the moments is rounded as it is written, so the codes and factors are, bit by bit, those of
+    elementary tensor operations in the same order, also for values next to a border between two codes."""
+    n, lr, b1, b2, eps = 256 * 8000, 1e-3, 0.9, 0.999, 1e-8
+    md = Model([n], 8, 31)
+    m, v, mc, vc = (x[0].clone() for x in (md.ms, md.vs, md.mc, md.vc))
+    g = md.grads[0].view(-1, 256)
+    for t in (1, 2, 3):
+        ops.apply_adamw_multi(md.vars, md.ms, md.vs, md.grads, lr, b1, b2, eps, t, m_scales=md.mc, v_scales=md.vc, bits=8)
+        m1 = b1 * (m.float().view(-1, 256) * mc[:, None]) + (1 - b1) * g
+        root = torch.sqrt(b2 * (v.float().view(-1, 256) * vc[:, None]).square() + (1 - b2) * g * g)
+        top = m1.abs().amax(1), root.amax(1)
+        m = (m1 * (448.0 / top[0])[:, None]).clamp(-448, 448).to(FP8).view(-1)
+        v = (root * (448.0 / top[1])[:, None]).clamp(2.0 ** -9, 448).to(FP8).view(-1)
+        mc, vc = top[0] / 448.0, top[1] / 448.0
+        for got, want in ((md.ms[0], m), (md.vs[0], v)):
+            assert torch.equal(got.view(torch.uint8), want.view(torch.uint8)), t
+        assert torch.equal(md.mc[0], mc) and torch.equal(md.vc[0], vc), t
