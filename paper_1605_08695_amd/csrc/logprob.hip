@@ -4,16 +4,21 @@
 // With x = logits + bias, m = max x, u = (x - m) / T, s = sum e^u, W = sum u e^u:
 //   lse = m / T + log s     logp = u_token - log s     entropy = log s - W / s
 //   dx_j = (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)) / T,   p_j = e^(x_j / T - lse)
-// A class of -inf has p = 0 and no term.  Exponentials are powers of two of exact differences, so that a row of
-// masks alone (-1e9, -1e30, the type's lowest value) is a row like any other.  The largest classes are ordered by x,
-// then by the lower class.
+// A class of -inf has p = 0 and no term; rows of masks alone (-1e9, -1e30, the type's lowest value) are rows like any
+// other.  The largest classes are ordered by x, then by the lower class.
 //
-// A workgroup has a row and reads it once.  A lane's sums are relative to a value of its own, which it raises
+// A workgroup has a row and reads it once.  A lane's sums are relative to a number of its own, which it raises
 // only when one passes it by 2^kSlack: rescaling costs an exponential, and without the slack nearly every step
-// of a wave has a lane with a new maximum.  Each lane keeps the largest x it saw.  The k-th largest of these, tau, is
-// at most the row's k-th largest, so the classes on the list are in the few lanes whose largest is at least tau, and
-// only what those lanes read is read again (by whole waves, from the caches) to find the candidates, which then
-// count how many are before them.
+// of a wave has a lane with a new maximum.  That number is a power of two's exponent, so that a class costs one fma and
+// one exponential; a row whose sum then is no positive number is read again by exact differences (Part below).  Each
+// lane keeps the largest x it saw, and for a list the largest of each group of its batches of pieces.  The k-th largest
+// of the lanes' is at most the row's k-th largest, so the classes on the list are in the few groups whose largest is not
+// below it, and only those are read again, shared out to all lanes, to find the candidates, which then count how many
+// are before them.
+//
+// Bound by HBM: a row is read once, and for the gradient once more and written.  Measured, in bf16: 2560 x 40000 with 10
+// classes 62 us (3.3 TB/s), 4096 x 131072 with classes 272 us (4.0 TB/s), its gradient 407 us (5.3 TB/s); 1021 x 50021
+// in fp32 with a bias 43 us and 71 us.  A bias is read from the L2 for each row (4096 x 131072: 188 us without, 245 with).
 #include "common.h"
 #include "kernels.h"
 #include "rowvec.h"
@@ -24,7 +29,9 @@ namespace tfk {
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kSlack = 32.f, kFar = 1e4f, kEdge = 0x1p28f;      // in powers of two
-constexpr int kBatch = 2, kGroups = 16;          // pieces in flight of a lane; groups of them that a lane's maxima are kept for
+// Pieces in flight of a lane (8192 x 10000 with 32 classes: 56 us, 80 with four, whose groups are twice as long; 4096 x 131072
+// with a bias and 32 classes 267, 274), and groups of its batches that a lane's maxima are kept for.
+constexpr int kBatch = 2, kGroups = 16;
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -224,6 +231,12 @@ __device__ __forceinline__ uint32_t kth_of(const uint32_t *orders, int k, int lo
     return t;
 }
 
+template <int NT>
+struct Trials {
+    u64 differ[NT / 64];
+    int counts[2][NT / 64];
+};
+
 template <int NT, int CANDS>
 struct ListShared {
     static constexpr int kCands = CANDS;       // candidates for the list
@@ -234,6 +247,7 @@ struct ListShared {
     int nhot, n, above;
     int counts[NT / 64];
     u64 best[NT / 64];
+    Trials<NT> trials;
     u64 cand[kCands];
 };
 
@@ -315,6 +329,57 @@ __device__ __forceinline__ u64 next_below(const T *z, const float *bias, int c, 
     return mine;
 }
 
+// Of n > kRankAll candidates, all different and none 0, the k < n largest to the front of cand, in any order, found by all
+// waves bit by bit of those that differ (each round counts the candidates that are not below a trial), where a rank for
+// each would look at n^2 (2560 x 1000 with 128 classes: 29 us, 283).  Returns k.
+constexpr int kRankAll = 256;
+
+template <int NT, int MOST>
+__device__ __forceinline__ int shrink(u64 *cand, int n, int k, Trials<NT> &sh, int *next) {
+    constexpr int U = MOST / NT;
+    static_assert(MOST % NT == 0);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const u64 one = cand[0];
+    u64 mine[U], differ = 0;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const bool there = (int)threadIdx.x + i * NT < n;
+        mine[i] = there ? cand[threadIdx.x + i * NT] : 0;
+        differ |= there ? mine[i] ^ one : 0;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) differ |= __shfl_xor(differ, o, 64);
+    if (lane == 0) sh.differ[w] = differ;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < NT / 64; ++v) differ |= sh.differ[v];
+    u64 t = one & ~differ;                   // bits that all have alike change no count
+    for (int round = 0; differ; ++round) {
+        const u64 bit = 1ull << (63 - __builtin_clzll(differ)), trial = t | bit;
+        differ ^= bit;
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < U; ++i) c += __popcll(__ballot(mine[i] >= trial));
+        if (NT > 64) {
+            if (lane == 0) sh.counts[round & 1][w] = c;
+            __syncthreads();
+            c = 0;
+#pragma unroll
+            for (int v = 0; v < NT / 64; ++v) c += sh.counts[round & 1][v];
+        }
+        if (c >= k) t = trial;
+        if (c == k) break;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *next = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+        if (mine[i] >= t) cand[atomicAdd(next, 1)] = mine[i];
+    __syncthreads();
+    return k;
+}
+
 // The k largest classes of a row (or of a part of one) that has one, largest first, to emit(rank, key); behind the
 // last class that is not -inf emit(rank, 0).  top: each lane's largest.
 template <typename T, int NT, int CANDS, typename Emit>
@@ -355,6 +420,7 @@ __device__ __forceinline__ void largest(const T *z, const float *bias, int c, in
         }
     }
     if (n <= kCands) {
+        if (n > kRankAll) n = shrink<NT, CANDS>(sh.cand, n, k, sh.trials, &sh.n);
         for (int i = threadIdx.x; i < n; i += NT) {
             const u64 key = sh.cand[i];
             int rank = 0;
@@ -431,7 +497,8 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
 }
 
 // Few long rows: each cut into parts, a workgroup each, which leave their maximum, sums and k largest classes in the
-// workspace; then a workgroup joins each row's parts.
+// workspace; then a workgroup joins each row's parts.  Both are chains of waits: 16 x 131072 in bf16 takes 6.6 us without
+// a list, 12.9 with 20 classes, 24 with 128.
 struct PartStats {
     float m, s, W;
 };
@@ -460,7 +527,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, const PartStats *stats, const u64 *lists, int parts) {
     constexpr int NT = 256, U = 4;
     __shared__ u64 cand[kPartMost * 128];
-    __shared__ u64 least[NT / 64];
+    __shared__ Trials<NT> trials;
     __shared__ int count;
     const int64_t r = blockIdx.x;
     const int lane = threadIdx.x & 63, total = parts * a.k;
@@ -471,6 +538,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, const 
     u64 key[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) key[i] = (int)threadIdx.x + i * NT < total ? list[threadIdx.x + i * NT] : 0;
+    const int half = min(a.k, (parts + 1) / 2), deep = half > 0 ? (a.k + half - 1) / half : 0;
+    const u64 bar = deep > 0 && lane < parts ? list[lane * a.k + deep - 1] : 0;
     if (padding<NT>(a, r, token)) return;
     const float ct = kLog2e / a.temperature;
     const float xt = logit((const T *)a.z + r * a.zld, a.bias, token);
@@ -479,19 +548,15 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, const 
     const float s = wave_sumf(own.s * e), W = wave_sumf((own.W - D * own.s) * e);
     float ls;
     if (!finish_row<NT>(a, r, xt, m, s, W, ls)) return;
-    // the row's k-th largest is at least each part's own k-th
-    u64 t = 0;
+    // of half the parts, those with the largest ones, each has `deep` classes that are not below the least of these
+    int before = 0;
+    for (int v = 0; v < parts; ++v) before += (u64)__shfl(bar, v, 64) > bar;
+    u64 t = before < half ? bar : ~0ull;
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-        if ((threadIdx.x + i * NT) % a.k == a.k - 1) t = max(t, key[i]);
-    for (int q = threadIdx.x + U * NT; q < total; q += NT)
-        if (q % a.k == a.k - 1) t = max(t, list[q]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) t = max(t, (u64)__shfl_xor(t, o, 64));
-    if (lane == 0) least[threadIdx.x >> 6] = t;
+    for (int o = 32; o > 0; o >>= 1) t = min(t, (u64)__shfl_xor(t, o, 64));
+    t = max(t, (u64)1);
     if (threadIdx.x == 0) count = 0;
     __syncthreads();
-    t = max(max(least[0], least[1]), max(max(least[2], least[3]), (u64)1));
 #pragma unroll
     for (int i = 0; i < U; ++i)
         if (key[i] >= t) cand[atomicAdd(&count, 1)] = key[i];
@@ -500,7 +565,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, const 
         if (x >= t) cand[atomicAdd(&count, 1)] = x;
     }
     __syncthreads();
-    const int n = count;
+    int n = count;
+    if (n > kRankAll) n = shrink<NT, kPartMost * 128>(cand, n, a.k, trials, &count);
     for (int i = threadIdx.x; i < n; i += NT) {
         const u64 x = cand[i];
         int rank = 0;
@@ -572,7 +638,9 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int p
 }
 
 // Parts of a row, 0 for rows that one workgroup reads: enough for two workgroups a CU, of at least kPartLeast classes.
-// (The list asked for has no say in it, and so none in the sums' order.)
+// (The list asked for has no say in it, and so none in the sums' order.)  Measured with 20 classes, in parts and by one
+// workgroup a row: 131072 classes, 16 rows 12.9 and 18.7 us, 128 rows 17.9 and 20.3, 256 rows 25.7 and 21.0; 40000
+// classes, 16 rows 12.3 and 13.1, 128 rows 13.7 and 14.0, 256 rows 16.2 and 14.9.
 static int row_parts(int64_t n, int c) {
     if (n > 128 || c < 4 * kPartLeast) return 0;
     return (int)std::min<int64_t>({kPartMost, c / kPartLeast, (512 + n - 1) / n});
@@ -583,6 +651,10 @@ size_t logprob_ws_bytes(int64_t n, int c, int k) {
     return (size_t)(n * parts * (sizeof(u64) * k + sizeof(PartStats)));
 }
 
+// Short rows by one wave, for lists up to 32 with room for few candidates (65536 x 1024: 38 us without a list, 84 with 20
+// classes; by four waves 84 and 197; with room for 1024 candidates 49 and 123, as fewer rows fit a CU).  Few rows too long
+// for four waves, and too many to be cut, by sixteen (256 x 131072 with 20 classes 21 us, 31 by four; 200 x 50000 15.0,
+// 17.3; but 200 x 20000 12.2, 10.6).
 template <typename T>
 static void launch_rows(const LogprobArgs &a, void *ws, hipStream_t st) {
     const int parts = row_parts(a.n, a.c);
@@ -597,7 +669,7 @@ static void launch_rows(const LogprobArgs &a, void *ws, hipStream_t st) {
     } else if (a.c <= 1024) {
         if (a.k <= 32) hipLaunchKernelGGL((logprob_kernel<T, 64, 320>), grid_2d(a.n), dim3(64), 0, st, a);
         else hipLaunchKernelGGL((logprob_kernel<T, 64, 1024>), grid_2d(a.n), dim3(64), 0, st, a);
-    } else if (a.n > 256 || a.c <= 16384) {
+    } else if (a.n > 256 || a.c < 4 * kPartLeast) {
         hipLaunchKernelGGL((logprob_kernel<T, 256, 1024>), grid_2d(a.n), dim3(256), 0, st, a);
     } else {
         hipLaunchKernelGGL((logprob_kernel<T, 1024, 1024>), grid_2d(a.n), dim3(1024), 0, st, a);
@@ -610,6 +682,7 @@ hipError_t launch_logprob(int dt, const LogprobArgs &a, void *ws, hipStream_t st
     return hipGetLastError();
 }
 
+// Short rows by one wave (65536 x 1000: 46 us, 87 by four); longer ones in parts, a workgroup each.
 template <typename T>
 static void launch_bwd_rows(const LogprobBwdArgs &a, hipStream_t st) {
     // parts of a row read the whole of it where lse is far out: in place a row is one workgroup's

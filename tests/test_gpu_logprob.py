@@ -117,7 +117,8 @@ def toks(n, c, seed, pad=True):
 CASES = [(1, 1, 1, 1.0, 0, True), (3, 2, 5, 0.7, 0, False), (5, 7, 7, 1.0, 1, True), (4, 63, 20, 2.0, 0, True),
          (33, 1000, 5, 4.0, 0, True), (9, 1023, 128, 1.0, 3, False), (7, 2049, 1, 0.5, 0, True), (6, 4100, 100, 1.0, 8, True),
          (3, 20011, 64, 1.3, 1, True), (2, 70001, 128, 1.0, 0, False), (2, 160000, 33, 0.9, 0, True), (1, 131072, 20, 0.8, 0, False),
-         (300, 40, 40, 1.0, 0, False), (2, 300001, 50, 1.0, 0, True)]
+         (300, 40, 40, 1.0, 0, False), (2, 300001, 50, 1.0, 0, True),
+         (12, 500, 100, 1.0, 0, True), (140, 33001, 128, 1.0, 0, True), (16, 131072, 128, 1.0, 0, False)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF16], ids=str)
