@@ -7,6 +7,9 @@
 // second moment is kept as its square root, which halves its range in powers of two, and never becomes 0 where it
 // was not: its smallest value is e4m3's smallest, 2^-9 of 448, so that a rounded moment makes a step smaller and
 // not larger.  The step itself is made with the moments before they are rounded.
+//
+// One pass, bound by HBM: 277 million values in 9 variables with bf16 copies, in 8 bits 842 us (5.9 TB/s); 24 million in 190
+// variables, in fp32 134 us (5.4 TB/s); two of 0.8 million in all 5.8 us, which the caches hold.
 #include "common.h"
 #include "kernels.h"
 #include "rowvec.h"
