@@ -528,7 +528,7 @@ TFK_API tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n,
  *   ws       : at least tfk_token_logprobs_workspace_bytes(n, c, k) bytes (may be NULL when that is 0), 16-byte
  *              aligned; calls that may overlap in time need one each.
  * Finite logits are numbers whatever their size (masks of -1e9, -1e30 or the type's lowest value), where
- * fp32 holds the differences between the row's.  A row of -inf throughout has lse -inf, logp -inf, entropy
+ * fp32 holds the differences between the row's (lse alone is infinite where x / T is past its range).  A row of -inf throughout has lse -inf, logp -inf, entropy
  * 0 and no list.  A row with a NaN or +inf has NaN in logp, entropy, lse and top_logp, and -1 in top_idx.
  * top_idx and top_logp are what tfk_distill_xent takes as top_idx and top at T = 1 (with top_lse = 0 the
  * rest of the mass counts as one class); at another T the teacher's logits are T top_logp.

@@ -576,8 +576,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, const 
     for (int q = n + threadIdx.x; q < a.k; q += NT) put_class(a, r, q, 0ull, m, ls);
 }
 
-// The gradient.  Where lse is so large that fp32 no longer tells x / T from it (a row of masks alone), its maximum
-// and sum are formed again from the row.
+// The gradient.  Where lse is so large that fp32 no longer tells x / T from it (a row of masks alone; past fp32's range,
+// m / T is infinite), the row's maximum and sum are formed again from the row.
 constexpr float kFarLse = 128.f;
 
 template <typename T, int NT>
@@ -591,15 +591,16 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int p
     T *const dz = (T *)a.dz + r * a.dld;
     const int token = a.tokens[r];
     const float lse = a.lse[r];
-    const bool none = token < 0 || token >= a.c || lse == -INFINITY;
+    bool none = token < 0 || token >= a.c;
     const float invT = 1.f / a.temperature, ct = kLog2e / a.temperature;
     const float dl = none ? 0.f : a.dlogp[r] * invT, de = none || !a.dentropy ? 0.f : a.dentropy[r] * invT;
     const float H = none || !a.dentropy ? 0.f : a.entropy[r];
     // log p = (x - m) / T - ls
     float m = 0.f, ls = lse;
-    if (!none && __builtin_fabsf(lse) > kFarLse && __builtin_fabsf(lse) < INFINITY) {
+    if (!none && __builtin_fabsf(lse) > kFarLse) {
         float s, W;
         join_row<true, NT>(read_row<true, T, NT>(z, a.bias, a.c, ct, nullptr), ct, st, m, s, W);
+        none = m == -INFINITY && s == 0.f;                  // -inf throughout
         ls = __builtin_amdgcn_logf(fmaxf(s, 1.f)) * kLn2;
     }
     const float base = dl + de * H;

@@ -43,7 +43,8 @@ class GatedRecurrence:
         return z.view(*x.shape[:-1], z.shape[-1])
 
     def forward(self, x: torch.Tensor, h0=None, lengths=None, save: bool = True, stream=None):
-        """x (sequences x tokens x d_in, bf16, contiguous): returns (y, the last states, what backward needs)."""
+        """x (sequences x tokens x d_in, bf16, contiguous; its padding finite, as backward multiplies it by zeros):
+        returns (y, the last states, what backward needs)."""
         z = self._product(x, stream)
         y, last, states = ops.gated_scan_fwd(z, self.output_gate, self.b, h0, lengths, save=save, stream=stream)
         return y, last, Saved(x, z, lengths, states) if save else None

@@ -1,4 +1,6 @@
 """Token log-probabilities, entropy, largest classes and their gradient on the GPU, against float64."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -278,6 +280,38 @@ def test_gradient(n, c, T, extra, bias, with_entropy, dt):
         room = strided(torch.zeros_like(d), extra)
         assert torch.equal(ops.token_logprobs_bwd(z, tokens, r.lse, a, r.entropy, e, T, b, dlogits=room), d)
         assert room._base.isnan().sum().item() == n * extra
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("c", [9, 1000, 9000])
+def test_gradient_where_lse_is_past_the_range(c, dt):
+    """Rows of the type's lowest or of large numbers at a temperature below 1: lse is infinite, and log p is not."""
+    T, low = 0.5, torch.finfo(dt).min
+    z = torch.full((4, c), low, dtype=dt, device=DEV)
+    z[1].fill_(-low)
+    z[2].fill_(0.0)
+    z[2, [3, c - 1]] = -low
+    z[3].fill_(-INF)
+    tokens = torch.tensor([1, 2, 3, 4], dtype=torch.int32, device=DEV)
+    r = ops.token_logprobs(z, tokens, 0, T)
+    a, e = torch.full((4,), 0.75, device=DEV), torch.full((4,), 0.5, device=DEV)
+    d = ops.token_logprobs_bwd(z, tokens, r.lse, a, r.entropy, e, T)
+    mine = z.clone()
+    ops.token_logprobs_bwd(mine, tokens, r.lse, a, r.entropy, e, T, dlogits=mine)
+    torch.cuda.synchronize()
+    assert r.lse.tolist() == [-INF, INF, INF, -INF]
+    n = torch.tensor([c, c, 2.0], dtype=torch.float64, device=DEV)
+    close(r.logp[:3], -torch.log(n), 8 * U * torch.log(n) + (c / 64 + 100) * U, "logp")
+    p = torch.zeros(4, c, dtype=torch.float64, device=DEV)
+    p[0] = p[1] = 1.0 / c
+    p[2, [3, c - 1]] = 0.5
+    one = torch.zeros(4, c, dtype=torch.float64, device=DEV).scatter_(1, tokens.long()[:, None], 1.0)
+    one[3] = 0.0
+    # log p + H = 0 here, but for errors of the sum and its logarithm
+    want = 0.75 * (one - p) / T
+    tol = (p * 1.25 * (c / 64 + 100) * U * (2 + math.log(c)) + 8 * U * one) / T
+    close(d, want, tol * (1 + half(dt)) + half(dt) * want.abs(), "gradient")
+    assert torch.equal(mine, d)
 
 
 def test_gradient_against_differences():
