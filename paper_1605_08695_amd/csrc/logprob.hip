@@ -605,7 +605,7 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int p
     }
     const float base = dl + de * H;
     const auto grad = [&](float x) {
-        const float lp = (x - m) * invT - ls, p = ex2(lp * kLog2e);
+        const float lp = __builtin_fmaf(x - m, invT, -ls), p = ex2(lp * kLog2e);
         return -p * __builtin_fmaf(de, fmaxf(lp, -kFar), base);
     };
     const int n = (j1 - j0) / V;
