@@ -18,7 +18,8 @@
 //
 // Bound by HBM: a row is read once, and for the gradient once more and written.  Measured, in bf16: 2560 x 40000 with 10
 // classes 62 us (3.3 TB/s), 4096 x 131072 with classes 272 us (4.0 TB/s), its gradient 407 us (5.3 TB/s); 1021 x 50021
-// in fp32 with a bias 43 us and 71 us.  A bias is read from the L2 for each row (4096 x 131072: 188 us without, 245 with).
+// in fp32 with a bias 43 us and 71 us.  A bias is read from the L2 for each row, or for two
+// (4096 x 131072: 187 us without, 218 with).
 #include "common.h"
 #include "kernels.h"
 #include "rowvec.h"
@@ -49,6 +50,11 @@ __device__ __forceinline__ u64 key_of(uint32_t order, int j) { return (u64)order
 __device__ __forceinline__ float wave_maxf(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+__device__ __forceinline__ int wave_sum(int v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
 __device__ __forceinline__ float wave_sumf(float v) {
@@ -117,54 +123,97 @@ __device__ __forceinline__ float logit(const T *z, const float *bias, int j) {
     return Elem<T>::load(z + j) + (bias ? bias[j] : 0.f);
 }
 
-// All of the workgroup's NT lanes' parts of a row of c classes: pieces lane, lane + NT ..., in batches of kBatch, and
+// Pieces at the same classes of R rows, with one reading of the bias.
+template <typename T, int R>
+struct Pieces {
+    static constexpr int V = Elem<T>::kPerChunk;
+    typename RowVec<T, V>::raw z[R];
+    typename RowVec<float, V>::raw b;
+    __device__ __forceinline__ void load(const T *const (&zp)[R], const float *bias, int j) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) z[i] = RowVec<T, V>::load(zp[i] + j);
+        if (bias) b = RowVec<float, V>::load(bias + j);
+    }
+    __device__ __forceinline__ void values(int i, const float *bias, float *x) const {
+        RowVec<T, V>::unpack(z[i], x);
+        if (bias) {
+            float y[V];
+            RowVec<float, V>::unpack(b, y);
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] += y[e];
+        }
+    }
+};
+
+// All of the workgroup's NT lanes' parts of R rows of c classes: pieces lane, lane + NT ..., in batches of kBatch, and
 // single classes behind the last whole piece.  groups, if given: the upper halves of the orders of each lane's largest in
-// each kGroups-th batch.
-template <bool EXACT, typename T, int NT>
-__device__ __forceinline__ Part<EXACT> read_row(const T *z, const float *bias, int c, float ct, uint16_t (*groups)[NT]) {
-    constexpr int V = Piece<T>::V;
-    Part<EXACT> p = Part<EXACT>::none();
+// each kGroups-th batch, kGroups rows of them for each row.
+template <bool EXACT, typename T, int NT, int R>
+__device__ __forceinline__ void read_rows(const T *const (&z)[R], const float *bias, int c, float ct, uint16_t (*groups)[NT],
+                                          Part<EXACT> (&p)[R]) {
+    constexpr int V = Pieces<T, R>::V;
+#pragma unroll
+    for (int k = 0; k < R; ++k) p[k] = Part<EXACT>::none();
     const int n = c / V;
     int g = 0;
-    const auto note = [&](float t) {
-        p.top = fmaxf(p.top, t);
-        if (groups) {
-            const uint16_t o = (uint16_t)(order_of(t) >> 16);
-            uint16_t *const at = &groups[g % kGroups][threadIdx.x];
-            *at = g < kGroups ? o : max(*at, o);
-            ++g;
+    const auto note = [&](const float (&t)[R]) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            p[k].top = fmaxf(p[k].top, t[k]);
+            if (groups) {
+                const uint16_t o = (uint16_t)(order_of(t[k]) >> 16);
+                uint16_t *const at = &groups[k * kGroups + g % kGroups][threadIdx.x];
+                *at = g < kGroups ? o : max(*at, o);
+            }
+        }
+        ++g;
+    };
+    const auto add = [&](const Pieces<T, R> &b, float (&t)[R]) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            float x[V];
+            b.values(k, bias, x);
+            t[k] = fmaxf(t[k], p[k].template add<V>(x, ct));
         }
     };
     int q = threadIdx.x;
     for (; q + (kBatch - 1) * NT < n; q += kBatch * NT) {
-        Piece<T> b[kBatch];
+        Pieces<T, R> b[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) b[i].load(z, bias, (q + i * NT) * V);
-        float t = -INFINITY;
+        float t[R];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            float x[V];
-            b[i].values(bias, x);
-            t = fmaxf(t, p.template add<V>(x, ct));
-        }
+        for (int k = 0; k < R; ++k) t[k] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) add(b[i], t);
         note(t);
     }
     if (q < n) {
-        float t = -INFINITY;
+        float t[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) t[k] = -INFINITY;
         for (; q < n; q += NT) {
-            Piece<T> b;
+            Pieces<T, R> b;
             b.load(z, bias, q * V);
-            float x[V];
-            b.values(bias, x);
-            t = fmaxf(t, p.template add<V>(x, ct));
+            add(b, t);
         }
         note(t);
     }
     if (threadIdx.x < c - n * V) {
-        const float x = logit(z, bias, n * V + threadIdx.x);
-        p.top = fmaxf(p.top, p.template add<1>(&x, ct));
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const float x = logit(z[k], bias, n * V + threadIdx.x);
+            p[k].top = fmaxf(p[k].top, p[k].template add<1>(&x, ct));
+        }
     }
-    return p;
+}
+
+template <bool EXACT, typename T, int NT>
+__device__ __forceinline__ Part<EXACT> read_row(const T *z, const float *bias, int c, float ct, uint16_t (*groups)[NT]) {
+    const T *const one[1] = {z};
+    Part<EXACT> p[1];
+    read_rows<EXACT, T, NT, 1>(one, bias, c, ct, groups, p);
+    return p[0];
 }
 
 template <int NT>
@@ -201,30 +250,24 @@ __device__ __forceinline__ void join_row(const Part<EXACT> &p, float ct, RowStat
     }
 }
 
-// Both, and again with exact differences where the row needs them.  top: the lane's largest class.
+// The same, and the row again with exact differences where it needs them.
 template <typename T, int NT>
-__device__ __forceinline__ void row_sums(const T *z, const float *bias, int c, float ct, uint16_t (*groups)[NT], RowStats<NT> &sh,
-                                         float &top, float &m, float &s, float &W) {
-    {
-        const Part<false> p = read_row<false, T, NT>(z, bias, c, ct, groups);
-        top = p.top;
-        join_row<false, NT>(p, ct, sh, m, s, W);
-    }
+__device__ __forceinline__ void join_sums(const T *z, const float *bias, int c, float ct, const Part<false> &p, RowStats<NT> &sh,
+                                          float &m, float &s, float &W) {
+    join_row<false, NT>(p, ct, sh, m, s, W);
     if (!(s > 0.f && s < INFINITY)) join_row<true, NT>(read_row<true, T, NT>(z, bias, c, ct, nullptr), ct, sh, m, s, W);
 }
 
-// The largest number, of those whose bits below `low` are 0, that at least k of the NT orders are not below (0: fewer than k
-// are above 0), by one wave, from its highest bit down; at most as many as k stop the search.
-template <int NT>
-__device__ __forceinline__ uint32_t kth_of(const uint32_t *orders, int k, int low) {
-    uint32_t mine[NT / 64], t = 0;
-#pragma unroll
-    for (int i = 0; i < NT / 64; ++i) mine[i] = orders[i * 64 + (threadIdx.x & 63)];
+// The largest number, of those whose bits below `low` are 0, that at least k of a wave's orders (U a lane) are not below (0:
+// fewer than k are above 0), from its highest bit down; exactly k of them stop the search.
+template <int U>
+__device__ __forceinline__ uint32_t kth_of(const uint32_t (&mine)[U], int k, int low) {
+    uint32_t t = 0;
     for (int bit = 31; bit >= low; --bit) {
         const uint32_t trial = t | 1u << bit;
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < NT / 64; ++i) n += __popcll(__ballot(mine[i] >= trial));
+        for (int i = 0; i < U; ++i) n += __popcll(__ballot(mine[i] >= trial));
         if (n >= k) t = trial;
         if (n == k) break;
     }
@@ -241,7 +284,6 @@ template <int NT, int CANDS>
 struct ListShared {
     static constexpr int kCands = CANDS;       // candidates for the list
     uint32_t orders[NT];       // of each lane's largest class
-    uint16_t groups[kGroups][NT];
     int hot[NT];               // lanes whose largest is on the list, at most k, or more of equal ones
     uint32_t tau;
     int nhot, n, above;
@@ -255,7 +297,8 @@ struct ListShared {
 // which such a class can be are shared out to all lanes.  (A hot lane's pieces lie NT pieces apart, so reading all of them
 // again would fetch as many lines as the row has.)
 template <typename T, int NT, int CANDS>
-__device__ __forceinline__ void collect(const T *z, const float *bias, int c, ListShared<NT, CANDS> &sh, uint32_t least) {
+__device__ __forceinline__ void collect(const T *z, const float *bias, int c, const uint16_t (*groups)[NT], ListShared<NT, CANDS> &sh,
+                                        uint32_t least) {
     constexpr int V = Piece<T>::V, kCands = CANDS;
     const int n = c / V, per = (n + kBatch * NT - 1) / (kBatch * NT), all = sh.nhot * per;
     const auto take = [&](float x, int j) {
@@ -266,7 +309,7 @@ __device__ __forceinline__ void collect(const T *z, const float *bias, int c, Li
     };
     for (int q = threadIdx.x; q < all; q += NT) {
         const int h = q / per, g = q - h * per, lane = sh.hot[h];
-        if (sh.groups[g % kGroups][lane] < (uint16_t)(least >> 16)) continue;
+        if (groups[g % kGroups][lane] < (uint16_t)(least >> 16)) continue;
         const int at = g * kBatch * NT + lane;
         Piece<T> b[kBatch];
 #pragma unroll
@@ -383,8 +426,10 @@ __device__ __forceinline__ int shrink(u64 *cand, int n, int k, Trials<NT> &sh, i
 // The k largest classes of a row (or of a part of one) that has one, largest first, to emit(rank, key); behind the
 // last class that is not -inf emit(rank, 0).  top: each lane's largest.
 template <typename T, int NT, int CANDS, typename Emit>
-__device__ __forceinline__ void largest(const T *z, const float *bias, int c, int k, float top, ListShared<NT, CANDS> &sh, const Emit &emit) {
+__device__ __forceinline__ void largest(const T *z, const float *bias, int c, int k, float top, const uint16_t (*groups)[NT],
+                                        ListShared<NT, CANDS> &sh, const Emit &emit) {
     constexpr int kCands = CANDS;
+    constexpr bool kGroupwise = NT == 64 && CANDS >= 1024;
     const int lane = threadIdx.x & 63;
     sh.orders[threadIdx.x] = order_of(top);
     __syncthreads();
@@ -392,7 +437,29 @@ __device__ __forceinline__ void largest(const T *z, const float *bias, int c, in
     // first of those equal to it (masks of a finite number)
     const auto set_tau = [&](int low) {
         if (threadIdx.x < 64) {
-            const uint32_t t = kth_of<NT>(sh.orders, k, low);
+            uint32_t t;
+            if (kGroupwise && low == 16) {
+                // a wave's maxima are too few to tell: those of its groups
+                constexpr int V = Piece<T>::V;
+                uint32_t mine[kGroups];
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+                    mine[g] = g * kBatch * NT + lane < c / V ? (uint32_t)groups[g][lane] << 16 : 0;
+                t = kth_of(mine, k, low);
+            } else if (kGroupwise) {
+                // exactly, of all classes
+                t = 0;
+                for (int bit = 31; bit >= 0; --bit) {
+                    int n = 0;
+                    for (int j = lane; j < c; j += 64) n += order_of(logit(z, bias, j)) >= (t | 1u << bit);
+                    if (wave_sum(n) >= k) t |= 1u << bit;
+                }
+            } else {
+                uint32_t mine[NT / 64];
+#pragma unroll
+                for (int i = 0; i < NT / 64; ++i) mine[i] = sh.orders[i * 64 + lane];
+                t = kth_of(mine, k, low);
+            }
             if (lane == 0) {
                 sh.tau = max(t, 1u);
                 sh.nhot = sh.n = 0;
@@ -403,13 +470,13 @@ __device__ __forceinline__ void largest(const T *z, const float *bias, int c, in
         __syncthreads();
     };
     set_tau(16);
-    collect<T, NT, CANDS>(z, bias, c, sh, sh.tau);
+    collect<T, NT, CANDS>(z, bias, c, groups, sh, sh.tau);
     __syncthreads();
     int n = sh.n;
     if (n > kCands) {
         __syncthreads();
         set_tau(0);
-        collect<T, NT, CANDS>(z, bias, c, sh, sh.tau + 1);
+        collect<T, NT, CANDS>(z, bias, c, groups, sh, sh.tau + 1);
         __syncthreads();
         n = sh.n;
         if (n <= kCands - 128) {
@@ -483,6 +550,7 @@ template <typename T, int NT, int CANDS>
 __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
     __shared__ RowStats<NT> st;
     __shared__ ListShared<NT, CANDS> sh;
+    __shared__ uint16_t groups[kGroups][NT];
     const int64_t r = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (r >= a.n) return;
     const float ct = kLog2e / a.temperature;
@@ -490,10 +558,40 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
     if (padding<NT>(a, r, token)) return;
     const T *const z = (const T *)a.z + r * a.zld;
     const float xt = logit(z, a.bias, token);
-    float m, s, W, ls, top;
-    row_sums<T, NT>(z, a.bias, a.c, ct, a.k > 0 ? sh.groups : nullptr, st, top, m, s, W);
+    float m, s, W, ls;
+    const Part<false> p = read_row<false, T, NT>(z, a.bias, a.c, ct, a.k > 0 ? groups : nullptr);
+    join_sums<T, NT>(z, a.bias, a.c, ct, p, st, m, s, W);
     if (finish_row<NT>(a, r, xt, m, s, W, ls))
-        largest<T, NT, CANDS>(z, a.bias, a.c, a.k, top, sh, [&](int rank, u64 key) { put_class(a, r, rank, key, m, ls); });
+        largest<T, NT, CANDS>(z, a.bias, a.c, a.k, p.top, groups, sh, [&](int rank, u64 key) { put_class(a, r, rank, key, m, ls); });
+}
+
+// R neighbouring rows by one workgroup, without lists: read together, which reads the bias once, unless one of them is padding.
+template <typename T, int NT, int R>
+__global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobArgs a) {
+    __shared__ RowStats<NT> st;
+    const int64_t r0 = (blockIdx.x + (int64_t)blockIdx.y * gridDim.x) * R;
+    if (r0 >= a.n) return;
+    const float ct = kLog2e / a.temperature;
+    const T *z[R];
+    int token[R], rows = 0;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int64_t r = min(r0 + k, a.n - 1);
+        token[k] = a.tokens ? a.tokens[r] : 0;
+        z[k] = (const T *)a.z + r * a.zld;
+        rows += r0 + k < a.n && token[k] >= 0 && token[k] < a.c;
+    }
+    Part<false> p[R];
+    if (rows == R) read_rows<false, T, NT, R>(z, a.bias, a.c, ct, nullptr, p);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        if (r0 + k >= a.n || padding<NT>(a, r0 + k, token[k])) continue;
+        const float xt = logit(z[k], a.bias, token[k]);
+        if (rows < R) p[k] = read_row<false, T, NT>(z[k], a.bias, a.c, ct, nullptr);
+        float m, s, W, ls;
+        join_sums<T, NT>(z[k], a.bias, a.c, ct, p[k], st, m, s, W);
+        finish_row<NT>(a, r0 + k, xt, m, s, W, ls);
+    }
 }
 
 // Few long rows: each cut into parts, a workgroup each, which leave their maximum, sums and k largest classes in the
@@ -509,18 +607,20 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobArgs a, PartSt
     constexpr int NT = 256;
     __shared__ RowStats<NT> st;
     __shared__ ListShared<NT, 1024> sh;
+    __shared__ uint16_t groups[kGroups][NT];
     const int64_t r = blockIdx.y;
     const int part = blockIdx.x, j0 = part * part_len, c = min(part_len, a.c - j0);
     const float ct = kLog2e / a.temperature;
     if (a.tokens && (a.tokens[r] < 0 || a.tokens[r] >= a.c)) return;
     const T *const z = (const T *)a.z + r * a.zld + j0;
     const float *const bias = a.bias ? a.bias + j0 : nullptr;
-    float m, s, W, top;
-    row_sums<T, NT>(z, bias, c, ct, a.k > 0 ? sh.groups : nullptr, st, top, m, s, W);
+    float m, s, W;
+    const Part<false> p = read_row<false, T, NT>(z, bias, c, ct, a.k > 0 ? groups : nullptr);
+    join_sums<T, NT>(z, bias, c, ct, p, st, m, s, W);
     if (threadIdx.x == 0) stats[r * parts + part] = PartStats{m, s, W};
     if (a.k == 0 || !(s < INFINITY)) return;         // (a NaN row has no list)
     u64 *const list = lists + (r * parts + part) * a.k;
-    largest<T, NT, 1024>(z, bias, c, a.k, top, sh, [&](int rank, u64 key) { list[rank] = key ? key - (u64)j0 : 0ull; });
+    largest<T, NT, 1024>(z, bias, c, a.k, p.top, groups, sh, [&](int rank, u64 key) { list[rank] = key ? key - (u64)j0 : 0ull; });
 }
 
 template <typename T>
@@ -579,68 +679,94 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, const 
 // The gradient.  Where lse is so large that fp32 no longer tells x / T from it (a row of masks alone; past fp32's range,
 // m / T is infinite), the row's maximum and sum are formed again from the row.
 constexpr float kFarLse = 128.f;
+constexpr int kBwdPart = 1024;             // pieces of 16 bytes of a part
 
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int parts, int part_len) {
-    constexpr int V = Piece<T>::V, U = 4;
-    __shared__ RowStats<NT> st;
-    const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x, r = job / parts;
-    if (r >= a.n) return;
-    const int j0 = (int)(job - r * parts) * part_len, j1 = min(a.c, j0 + part_len);
-    const T *const z = (const T *)a.z + r * a.zld;
-    T *const dz = (T *)a.dz + r * a.dld;
-    const int token = a.tokens[r];
-    const float lse = a.lse[r];
-    bool none = token < 0 || token >= a.c;
-    const float invT = 1.f / a.temperature, ct = kLog2e / a.temperature;
-    const float dl = none ? 0.f : a.dlogp[r] * invT, de = none || !a.dentropy ? 0.f : a.dentropy[r] * invT;
-    const float H = none || !a.dentropy ? 0.f : a.entropy[r];
-    // log p = (x - m) / T - ls
-    float m = 0.f, ls = lse;
-    if (!none && __builtin_fabsf(lse) > kFarLse) {
-        float s, W;
-        join_row<true, NT>(read_row<true, T, NT>(z, a.bias, a.c, ct, nullptr), ct, st, m, s, W);
-        none = m == -INFINITY && s == 0.f;                  // -inf throughout
-        ls = __builtin_amdgcn_logf(fmaxf(s, 1.f)) * kLn2;
-    }
-    const float base = dl + de * H;
-    const auto grad = [&](float x) {
+// What a row's gradient is made of: log p = (x - m) / T - ls, then -p (de log p + base), and dl where the token is.
+struct RowGrad {
+    int token;
+    bool there, none;              // whether there is such a row; whether its gradient is 0
+    float m, ls, dl, de, base;
+    __device__ __forceinline__ float of(float x, float invT) const {
         const float lp = __builtin_fmaf(x - m, invT, -ls), p = ex2(lp * kLog2e);
         return -p * __builtin_fmaf(de, fmaxf(lp, -kFar), base);
-    };
+    }
+};
+
+// A part of R neighbouring rows by each workgroup, with one reading of the bias.
+template <typename T, int NT, int R>
+__global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int parts, int part_len) {
+    constexpr int V = Pieces<T, R>::V, U = 4 / R;
+    __shared__ RowStats<NT> st;
+    const int64_t job = blockIdx.x + (int64_t)blockIdx.y * gridDim.x, r0 = job / parts * R;
+    if (r0 >= a.n) return;
+    const int j0 = (int)(job % parts) * part_len, j1 = min(a.c, j0 + part_len);
+    const float invT = 1.f / a.temperature, ct = kLog2e / a.temperature;
+    const T *z[R];
+    T *dz[R];
+    RowGrad g[R];
+    bool all_none = true;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int64_t r = min(r0 + k, a.n - 1);
+        z[k] = (const T *)a.z + r * a.zld;
+        dz[k] = (T *)a.dz + r * a.dld;
+        g[k].there = r0 + k < a.n;
+        g[k].token = a.tokens[r];
+        g[k].none = g[k].token < 0 || g[k].token >= a.c || !g[k].there;
+        const float lse = a.lse[r];
+        g[k].dl = g[k].none ? 0.f : a.dlogp[r] * invT;
+        g[k].de = g[k].none || !a.dentropy ? 0.f : a.dentropy[r] * invT;
+        g[k].base = g[k].none || !a.dentropy ? g[k].dl : g[k].dl + g[k].de * a.entropy[r];
+        g[k].m = 0.f;
+        g[k].ls = lse;
+        if (!g[k].none && __builtin_fabsf(lse) > kFarLse) {
+            float s, W;
+            join_row<true, NT>(read_row<true, T, NT>(z[k], a.bias, a.c, ct, nullptr), ct, st, g[k].m, s, W);
+            g[k].none = g[k].m == -INFINITY && s == 0.f;                  // -inf throughout
+            g[k].ls = __builtin_amdgcn_logf(fmaxf(s, 1.f)) * kLn2;
+        }
+        all_none = all_none && g[k].none;
+    }
     const int n = (j1 - j0) / V;
     for (int q = threadIdx.x; q < n; q += U * NT) {
-        Piece<T> b[U];
+        Pieces<T, R> b[U];
 #pragma unroll
         for (int i = 0; i < U; ++i)
-            if (!none && q + i * NT < n) b[i].load(z, a.bias, j0 + (q + i * NT) * V);
+            if (!all_none && q + i * NT < n) b[i].load(z, a.bias, j0 + (q + i * NT) * V);
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int j = j0 + (q + i * NT) * V;
             if (q + i * NT >= n) break;
-            float x[V];
-            if (none) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) x[e] = 0.f;
-            } else {
-                b[i].values(a.bias, x);
+            for (int k = 0; k < R; ++k) {
+                float x[V];
+                if (g[k].none) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) x[e] = grad(x[e]);
-                if ((unsigned)(token - j) < (unsigned)V) {
+                    for (int e = 0; e < V; ++e) x[e] = 0.f;
+                } else {
+                    b[i].values(k, a.bias, x);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) x[e] += token == j + e ? dl : 0.f;
+                    for (int e = 0; e < V; ++e) x[e] = g[k].of(x[e], invT);
+                    if ((unsigned)(g[k].token - j) < (unsigned)V) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) x[e] += g[k].token == j + e ? g[k].dl : 0.f;
+                    }
                 }
+                if (g[k].there) RowVec<T, V>::store(dz[k] + j, x);
             }
-            RowVec<T, V>::store(dz + j, x);
         }
     }
     const int j = j0 + n * V + threadIdx.x;
-    if (j < j1) Elem<T>::store(dz + j, none ? 0.f : grad(logit(z, a.bias, j)) + (j == token ? dl : 0.f));
+    if (j >= j1) return;
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+        if (g[k].there)
+            Elem<T>::store(dz[k] + j, g[k].none ? 0.f : g[k].of(logit(z[k], a.bias, j), invT) + (j == g[k].token ? g[k].dl : 0.f));
 }
 
 // Parts of a row, 0 for rows that one workgroup reads: enough for two workgroups a CU, of at least kPartLeast classes.
-// (The list asked for has no say in it, and so none in the sums' order.)  Measured with 20 classes, in parts and by one
-// workgroup a row: 131072 classes, 16 rows 12.9 and 18.7 us, 128 rows 17.9 and 20.3, 256 rows 25.7 and 21.0; 40000
+// (The list asked for has no say in it, nor below in how many waves read a row, and so none in the sums' order.)
+// Measured with 20 classes, in parts and by one workgroup a row: 131072 classes, 16 rows 12.9 and 18.7 us, 128 rows 17.9 and 20.3, 256 rows 25.7 and 21.0; 40000
 // classes, 16 rows 12.3 and 13.1, 128 rows 13.7 and 14.0, 256 rows 16.2 and 14.9.
 static int row_parts(int64_t n, int c) {
     if (n > 128 || c < 4 * kPartLeast) return 0;
@@ -653,9 +779,13 @@ size_t logprob_ws_bytes(int64_t n, int c, int k) {
 }
 
 // Short rows by one wave, for lists up to 32 with room for few candidates (65536 x 1024: 38 us without a list, 84 with 20
-// classes; by four waves 84 and 197; with room for 1024 candidates 49 and 123, as fewer rows fit a CU).  Few rows too long
-// for four waves, and too many to be cut, by sixteen (256 x 131072 with 20 classes 21 us, 31 by four; 200 x 50000 15.0,
-// 17.3; but 200 x 20000 12.2, 10.6).
+// classes; by four waves 84 and 197; with room for 1024 candidates 49 and 123, as fewer rows fit a CU).  Up to 4096
+// classes, where there are rows enough (65536 x 1500: 50 us and with 10 classes 94, by four waves 94 and 202; 2560 x 4000 8.2
+// and 12.2, 9.0 and 16.1; but 256 x 2000 4.3, 3.8).
+// With a bias and no list two rows by four waves (4096 x 131072 218 us, 247 by one row; 2560 x 40000 46, 54; 20000 x 10000
+// 87, 97; but 1500 x 10000 11.4, 10.1; with lists, which follow one another then, 2560 x 40000 76, 64).  Few rows too long for
+// four waves, and too many to be cut, by sixteen (256 x 131072 with 20 classes 21 us, 31 by four; 200 x 50000 15.0, 17.3;
+// but 200 x 20000 12.2, 10.6).
 template <typename T>
 static void launch_rows(const LogprobArgs &a, void *ws, hipStream_t st) {
     const int parts = row_parts(a.n, a.c);
@@ -667,11 +797,14 @@ static void launch_rows(const LogprobArgs &a, void *ws, hipStream_t st) {
         const int used = (a.c + len - 1) / len;
         hipLaunchKernelGGL((logprob_part_kernel<T>), dim3(used, (unsigned)a.n), dim3(256), 0, st, a, stats, lists, used, len);
         hipLaunchKernelGGL((logprob_join_kernel<T>), dim3((unsigned)a.n), dim3(256), 0, st, a, stats, lists, used);
-    } else if (a.c <= 1024) {
+    } else if (a.c <= 1024 || (a.c <= 4096 && a.n >= 1024)) {
         if (a.k <= 32) hipLaunchKernelGGL((logprob_kernel<T, 64, 320>), grid_2d(a.n), dim3(64), 0, st, a);
-        else hipLaunchKernelGGL((logprob_kernel<T, 64, 1024>), grid_2d(a.n), dim3(64), 0, st, a);
+        else if (a.c <= 1024 || a.k <= 64) hipLaunchKernelGGL((logprob_kernel<T, 64, 1024>), grid_2d(a.n), dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((logprob_kernel<T, 64, 2048>), grid_2d(a.n), dim3(64), 0, st, a);
     } else if (a.n > 256 || a.c < 4 * kPartLeast) {
-        hipLaunchKernelGGL((logprob_kernel<T, 256, 1024>), grid_2d(a.n), dim3(256), 0, st, a);
+        if (a.k == 0 && a.bias && a.n >= 1024 && a.n * a.c >= (int64_t)1 << 25)
+            hipLaunchKernelGGL((logprob_rows_kernel<T, 256, 2>), grid_2d((a.n + 1) / 2), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((logprob_kernel<T, 256, 1024>), grid_2d(a.n), dim3(256), 0, st, a);
     } else {
         hipLaunchKernelGGL((logprob_kernel<T, 1024, 1024>), grid_2d(a.n), dim3(1024), 0, st, a);
     }
@@ -683,13 +816,22 @@ hipError_t launch_logprob(int dt, const LogprobArgs &a, void *ws, hipStream_t st
     return hipGetLastError();
 }
 
-// Short rows by one wave (65536 x 1000: 46 us, 87 by four); longer ones in parts, a workgroup each.
+// Short rows by one wave (65536 x 1000: 46 us, 87 by four); longer ones in parts of the same length, a workgroup each
+// (20000 x 10000 in two halves 152 us, in 8192 and 1808 163).  Two rows a workgroup where one is not much work for it
+// (65536 x 1500 76 us, 145), or has a bias to read (4096 x 131072 387, 410; 20000 x 10000 160; but 1600 x 131072 181, 166).
 template <typename T>
 static void launch_bwd_rows(const LogprobBwdArgs &a, hipStream_t st) {
     // parts of a row read the whole of it where lse is far out: in place a row is one workgroup's
-    const int len = a.dz == a.z ? a.c : 256 * 4 * 16 / (int)sizeof(T), parts = (a.c + len - 1) / len;
-    if (a.c <= 1024) hipLaunchKernelGGL((logprob_bwd_kernel<T, 64>), grid_2d(a.n), dim3(64), 0, st, a, 1, a.c);
-    else hipLaunchKernelGGL((logprob_bwd_kernel<T, 256>), grid_2d(a.n * parts), dim3(256), 0, st, a, parts, len);
+    const int most = kBwdPart * 16 / (int)sizeof(T), parts = a.dz == a.z ? 1 : (a.c + most - 1) / most;
+    const int len = ((a.c + parts - 1) / parts + 63) / 64 * 64;
+    const bool pairs = (a.n >= 1024 && a.c * sizeof(T) <= 6144) || (a.bias && a.n >= 2048 && a.n * a.c >= (int64_t)1 << 25);
+    if (a.c <= 1024) {
+        hipLaunchKernelGGL((logprob_bwd_kernel<T, 64, 1>), grid_2d(a.n), dim3(64), 0, st, a, 1, a.c);
+    } else if (pairs) {
+        hipLaunchKernelGGL((logprob_bwd_kernel<T, 256, 2>), grid_2d((a.n + 1) / 2 * parts), dim3(256), 0, st, a, parts, len);
+    } else {
+        hipLaunchKernelGGL((logprob_bwd_kernel<T, 256, 1>), grid_2d(a.n * parts), dim3(256), 0, st, a, parts, len);
+    }
 }
 
 hipError_t launch_logprob_bwd(int dt, const LogprobBwdArgs &a, hipStream_t st) {

@@ -120,7 +120,8 @@ CASES = [(1, 1, 1, 1.0, 0, True), (3, 2, 5, 0.7, 0, False), (5, 7, 7, 1.0, 1, Tr
          (33, 1000, 5, 4.0, 0, True), (9, 1023, 128, 1.0, 3, False), (7, 2049, 1, 0.5, 0, True), (6, 4100, 100, 1.0, 8, True),
          (3, 20011, 64, 1.3, 1, True), (2, 70001, 128, 1.0, 0, False), (2, 160000, 33, 0.9, 0, True), (1, 131072, 20, 0.8, 0, False),
          (300, 40, 40, 1.0, 0, False), (2, 300001, 50, 1.0, 0, True),
-         (12, 500, 100, 1.0, 0, True), (140, 33001, 128, 1.0, 0, True), (16, 131072, 128, 1.0, 0, False)]
+         (12, 500, 100, 1.0, 0, True), (1030, 1500, 64, 1.0, 1, True), (1025, 4096, 10, 0.8, 0, False), (1027, 1100, 128, 1.0, 0, True),
+         (140, 33001, 128, 1.0, 0, True), (16, 131072, 128, 1.0, 0, False)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF16], ids=str)
@@ -151,6 +152,21 @@ def test_largest_where_they_lie_badly(kind, c, dt):
     z = torch.from_numpy(np.stack([rows, rows[::-1].copy(), np.roll(rows, 3)])).to(dt).to(DEV)
     for k in (1, 17, 128):
         check(z, None, None, 1.0, k)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("c", [1100, 2500, 4096])
+def test_short_rows_of_large_batches(c, dt):
+    """Rows of up to 4096 classes, which one wave each reads: equal classes, classes in few places, masks, long lists."""
+    i = np.arange(c)
+    rng = np.random.default_rng(c)
+    one = [np.zeros(c), np.where(i % 512 // 8 == 5, 8.0 + rng.random(c), rng.random(c)), rng.standard_normal(c) * 3,
+           np.where(i % 97 == 3, rng.random(c), -1e9), np.where(i < 5, 1.0, -np.inf), np.where(i < 5, 1.0, -1e9), i / c, -i / c]
+    z = torch.from_numpy(np.stack(one * 130)).to(dt).to(DEV)
+    tokens = toks(z.shape[0], c, 3)
+    tokens[tokens > 0] = 3
+    for k in (4, 33, 64, 65, 128):
+        check(z, None, tokens, 1.0, k)
 
 
 @pytest.mark.parametrize("dt", [F32, BF16], ids=str)
@@ -247,7 +263,8 @@ def test_padding_is_not_read():
 @pytest.mark.parametrize("dt", [F32, BF16], ids=str)
 @pytest.mark.parametrize("with_entropy", [False, True])
 @pytest.mark.parametrize("n,c,T,extra,bias", [(1, 1, 1.0, 0, True), (5, 7, 0.5, 1, False), (33, 1000, 2.0, 0, True),
-                                              (7, 2049, 1.0, 3, True), (3, 50021, 1.0, 0, True), (2, 160000, 1.3, 8, False)])
+                                              (7, 2049, 1.0, 3, True), (3, 50021, 1.0, 0, True), (2, 160000, 1.3, 8, False),
+                                              (1027, 1501, 1.0, 1, False), (2049, 16400, 1.0, 0, True)])
 def test_gradient(n, c, T, extra, bias, with_entropy, dt):
     say("gradient", n, c, T, extra, bias, with_entropy, dt)
     z = strided(logits(n, c, dt, c), extra)
