@@ -16,10 +16,10 @@
 // below it, and only those are read again, shared out to all lanes, to find the candidates, which then count how many
 // are before them.
 //
-// Bound by HBM: a row is read once, and for the gradient once more and written.  Measured, in bf16: 2560 x 40000 with 10
-// classes 62 us (3.3 TB/s), 4096 x 131072 with classes 272 us (4.0 TB/s), its gradient 407 us (5.3 TB/s); 1021 x 50021
-// in fp32 with a bias 43 us and 71 us.  A bias is read from the L2 for each row, or for two
-// (4096 x 131072: 187 us without, 218 with).
+// Bound by HBM: a row is read once, and for the gradient once more and written.  Measured, in bf16: 2560 x 40000 with a bias
+// and 32 classes 62 us (3.3 TB/s), 4096 x 131072 with a bias 218 us (4.9 TB/s), its gradient 387 us (5.5 TB/s); 1021 x 50021
+// in fp32 with a bias and 5 classes 43 us, its gradient 70.  A bias is read from the L2 for each row, or for two (4096 x
+// 131072 without one: 187 us and 358).
 #include "common.h"
 #include "kernels.h"
 #include "rowvec.h"
