@@ -766,8 +766,8 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(LogprobBwdArgs a, int p
 
 // Parts of a row, 0 for rows that one workgroup reads: enough for two workgroups a CU, of at least kPartLeast classes.
 // (The list asked for has no say in it, nor below in how many waves read a row, and so none in the sums' order.)
-// Measured with 20 classes, in parts and by one workgroup a row: 131072 classes, 16 rows 12.9 and 18.7 us, 128 rows 17.9 and 20.3, 256 rows 25.7 and 21.0; 40000
-// classes, 16 rows 12.3 and 13.1, 128 rows 13.7 and 14.0, 256 rows 16.2 and 14.9.
+// Measured with 20 classes, in parts and by one workgroup a row: 131072 classes, 16 rows 12.9 and 18.7 us, 128 rows 17.9
+// and 20.3, 256 rows 25.7 and 21.0; 40000 classes, 16 rows 12.3 and 13.1, 128 rows 13.7 and 14.0, 256 rows 16.2 and 14.9.
 static int row_parts(int64_t n, int c) {
     if (n > 128 || c < 4 * kPartLeast) return 0;
     return (int)std::min<int64_t>({kPartMost, c / kPartLeast, (512 + n - 1) / n});
