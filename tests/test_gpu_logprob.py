@@ -410,3 +410,34 @@ def test_two_streams_and_a_captured_graph():
         both(zs[1])
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want[k % 2]))
+
+
+def test_rows_in_parts_recorded_and_captured():
+    """Few long rows, whose parts meet in a workspace: on two streams at once, in a program and in two graphs."""
+    zs = [logits(6, 40000, BF16, s) for s in (1, 2, 3)]
+    tokens = toks(6, 40000, 1)
+    assert ops.token_logprobs_workspace_bytes(6, 40000, 128) > 0
+    want = [ops.token_logprobs(z, tokens, 128) for z in zs]
+    torch.cuda.synchronize()
+    same = lambda r, w: all(torch.equal(a, b) for a, b in zip(r, w))  # noqa: E731
+    got = [ops.token_logprobs(z, tokens, 128, stream=torch.cuda.Stream()) for z in zs]
+    torch.cuda.synchronize()
+    assert all(same(a, b) for a, b in zip(got, want))
+    mine = [zs[0].clone(), zs[0].clone()]
+    prog, graphs, outs = ops.Program(), [], []
+    with prog.recording():
+        recorded = ops.token_logprobs(mine[0], tokens, 128)
+    for z in mine:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(ops.token_logprobs(z, tokens, 128))
+    for k in range(4):
+        mine[0].copy_(zs[k % 3])
+        mine[1].copy_(zs[(k + 1) % 3])
+        prog.run()
+        for g in graphs:
+            g.replay()
+        other = ops.token_logprobs(zs[2], tokens, 128)
+        torch.cuda.synchronize()
+        assert same(recorded, want[k % 3]) and same(outs[0], want[k % 3]) and same(outs[1], want[(k + 1) % 3])
+        assert same(other, want[2])
