@@ -439,7 +439,8 @@ __device__ __forceinline__ void largest(const T *z, const float *bias, int c, in
         if (threadIdx.x < 64) {
             uint32_t t;
             if (kGroupwise && low == 16) {
-                // a wave's maxima are too few to tell: those of its groups
+                // a wave's maxima are too few to tell: those of its groups (2560 x 4000 with 64 classes 25 us, 1200 by the
+                // lanes' own, which let most classes be candidates)
                 constexpr int V = Piece<T>::V;
                 uint32_t mine[kGroups];
 #pragma unroll
@@ -781,7 +782,8 @@ size_t logprob_ws_bytes(int64_t n, int c, int k) {
 // Short rows by one wave, for lists up to 32 with room for few candidates (65536 x 1024: 38 us without a list, 84 with 20
 // classes; by four waves 84 and 197; with room for 1024 candidates 49 and 123, as fewer rows fit a CU).  Up to 4096
 // classes, where there are rows enough (65536 x 1500: 50 us and with 10 classes 94, by four waves 94 and 202; 2560 x 4000 8.2
-// and 12.2, 9.0 and 16.1; but 256 x 2000 4.3, 3.8).
+// and 12.2, 9.0 and 16.1; but 256 x 2000 4.3, 3.8), with lists of more than 64 with room for 2048 candidates (2560 x 1100
+// with 128 classes 65 us: its 74 groups are too few, so that all classes are candidates).
 // With a bias and no list two rows by four waves (4096 x 131072 218 us, 247 by one row; 2560 x 40000 46, 54; 20000 x 10000
 // 87, 97; but 1500 x 10000 11.4, 10.1; with lists, which follow one another then, 2560 x 40000 76, 64).  Few rows too long for
 // four waves, and too many to be cut, by sixteen (256 x 131072 with 20 classes 21 us, 31 by four; 200 x 50000 15.0, 17.3;
