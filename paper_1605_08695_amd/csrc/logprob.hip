@@ -7,11 +7,14 @@
 // A class of -inf has p = 0 and no term; rows of masks alone (-1e9, -1e30, the type's lowest value) are rows like any
 // other.  The largest classes are ordered by x, then by the lower class.
 //
-// A workgroup has a row and reads it once.  A lane's sums are relative to a number of its own, which it raises
-// only when one passes it by 2^kSlack: rescaling costs an exponential, and without the slack nearly every step
-// of a wave has a lane with a new maximum.  That number is a power of two's exponent, so that a class costs one fma and
-// one exponential; a row whose sum then is no positive number is read again by exact differences (Part below).  Each
-// lane keeps the largest x it saw, and for a list the largest of each group of its batches of pieces.  The k-th largest
+// A workgroup has a row and reads it once.  A lane's sums are relative to a power of two of its own, which it raises only
+// when a class passes it by 2^kSlack: without the slack nearly every step of a wave has a lane with a new maximum.  A class
+// costs one fma and one exponential, and raising costs none; a row whose sum then is no positive number is read again by exact
+// differences (Part below).  The slack also bounds what a row with one class far above the others loses: W's terms at that
+// class and its lane's later sums are up to kSlack times s, and entropy is what is left of them.  With 4 and the terms of
+// a piece added up before they join the lane's, it is off by 2.2e-6 at most, fp32 operations on whole rows by 1.5e-6
+// (2560 x 40000 and 256 x 131072, a class 12 to 25 above the mean; with a slack of 32 and term by term 4e-5), in the same time
+// as with 1, 2, 8 or 32.  Each lane keeps the largest x it saw, and for a list the largest of each group of its batches of pieces.  The k-th largest
 // of the lanes' is at most the row's k-th largest, so the classes on the list are in the few groups whose largest is not
 // below it, and only those are read again, shared out to all lanes, to find the candidates, which then count how many
 // are before them.
@@ -29,7 +32,7 @@
 namespace tfk {
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
-constexpr float kSlack = 32.f, kFar = 1e4f, kEdge = 0x1p28f;      // in powers of two
+constexpr float kSlack = 4.f, kFar = 1e4f, kEdge = 0x1p28f;      // in powers of two
 // Pieces in flight of a lane (8192 x 10000 with 32 classes: 56 us, 80 with four, whose groups are twice as long; 4096 x 131072
 // with a bias and 32 classes 267, 274), and groups of its batches that a lane's maxima are kept for.
 constexpr int kBatch = 2, kGroups = 16;
@@ -63,8 +66,8 @@ __device__ __forceinline__ float wave_sumf(float v) {
     return v;
 }
 
-// A lane's part of a row: sums relative to a power of two, and its largest x.  EXACT false: x ct - R by one fma, R a number
-// near the largest x ct, rounded once and used as it is; rows that this cannot hold (s is not a positive number
+// A lane's part of a row: sums relative to a power of two, and its largest x.  EXACT false: x ct - R by one fma, R a whole
+// number near the largest x ct, so that sums go from one to the next by a change of their exponents; rows that this cannot hold (s is not a positive number
 // then: the largest class beyond +-2^28, infinite or NaN) are read again with EXACT, relative to a ref by exact
 // differences.
 template <bool EXACT>
@@ -75,10 +78,17 @@ struct Part {
         return EXACT ? (x - ref) * ct : __builtin_fmaf(x, ct, -ref);
     }
     __device__ __forceinline__ void raise(float x, float ct) {
-        const float to = EXACT ? x : __builtin_amdgcn_fmed3f(x * ct, -kEdge, kEdge);
-        const float D = fminf(EXACT ? (x - ref) * ct : to - ref, kFar), r = ex2(-D);
-        W = (W - D * s) * r;
-        s *= r;
+        const float to = EXACT ? x : __builtin_rintf(__builtin_amdgcn_fmed3f(x * ct, -kEdge, kEdge));
+        const float D = fminf(EXACT ? (x - ref) * ct : to - ref, kFar);
+        W -= D * s;
+        if (EXACT) {
+            const float r = ex2(-D);
+            W *= r;
+            s *= r;
+        } else {
+            W = __builtin_amdgcn_ldexpf(W, -(int)D);
+            s = __builtin_amdgcn_ldexpf(s, -(int)D);
+        }
         ref = to;
     }
     template <int V>
@@ -87,12 +97,15 @@ struct Part {
 #pragma unroll
         for (int e = 1; e < V; ++e) t = fmaxf(t, x[e]);
         if (power(t, ct) > kSlack) raise(t, ct);
+        float ps = 0.f, pW = 0.f;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float u = power(x[e], ct), p = ex2(u);
-            s += p;
-            W = __builtin_fmaf(p, fmaxf(u, -kFar), W);      // (p is 0 where the bound is reached)
+            ps = e ? ps + p : p;
+            pW = __builtin_fmaf(p, fmaxf(u, -kFar), pW);    // (p is 0 where the bound is reached)
         }
+        s += ps;
+        W += pW;
         return t;
     }
 };

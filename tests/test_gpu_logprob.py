@@ -169,6 +169,34 @@ def test_short_rows_of_large_batches(c, dt):
         check(z, None, tokens, 1.0, k)
 
 
+# Rows with one class far above the others.  Their lane's sums follow that class's by at most 4 powers of two and half of
+# one, D <= 4.5 of them or 3.2 in the exponent's units: so s has a rounding of U s for each piece that the lane adds to
+# it, and W one of U (3.2 + w) s, w = sum p |u|.  The class's own piece has 8 terms, W - D s two roundings of 4.5 U s, and what
+# joins lanes and waves 16 of U (1 + w) s.  A term's exponent is off by (4 |u| + 8) U.
+@pytest.mark.parametrize("n,c,dt,lanes", [(2048, 4096, BF16, 64), (2560, 40000, BF16, 256), (512, 50021, F32, 256), (256, 131072, BF16, 1024),
+                                          (300, 131072, BF16, 256)], ids=str)
+@pytest.mark.parametrize("gap", [13, 16, 19, 23])
+def test_rows_with_a_peak(n, c, dt, lanes, gap):
+    say("peak", n, c, dt, gap)
+    rng = np.random.default_rng(gap)
+    v = torch.from_numpy(rng.standard_normal((n, c), dtype=np.float32) * 2)
+    at = torch.from_numpy(rng.integers(0, c, n))
+    v.scatter_(1, at[:, None], gap + torch.from_numpy(rng.random((n, 1), dtype=np.float32)))
+    z, tokens = v.to(dt).to(DEV), at.to(torch.int32).to(DEV)
+    r = ops.token_logprobs(z, tokens)
+    torch.cuda.synchronize()
+    ref = reference(z, None, tokens, 1.0)
+    pieces = -(-c // (lanes * (4 if dt == F32 else 8)))
+    p, u = ref["p"], ref["u"].abs()
+    w = (p * u).sum(1)
+    ds = (p * (4 * u + 8)).sum(1) * U + (pieces + 8 + 16) * U
+    dls = ds + 4 * U * ref["ls"].abs() + 2 * U
+    dH = dls + (p * u * (8 * u + 16)).sum(1) * U + U * (pieces * (3.2 + w) + 8 * 3.2 + 9 + 16 * w) + w * (ds + 6 * U) + 2 * U * ref["H"]
+    say("peak", n, c, gap, "entropy", ref["H"].mean().item(), "off by", (r.entropy - ref["H"]).abs().max().item(), "of", dH.max().item())
+    close(r.entropy, ref["H"], dH, "entropy")
+    close(r.logp, ref["logp"], 4 * U * ref["logp"].abs() + dls, "logp")
+
+
 @pytest.mark.parametrize("dt", [F32, BF16], ids=str)
 @pytest.mark.parametrize("c", [2000, 70001])
 def test_long_rows_of_large_batches(c, dt):
