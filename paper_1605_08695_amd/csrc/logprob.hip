@@ -9,7 +9,7 @@
 //
 // A workgroup has a row and reads it once.  A lane's sums are relative to a power of two of its own, which it raises only
 // when a class passes it by 2^kSlack: without the slack nearly every step of a wave has a lane with a new maximum.  A class
-// costs one fma and one exponential, and raising costs none; a row whose sum then is no positive number is read again by exact
+// costs one fma and one exponential, and raising costs none; a row too far out for that (beyond 2^27, infinite or NaN) is read again by exact
 // differences (Part below).  The slack also bounds what a row with one class far above the others loses: W's terms at that
 // class and its lane's later sums are up to kSlack times s, and entropy is what is left of them.  With 4 and the terms of
 // a piece added up before they join the lane's, it is off by 2.2e-6 at most, fp32 operations on whole rows by 1.5e-6
@@ -67,9 +67,9 @@ __device__ __forceinline__ float wave_sumf(float v) {
 }
 
 // A lane's part of a row: sums relative to a power of two, and its largest x.  EXACT false: x ct - R by one fma, R a whole
-// number near the largest x ct, so that sums go from one to the next by a change of their exponents; rows that this cannot hold (s is not a positive number
-// then: the largest class beyond +-2^28, infinite or NaN) are read again with EXACT, relative to a ref by exact
-// differences.
+// number near the largest x ct, so that sums go from one to the next by a change of their exponents; rows that this cannot
+// hold (the largest x ct beyond +-2^27, or infinite or NaN: s is no positive number then) are read again with EXACT, relative
+// to a ref by exact differences.
 template <bool EXACT>
 struct Part {
     float ref, s, W, top;              // ref: R, or an x
@@ -268,7 +268,8 @@ template <typename T, int NT>
 __device__ __forceinline__ void join_sums(const T *z, const float *bias, int c, float ct, const Part<false> &p, RowStats<NT> &sh,
                                           float &m, float &s, float &W) {
     join_row<false, NT>(p, ct, sh, m, s, W);
-    if (!(s > 0.f && s < INFINITY)) join_row<true, NT>(read_row<true, T, NT>(z, bias, c, ct, nullptr), ct, sh, m, s, W);
+    // (towards the edge terms and W leave fp32's exponents before s does)
+    if (!(s > 0.f && s < INFINITY && __builtin_fabsf(m) * ct < kEdge / 2)) join_row<true, NT>(read_row<true, T, NT>(z, bias, c, ct, nullptr), ct, sh, m, s, W);
 }
 
 // The largest number, of those whose bits below `low` are 0, that at least k of a wave's orders (U a lane) are not below (0:

@@ -261,6 +261,24 @@ def test_temperatures(T):
         assert torch.isfinite(d).all()
 
 
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("c", [9, 1000, 9000, 140000])
+def test_rows_at_the_edge_of_what_is_held_by_one_fma(c, dt):
+    """Rows whose x / T is about 2^28 powers of two, on both sides of it by as much as fp32's exponents span: equal
+    classes, and one class an fp32 step above the others."""
+    for sign in (1, -1):
+        X = torch.tensor(sign * 19968.0, device=DEV)
+        for past in (-1000.0, -140.0, -115.0, -60.0, 0.0, 60.0, 122.0, 127.0, 140.0, 1000.0):
+            near = np.float32(X.item() * math.log2(math.e) / (sign * 2.0 ** 28 + past))
+            say("edge", c, dt, sign, past, near)
+            z = X.to(dt).expand(3, c).clone()
+            if dt == F32 and c > 1:
+                z[1, :-1] = torch.nextafter(X, torch.full_like(X, -INF))
+                z[2, 1:] = torch.nextafter(X, torch.full_like(X, -INF))
+            for T in (np.nextafter(near, np.float32(0)), near, np.nextafter(near, np.float32(1))):
+                check(z, None, toks(3, c, 1, pad=False), float(T), 5)
+
+
 def test_nan_and_infinite_rows():
     for c in (5, 3000, 70000, 140000):
         z = logits(4, c, F32, c)
