@@ -578,7 +578,9 @@ TFK_API tfk_status tfk_token_logprobs_bwd(const void *logits, tfk_dtype dt, int6
  *              tfk_gated_scan_bwd (undefined for blocks of padding alone).
  *   ws       : at least tfk_gated_scan_workspace_bytes(0, b, t, d) bytes (may be NULL when that is 0); calls
  *              that may overlap in time need one each.
- * A NaN in z makes its channel NaN from there on.
+ * A NaN in z makes its channel NaN from there on.  An infinity in x or h0 makes the state infinite from there on, NaN
+ * where one of the other sign joins it or a gate's smaller share is 0 in fp32 (|a| past 87); x and a state further apart
+ * than fp32's largest number count as that.  Earlier rows and other channels keep their results.
  * Errors: b, t < 0, d < 1, rows that overlap (SHAPE); gates not 2 or 3 (ARG); b > 2^31 - 1, t > 2^30 - 1, d > 2^24,
  * more than 2^40 elements, rows of a sequence more than 2^25 elements apart, negative strides (OVERFLOW); NULL,
  * misaligned or overlapping buffers (NULL, ALIGN, ALIAS); WORKSPACE.  b == 0 is a no-op; t == 0 sets h_last to h0. */

@@ -61,12 +61,27 @@ __device__ __forceinline__ float fresh(float s) {
     return s;
 }
 
-// f h + (1 - f) x
-__device__ __forceinline__ float move(float h, float s, float x) { return __builtin_fmaf(s, x - h, shut(s) ? x : h); }
+// The nearest finite number: what an infinity may be multiplied by a share as, where it stays as a summand (its difference
+// from a finite number, or from itself, would be NaN).  Finite results are the same bits with and without it.
+__device__ __forceinline__ float finite(float x) { return __builtin_amdgcn_fmed3f(x, -__FLT_MAX__, __FLT_MAX__); }
+
+// f h + (1 - f) x: from the one with the larger share towards the other
+__device__ __forceinline__ float move(float h, float s, float x) {
+    const float most = shut(s) ? x : h, least = shut(s) ? h : x;
+    return __builtin_fmaf(__builtin_fabsf(s), least - finite(most), most);
+}
 // f g
-__device__ __forceinline__ float kept(float g, float s) { return __builtin_fmaf(-s, g, shut(s) ? 0.f : g); }
-// S + P h
-__device__ __forceinline__ float join(float h, float s, float S) { return (shut(s) ? 0.f : h) + __builtin_fmaf(-s, h, S); }
+__device__ __forceinline__ float kept(float g, float s) {
+    return __builtin_fmaf(-s, shut(s) ? g : finite(g), shut(s) ? 0.f : g);
+}
+// The same of a product of gates, which is finite: P f, and 1 - P with what 1 - f adds to it.
+__device__ __forceinline__ float kept_of(float P, float s) { return __builtin_fmaf(-s, P, shut(s) ? 0.f : P); }
+__device__ __forceinline__ float gone_of(float Q, float s) { return __builtin_fmaf(s, 1.f - Q, shut(s) ? 1.f : Q); }
+// S + P h (an infinite h stays where P is too small for fp32: no gate's f is 0)
+__device__ __forceinline__ float join(float h, float s, float S) {
+    const float c = finite(h);
+    return (shut(s) ? h - c : h) + __builtin_fmaf(-s, c, S);
+}
 // The smaller of 1 - P and P of a span, from both.
 __device__ __forceinline__ float span(float Q, float P) { return Q < 0.5f ? Q : -P; }
 
@@ -166,8 +181,8 @@ struct Span {
     float S, Q, P;
     __device__ __forceinline__ void add(float s, float x) {
         S = move(S, s, x);
-        Q = move(Q, s, 1.f);
-        P = kept(P, s);
+        Q = gone_of(Q, s);
+        P = kept_of(P, s);
     }
     // This span, then o.
     __device__ __forceinline__ Span then(const Span &o) const {
@@ -260,8 +275,8 @@ __global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(ScanSegArgs 
                 if (!INSIDE && t0 + i >= len) s = v = 0.f;
                 if (BWD) n[e].S = kept(n[e].S + v, s);
                 else n[e].S = move(n[e].S, s, v);
-                n[e].Q = move(n[e].Q, s, 1.f);
-                n[e].P = kept(n[e].P, s);
+                n[e].Q = gone_of(n[e].Q, s);
+                n[e].P = kept_of(n[e].P, s);
             }
         }
 #pragma unroll
@@ -499,8 +514,8 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_k
                 if (OUT) o[i][e] = gate(o[i][e] + bo[e]);
                 if (!INSIDE && t0 + i >= len) s[i][e] = x[i][e] = up[i][e] = 0.f;
                 if (!DIRECT) m[e].S = move(m[e].S, s[i][e], x[i][e]);
-                m[e].Q = move(m[e].Q, s[i][e], 1.f);
-                m[e].P = kept(m[e].P, s[i][e]);
+                m[e].Q = gone_of(m[e].Q, s[i][e]);
+                m[e].P = kept_of(m[e].P, s[i][e]);
             }
             float out[V];
             if (DIRECT) forward(i, out);

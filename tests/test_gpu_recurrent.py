@@ -289,6 +289,52 @@ def test_padding_is_not_read_and_nan_stays_in_its_channel():
     torch.cuda.synchronize()
 
 
+def like(got, want, bound, dt, what):
+    """near() where a result is finite, and the same infinities and NaN elsewhere."""
+    got = f64(got)
+    fin = torch.isfinite(want)
+    wrong = ((got.isnan() != want.isnan()) | (torch.isinf(want) & (got != want))).nonzero().tolist()
+    assert not wrong, (what, len(wrong), wrong[:3])
+    assert torch.isfinite(bound[fin]).all().item()
+    near(got[fin], want[fin], bound[fin], dt, what)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("gates", [2, 3])
+@pytest.mark.parametrize("b,t,d", [(3, 1, 9), (2, 40, 70), (3, 300, 65), (1, 3000, 64), (520, 140, 6)])
+def test_infinite_inputs_give_what_the_formula_gives(b, t, d, gates, dt):
+    """Infinities in x, in the first states and in dy, at gates on both sides of 0: the state is infinite from there on,
+    NaN where two of different signs meet, and no other channel or earlier row knows of it."""
+    say("infinite", b, t, d, gates, dt)
+    inf = float("inf")
+    z = make(b, t, d, gates, dt, 4)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    h0, dh = (torch.randn(b, d, generator=g, device=DEV) for _ in range(2))
+    dy = torch.randn(b, t, d, generator=g, device=DEV).to(dt)
+    last = b - 1
+    z[0, t // 3, 0], z[0, t // 3, d] = inf, 2.0
+    z[0, t // 3, 1], z[0, t // 3, d + 1] = -inf, -2.0
+    z[last, t // 2, 2] = inf
+    z[last, t - 1, 2] = -inf
+    h0[0, 3], h0[last, 4] = -inf, inf
+    z[last, t // 2, 4] = -inf
+    dy[last, t // 2, 5] = inf
+    dh[0, 5] = -inf
+    y, end, saved = ops.gated_scan_fwd(z, gates == 3, h0=h0, save=True)
+    dz, dh0 = ops.gated_scan_bwd(z, dy, saved, gates == 3, dh_last=dh)
+    torch.cuda.synchronize()
+    r = reference(z, None, h0, None, gates, dy, dh)
+    like(y, r["y"], r["Ey"], dt, "y")
+    like(end, r["last"], r["Elast"], F32, "last")
+    like(dz, r["dz"], r["Edz"], dt, "dz")
+    like(dh0, r["dh0"], r["Edh0"], F32, "dh0")
+    state = h0.clone()
+    ys = ops.gated_scan_step(z[:, 0].contiguous(), state, None, gates == 3)
+    r = reference(z[:, :1], None, h0, None, gates)
+    like(ys, r["y"][:, 0], r["Ey"][:, 0], dt, "step")
+    like(state, r["last"], r["Elast"], F32, "state")
+
+
 def test_empty_batches_and_sequences():
     for b, t in ((0, 5), (3, 0), (0, 0)):
         z = torch.zeros(b, t, 8, device=DEV)
