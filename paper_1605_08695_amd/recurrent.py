@@ -54,7 +54,7 @@ class GatedRecurrence:
         x, z, lengths, states = saved
         dz, dh0 = ops.gated_scan_bwd(z, dy, states, self.output_gate, self.b, lengths, dh_last, dz=z, stream=stream)
         n = x.numel() // self.d_in
-        x4, dz4 = x.view(n, 1, 1, self.d_in), dz.view(n, 1, 1, -1)
+        x4, dz4 = x.view(n, 1, 1, self.d_in), dz.view(n, 1, 1, dz.shape[-1])
         w4 = self.W_lp.view(1, 1, self.d_in, -1)
         _, db = ops.bias_relu_bwd(None, dz4, dpre=dz4, stream=stream)
         dW = ops.conv2d_bwd_filter(x4, dz4, (1, 1), 1, (0, 0, 0, 0), stream=stream).view(self.d_in, -1)

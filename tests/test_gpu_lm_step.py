@@ -189,3 +189,31 @@ def test_asked_token_by_token():
     order = torch.argsort(logits.float() + md.head.b, dim=1, descending=True, stable=True)[:, :5]
     assert torch.equal(scores.top_idx.long(), order) and scores.logp is None
     assert (scores.top_logp[:, 1:] <= scores.top_logp[:, :-1]).all()
+
+
+@pytest.mark.parametrize("b,t", [(0, 5), (3, 0)])
+def test_layer_without_rows(b, t):
+    """No sequences, or sequences without tokens: the states pass through, and the variables' gradients are 0."""
+    rec = Model(32).rec
+    x = torch.zeros(b, t, D, dtype=BF16, device=DEV)
+    h0, dh = torch.randn(b, H, device=DEV), torch.randn(b, H, device=DEV)
+    y, last, saved = rec.forward(x, h0)
+    dx, dh0, dW, db = rec.backward(saved, torch.zeros_like(y), dh)
+    assert y.shape == (b, t, H) and torch.equal(last, h0)
+    assert dx.shape == x.shape and torch.equal(dh0, dh)
+    assert dW.shape == (D, 3 * H) and not dW.any() and db.shape == (3 * H,) and not db.any()
+    state = torch.randn(4, H, device=DEV)
+    before = state.clone()
+    assert rec.step(x.view(0, D), state, torch.zeros(0, dtype=torch.int32, device=DEV)).shape == (0, H)
+    torch.cuda.synchronize()
+    assert torch.equal(state, before)
+
+
+def test_head_without_rows():
+    head = Model(32).head
+    h, tokens = torch.zeros(0, H, dtype=BF16, device=DEV), torch.zeros(0, dtype=torch.int32, device=DEV)
+    scores, z = head.score(h, tokens, k=3)
+    assert scores.logp.shape == (0,) and scores.top_idx.shape == (0, 3) and z.shape == (0, V)
+    dh, dW, db = head.score_gradients(h, z, tokens, scores, torch.zeros(0, device=DEV), torch.zeros(0, device=DEV))
+    torch.cuda.synchronize()
+    assert dh.shape == (0, H) and dW.shape == (H, V) and not dW.any() and db.shape == (V,) and not db.any()
