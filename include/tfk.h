@@ -528,8 +528,9 @@ TFK_API tfk_status tfk_distill_xent(const void *logits, tfk_dtype dt, int64_t n,
  *   ws       : at least tfk_token_logprobs_workspace_bytes(n, c, k) bytes (may be NULL when that is 0), 16-byte
  *              aligned; calls that may overlap in time need one each.
  * Finite logits are numbers whatever their size (masks of -1e9, -1e30 or the type's lowest value), where
- * fp32 holds the differences between the row's (lse alone is infinite where x / T is past its range).  A row of -inf throughout has lse -inf, logp -inf, entropy
- * 0 and no list.  A row with a NaN or +inf has NaN in logp, entropy, lse and top_logp, and -1 in top_idx.
+ * fp32 holds the differences between the row's; lse, and the logp of a class that far below the others, are
+ * infinite where they are past its range.  A row of -inf throughout has lse -inf, logp -inf, entropy 0 and
+ * no list.  A row with a NaN or +inf has NaN in logp, entropy, lse and top_logp, and -1 in top_idx.
  * top_idx and top_logp are what tfk_distill_xent takes as top_idx and top at T = 1 (with top_lse = 0 the
  * rest of the mass counts as one class); at another T the teacher's logits are T top_logp.
  * Errors: n < 0, c < 1, k not in 0..128, a row distance below c (SHAPE); temperature not in [1e-4, 1e4] (ARG);
@@ -551,7 +552,9 @@ TFK_API size_t tfk_token_logprobs_workspace_bytes(int64_t n, int32_t c, int32_t 
  *   dlogp     : fp32 [n].     dentropy : fp32 [n], or NULL for none (entropy is not read then).
  *   dlogits   : n rows of c values, type dt, dlogits_ld elements apart (0 = c); may equal logits with the same
  *               row distance (in place).
- * Classes of -inf get 0.  Errors as above. */
+ * Classes of -inf get 0.  Up to |lse| = 128 p_j is exp(x_j / T - lse), so that lse's rounding is in it (2^-21 of p
+ * where |lse| is 8 to 16, 2^-18 from 64 on); past 128 the row's maximum and sum are formed again from the row,
+ * which takes a reading more for each part of it that a workgroup has (see csrc/logprob.hip).  Errors as above. */
 TFK_API tfk_status tfk_token_logprobs_bwd(const void *logits, tfk_dtype dt, int64_t n, int32_t c, int64_t logits_ld,
                               const float *bias, const int32_t *tokens, float temperature, const float *lse,
                               const float *entropy, const float *dlogp, const float *dentropy, void *dlogits,

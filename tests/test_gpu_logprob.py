@@ -346,6 +346,96 @@ def test_gradient(n, c, T, extra, bias, with_entropy, dt):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("T", [1.0, 0.8])
+def test_rows_in_pairs(T, dt):
+    """Many long rows with a bias and no list, which a workgroup reads two at once: padding in either place of a pair and in
+    the odd last one's, masks, rows that are read again, and a NaN beside ordinary rows."""
+    n, c = 4099, 8201
+    low = torch.finfo(dt).min
+    z = logits(n, c, dt, 5)
+    b = torch.from_numpy(np.random.default_rng(5).standard_normal(c)).float().to(DEV)
+    tokens = toks(n, c, 5, pad=False)
+    tokens[[10, 13, 20, 21, 30, 42, 44]] = torch.tensor([-1, c, -1, -1, -7, -1, -1], dtype=torch.int32, device=DEV)
+    z[[10, 13, 20, 21]] = NAN
+    z[31].fill_(-1e9)                                # beside padding
+    z[43].fill_(low)
+    z[45].fill_(-INF)
+    z[50].fill_(low), z[51].fill_(-1e30)             # both of a pair
+    z[60, 7] = NAN
+    z[63, c - 1] = INF
+    z[70].fill_(-INF), z[71].fill_(-INF)
+    z[80, 1::3], z[81, ::2] = -INF, low
+    z[90].fill_(low)
+    z[90, 5] = 3.0
+    for rows in (n, n - 1):                          # an odd one at the end, and none
+        say("pairs", rows, c, T, dt)
+        if rows == n:
+            tokens[n - 1] = -1
+        r = ops.token_logprobs(z[:rows], tokens[:rows], 0, T, b)
+        listed = ops.token_logprobs(z[:rows], tokens[:rows], 2, T, b)
+        torch.cuda.synchronize()
+        for one, two in zip(r[:3], listed[:3]):
+            assert torch.equal(one.view(torch.int32), two.view(torch.int32))
+        empty, nan = [45, 70, 71], [60, 63]
+        live = (tokens[:rows] >= 0) & (tokens[:rows] < c)
+        pad = (~live).nonzero()[:, 0]
+        assert pad.numel() == (8 if rows == n else 7)
+        assert all(not v[pad].any().item() for v in r[:3])
+        assert r.logp[empty].tolist() == [-INF] * 3 and r.lse[empty].tolist() == [-INF] * 3 and r.entropy[empty].tolist() == [0.0] * 3
+        assert all(v[nan].isnan().all().item() for v in r[:3])
+        live[empty + nan] = False
+        at = live.nonzero()[:, 0]
+        for part in at.split(600):
+            ref = reference(z[part], b, tokens[part], T)
+            close(r.entropy[part], ref["H"], ref["dH"], "entropy")
+            # past fp32's range (the lowest number at T < 1) lse and logp are infinite
+            ends = lambda v: torch.where(v.abs() > torch.finfo(F32).max, v.sign() * INF, v)  # noqa: E731
+            close(r.lse[part], ends(ref["lse"]), ref["dlse"], "lse")
+            close(r.logp[part], ends(ref["logp"]), ref["dlogp"], "logp")
+
+
+# log p is (x - m) / T - log s where |lse| is past 128 (4 U |u|, log s's own error and 2 U of itself), and x / T - lse
+# elsewhere: a rounding of 1 / T and one of the result, and the errors of lse, which has log s's, two roundings of
+# m / T and one of itself.  The exponential flushes a p below 2^-126, which then is off by all of itself.
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
+@pytest.mark.parametrize("n,c,T,bias", [(9, 999, 1.0, False), (10, 70001, 1.0, True), (10, 70001, 0.7, False), (6, 40000, 0.02, True),
+                                        (1027, 1501, 1.0, False), (1027, 1501, 0.02, False), (2051, 16400, 1.0, True)])
+def test_gradient_on_both_sides_of_where_lse_is_used(n, c, T, bias, dt):
+    """Rows shifted by a constant, so that their lse is past 128, between 64 and 128 or small, in neighbouring rows."""
+    say("shifted", n, c, T, bias, dt)
+    shift = torch.tensor([0.0, 300.0, -500.0, 90.0, 100.0, -110.0, 5000.0], device=DEV)[torch.arange(n, device=DEV) % 7] * T
+    z = (logits(n, c, F32, c) + shift[:, None]).to(dt)
+    b = torch.from_numpy(np.random.default_rng(c).standard_normal(c)).float().to(DEV) if bias else None
+    tokens = toks(n, c, n)
+    rng = np.random.default_rng(n)
+    a, e = (torch.from_numpy(rng.standard_normal(n)).float().to(DEV) for _ in range(2))
+    r = ops.token_logprobs(z, tokens, 0, T, b)
+    d = ops.token_logprobs_bwd(z, tokens, r.lse, a, r.entropy, e, T, b)
+    mine = z.clone()
+    ops.token_logprobs_bwd(mine, tokens, r.lse, a, r.entropy, e, T, b, dlogits=mine)
+    torch.cuda.synchronize()
+    assert torch.equal(mine, d)
+    assert n < 1000 or ((r.lse.abs() > 128).any() and (r.lse.abs() < 128).any()).item()
+    for part in torch.arange(n, device=DEV).split(700):
+        ref = reference(z[part], b, tokens[part].clamp(min=0), T)
+        live = (tokens[part] >= 0)[:, None]
+        A, E = a[part].double()[:, None], e[part].double()[:, None]
+        u, p, H, lse = ref["u"], ref["p"], ref["H"][:, None], ref["lse"][:, None]
+        lp = u - ref["ls"][:, None]
+        one = torch.zeros_like(p).scatter_(1, tokens[part].clamp(min=0).long()[:, None], 1.0)
+        want = (A * (one - p) - E * p * (lp + H)) / T
+        m = lse - ref["ls"][:, None]
+        near = U * (lp + lse).abs() + ref["dls"][:, None] + 2 * U * m.abs() + U * lse.abs() + 2 * U * lp.abs()
+        dlp = torch.where(lse.abs() > 127.9, torch.maximum(4 * U * u.abs() + ref["dls"][:, None] + 2 * U * lp.abs(),
+                                                           torch.where(lse.abs() < 128.1, near, near * 0)), near)
+        tol = (p * (dlp + (2 * lp.abs() + 8) * U) * (A.abs() + E.abs() * (lp + H).abs()) + E.abs() * p * (dlp + ref["dH"][:, None] +
+               4 * U * (lp.abs() + H)) + 6 * U * (A.abs() * (one + p) + E.abs() * p * (lp.abs() + H))) / T
+        tol = tol + torch.where(p < 2.0 ** -125, p, torch.zeros_like(p)) * (A.abs() + E.abs() * (lp.abs() + H)) / T
+        want, tol = torch.where(live, want, torch.zeros_like(want)), torch.where(live, tol, torch.zeros_like(tol))
+        close(d[part], want, tol * (1 + half(dt)) + half(dt) * want.abs(), "gradient")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=str)
 @pytest.mark.parametrize("c", [9, 1000, 9000])
 def test_gradient_where_lse_is_past_the_range(c, dt):
     """Rows of the type's lowest or of large numbers at a temperature below 1: lse is infinite, and log p is not."""
