@@ -714,6 +714,12 @@ TFK_API tfk_status tfk_apply_adam(float *var, float *m, float *v, const float *g
  *              even, and a second moment that is not 0 is at least 2^-9 of its block's factor.  The step is made
  *              with the moments before they are rounded.  A block whose largest magnitude is below 2^-100
  *              becomes 0; one with a NaN or an infinity becomes NaN throughout.  Zeros are the first state.
+ *              Rounding to nearest keeps a moment where it is, relative to its block's largest, until one step moves
+ *              it by half of e4m3's step, up to 2^-4 of itself (more for values below 2^-6 of the factor): beside
+ *              gradients g of one size, sqrt(v) may stay below |g| by up to sqrt(1 + (2^-3 + 2^-8) / (1 - beta2)),
+ *              11.4 at beta2 = 0.999, 3.7 at 0.99, 1.5 at 0.9, and above it as long as the block's largest does not
+ *              fall; m by 1 + 2^-4 / (1 - beta1).  Steps are then as much too large or small: a beta2 of 0.99 or
+ *              less suits 8 bits.
  *   weight_decay : one value for each variable, or NULL for none.
  *   shadows  : NULL, or one bf16 copy for each variable, entries may be NULL.
  * The arrays are host memory, read during the call; ns[i] values in variable i (0: skipped).

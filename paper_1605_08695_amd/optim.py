@@ -17,6 +17,11 @@ class AdamW:
     as its square root (a quarter of their memory, and 18 bytes a value moved in place of 30); bits=32 in fp32.
     weight_decay is one number, or one for each variable.
 
+    In 8 bits a second moment follows its block's largest exactly, and its own gradients only by changes of more than
+    half a code in one step: gradients that grow beside the rest of their block may take steps up to
+    sqrt(1 + 0.129 / (1 - beta2)) times too large, 11 at 0.999 and 3.7 at 0.99, until they do; a beta2 of 0.99 or less
+    suits it.  A step that is recorded or captured is replayed as the step t that it was.
+
     moments = (ms, vs, m_scales, v_scales) continues with moments that are there (the scales None with bits=32), for
     instance those of a checkpoint, with ``t`` the number of steps made.  The handle keeps all these tensors, whose
     memory must stay where it is while it is used."""

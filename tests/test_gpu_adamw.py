@@ -282,3 +282,39 @@ def test_codes_agree_with_elementary_operations():
         for got, want in ((md.ms[0], m), (md.vs[0], v)):
             assert torch.equal(got.view(torch.uint8), want.view(torch.uint8)), t
         assert torch.equal(md.mc[0], mc) and torch.equal(md.vc[0], vc), t
+
+
+# A root r beside a steady |g| is rounded back to where it was, relative to its block's largest, while b2 r^2 + (1 - b2) g^2
+# lies below (1 + 2^-4)^2 r^2, half of e4m3's widest step above it: until g^2 > (1 + (2^-3 + 2^-8) / (1 - b2)) r^2.  Beyond
+# that each step moves it up a code, 2^-4 of itself or more.  The largest is exact, and at the end as far from its own |g|
+# as b2^t says; the rest of the block was scaled with it, so each root lies between the bound (and its rounding, 2^-4) and
+# the larger of its |g| before and after, rounded.
+@pytest.mark.parametrize("b2", [0.9, 0.99, 0.999])
+def test_second_moments_in_8_bits_follow_as_far_as_stated(b2):
+    say("follow", b2)
+    k = 1 - b2
+    steps = first = int(12 / k)
+    sizes = torch.ones(256, device=DEV)
+    sizes[0] = 2000.0
+    before, after = sizes.clone(), sizes.clone()
+    for i, (a, b) in enumerate([(1.0, 1.3), (1.0, 6.0), (1.0, 100.0), (3.0, 1500.0), (100.0, 1.0), (40.0, 30.0)]):
+        before[1 + 40 * i:31 + 40 * i], after[1 + 40 * i:31 + 40 * i] = a, b
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    var = [torch.zeros(256, device=DEV) for _ in range(2)]
+    short, exact = AdamW(var[:1], 1e-3, 0.9, b2, bits=8), AdamW(var[1:], 1e-3, 0.9, b2, bits=32)
+    for t in range(first + steps):
+        g = (before if t < first else after) * (torch.rand(256, generator=gen, device=DEV) - 0.5).sign()
+        short.step([g]), exact.step([g])
+    torch.cuda.synchronize()
+    r = short.vs[0].double() * short.v_scales[0].double()
+    full = exact.vs[0].double().sqrt()
+    # b2^steps < e^-12 of what was there before is left: (before / after)^2 e^-12 of v, half of that of its root
+    assert ((full / after - 1).abs() <= ((before / after).double() ** 2 + 1) * np.exp(-12) / 2 + 1e-4).all().item()
+    assert abs(r[0].item() / 2000.0 - 1) < 1e-3
+    least = after.double() / (1 + (2.0 ** -3 + 2.0 ** -8) / k) ** 0.5
+    most = torch.maximum(before, after).double()
+    say("follow", b2, "of the exact root, least", (r / full).min().item(), "most", (r / full).max().item())
+    assert (r >= least * (1 - 2.0 ** -4) * (1 - 1e-3)).all().item()
+    assert (r <= most * (1 + 2.0 ** -4) * (1 + 1e-3)).all().item()
+    steady = before == after
+    assert ((r / full - 1).abs()[steady] <= 2.0 ** -4 * (1 + 1e-2)).all().item()
