@@ -26,8 +26,9 @@ EXPORTS = ["tfk_conv2d_fwd", "tfk_conv2d_fwd_bias_relu", "tfk_maxpool_bwd_relu_b
            "tfk_apply_momentum", "tfk_apply_adam", "tfk_softmax_xent", "tfk_gather_rows_t",
            "tfk_sampled_softmax_xent", "tfk_scatter_apply_sgd", "tfk_distill_xent", "tfk_embedding_fwd",
            "tfk_embedding_bwd", "tfk_embedding_apply_sgd", "tfk_embedding_workspace_bytes",
-           "tfk_token_logprobs", "tfk_token_logprobs_workspace_bytes", "tfk_token_logprobs_bwd", "tfk_gated_scan_fwd", "tfk_gated_scan_bwd", "tfk_gated_scan_step",
-           "tfk_gated_scan_workspace_bytes", "tfk_apply_adamw_multi", "tfk_stream_wait", "tfk_mark_create", "tfk_mark_destroy",
+           "tfk_token_logprobs", "tfk_token_logprobs_workspace_bytes", "tfk_token_logprobs_bwd",
+           "tfk_gated_scan_fwd", "tfk_gated_scan_bwd", "tfk_gated_scan_step", "tfk_gated_scan_workspace_bytes",
+           "tfk_apply_adamw_multi", "tfk_stream_wait", "tfk_mark_create", "tfk_mark_destroy",
            "tfk_mark_record", "tfk_stream_wait_mark", "tfk_program_create",
            "tfk_program_destroy", "tfk_program_begin", "tfk_program_end", "tfk_program_length", "tfk_program_run",
            "tfk_status_string", "tfk_last_error", "tfk_abi_version"]

@@ -1218,7 +1218,7 @@ static tfk_status check_scan(tfk_dtype dt, int64_t b, int64_t t, int32_t d, int3
 
 size_t tfk_gated_scan_workspace_bytes(int32_t op, int64_t b, int64_t t, int32_t d) {
     if (op < 0 || op > 1 || check_scan(TFK_F32, b, t, d, 2) != TFK_OK || b == 0 || t == 0) return 0;
-    return scan_ws_bytes(op == 1, b, t, d);
+    return scan_ws_bytes(b, t, d);
 }
 
 tfk_status tfk_gated_scan_fwd(const void *z, tfk_dtype dt, int64_t b, int64_t t, int32_t d, int32_t gates, int64_t z_bs,
@@ -1235,7 +1235,7 @@ tfk_status tfk_gated_scan_fwd(const void *z, tfk_dtype dt, int64_t b, int64_t t,
         TRY(need_ptr(y, "y"));
     }
     const int64_t es = esize(dt), hb = b * d * 4, sb = (t + kScanBlock - 1) / kScanBlock * hb;
-    const size_t need = t == 0 ? 0 : scan_ws_bytes(false, b, t, d);
+    const size_t need = t == 0 ? 0 : scan_ws_bytes(b, t, d);
     TRY(check_ws(ws, ws_bytes, need));
     TRY(need_align(z, es, "z"));
     TRY(need_align(y, es, "y"));
@@ -1271,7 +1271,7 @@ tfk_status tfk_gated_scan_bwd(const void *z, tfk_dtype dt, int64_t b, int64_t t,
         TRY(need_ptr(dz, "dz"));
     }
     const int64_t es = esize(dt), hb = b * d * 4, sb = (t + kScanBlock - 1) / kScanBlock * hb;
-    const size_t need = t == 0 ? 0 : scan_ws_bytes(true, b, t, d);
+    const size_t need = t == 0 ? 0 : scan_ws_bytes(b, t, d);
     TRY(check_ws(ws, ws_bytes, need));
     TRY(need_align(z, es, "z"));
     TRY(need_align(dy, es, "dy"));
@@ -1548,12 +1548,14 @@ tfk_status tfk_apply_adamw_multi(int32_t count, int32_t bits, float *const *vars
     const double c1 = 1.0 - pow(beta1, (double)t), c2 = 1.0 - pow(beta2, (double)t);
     const AdamwParams q{(float)(lr / c1), (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2),
                         (float)(1.0 / sqrt(c2)), (float)epsilon};
-    if (!isfinite(q.lr) || !isfinite(q.rrc2) || !isfinite(q.eps)) return fail(TFK_ERR_OVERFLOW, "bias-corrected step overflows fp32");
+    if (!isfinite(q.lr) || !isfinite(q.rrc2) || !isfinite(q.eps))
+        return fail(TFK_ERR_OVERFLOW, "bias-corrected step overflows fp32");
     for (int i = 0; i < count; ++i) {
         const double wd = weight_decay ? weight_decay[i] : 0.;
         const int64_t n = ns[i], blocks = (n + 255) / 256, mb = bits == 8 ? n : n * 4;
         tfk_status s = TFK_OK;
-        if (!(wd >= 0.) || !isfinite((float)wd) || !isfinite((float)(lr * wd))) s = fail(TFK_ERR_ARG, "weight decay must be finite and >= 0");
+        if (!(wd >= 0.) || !isfinite((float)wd) || !isfinite((float)(lr * wd)))
+            s = fail(TFK_ERR_ARG, "weight decay must be finite and >= 0");
         else if (n < 0) s = fail(TFK_ERR_SHAPE, "n must be >= 0");
         else if (n > ((int64_t)1 << 38)) s = fail(TFK_ERR_OVERFLOW, "n too large");
         if (s == TFK_OK && n > 0) {

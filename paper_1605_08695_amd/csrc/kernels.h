@@ -251,7 +251,7 @@ struct ScanStepArgs {
     int64_t n;
     int d;
 };
-size_t scan_ws_bytes(bool bwd, int64_t b, int64_t t, int d);
+size_t scan_ws_bytes(int64_t b, int64_t t, int d);
 hipError_t launch_scan_fwd(int dt, int gates, const ScanArgs &a, void *ws, hipStream_t st);
 hipError_t launch_scan_bwd(int dt, int gates, const ScanBwdArgs &a, void *ws, hipStream_t st);
 hipError_t launch_scan_step(int dt, int gates, const ScanStepArgs &a, hipStream_t st);

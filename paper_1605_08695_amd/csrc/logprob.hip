@@ -9,12 +9,14 @@
 //
 // A workgroup has a row and reads it once.  A lane's sums are relative to a power of two of its own, which it raises only
 // when a class passes it by 2^kSlack: without the slack nearly every step of a wave has a lane with a new maximum.  A class
-// costs one fma and one exponential, and raising costs none; a row too far out for that (beyond 2^27, infinite or NaN) is read again by exact
-// differences (Part below).  The slack also bounds what a row with one class far above the others loses: W's terms at that
-// class and its lane's later sums are up to kSlack times s, and entropy is what is left of them.  With 4 and the terms of
-// a piece added up before they join the lane's, it is off by 2.2e-6 at most, fp32 operations on whole rows by 1.5e-6
-// (2560 x 40000 and 256 x 131072, a class 12 to 25 above the mean; with a slack of 32 and term by term 4e-5), in the same time
-// as with 1, 2, 8 or 32.  Each lane keeps the largest x it saw, and for a list the largest of each group of its batches of pieces.  The k-th largest
+// costs one fma and one exponential, and raising costs none; a row too far out for that (beyond 2^27, infinite or NaN) is
+// read again by exact differences (Part below).  The slack also bounds what a row with one class far above the others loses:
+// W's terms at that class and its lane's later sums are up to kSlack times s, and entropy is what is left of them.  With 4
+// and the terms of a piece added up before they join the lane's, it is off by 2.2e-6 at most, fp32 operations on whole rows
+// by 1.5e-6 (2560 x 40000 and 256 x 131072, a class 12 to 25 above the mean; with a slack of 32 and term by term 4e-5), in the
+// same time as with 1, 2, 8 or 32.
+//
+// Each lane keeps the largest x it saw, and for a list the largest of each group of its batches of pieces.  The k-th largest
 // of the lanes' is at most the row's k-th largest, so the classes on the list are in the few groups whose largest is not
 // below it, and only those are read again, shared out to all lanes, to find the candidates, which then count how many
 // are before them.
@@ -110,33 +112,12 @@ struct Part {
     }
 };
 
-// 16 bytes of a row and the bias beside them.
-template <typename T>
-struct Piece {
-    static constexpr int V = Elem<T>::kPerChunk;
-    typename RowVec<T, V>::raw z;
-    typename RowVec<float, V>::raw b;
-    __device__ __forceinline__ void load(const T *zp, const float *bias, int j) {
-        z = RowVec<T, V>::load(zp + j);
-        if (bias) b = RowVec<float, V>::load(bias + j);
-    }
-    __device__ __forceinline__ void values(const float *bias, float *x) const {
-        RowVec<T, V>::unpack(z, x);
-        if (bias) {
-            float y[V];
-            RowVec<float, V>::unpack(b, y);
-#pragma unroll
-            for (int e = 0; e < V; ++e) x[e] += y[e];
-        }
-    }
-};
-
 template <typename T>
 __device__ __forceinline__ float logit(const T *z, const float *bias, int j) {
     return Elem<T>::load(z + j) + (bias ? bias[j] : 0.f);
 }
 
-// Pieces at the same classes of R rows, with one reading of the bias.
+// 16 bytes at the same classes of each of R rows, and the bias beside them, read once.
 template <typename T, int R>
 struct Pieces {
     static constexpr int V = Elem<T>::kPerChunk;
@@ -269,7 +250,8 @@ __device__ __forceinline__ void join_sums(const T *z, const float *bias, int c, 
                                           float &m, float &s, float &W) {
     join_row<false, NT>(p, ct, sh, m, s, W);
     // (towards the edge terms and W leave fp32's exponents before s does)
-    if (!(s > 0.f && s < INFINITY && __builtin_fabsf(m) * ct < kEdge / 2)) join_row<true, NT>(read_row<true, T, NT>(z, bias, c, ct, nullptr), ct, sh, m, s, W);
+    if (!(s > 0.f && s < INFINITY && __builtin_fabsf(m) * ct < kEdge / 2))
+        join_row<true, NT>(read_row<true, T, NT>(z, bias, c, ct, nullptr), ct, sh, m, s, W);
 }
 
 // The largest number, of those whose bits below `low` are 0, that at least k of a wave's orders (U a lane) are not below (0:
@@ -300,7 +282,7 @@ struct ListShared {
     uint32_t orders[NT];       // of each lane's largest class
     int hot[NT];               // lanes whose largest is on the list, at most k, or more of equal ones
     uint32_t tau;
-    int nhot, n, above;
+    int nhot, n;
     int counts[NT / 64];
     u64 best[NT / 64];
     Trials<NT> trials;
@@ -311,9 +293,10 @@ struct ListShared {
 // which such a class can be are shared out to all lanes.  (A hot lane's pieces lie NT pieces apart, so reading all of them
 // again would fetch as many lines as the row has.)
 template <typename T, int NT, int CANDS>
-__device__ __forceinline__ void collect(const T *z, const float *bias, int c, const uint16_t (*groups)[NT], ListShared<NT, CANDS> &sh,
-                                        uint32_t least) {
-    constexpr int V = Piece<T>::V, kCands = CANDS;
+__device__ __forceinline__ void collect(const T *z, const float *bias, int c, const uint16_t (*groups)[NT],
+                                        ListShared<NT, CANDS> &sh, uint32_t least) {
+    constexpr int V = Pieces<T, 1>::V, kCands = CANDS;
+    const T *const row[1] = {z};
     const int n = c / V, per = (n + kBatch * NT - 1) / (kBatch * NT), all = sh.nhot * per;
     const auto take = [&](float x, int j) {
         const uint32_t o = order_of(x);
@@ -325,15 +308,15 @@ __device__ __forceinline__ void collect(const T *z, const float *bias, int c, co
         const int h = q / per, g = q - h * per, lane = sh.hot[h];
         if (groups[g % kGroups][lane] < (uint16_t)(least >> 16)) continue;
         const int at = g * kBatch * NT + lane;
-        Piece<T> b[kBatch];
+        Pieces<T, 1> b[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i)
-            if (at + i * NT < n) b[i].load(z, bias, (at + i * NT) * V);
+            if (at + i * NT < n) b[i].load(row, bias, (at + i * NT) * V);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             if (at + i * NT >= n) continue;
             float x[V];
-            b[i].values(bias, x);
+            b[i].values(0, bias, x);
 #pragma unroll
             for (int e = 0; e < V; ++e) take(x[e], (at + i * NT) * V + e);
         }
@@ -388,11 +371,11 @@ __device__ __forceinline__ u64 next_below(const T *z, const float *bias, int c, 
 
 // Of n > kRankAll candidates, all different and none 0, the k < n largest to the front of cand, in any order, found by all
 // waves bit by bit of those that differ (each round counts the candidates that are not below a trial), where a rank for
-// each would look at n^2 (2560 x 1000 with 128 classes: 29 us, 283).  Returns k.
+// each would look at n^2 (2560 x 1000 with 128 classes: 29 us, 283).
 constexpr int kRankAll = 256;
 
 template <int NT, int MOST>
-__device__ __forceinline__ int shrink(u64 *cand, int n, int k, Trials<NT> &sh, int *next) {
+__device__ __forceinline__ void shrink(u64 *cand, int n, int k, Trials<NT> &sh, int *next) {
     constexpr int U = MOST / NT;
     static_assert(MOST % NT == 0);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -434,7 +417,6 @@ __device__ __forceinline__ int shrink(u64 *cand, int n, int k, Trials<NT> &sh, i
     for (int i = 0; i < U; ++i)
         if (mine[i] >= t) cand[atomicAdd(next, 1)] = mine[i];
     __syncthreads();
-    return k;
 }
 
 // The k largest classes of a row (or of a part of one) that has one, largest first, to emit(rank, key); behind the
@@ -455,7 +437,7 @@ __device__ __forceinline__ void largest(const T *z, const float *bias, int c, in
             if (kGroupwise && low == 16) {
                 // a wave's maxima are too few to tell: those of its groups (2560 x 4000 with 64 classes 25 us, 1200 by the
                 // lanes' own, which let most classes be candidates)
-                constexpr int V = Piece<T>::V;
+                constexpr int V = Pieces<T, 1>::V;
                 uint32_t mine[kGroups];
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g)
@@ -502,7 +484,10 @@ __device__ __forceinline__ void largest(const T *z, const float *bias, int c, in
         }
     }
     if (n <= kCands) {
-        if (n > kRankAll) n = shrink<NT, CANDS>(sh.cand, n, k, sh.trials, &sh.n);
+        if (n > kRankAll) {
+            shrink<NT, CANDS>(sh.cand, n, k, sh.trials, &sh.n);
+            n = k;
+        }
         for (int i = threadIdx.x; i < n; i += NT) {
             const u64 key = sh.cand[i];
             int rank = 0;
@@ -681,7 +666,10 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, const 
     }
     __syncthreads();
     int n = count;
-    if (n > kRankAll) n = shrink<NT, kPartMost * 128>(cand, n, a.k, trials, &count);
+    if (n > kRankAll) {
+        shrink<NT, kPartMost * 128>(cand, n, a.k, trials, &count);
+        n = a.k;
+    }
     for (int i = threadIdx.x; i < n; i += NT) {
         const u64 x = cand[i];
         int rank = 0;

@@ -219,7 +219,8 @@ __device__ __forceinline__ void join_segments(const float2 *agg, int64_t at, int
     }
 }
 
-// What each segment but the last makes of the state before it (BWD: each but the first of what comes from behind it),
+// What each segment but the last makes of the state before it (BWD: each but the first of what comes from behind it, where
+// OUT says whether there is an output gate),
 // to agg[b][segment][channel].  Each wave takes a part of the segment, run by run.
 template <typename T, int V, bool OUT, bool BWD, int RUN>
 __global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(ScanSegArgs a, float2 *agg, int segments, int seg_len) {
@@ -308,7 +309,8 @@ __global__ __launch_bounds__(64 * kWaves) void scan_segments_kernel(ScanSegArgs 
 }
 
 template <typename T, int V, bool OUT, int RUN>
-__global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 3) void scan_fwd_kernel(ScanArgs a, const float2 *agg, int segments, int seg_len) {
+__global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 3) void scan_fwd_kernel(ScanArgs a, const float2 *agg,
+                                                                                        int segments, int seg_len) {
     typedef Lane<T, V, RUN> L;
     constexpr int kSteps = L::kSteps, kBlock = kWaves * RUN;
     __shared__ float2 spans[2][kWaves][kStrip];
@@ -426,7 +428,8 @@ __global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 3) void scan_fwd_k
 }
 
 template <typename T, int V, bool OUT, int RUN>
-__global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg, int segments, int seg_len) {
+__global__ __launch_bounds__(64 * kWaves, RUN == kShort ? 4 : 2) void scan_bwd_kernel(ScanBwdArgs a, const float2 *agg,
+                                                                                        int segments, int seg_len) {
     typedef Lane<T, V, RUN> L;
     // DIRECT: a state was saved for each lane's first token; else the runs since the last one are joined
     constexpr int kSteps = L::kSteps, kBlock = kWaves * RUN;
@@ -650,7 +653,8 @@ static ScanPlan scan_plan(int64_t b, int64_t t, int d) {
     return {fine, (int)((blocks + per - 1) / per), (int)(per * block)};
 }
 
-size_t scan_ws_bytes(bool, int64_t b, int64_t t, int d) {
+// (Forward and backward are cut alike.)
+size_t scan_ws_bytes(int64_t b, int64_t t, int d) {
     const ScanPlan p = scan_plan(b, t, d);
     return p.segments > 1 ? (size_t)b * p.segments * d * sizeof(float2) : 0;
 }
@@ -660,8 +664,8 @@ static void launch_fwd_run(const ScanArgs &a, float2 *ws, const ScanPlan &p, hip
     const int64_t strips = a.b * ((a.d + kStrip - 1) / kStrip);
     if (p.segments > 1) {
         const ScanSegArgs g{a.z, a.z_bs, a.z_ts, a.bias, a.lengths, nullptr, 0, 0, a.b, a.t, a.d};
-        hipLaunchKernelGGL((scan_segments_kernel<T, V, OUT, false, RUN>), grid_2d(strips * (p.segments - 1)), dim3(64 * kWaves), 0,
-                           st, g, ws, p.segments, p.seg_len);
+        hipLaunchKernelGGL((scan_segments_kernel<T, V, false, false, RUN>), grid_2d(strips * (p.segments - 1)), dim3(64 * kWaves),
+                           0, st, g, ws, p.segments, p.seg_len);
     }
     hipLaunchKernelGGL((scan_fwd_kernel<T, V, OUT, RUN>), grid_2d(strips * p.segments), dim3(64 * kWaves), 0, st, a, ws, p.segments,
                        p.seg_len);
@@ -718,7 +722,7 @@ hipError_t launch_scan_bwd(int dt, int gates, const ScanBwdArgs &a, void *ws, hi
     return hipGetLastError();
 }
 
-template <typename T, int V, bool OUT>
+template <typename T, bool OUT>
 static void launch_step(const ScanStepArgs &a, hipStream_t st) {
     const unsigned gy = (unsigned)std::min<int64_t>(a.n, 32768);
     hipLaunchKernelGGL((scan_step_kernel<T, OUT>), dim3((a.d + 255) / 256, gy, (unsigned)((a.n + gy - 1) / gy)), dim3(256), 0, st,
@@ -726,7 +730,10 @@ static void launch_step(const ScanStepArgs &a, hipStream_t st) {
 }
 
 hipError_t launch_scan_step(int dt, int gates, const ScanStepArgs &a, hipStream_t st) {
-    SCAN_CASES(launch_step, a, st);
+    if (dt == 0 && gates == 2) launch_step<float, false>(a, st);
+    else if (dt == 0) launch_step<float, true>(a, st);
+    else if (gates == 2) launch_step<bf16_t, false>(a, st);
+    else launch_step<bf16_t, true>(a, st);
     return hipGetLastError();
 }
 

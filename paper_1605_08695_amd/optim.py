@@ -57,7 +57,8 @@ class AdamW:
         self._ns = (ctypes.c_int64 * max(n, 1))(*self._sizes)
         self._decay = (ctypes.c_double * max(n, 1))(*decay)
         self._shadows = None if self.shadows is None else p(self.shadows)
-        spans = sorted((x.data_ptr(), x.data_ptr() + x.numel() * x.element_size()) for x in self._kept if x is not None and x.numel())
+        spans = sorted((x.data_ptr(), x.data_ptr() + x.numel() * x.element_size())
+                       for x in self._kept if x is not None and x.numel())
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("variables, moments, scales and shadows must not share memory")
         devices = {t_.get_device() for t_ in self._kept if t_ is not None}
