@@ -21,10 +21,11 @@
 // below it, and only those are read again, shared out to all lanes, to find the candidates, which then count how many
 // are before them.
 //
-// Bound by HBM: a row is read once, and for the gradient once more and written.  Measured, in bf16: 2560 x 40000 with a bias
-// and 32 classes 62 us (3.3 TB/s), 4096 x 131072 with a bias 218 us (4.9 TB/s), its gradient 387 us (5.5 TB/s); 1021 x 50021
-// in fp32 with a bias and 5 classes 43 us, its gradient 70.  A bias is read from the L2 for each row, or for two (4096 x
-// 131072 without one: 187 us and 358).
+// Bound by HBM, in bf16 with a bias and a list nearly as much by the vector unit: a row is read once, and for the gradient
+// once more and written.  Measured, in bf16: 2560 x 40000 with a bias and 32 classes 62 us (48 with the logits in the caches,
+// where the vector unit is 87 % busy; without a list 44), 4096 x 131072 with a bias 210 us (5.1 TB/s; 247 between calls of its
+// gradient, whose last writes it waits for), its gradient 387 us (5.5 TB/s); 1021 x 50021 in fp32 with a bias and 5 classes 43
+// us, its gradient 70.  A bias is read from the L2 for each row, or for two (4096 x 131072 without one: 187 us and 358).
 #include "common.h"
 #include "kernels.h"
 #include "rowvec.h"
@@ -681,6 +682,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, const 
 
 // The gradient.  Where lse is so large that fp32 no longer tells x / T from it (a row of masks alone; past fp32's range,
 // m / T is infinite), the row's maximum and sum are formed again from the row.
+// (Each part of a row does: 4096 x 131072 bf16 2742 us, where 393 without; a row that is one workgroup's, as in place, 698,
+// 445 without.)
 constexpr float kFarLse = 128.f;
 constexpr int kBwdPart = 1024;             // pieces of 16 bytes of a part
 
@@ -786,7 +789,7 @@ size_t logprob_ws_bytes(int64_t n, int c, int k) {
 // classes, where there are rows enough (65536 x 1500: 50 us and with 10 classes 94, by four waves 94 and 202; 2560 x 4000 8.2
 // and 12.2, 9.0 and 16.1; but 256 x 2000 4.3, 3.8), with lists of more than 64 with room for 2048 candidates (2560 x 1100
 // with 128 classes 65 us: its 74 groups are too few, so that all classes are candidates).
-// With a bias and no list two rows by four waves (4096 x 131072 218 us, 247 by one row; 2560 x 40000 46, 54; 20000 x 10000
+// With a bias and no list two rows by four waves (4096 x 131072 210 us, 247 by one row; 2560 x 40000 44, 54; 20000 x 10000
 // 87, 97; but 1500 x 10000 11.4, 10.1; with lists, which follow one another then, 2560 x 40000 76, 64).  Few rows too long for
 // four waves, and too many to be cut, by sixteen (256 x 131072 with 20 classes 21 us, 31 by four; 200 x 50000 15.0, 17.3;
 // but 200 x 20000 12.2, 10.6).
@@ -825,7 +828,8 @@ hipError_t launch_logprob(int dt, const LogprobArgs &a, void *ws, hipStream_t st
 // (65536 x 1500 76 us, 145), or has a bias to read (4096 x 131072 387, 410; 20000 x 10000 160; but 1600 x 131072 181, 166).
 template <typename T>
 static void launch_bwd_rows(const LogprobBwdArgs &a, hipStream_t st) {
-    // parts of a row read the whole of it where lse is far out: in place a row is one workgroup's
+    // parts of a row read the whole of it where lse is far out: in place a row is one workgroup's (4096 x 131072 445 us, apart 393;
+    // 1021 x 50021 fp32 92, 81; but 64 x 131072 35, 11)
     const int most = kBwdPart * 16 / (int)sizeof(T), parts = a.dz == a.z ? 1 : (a.c + most - 1) / most;
     const int len = ((a.c + parts - 1) / parts + 63) / 64 * 64;
     const bool pairs = (a.n >= 1024 && a.c * sizeof(T) <= 6144) || (a.bias && a.n >= 2048 && a.n * a.c >= (int64_t)1 << 25);

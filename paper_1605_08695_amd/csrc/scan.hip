@@ -20,10 +20,10 @@
 // each time.
 //
 // Bound by HBM and, with two bf16 channels a lane, nearly as much by the vector unit (a gate is an exponential and a
-// reciprocal; about 31 instructions a channel and token forwards, 27 for a segment, 45 to 51 backwards with the output
-// gate): z is read once and y written once; the backward pass reads z and dy and writes dz, with the states of each
-// kScanBlock-th token from the forward pass.  Measured, in bf16 with the output gate at 65536 x 768: segments 49 us, forward
-// 90 us (4.6 TB/s), segments backwards 73 us, backward 170 us (4.2 TB/s).
+// reciprocal; with the output gate 46 vector instructions a channel and token forwards, 23 for a segment, 72 backwards, 35 for
+// a segment): z is read once and y written once; the backward pass reads z and dy and writes dz, with the states of each
+// kScanBlock-th token from the forward pass.  Measured, in bf16 with the output gate at 65536 x 768: segments 50 us, forward
+// 97 us (4.2 TB/s, vector unit 76 % busy), segments backwards 78 us, backward 177 us (4.0 TB/s, 63 %).
 //
 // Tried and slower: the next block's loads before a block is joined (spills, or half the waves); 16 waves of short runs or
 // 8 waves of runs of 16 tokens (5 to 30 %); blocks of the time in turn, so that the second launch finds what the first read
@@ -630,12 +630,14 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStepArgs a) {
     Elem<T>::store(y, OUT ? o * h : h);
 }
 
-// How the time axis is cut: segments of seg_len tokens, a whole number of blocks.  Measured, forward and backward in bf16:
-//   blocks of four short runs: for up to 32 tokens (128 x 20 x 512: 18 us, 22 by blocks of 128), and for more than 128
-//     where blocks of 128 are fewer than 512 (1 x 500 x 512: 17 us, 42; 4 x 200 x 1024: 19, 28; but a single block of 128
-//     is better read by one workgroup: 8 x 128 x 1024: 12 us, 17 by short runs)
-//   segments: below 512 strips, towards 2048 workgroups (8 x 4096 x 2048 ragged: 298 us, 348 towards 512; 65536 x 768:
-//     376, 416); from 512 on one workgroup reads all of a strip (32 x 2048 x 1024: 232 us, 300 in segments)
+// How the time axis is cut: segments of seg_len tokens, a whole number of blocks.  Measured, forward and backward in bf16 with
+// the output gate, replayed as a graph:
+//   blocks of four short runs: for up to 32 tokens (128 x 20 x 512: 22 us, 48 by blocks of 128), and for more than 128
+//     where blocks of 128 are fewer than 512 (1 x 500 x 512: 25 us, 49; 4 x 200 x 1024: 27, 35; but a single block of 128
+//     is better read by one workgroup: 8 x 128 x 1024: 21 us, 27 by short runs)
+//   segments: below 512 strips, towards 2048 workgroups (65536 x 768: 377 us, 410 towards 512; 8 x 4096 x 2048 without the
+//     output gate, ragged: 309 to 320, 323 to 326; but of full lengths 369, 338); from 512 on one workgroup reads all of a
+//     strip (32 x 2048 x 1024: 356 us, 478 in segments)
 struct ScanPlan {
     bool fine;
     int segments, seg_len;
