@@ -23,7 +23,7 @@
 //
 // Bound by HBM, in bf16 with a bias and a list nearly as much by the vector unit: a row is read once, and for the gradient
 // once more and written.  Measured, in bf16: 2560 x 40000 with a bias and 32 classes 62 us (48 with the logits in the caches,
-// where the vector unit is 87 % busy; without a list 44), 4096 x 131072 with a bias 210 us (5.1 TB/s; 247 between calls of its
+// where the vector unit is 87 % busy; without a list 46), 4096 x 131072 with a bias 218 us (4.9 TB/s; 247 between calls of its
 // gradient, whose last writes it waits for), its gradient 387 us (5.5 TB/s); 1021 x 50021 in fp32 with a bias and 5 classes 43
 // us, its gradient 70.  A bias is read from the L2 for each row, or for two (4096 x 131072 without one: 187 us and 358).
 #include "common.h"
@@ -789,8 +789,8 @@ size_t logprob_ws_bytes(int64_t n, int c, int k) {
 // classes, where there are rows enough (65536 x 1500: 50 us and with 10 classes 94, by four waves 94 and 202; 2560 x 4000 8.2
 // and 12.2, 9.0 and 16.1; but 256 x 2000 4.3, 3.8), with lists of more than 64 with room for 2048 candidates (2560 x 1100
 // with 128 classes 65 us: its 74 groups are too few, so that all classes are candidates).
-// With a bias and no list two rows by four waves (4096 x 131072 210 us, 247 by one row; 2560 x 40000 44, 54; 20000 x 10000
-// 87, 97; but 1500 x 10000 11.4, 10.1; with lists, which follow one another then, 2560 x 40000 76, 64).  Few rows too long for
+// With a bias and no list two rows by four waves (4096 x 131072 218 us, 250 by one row; 2560 x 40000 46, 54; 20000 x 10000
+// 87, 98; but 1500 x 10000 12.4, 11.7; with lists, which follow one another then, 2560 x 40000 76, 64).  Few rows too long for
 // four waves, and too many to be cut, by sixteen (256 x 131072 with 20 classes 21 us, 31 by four; 200 x 50000 15.0, 17.3;
 // but 200 x 20000 12.2, 10.6).
 template <typename T>
